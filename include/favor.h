@@ -346,6 +346,112 @@ FAVOR_API favor_status favor_attn_both_backward(const favor_desc *g, const void 
                                                 void *dV, float *dstate_in, void *ws,
                                                 size_t ws_bytes, hipStream_t stream);
 
+/*
+ * Linear attention with a decay per head (no random features: Q and K enter as they
+ * are, for instance as favor_feature_map wrote them):
+ *   S_t = a_h S_{t-1} + k_t v_t^T,   out_t = scale q_t^T S_t,   a_h = exp(log_decay[h]),
+ * that is out_i = scale (sum_{j <= i} a^(i-j) (q_i . k_j) v_j + a^(i+1) q_i^T S_in).
+ * log_decay [H] fp32: at most 0; 0 keeps everything, -Inf only the token itself. (A
+ * positive value grows as the formula says.)
+ *
+ * Layouts: Q, K [B][H][L][dk], V, out [B][H][L][dv] with rows of contiguous elements and
+ * any strides between them, in elements (favor_strides; all three 0 = the contiguous
+ * layout above): [B][L][H][d] tensors, slices of one QKV projection and broadcast inputs
+ * (a stride of 0) need no copy. Strides and base addresses are multiples of 16 bytes;
+ * rows of an output must not share elements (FAVOR_ERR_INVALID_ARGUMENT), and outputs
+ * must not overlap inputs. state [B][H][dk][dv] fp32, contiguous.
+ *
+ * Supported: dk and dv multiples of 8 up to 256; dtype (inputs, out, gradients) F32 or
+ * BF16; 0 <= L <= 2^30; B*H <= 65535. F32 uses fp32 matrix cores, BF16 bf16 ones with
+ * fp32 sums; states are fp32 throughout and as exact for BF16 inputs as for F32 ones.
+ *
+ * lengths [B] int32 (nullable, device): sequence b has its first lengths[b] tokens
+ * (values outside 0 .. L are taken as 0 or L), and rows behind them are padding: their
+ * inputs are not read, their rows of out and of the gradients are written as zeros. A
+ * NaN or infinity in a token reaches the results of its own chunk of 64 tokens and of
+ * those behind it (in a gradient, before it).
+ */
+typedef struct {
+  int64_t batch, head, token;
+} favor_strides;
+
+typedef struct {
+  int32_t B, H, L, dk, dv;
+  favor_dtype dtype;        /* Q, K, V, out and the gradients */
+  float scale;
+  favor_strides q, k, v, out;
+  favor_strides grad_out, grad_q, grad_k, grad_v;   /* read by the backward pass only */
+} favor_decay_desc;
+
+/* Bytes of device workspace for favor_attn_decay (backward = 0) or
+ * favor_attn_decay_backward (1), 256-byte aligned; 0 if none is needed (then ws may be
+ * NULL) or g is invalid. Its contents on entry do not matter. */
+FAVOR_API size_t favor_decay_workspace_size(const favor_decay_desc *g, int backward);
+
+/*
+ * favor_attn_decay - the chunked form, for prompts and training. state_in (nullable): S
+ * before the first token; state_out (nullable; may be state_in): S after each sequence's
+ * last one, so a sequence can be processed in pieces. Deterministic (no atomics).
+ */
+FAVOR_API favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q,
+                                        const void *K, const void *V, const float *log_decay,
+                                        const int32_t *lengths, void *out,
+                                        const float *state_in, float *state_out, void *ws,
+                                        size_t ws_bytes, hipStream_t stream);
+
+/*
+ * favor_attn_decay_backward - gradients of a loss that depends on out and state_out, from
+ * dout and dstate_out (nullable: zeros); state_in and lengths as in the forward call:
+ *   dq_i = scale (sum_{j <= i} a^(i-j) (dout_i . v_j) k_j + a^(i+1) S_in dout_i)
+ *   dk_j = scale sum_{i >= j} a^(i-j) (dout_i . v_j) q_i + a^(n-1-j) dS_out v_j
+ *   dv_j = scale sum_{i >= j} a^(i-j) (q_i . k_j) dout_i + a^(n-1-j) dS_out^T k_j
+ *   dS_in = a^n dS_out + scale sum_i a^(i+1) q_i dout_i^T
+ * dstate_in (nullable; may be dstate_out) receives the gradient of state_in. Nothing from
+ * the forward call is needed. log_decay receives no gradient. For a broadcast input every
+ * head (or batch entry) gets its own gradient, to be summed by the caller. Deterministic.
+ */
+FAVOR_API favor_status favor_attn_decay_backward(
+    const favor_decay_desc *g, const void *Q, const void *K, const void *V,
+    const float *log_decay, const int32_t *lengths, const float *state_in, const void *dout,
+    const float *dstate_out, void *dQ, void *dK, void *dV, float *dstate_in, void *ws,
+    size_t ws_bytes, hipStream_t stream);
+
+/*
+ * favor_attn_decay_step - the recurrent form, for single tokens: Q, K [B][H][dk], V, out
+ * [B][H][dv] (g->L and the token strides are not read), and the states state
+ * [n_slots][H][dk][dv] updated in place. slots [B] int32 (nullable, device): the place of
+ * each sequence's state, NULL: state b is sequence b's (n_slots >= B). A sequence with a
+ * place outside 0 .. n_slots - 1 (padding of a captured batch) has no state and out = 0.
+ * Sequences that name the same place take their turns in order, as tokens of one sequence.
+ */
+FAVOR_API favor_status favor_attn_decay_step(const favor_decay_desc *g, const void *Q,
+                                             const void *K, const void *V,
+                                             const float *log_decay, const int32_t *slots,
+                                             int32_t n_slots, float *state, void *out,
+                                             hipStream_t stream);
+
+/* Host-only validation of a descriptor for an operation (0 favor_attn_decay, 1 its
+ * backward pass, 2 favor_attn_decay_step). */
+FAVOR_API favor_status favor_validate_decay_desc(const favor_decay_desc *g, int op);
+
+/*
+ * favor_dropout - y_n = residual_n + [bits_n >= t] x_n / (1 - t / 2^16) with t = p 2^16
+ * rounded to the nearest (ties to even): p is taken to 16 bits, and p >= 1 - 2^-17 drops
+ * everything. residual nullable (0); y may be x or residual. x, residual, y: n elements
+ * of dtype, contiguous, 16-byte aligned. A dropped element is 0 whatever x holds.
+ *
+ * bits_n is 16-bit piece n % 8 of Philox4x32-10 (Salmon et al., SC'11) with key (seed low,
+ * seed high) and counter (c low, c high, offset low, offset high), c = n / 8: pieces 2 j
+ * and 2 j + 1 are the low and high half of word j. Calls with other (seed, offset) have
+ * independent masks. The mask is not stored: the gradient is the same call on dy with
+ * the same p, seed, offset and no residual. rng (nullable, device, 8-byte aligned): two
+ * words {seed, offset} read by the kernel in place of the arguments, so that a captured
+ * graph draws a new mask whenever the program changes them.
+ */
+FAVOR_API favor_status favor_dropout(const void *x, const void *residual, void *y, int64_t n,
+                                     favor_dtype dtype, double p, uint64_t seed,
+                                     uint64_t offset, const uint64_t *rng, hipStream_t stream);
+
 /* Host-only validation of a descriptor for an operation (0 feature map,
  * 1 bidirectional, 2 causal, 3 both, 4 bidirectional backward, 5 causal
  * backward, 6 backward of both directions); launches nothing and touches no

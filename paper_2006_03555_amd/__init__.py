@@ -26,6 +26,7 @@ from ._lib import (  # noqa: F401
     OP_BIDIR_BACKWARD, OP_CAUSAL_BACKWARD, OP_BOTH_BACKWARD, KERNEL_RELU, KERNEL_SOFTMAX, backward_workspace_size,
     FavorDesc, FavorError, FavorLibraryMissing, lib, lib_path, make_desc, status_string,
     validate_desc, workspace_size, last_error, timing_enable, timing_reset, timing_read,
+    FavorDecayDesc, decay_workspace_size, make_decay_desc, validate_decay_desc,
 )
 
 __all__ = [
@@ -33,6 +34,8 @@ __all__ = [
     "attn_bidir_backward", "attn_causal_backward", "attn_both_backward",
     "backward_workspace_size", "make_desc",
     "attn_both_noalloc", "noalloc_scratch_bytes",
+    "attn_decay", "attn_decay_backward", "attn_decay_step", "decay_workspace_size",
+    "make_decay_desc", "validate_decay_desc", "dropout", "dropout_backward",
     "validate_desc", "FavorError", "FavorLibraryMissing", "lib", "lib_path",
 ]
 
@@ -534,3 +537,232 @@ def attn_both_backward(Q, K, V, W, b, input_scale, dout_bidir, dout_causal, deno
 def library_loaded_from():
     """Absolute path of the libfavor.so this process uses."""
     return os.path.realpath(lib_path())
+
+
+# ------------------------------------------------- linear attention with a decay per head
+def _require_here(*ts):
+    """The kernels run on the current device and read raw addresses there."""
+    here = None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise FavorError(1, "tensors must be GPU tensors")
+        if here is None:
+            here = _torch().cuda.current_device()
+        if t.device.index != here:
+            raise FavorError(1, f"a tensor is on device {t.device.index}, the current device is "
+                                f"{here}")
+
+
+def _require_whole(*ts):
+    for t in ts:
+        if t is not None and not t.is_contiguous():
+            raise FavorError(1, "states, decays, lengths and slots must be contiguous")
+
+
+def _row_strides(t, name):
+    """(batch, head, token) strides of [B, H, L, d] rows (token: any for [B, H, d]).
+    Dimensions of one element have no stride; d stands in for it, since three zeros
+    mean the contiguous layout."""
+    shape, s = t.shape, t.stride()
+    d = shape[-1]
+    if d > 1 and s[-1] != 1:
+        raise FavorError(1, f"rows of {name} must be contiguous")
+    got = tuple(s[i] if shape[i] > 1 else d for i in range(len(shape) - 1))
+    if len(got) == 2:
+        got += (d,)
+    if not any(got):
+        raise FavorError(1, f"{name} is one row broadcast to all")
+    return got
+
+
+_DECAY_STRIDES = ("q", "k", "v", "out", "grad_out", "grad_q", "grad_k", "grad_v")
+
+
+class _DecayCall:
+    """A decay descriptor with its by-reference argument and workspace sizes (see _Call)."""
+    __slots__ = ("g", "ref", "sizes")
+
+    def __init__(self, g):
+        self.g = g
+        self.ref = ctypes.byref(g)
+        self.sizes = [None, None]
+
+    def workspace(self, backward):
+        n = self.sizes[backward]
+        if n is None:
+            n = self.sizes[backward] = decay_workspace_size(self.g, backward)
+        return n
+
+
+@functools.lru_cache(maxsize=256)
+def _decay_call(B, H, L, dk, dv, code, scale, strides):
+    return _DecayCall(make_decay_desc(B, H, L, dk, dv, code, scale,
+                                      **dict(zip(_DECAY_STRIDES, strides))))
+
+
+def _decay_shapes(Q, K, V, log_decay, dims):
+    torch = _torch()
+    if Q.dim() != dims or V.dim() != dims:
+        want = "[B, H, L, d]" if dims == 4 else "[B, H, d]"
+        raise FavorError(1, f"inputs must be {want}, got {tuple(Q.shape)} and {tuple(V.shape)}")
+    if Q.shape[-1] == 0 or V.shape[-1] == 0:
+        raise FavorError(1, "dk and dv must be positive")
+    _require_like(K, Q.shape, Q.dtype, "K")
+    _require_like(V, Q.shape[:-1] + V.shape[-1:], Q.dtype, "V")
+    _require_like(log_decay, (Q.shape[1],), torch.float32, "log_decay")
+
+
+def _decay_workspace(n, workspace):
+    if n == 0 and workspace is None:
+        return None, 0
+    if workspace is not None:
+        _require_here(workspace)
+        _require_whole(workspace)
+    return _workspace_of(n, workspace)
+
+
+@_on_stream
+def attn_decay(Q, K, V, log_decay, scale=1.0, lengths=None, state_in=None, return_state=False,
+               out=None, state_out=None, workspace=None, stream=None):
+    """Linear attention with a decay per head (favor_attn_decay):
+    out_i = scale (sum_{j <= i} a^(i - j) (q_i . k_j) v_j + a^(i + 1) q_i state_in) with
+    a = exp(log_decay[h]).
+
+    Q, K [B, H, L, dk], V [B, H, L, dv]: bfloat16 or float32, rows contiguous, any other
+    strides (a transposed [B, L, H, d], slices of a projection, expanded tensors); dk and
+    dv multiples of 8 up to 256. lengths [B] int32: tokens of each right-padded sequence.
+    State tensors [B, H, dk, dv] float32. Returns out [B, H, L, dv] (in V's layout unless
+    given), or (out, state_out) when return_state is true.
+    """
+    torch = _torch()
+    _decay_shapes(Q, K, V, log_decay, 4)
+    B, H, L, dk = Q.shape
+    dv = V.shape[3]
+    sshape = (B, H, dk, dv)
+    if out is None:
+        out = torch.empty_like(V)
+    if return_state and state_out is None:
+        state_out = torch.empty(sshape, dtype=torch.float32, device=Q.device)
+    _require_like(out, V.shape, V.dtype, "out")
+    _require_like(lengths, (B,), torch.int32, "lengths")
+    _require_like(state_in, sshape, torch.float32, "state_in")
+    _require_like(state_out, sshape, torch.float32, "state_out")
+    _require_here(Q, K, V, log_decay, lengths, out, state_in, state_out)
+    _require_whole(log_decay, lengths, state_in, state_out)
+    c = _decay_call(B, H, L, dk, dv, _dtype_code(Q.dtype), float(scale),
+                    (_row_strides(Q, "Q"), _row_strides(K, "K"), _row_strides(V, "V"),
+                     _row_strides(out, "out")))
+    ws, nbytes = _decay_workspace(c.workspace(0), workspace)
+    _check(lib().favor_attn_decay(c.ref, _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay),
+                                  _ptr(lengths), _ptr(out), _ptr(state_in), _ptr(state_out),
+                                  _ptr(ws), nbytes, _stream(stream)))
+    return (out, state_out) if return_state else out
+
+
+@_on_stream
+def attn_decay_backward(Q, K, V, log_decay, dout, scale=1.0, lengths=None, state_in=None,
+                        dstate_out=None, return_state_grad=False, dQ=None, dK=None, dV=None,
+                        dstate_in=None, workspace=None, stream=None):
+    """Gradients of attn_decay (favor_attn_decay_backward). dout: the gradient of out, and
+    dstate_out (default zeros) of state_out. log_decay receives none; an expanded input's
+    gradients come for every head and batch entry.
+
+    Returns (dQ, dK, dV), or (dQ, dK, dV, dstate_in) when return_state_grad is true.
+    """
+    torch = _torch()
+    _decay_shapes(Q, K, V, log_decay, 4)
+    B, H, L, dk = Q.shape
+    dv = V.shape[3]
+    sshape = (B, H, dk, dv)
+    grads = []
+    for name, t, x in (("dQ", dQ, Q), ("dK", dK, K), ("dV", dV, V)):
+        if t is None:
+            t = torch.empty_like(x)
+        _require_like(t, x.shape, x.dtype, name)
+        grads.append(t)
+    dQ, dK, dV = grads
+    if return_state_grad and dstate_in is None:
+        dstate_in = torch.empty(sshape, dtype=torch.float32, device=Q.device)
+    _require_like(dout, V.shape, V.dtype, "dout")
+    _require_like(lengths, (B,), torch.int32, "lengths")
+    for name, t in (("state_in", state_in), ("dstate_out", dstate_out),
+                    ("dstate_in", dstate_in)):
+        _require_like(t, sshape, torch.float32, name)
+    _require_here(Q, K, V, log_decay, lengths, dout, dQ, dK, dV, state_in, dstate_out, dstate_in)
+    _require_whole(log_decay, lengths, state_in, dstate_out, dstate_in)
+    c = _decay_call(B, H, L, dk, dv, _dtype_code(Q.dtype), float(scale),
+                    (_row_strides(Q, "Q"), _row_strides(K, "K"), _row_strides(V, "V"), (0, 0, 0),
+                     _row_strides(dout, "dout"), _row_strides(dQ, "dQ"), _row_strides(dK, "dK"),
+                     _row_strides(dV, "dV")))
+    ws, nbytes = _decay_workspace(c.workspace(1), workspace)
+    _check(lib().favor_attn_decay_backward(
+        c.ref, _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(lengths), _ptr(state_in),
+        _ptr(dout), _ptr(dstate_out), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(dstate_in), _ptr(ws),
+        nbytes, _stream(stream)))
+    return (dQ, dK, dV, dstate_in) if return_state_grad else (dQ, dK, dV)
+
+
+@_on_stream
+def attn_decay_step(q, k, v, log_decay, state, scale=1.0, slots=None, out=None, stream=None):
+    """The next token of B sequences (favor_attn_decay_step): state <- a state + k v^T in
+    place, out = scale q state.
+
+    q, k [B, H, dk], v [B, H, dv] (rows contiguous, any other strides); state
+    [n, H, dk, dv] float32. slots [B] int32: the place of each sequence's state (default:
+    its own index); one outside 0 .. n - 1 is padding and gives out = 0. Returns out
+    [B, H, dv].
+    """
+    torch = _torch()
+    _decay_shapes(q, k, v, log_decay, 3)
+    B, H, dk = q.shape
+    dv = v.shape[2]
+    if state.dim() != 4:
+        raise FavorError(1, f"state must be [n, H, dk, dv], got {tuple(state.shape)}")
+    _require_like(state, (state.shape[0], H, dk, dv), torch.float32, "state")
+    _require_like(slots, (B,), torch.int32, "slots")
+    if out is None:
+        out = torch.empty((B, H, dv), dtype=v.dtype, device=v.device)
+    _require_like(out, v.shape, v.dtype, "out")
+    _require_here(q, k, v, log_decay, state, slots, out)
+    _require_whole(log_decay, state, slots)
+    c = _decay_call(B, H, 1, dk, dv, _dtype_code(q.dtype), float(scale),
+                    (_row_strides(q, "q"), _row_strides(k, "k"), _row_strides(v, "v"),
+                     _row_strides(out, "out")))
+    _check(lib().favor_attn_decay_step(c.ref, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay),
+                                       _ptr(slots), state.shape[0], _ptr(state), _ptr(out),
+                                       _stream(stream)))
+    return out
+
+
+# ------------------------------------------------------------------------------- dropout
+@_on_stream
+def dropout(x, p, seed=0, offset=0, residual=None, out=None, rng=None, stream=None):
+    """residual + x with a share p of its elements dropped and the others divided by
+    1 - p (favor_dropout; p to 16 bits). The mask is Philox4x32-10's at (seed, offset) and
+    is not stored: advance offset from call to call, and give dropout_backward the same.
+    rng: a device tensor of two int64 words {seed, offset} read in their place when the
+    kernel runs (for captured graphs). out may be x or residual.
+    """
+    torch = _torch()
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    _require_like(residual, x.shape, x.dtype, "residual")
+    _require_like(out, x.shape, x.dtype, "out")
+    if rng is not None and (rng.shape != (2,) or rng.dtype not in (torch.int64, torch.uint64)):
+        raise FavorError(1, f"rng must be two 64-bit words, got {tuple(rng.shape)} {rng.dtype}")
+    _require_here(x, residual, out, rng)
+    _require_cuda(x, residual, out, rng)
+    for name, v in (("seed", seed), ("offset", offset)):
+        if not 0 <= operator.index(v) < 1 << 64:
+            raise FavorError(1, f"{name} must be a 64-bit unsigned number, got {v}")
+    _check(lib().favor_dropout(_ptr(x), _ptr(residual), _ptr(out), x.numel(),
+                               _dtype_code(x.dtype), float(p), seed, offset, _ptr(rng),
+                               _stream(stream)))
+    return out
+
+
+def dropout_backward(dout, p, seed=0, offset=0, dx=None, rng=None, stream=None):
+    """The gradient of dropout's x (its residual's is dout): the same mask on dout."""
+    return dropout(dout, p, seed, offset, out=dx, rng=rng, stream=stream)

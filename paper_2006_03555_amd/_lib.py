@@ -44,6 +44,21 @@ class FavorDesc(ctypes.Structure):
     ]
 
 
+class FavorStrides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class FavorDecayDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32),
+        ("dk", ctypes.c_int32), ("dv", ctypes.c_int32),
+        ("dtype", ctypes.c_int), ("scale", ctypes.c_float),
+        ("q", FavorStrides), ("k", FavorStrides), ("v", FavorStrides), ("out", FavorStrides),
+        ("grad_out", FavorStrides), ("grad_q", FavorStrides), ("grad_k", FavorStrides),
+        ("grad_v", FavorStrides),
+    ]
+
+
 def lib_path():
     return os.environ.get("FAVOR_LIBRARY", os.path.join(_HERE, "libfavor.so"))
 
@@ -60,6 +75,7 @@ def lib():
     L = ctypes.CDLL(path)
     vp, i32, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
     dp = ctypes.POINTER(FavorDesc)
+    ddp, i64 = ctypes.POINTER(FavorDecayDesc), ctypes.c_int64
     sig = {
         "favor_orf_draw": (ctypes.c_int, [u64, i32, i32, i32, ctypes.c_int, vp, vp, vp]),
         "favor_feature_map": (ctypes.c_int, [dp, vp, vp, vp, vp, vp]),
@@ -87,6 +103,15 @@ def lib():
                                                     vp, vp, vp, vp, i32, vp, vp, vp, vp, vp,
                                                     vp, sz, vp]),
         "favor_validate_desc": (ctypes.c_int, [dp, ctypes.c_int]),
+        "favor_decay_workspace_size": (sz, [ddp, ctypes.c_int]),
+        "favor_attn_decay": (ctypes.c_int,
+                             [ddp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "favor_attn_decay_backward": (ctypes.c_int, [ddp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                                     vp, vp, vp, vp, sz, vp]),
+        "favor_attn_decay_step": (ctypes.c_int, [ddp, vp, vp, vp, vp, vp, i32, vp, vp, vp]),
+        "favor_validate_decay_desc": (ctypes.c_int, [ddp, ctypes.c_int]),
+        "favor_dropout": (ctypes.c_int, [vp, vp, vp, i64, ctypes.c_int, ctypes.c_double, u64, u64,
+                                         vp, vp]),
         "favor_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "favor_last_error": (ctypes.c_char_p, []),
         "favor_abi_version": (i32, []),
@@ -131,6 +156,25 @@ def make_desc(B, H, L, d, M, in_dtype, out_dtype, input_scale, denom_eps=0.0, se
 
 def validate_desc(g, op):
     return lib().favor_validate_desc(ctypes.byref(g), op)
+
+
+def make_decay_desc(B, H, L, dk, dv, dtype, scale=1.0, **strides):
+    """Descriptor of the decayed linear attention; strides: (batch, head, token) element
+    strides by field (q, k, v, out, grad_out, grad_q, grad_k, grad_v), those not given
+    contiguous."""
+    g = FavorDecayDesc(B, H, L, dk, dv, dtype, float(scale))
+    for name, s in strides.items():
+        setattr(g, name, FavorStrides(*s))
+    return g
+
+
+def validate_decay_desc(g, op):
+    """op: 0 forward, 1 backward, 2 single tokens."""
+    return lib().favor_validate_decay_desc(ctypes.byref(g), op)
+
+
+def decay_workspace_size(g, backward=False):
+    return lib().favor_decay_workspace_size(ctypes.byref(g), 1 if backward else 0)
 
 
 def backward_workspace_size(g, causal):

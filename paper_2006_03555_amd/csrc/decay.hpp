@@ -1,0 +1,80 @@
+// decay.hpp - launchers of the decayed linear attention and the dropout (internal to
+// libfavor; decay.hip, decay_step.hip, dropout.hip; called from decay_api.cpp).
+#pragma once
+
+#include "kernels.hpp"
+
+namespace favor {
+
+// Element strides of a [B][H][L][d] tensor whose rows are contiguous.
+struct Rows {
+  int64_t b, h, t;
+};
+
+// One scan over a sequence per (batch, head), in one of two time orders (r = the row's
+// place in the scan's order, a = the head's decay, n = the sequence's length):
+//   o_r = row_scale a^(r + shift) q_r X_0 + pair_scale sum_{s <= r} a^(r - s) (q_r . k_s) v_s
+//   X_n = a^n X_0 + sum_s sum_scale a^(n - shift - s) k_s v_s^T
+// The forward pass is (q, k, v) with shift 1, X the state after the last token; dQ is
+// (dout, V, K) on the transposed state; dV is (K, Q, dout) and dK (V, dout, Q) in
+// reversed order with shift 0, X the state's gradient with its decay applied.
+struct DecayScan {
+  const void *q, *k, *v;   // kd, kd and vd columns
+  void *o;                 // vd columns
+  Rows qs, ks, vs, os;
+  const float *log_decay;  // [H]
+  const int32_t *lengths;  // [B], or null: every sequence has L tokens
+  const float *x_in;       // X_0 [BH][kd][vd] (x_t: [BH][vd][kd]), or null for zeros
+  float *x_out;            // X_n in the same layout, or null
+  float *part;             // [BH][nseg - 1][slices][X of a slice]: sums, then prefixes
+  int x_t;
+  int BH, H, L, kd, vd;
+  int seg_len, nseg;       // segments of seg_len rows (a multiple of 64)
+  int reverse, shift;
+  float pair_scale, row_scale, sum_scale;
+};
+
+// Columns of v that one workgroup takes, and slices of them; floats of one slice's X in
+// the workspace.
+int decay_slice(int kd, int vd);
+inline int decay_slices(int kd, int vd) {
+  const int s = decay_slice(kd, vd);
+  return (vd + s - 1) / s;
+}
+inline size_t decay_slice_floats(int kd, int vd) {
+  return (size_t)(kd <= 64 ? 64 : kd <= 128 ? 128 : 256) * decay_slice(kd, vd);
+}
+
+// The sums of every segment but the last, in part.
+hipError_t launch_decay_sums(const DecayScan &a, Dt dt, hipStream_t st);
+// part: from each segment's sums to X before the segment that follows it.
+hipError_t launch_decay_prefix(const DecayScan &a, hipStream_t st);
+// The rows, each segment from the X before it.
+hipError_t launch_decay_scan(const DecayScan &a, Dt dt, hipStream_t st);
+
+// One token of B sequences on the states [n_slots][H][dk][dv], in place.
+struct DecayStep {
+  const void *q, *k, *v;
+  void *o;
+  Rows qs, ks, vs, os;     // t unused
+  const float *log_decay;
+  const int32_t *slots;    // [B] places of the sequences' states, or null: b
+  float *state;
+  int n_slots;
+  int B, H, dk, dv;
+  float scale;
+};
+hipError_t launch_decay_step(const DecayStep &a, Dt dt, hipStream_t st);
+
+struct Dropout {
+  const void *x, *residual;   // residual nullable
+  void *y;
+  int64_t n;
+  uint32_t threshold;         // of 2^16: an element stays if its 16 bits are not below
+  float scale;                // of the elements that stay
+  uint64_t seed, offset;
+  const uint64_t *rng;        // {seed, offset} in device memory, or null
+};
+hipError_t launch_dropout(const Dropout &a, Dt dt, hipStream_t st);
+
+}  // namespace favor

@@ -1,0 +1,427 @@
+// decay_api.cpp - the C ABI of the decayed linear attention and the dropout: argument
+// validation, workspace sizing, launch planning and dispatch. As in favor_api.cpp,
+// validation is plain host code that touches no device.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+
+#include "../../include/favor.h"
+#include "decay.hpp"
+
+namespace {
+
+using favor::DecayScan;
+using favor::Rows;
+
+favor_status fail(favor_status st, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  return favor::report(st, buf);
+}
+favor_status ok() { return favor::report(FAVOR_OK, ""); }
+
+#define FAVOR_TRY(expr)                \
+  do {                                 \
+    favor_status st__ = (expr);        \
+    if (st__ != FAVOR_OK) return st__; \
+  } while (0)
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+// The integer in an enum-typed field (a C caller may store any int there).
+int raw_enum(const void *p) {
+  int v;
+  std::memcpy(&v, p, sizeof v);
+  return v;
+}
+
+favor_status check_ptr(const void *p, const char *name, bool needed, size_t align = 16) {
+  if (!needed) return FAVOR_OK;
+  if (!p) return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s is NULL", name);
+  if (!aligned(p, align))
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s is not %zu-byte aligned", name, align);
+  return FAVOR_OK;
+}
+favor_status check_optional(const void *p, const char *name, size_t align = 16) {
+  return check_ptr(p, name, p != nullptr, align);
+}
+
+favor_status device_result(hipError_t e, const char *what) {
+  if (e != hipSuccess) return fail(FAVOR_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
+  return ok();
+}
+
+constexpr int kMaxL = 1 << 30;
+constexpr int64_t kMaxStride = (int64_t)1 << 46;   // element offsets stay within 64 bits
+enum Op { kOpForward = 0, kOpBackward = 1, kOpStep = 2 };
+
+struct Tensor {
+  const char *name;
+  const favor_strides *s;
+  int d;
+  bool out;
+};
+
+// Strides of one tensor; dimensions of size 1 or less have none.
+favor_status check_strides(const favor_decay_desc *g, const Tensor &t, int op) {
+  const int64_t size[3] = {g->B, g->H, op == kOpStep ? 1 : g->L};
+  const int64_t stride[3] = {t.s->batch, t.s->head, t.s->token};
+  const int unit = raw_enum(&g->dtype) == FAVOR_BF16 ? 8 : 4;
+  if (!stride[0] && !stride[1] && !stride[2]) return FAVOR_OK;   // contiguous
+  int64_t reach = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (size[i] <= 1) continue;
+    if (stride[i] < 0)
+      return fail(FAVOR_ERR_INVALID_ARGUMENT, "a stride of %s is negative", t.name);
+    if (stride[i] % unit != 0)
+      return fail(FAVOR_ERR_INVALID_ARGUMENT,
+                  "strides of %s must be multiples of 16 bytes (%d elements)", t.name, unit);
+    if (stride[i] > kMaxStride / (size[i] - 1) || (reach += stride[i] * (size[i] - 1)) > kMaxStride)
+      return fail(FAVOR_ERR_UNSUPPORTED, "%s reaches past 2^46 elements", t.name);
+  }
+  if (!t.out) return FAVOR_OK;
+  // rows written must not share elements: taken by stride, each dimension steps over
+  // everything inside it
+  int at[3] = {0, 1, 2};
+  std::sort(at, at + 3, [&](int i, int j) { return stride[i] < stride[j]; });
+  int64_t inner = t.d;
+  for (int i : at) {
+    if (size[i] <= 1) continue;
+    if (stride[i] < inner)
+      return fail(FAVOR_ERR_INVALID_ARGUMENT, "rows of %s overlap", t.name);
+    inner += stride[i] * (size[i] - 1);
+  }
+  return FAVOR_OK;
+}
+
+favor_status validate(const favor_decay_desc *g, int op) {
+  if (!g) return fail(FAVOR_ERR_INVALID_ARGUMENT, "descriptor is NULL");
+  if (op < kOpForward || op > kOpStep)
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "unknown operation %d", op);
+  if (g->B < 0 || g->H < 0 || g->L < 0)
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "negative size B=%d H=%d L=%d", g->B, g->H, g->L);
+  if (g->dk <= 0 || g->dv <= 0)
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "dk=%d and dv=%d must be positive", g->dk, g->dv);
+  const int dt = raw_enum(&g->dtype);
+  if (dt != FAVOR_F32 && dt != FAVOR_BF16)
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "unknown dtype %d", dt);
+  if (!std::isfinite(g->scale))
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "scale must be finite");
+  if (g->L > kMaxL) return fail(FAVOR_ERR_UNSUPPORTED, "L=%d exceeds 2^30", g->L);
+  if (g->dk % 8 != 0 || g->dv % 8 != 0 || g->dk > 256 || g->dv > 256)
+    return fail(FAVOR_ERR_UNSUPPORTED,
+                "dk=%d dv=%d not supported (multiples of 8, at most 256)", g->dk, g->dv);
+  const long long bh = (long long)g->B * g->H;
+  if (bh > 65535) return fail(FAVOR_ERR_UNSUPPORTED, "B*H=%lld exceeds 65535", bh);
+  const Tensor ts[] = {{"Q", &g->q, g->dk, false},      {"K", &g->k, g->dk, false},
+                       {"V", &g->v, g->dv, false},      {"out", &g->out, g->dv, op != kOpBackward},
+                       {"dout", &g->grad_out, g->dv, false}, {"dQ", &g->grad_q, g->dk, true},
+                       {"dK", &g->grad_k, g->dk, true}, {"dV", &g->grad_v, g->dv, true}};
+  for (int i = 0; i < 8; ++i) {
+    if (i == 3 ? op == kOpBackward : i > 3 && op != kOpBackward) continue;
+    FAVOR_TRY(check_strides(g, ts[i], op));
+  }
+  return FAVOR_OK;
+}
+
+Rows rows_of(const favor_decay_desc *g, const favor_strides &s, int d) {
+  if (!s.batch && !s.head && !s.token)
+    return {(int64_t)g->H * g->L * d, (int64_t)g->L * d, d};
+  return {g->B > 1 ? s.batch : 0, g->H > 1 ? s.head : 0, g->L > 1 ? s.token : 0};
+}
+
+favor::Dt dt_of(const favor_decay_desc *g) {
+  return raw_enum(&g->dtype) == FAVOR_BF16 ? favor::Dt::BF16 : favor::Dt::F32;
+}
+
+// Segments of one scan with kd k columns and vd value columns: enough workgroups for two
+// on each of the 256 compute units, of at least 256 rows each.
+constexpr int kTargetWorkgroups = 512;
+constexpr int kMinRows = 256;
+
+void plan(DecayScan &a) {
+  const int tiles = std::max(1, (a.L + 63) / 64);
+  const int slices = favor::decay_slices(a.kd, a.vd);
+  const int have = a.BH * slices;
+  int want = (kTargetWorkgroups + have - 1) / have;
+  want = std::max(1, std::min(want, tiles / (kMinRows / 64)));
+  const int per = (tiles + want - 1) / want;
+  a.seg_len = 64 * per;
+  a.nseg = (tiles + per - 1) / per;
+}
+
+size_t part_bytes(const DecayScan &a) {
+  return round_up((size_t)a.BH * (a.nseg - 1) * favor::decay_slices(a.kd, a.vd) *
+                      favor::decay_slice_floats(a.kd, a.vd) * sizeof(float),
+                  256);
+}
+
+// A scan's shape (its tensors come later).
+DecayScan shape_of(const favor_decay_desc *g, bool swapped) {
+  DecayScan a{};
+  a.BH = g->B * g->H;
+  a.H = g->H;
+  a.L = g->L;
+  a.kd = swapped ? g->dv : g->dk;
+  a.vd = swapped ? g->dk : g->dv;
+  plan(a);
+  return a;
+}
+
+// Workspace of a call: the forward pass has one scan, the backward pass dV like it and dQ
+// and dK on the transposed state. They run one after another in the same memory.
+size_t workspace_of(const favor_decay_desc *g, int op) {
+  if ((long long)g->B * g->H == 0 || g->L == 0) return 0;
+  const size_t n = part_bytes(shape_of(g, false));
+  return op == kOpBackward ? std::max(n, part_bytes(shape_of(g, true))) : n;
+}
+
+favor_status check_workspace(const void *ws, size_t bytes, size_t need) {
+  if (need == 0) return FAVOR_OK;
+  if (!ws) return fail(FAVOR_ERR_INVALID_ARGUMENT, "workspace is NULL");
+  if (!aligned(ws, 256))
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "workspace is not 256-byte aligned");
+  if (bytes < need)
+    return fail(FAVOR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu bytes, need %zu", bytes, need);
+  return FAVOR_OK;
+}
+
+favor_status run_scan(const DecayScan &a, favor::Dt dt, hipStream_t st, const char *what) {
+  hipError_t e = hipSuccess;
+  if (a.nseg > 1) {
+    {
+      favor::LaunchTimer t(favor::kKerDecaySums, st);
+      e = favor::launch_decay_sums(a, dt, st);
+    }
+    if (e != hipSuccess) return device_result(e, what);
+    favor::LaunchTimer t(favor::kKerDecayPrefix, st);
+    e = favor::launch_decay_prefix(a, st);
+    if (e != hipSuccess) return device_result(e, what);
+  }
+  favor::LaunchTimer t(favor::kKerDecayScan, st);
+  e = favor::launch_decay_scan(a, dt, st);
+  return device_result(e, what);
+}
+
+}  // namespace
+
+extern "C" {
+
+favor_status favor_validate_decay_desc(const favor_decay_desc *g, int op) {
+  FAVOR_TRY(validate(g, op));
+  return ok();
+}
+
+size_t favor_decay_workspace_size(const favor_decay_desc *g, int backward) {
+  const int op = backward ? kOpBackward : kOpForward;
+  if (validate(g, op) != FAVOR_OK) return 0;
+  return workspace_of(g, op);
+}
+
+favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q, const void *K,
+                              const void *V, const float *log_decay, const int32_t *lengths,
+                              void *out, const float *state_in, float *state_out, void *ws,
+                              size_t ws_bytes, hipStream_t stream) {
+  FAVOR_TRY(validate(g, kOpForward));
+  const bool heads = (long long)g->B * g->H > 0, work = heads && g->L > 0;
+  const void *ptrs[] = {Q, K, V, out};
+  const char *names[] = {"Q", "K", "V", "out"};
+  for (int i = 0; i < 4; ++i) FAVOR_TRY(check_ptr(ptrs[i], names[i], work));
+  FAVOR_TRY(check_ptr(log_decay, "log_decay", heads, 4));
+  FAVOR_TRY(check_optional(lengths, "lengths", 4));
+  FAVOR_TRY(check_optional(state_in, "state_in"));
+  FAVOR_TRY(check_optional(state_out, "state_out"));
+  if (work && (out == Q || out == K || out == V))
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "out must not be an input");
+  if (!heads || (!work && !state_out)) return ok();
+  FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g, kOpForward)));
+  DecayScan a = shape_of(g, false);
+  a.q = Q;
+  a.k = K;
+  a.v = V;
+  a.o = out;
+  a.qs = rows_of(g, g->q, g->dk);
+  a.ks = rows_of(g, g->k, g->dk);
+  a.vs = rows_of(g, g->v, g->dv);
+  a.os = rows_of(g, g->out, g->dv);
+  a.log_decay = log_decay;
+  a.lengths = lengths;
+  a.x_in = state_in;
+  a.x_out = state_out;
+  a.part = static_cast<float *>(ws);
+  a.shift = 1;
+  a.pair_scale = a.row_scale = g->scale;
+  a.sum_scale = 1.f;
+  return run_scan(a, dt_of(g), stream, "favor_attn_decay");
+}
+
+favor_status favor_attn_decay_backward(const favor_decay_desc *g, const void *Q, const void *K,
+                                       const void *V, const float *log_decay,
+                                       const int32_t *lengths, const float *state_in,
+                                       const void *dout, const float *dstate_out, void *dQ,
+                                       void *dK, void *dV, float *dstate_in, void *ws,
+                                       size_t ws_bytes, hipStream_t stream) {
+  FAVOR_TRY(validate(g, kOpBackward));
+  const bool heads = (long long)g->B * g->H > 0, work = heads && g->L > 0;
+  const void *ptrs[] = {Q, K, V, dout, dQ, dK, dV};
+  const char *names[] = {"Q", "K", "V", "dout", "dQ", "dK", "dV"};
+  for (int i = 0; i < 7; ++i) FAVOR_TRY(check_ptr(ptrs[i], names[i], work));
+  FAVOR_TRY(check_ptr(log_decay, "log_decay", heads, 4));
+  FAVOR_TRY(check_optional(lengths, "lengths", 4));
+  FAVOR_TRY(check_optional(state_in, "state_in"));
+  FAVOR_TRY(check_optional(dstate_out, "dstate_out"));
+  FAVOR_TRY(check_optional(dstate_in, "dstate_in"));
+  if (work)
+    for (int o = 4; o < 7; ++o)
+      for (int i = 0; i < o; ++i)
+        if (ptrs[o] == ptrs[i])
+          return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s must not be %s", names[o], names[i]);
+  if (!heads || (!work && !dstate_in)) return ok();
+  FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g, kOpBackward)));
+  const favor::Dt dt = dt_of(g);
+  const Rows qs = rows_of(g, g->q, g->dk), ks = rows_of(g, g->k, g->dk),
+             vs = rows_of(g, g->v, g->dv), ds = rows_of(g, g->grad_out, g->dv);
+  const auto scan = [&](bool swapped) {
+    DecayScan a = shape_of(g, swapped);
+    a.log_decay = log_decay;
+    a.lengths = lengths;
+    a.part = static_cast<float *>(ws);
+    a.x_t = swapped;
+    a.pair_scale = g->scale;
+    return a;
+  };
+  if (work) {
+    DecayScan a = scan(true);   // dQ: queries dout, keys V, values K
+    a.q = dout;
+    a.k = V;
+    a.v = K;
+    a.o = dQ;
+    a.qs = ds;
+    a.ks = vs;
+    a.vs = ks;
+    a.os = rows_of(g, g->grad_q, g->dk);
+    a.x_in = state_in;
+    a.shift = 1;
+    a.row_scale = g->scale;
+    a.sum_scale = 1.f;
+    FAVOR_TRY(run_scan(a, dt, stream, "favor_attn_decay_backward dQ"));
+    a = scan(true);             // dK: queries V, keys dout, values Q, from the last token
+    a.q = V;
+    a.k = dout;
+    a.v = Q;
+    a.o = dK;
+    a.qs = vs;
+    a.ks = ds;
+    a.vs = qs;
+    a.os = rows_of(g, g->grad_k, g->dk);
+    a.x_in = dstate_out;
+    a.reverse = 1;
+    a.row_scale = 1.f;
+    a.sum_scale = g->scale;
+    FAVOR_TRY(run_scan(a, dt, stream, "favor_attn_decay_backward dK"));
+  }
+  DecayScan a = scan(false);    // dV: queries K, keys Q, values dout, from the last token
+  a.q = K;
+  a.k = Q;
+  a.v = dout;
+  a.o = dV;
+  a.qs = ks;
+  a.ks = qs;
+  a.vs = ds;
+  a.os = rows_of(g, g->grad_v, g->dv);
+  a.x_in = dstate_out;
+  a.x_out = dstate_in;
+  a.reverse = 1;
+  a.row_scale = 1.f;
+  a.sum_scale = g->scale;
+  return run_scan(a, dt, stream, "favor_attn_decay_backward dV");
+}
+
+favor_status favor_attn_decay_step(const favor_decay_desc *g, const void *Q, const void *K,
+                                   const void *V, const float *log_decay, const int32_t *slots,
+                                   int32_t n_slots, float *state, void *out,
+                                   hipStream_t stream) {
+  FAVOR_TRY(validate(g, kOpStep));
+  if (n_slots < 0) return fail(FAVOR_ERR_INVALID_ARGUMENT, "n_slots=%d is negative", n_slots);
+  if (!slots && n_slots < g->B)
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "%d sequences have only %d states", g->B, n_slots);
+  const bool work = (long long)g->B * g->H > 0;
+  const void *ptrs[] = {Q, K, V, out};
+  const char *names[] = {"Q", "K", "V", "out"};
+  for (int i = 0; i < 4; ++i) FAVOR_TRY(check_ptr(ptrs[i], names[i], work));
+  FAVOR_TRY(check_ptr(state, "state", work && n_slots > 0));
+  FAVOR_TRY(check_ptr(log_decay, "log_decay", work, 4));
+  FAVOR_TRY(check_optional(slots, "slots", 4));
+  if (work && (out == Q || out == K || out == V))
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "out must not be an input");
+  if (!work) return ok();
+  favor_decay_desc one = *g;
+  one.L = 1;
+  favor::DecayStep a{};
+  a.q = Q;
+  a.k = K;
+  a.v = V;
+  a.o = out;
+  a.qs = rows_of(&one, g->q, g->dk);
+  a.ks = rows_of(&one, g->k, g->dk);
+  a.vs = rows_of(&one, g->v, g->dv);
+  a.os = rows_of(&one, g->out, g->dv);
+  a.log_decay = log_decay;
+  a.slots = slots;
+  a.state = state;
+  a.n_slots = n_slots;
+  a.B = g->B;
+  a.H = g->H;
+  a.dk = g->dk;
+  a.dv = g->dv;
+  a.scale = g->scale;
+  hipError_t e;
+  {
+    favor::LaunchTimer t(favor::kKerDecayStep, stream);
+    e = favor::launch_decay_step(a, dt_of(g), stream);
+  }
+  return device_result(e, "favor_attn_decay_step");
+}
+
+favor_status favor_dropout(const void *x, const void *residual, void *y, int64_t n,
+                           favor_dtype dtype, double p, uint64_t seed, uint64_t offset,
+                           const uint64_t *rng, hipStream_t stream) {
+  const int dt = raw_enum(&dtype);
+  if (n < 0) return fail(FAVOR_ERR_INVALID_ARGUMENT, "n=%lld is negative", (long long)n);
+  if (dt != FAVOR_F32 && dt != FAVOR_BF16)
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "unknown dtype %d", dt);
+  if (!(p >= 0.0 && p <= 1.0))
+    return fail(FAVOR_ERR_INVALID_ARGUMENT, "p=%g is not between 0 and 1", p);
+  if (n > ((int64_t)1 << 60)) return fail(FAVOR_ERR_UNSUPPORTED, "n exceeds 2^60");
+  FAVOR_TRY(check_ptr(x, "x", n > 0));
+  FAVOR_TRY(check_ptr(y, "y", n > 0));
+  FAVOR_TRY(check_optional(residual, "residual"));
+  FAVOR_TRY(check_optional(rng, "rng", 8));
+  if (n == 0) return ok();
+  favor::Dropout a{};
+  a.x = x;
+  a.residual = residual;
+  a.y = y;
+  a.n = n;
+  a.threshold = (uint32_t)std::nearbyint(p * 65536.0);
+  a.scale = a.threshold < 65536 ? (float)(65536.0 / (65536 - a.threshold)) : 0.f;
+  a.seed = seed;
+  a.offset = offset;
+  a.rng = rng;
+  hipError_t e;
+  {
+    favor::LaunchTimer t(favor::kKerDropout, stream);
+    e = favor::launch_dropout(a, dt == FAVOR_BF16 ? favor::Dt::BF16 : favor::Dt::F32, stream);
+  }
+  return device_result(e, "favor_dropout");
+}
+
+}  // extern "C"

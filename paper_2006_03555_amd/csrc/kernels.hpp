@@ -194,6 +194,11 @@ enum KernelId {
   kKerBwdAgg,
   kKerSuffixScan,
   kKerBwdDkv,
+  kKerDecaySums,
+  kKerDecayPrefix,
+  kKerDecayScan,
+  kKerDecayStep,
+  kKerDropout,
   kNumKernels
 };
 const char *kernel_name(int k);

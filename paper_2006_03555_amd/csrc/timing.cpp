@@ -25,7 +25,9 @@ int64_t g_count[kNumKernels] = {};
 const char *const kNames[kNumKernels] = {"k_orf_draw",   "k_feature_map", "k_kside",
                                          "k_finalize",   "k_qside",       "k_seg_scan",
                                          "k_causal",     "k_sum_splits",  "k_bwd_dq",
-                                         "k_kside_agg",  "k_suffix_scan", "k_bwd_dkv"};
+                                         "k_kside_agg",  "k_suffix_scan", "k_bwd_dkv",
+                                         "k_decay_sums", "k_decay_prefix", "k_decay_scan",
+                                         "k_decay_step", "k_dropout"};
 
 hipEvent_t take_event() {
   if (!g_pool.empty()) {
