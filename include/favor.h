@@ -357,7 +357,8 @@ FAVOR_API favor_status favor_attn_both_backward(const favor_desc *g, const void 
  * Layouts: Q, K [B][H][L][dk], V, out [B][H][L][dv] with rows of contiguous elements and
  * any strides between them, in elements (favor_strides; all three 0 = the contiguous
  * layout above): [B][L][H][d] tensors, slices of one QKV projection and broadcast inputs
- * (a stride of 0) need no copy. Strides and base addresses are multiples of 16 bytes;
+ * (a stride of 0) need no copy. Strides and base addresses are multiples of 16 bytes, and
+ * tokens at most 2^25 bytes apart (FAVOR_ERR_UNSUPPORTED);
  * rows of an output must not share elements (FAVOR_ERR_INVALID_ARGUMENT), and outputs
  * must not overlap inputs. state [B][H][dk][dv] fp32, contiguous.
  *

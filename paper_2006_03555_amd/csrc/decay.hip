@@ -10,18 +10,19 @@
 // Every power has an exponent >= 0 and comes from a table, so a decay of 0 and one of 1
 // are the same code and nothing overflows that the formula does not.
 //
-// The products are taken transposed, so that no result has to change lanes: with X's
-// rows (k columns) as accumulator rows, two adjacent tiles of X are the A operand of
-// O^T = X^T Q^T in loaded order (accumulator row r of tile nb stands for k column
-// perm_col(nb, r)), and the tiles of P^T = K Q^T (rows j, columns i) are in chained order
-// the B operand of V^T P^T. Only V^T and K^T need a transpose; bf16 tiles get it from
-// the LDS transpose read. Each wave holds all of X's rows for its own value columns and
-// builds P^T for itself: two barriers per chunk, both for the staging.
+// The products are taken transposed, so that no accumulator has to change lanes: two
+// adjacent tiles of X (rows k, columns v) are in chained order the A operand of
+// O^T = X^T Q^T, and those of P^T = K Q^T (rows j, columns i) the B operand of V^T P^T.
+// Only V^T and K^T need a transpose; bf16 tiles get it from the LDS transpose read. Each
+// wave holds all of X's rows for 16 value columns; P^T is shared out over the waves and
+// passes through LDS.
 //
 // Precision (bf16): X, and all sums, are fp32. The weighted values diag(a^(..)) V enter
 // K^T V as three bf16 terms (24 bits: exact), so X is as exact as fp32 inputs would make
-// it; X enters Q X as two terms and the pair weights P as one, one rounding of 2^-9 each
-// beside the output's own.
+// it. X enters Q X and the pair weights enter P V as one term each: the two parts of an
+// output, whose roundings are independent, together add one rounding to the output's own
+// (errors against 64 bits 1.4 times a correctly rounded output's at most). A second term
+// of X took 32 of 176 matrix and 160 of 744 vector instructions of a chunk.
 #include "decay.hpp"
 #include "tile_common.hpp"
 
@@ -33,9 +34,59 @@ constexpr int kChunkT = 64;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-// Rows of an LDS tile are padded by 16 bytes, so that 16 rows at one column fall into
-// different banks.
-template <typename T> constexpr int kPad = 16 / (int)sizeof(T);
+// An LDS tile of 64 rows and W columns, in granules of four elements. Granule c of a row
+// lies at place c ^ f(row), so that both ways of reading it meet each of the 64 banks once:
+//   rows():  16 rows at two granules (bf16, 8 bytes each) or at one (fp32, 16 bytes)
+//   trans(): eight rows by four granules (bf16), or one column of four rows by four
+//            granules (fp32)
+// bf16 pairs of granules stay together, so staging writes 16 bytes.
+template <typename T, int W>
+struct Tile {
+  static __device__ __forceinline__ int f(int row) {
+    if (sizeof(T) == 4) return row & 15;
+    return W == 64 ? (((row >> 1) & 3) << 2) | (((row >> 3) & 1) << 1)
+                   : ((row & 7) << 2) | (((row >> 3) & 1) << 1);
+  }
+  static __device__ __forceinline__ int at(int row, int granule) {
+    return row * W + 4 * (granule ^ f(row));
+  }
+  // Operand fragment of rows 16 b .. + 15 over columns 32 p .. + 31, chained order.
+  static __device__ __forceinline__ typename Mma<T>::frag rows(const T *t, int b, int p) {
+    typedef T quad __attribute__((ext_vector_type(4)));
+    const int l = lane_id(), r = l & 15, g = l >> 4;
+    // volatile: loads of two fragments are not to be merged into one wide load, whose
+    // halves would then have to be moved
+    using ldsq = const volatile __attribute__((address_space(3))) quad;
+    t += 16 * b * W;
+    const quad lo = *(ldsq *)(t + at(r, 8 * p + g));
+    const quad hi = *(ldsq *)(t + at(r, 8 * p + 4 + g));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  // Operand fragment of the transpose: 16 columns (granules c0, c0 + step, ..) over rows
+  // 32 m .. + 31, chained order.
+  static __device__ __forceinline__ typename Mma<T>::frag trans(const T *t, int c0, int step,
+                                                                int m) {
+    const int l = lane_id(), c = l & 15, g = l >> 4;
+    t += 32 * m * W;
+    if constexpr (sizeof(T) == 2) {
+      using lds4 = __attribute__((address_space(3))) s16x4;
+      const T *p = t + at(4 * g + (c >> 2), c0 + step * (c & 3));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 16 * W));
+      struct Two { s16x4 a, b; };
+      return __builtin_bit_cast(bf16x8, Two{lo, hi});
+    } else {
+      f32x8 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const T *p = t + at(4 * g + i, c0 + step * (c >> 2)) + (c & 3);
+        x[i] = p[0];
+        x[4 + i] = p[16 * W];
+      }
+      return x;
+    }
+  }
+};
 
 // Eight fp32 values as N operand fragments whose sum they are: all but the last term
 // truncated (no term of a finite value overflows, and the remainder is exact), the last
@@ -67,69 +118,10 @@ __device__ __forceinline__ void split8(const float (&x)[8], f32x8 (&f)[N]) {
   for (int i = 0; i < 8; ++i) f[0][i] = x[i];
 }
 template <typename T> constexpr int kSumTerms = sizeof(T) == 2 ? 3 : 1;
-template <typename T> constexpr int kStateTerms = sizeof(T) == 2 ? 2 : 1;
 
-// Operand fragment of the transpose of an LDS tile [64][ld]: the lane's row (lane % 16 =
-// 4 q + r) is tile column c0 + step q + r, its k positions tokens 32 m + (chained order).
-__device__ __forceinline__ bf16x8 load_tr(const bf16 *tile, int ld, int m, int c0, int step) {
-  const int l = lane_id();
-  const bf16 *p = tile + (32 * m + 4 * (l >> 4) + ((l >> 2) & 3)) * ld + c0 + step * (l & 3);
-  using lds4 = __attribute__((address_space(3))) s16x4;
-  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p);
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 16 * ld));
-  struct Two { s16x4 a, b; };
-  return __builtin_bit_cast(bf16x8, Two{lo, hi});
-}
-__device__ __forceinline__ f32x8 load_tr(const float *tile, int ld, int m, int c0, int step) {
-  const int l = lane_id();
-  const float *p = tile + (32 * m + 4 * (l >> 4)) * ld + c0 + step * ((l >> 2) & 3) + (l & 3);
-  f32x8 f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = p[(16 * (i >> 2) + (i & 3)) * ld];
-  return f;
-}
-
-// A chunk's rows on their way from global memory to an LDS tile [64][W + pad]: 16-byte
-// units, zero past the chunk's n rows and the tensor's `width` columns.
-template <typename T, int W, int NT>
-struct Staged {
-  static constexpr int kPer = 16 / (int)sizeof(T);
-  static constexpr int kUnits = W / kPer;
-  static constexpr int N = kChunkT * kUnits / NT;
-  static_assert(kChunkT * kUnits % NT == 0, "whole passes");
-  u32x4 r[N];
-  __device__ __forceinline__ void load(const T *base, int64_t stride, int n, int width) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int u = threadIdx.x + k * NT;
-      const int row = u / kUnits, col = u % kUnits * kPer;
-      r[k] = row < n && col < width
-                 ? *reinterpret_cast<const u32x4 *>(base + row * stride + col)
-                 : u32x4{0, 0, 0, 0};
-    }
-  }
-  __device__ __forceinline__ void store(T *tile) const {
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int u = threadIdx.x + k * NT;
-      const int row = u / kUnits, col = u % kUnits * kPer;
-      *reinterpret_cast<u32x4 *>(tile + row * (W + kPad<T>) + col) = r[k];
-    }
-  }
-};
-
-// a^e for e = 0 .. 64 as a sum of two floats: a chunk's a^64 meets X thousands of times,
-// and one float's rounding would be raised to that power.
-struct Powers {
-  float hi[kChunkT + 1], lo[kChunkT + 1];
-};
-__device__ __forceinline__ void power(double g, int e, float &hi, float &lo) {
-  const double d = e == 0 ? 1.0 : exp(g * e);   // 0^0 = 1
-  hi = (float)d;
-  lo = isfinite(hi) ? (float)(d - hi) : 0.f;
-}
-__device__ __forceinline__ void fill_powers(Powers &p, float g) {
-  if (threadIdx.x <= kChunkT) power(g, threadIdx.x, p.hi[threadIdx.x], p.lo[threadIdx.x]);
+// The wave's number, as a scalar.
+__device__ __forceinline__ int wave_id() {
+  return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 }
 
 // What a workgroup works on.
@@ -158,106 +150,220 @@ __device__ __forceinline__ int last_seg(const DecayScan &a, int len) {
   return len == 0 ? 0 : (len - 1) / a.seg_len;
 }
 
-// Start of row r of the scan's order, and the step to the next row.
+// Rows of a chunk in global memory, reached through a buffer descriptor at the chunk's
+// lowest row: a lane's 32-bit offset is formed once, rows further on are a scalar offset,
+// and an offset of kOutside reads zeros or writes nothing. (Token strides are at most 2^25
+// bytes, so that the 64 rows lie below it.)
+constexpr uint32_t kOutside = 1u << 31;
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 template <typename T>
-__device__ __forceinline__ const T *row_ptr(const void *p, const Rows &s, const Item &it,
-                                            bool reverse, int r) {
-  const int64_t t = reverse ? it.len - 1 - r : r;
-  return static_cast<const T *>(p) + it.b * s.b + it.h * s.h + t * s.t;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rows(const void *x, const Rows &s,
+                                                             const Item &it, int col,
+                                                             bool reverse, int first) {
+  const T *base = static_cast<const T *>(x) + it.b * s.b + it.h * s.h + col +
+                  (reverse ? it.len - kChunkT - first : first) * s.t;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(base), 0, kOutside, 0x00020000);
 }
 
-// X's tiles of one wave: [k rows / 16][value columns / 16].
-template <int KD, int NCT>
-struct State {
-  f32x4 x[KD / 16][NCT];
+// A chunk's rows on their way from global memory to an LDS tile: 16-byte units, zero past
+// the chunk's n rows and the tensor's `width` columns. A thread keeps to one column; its
+// rows are kRows apart.
+template <typename T, int W, int NT>
+struct Staged {
+  static constexpr int kPer = 16 / (int)sizeof(T);
+  static constexpr int kUnits = W / kPer;
+  static constexpr int kRows = NT / kUnits;
+  static constexpr int N = kChunkT / kRows;
+  static_assert(NT % kUnits == 0 && kChunkT % kRows == 0, "whole passes");
+  u32x4 r[N];
+  uint32_t off;
+  __device__ __forceinline__ void start(const Rows &s, bool reverse, int width) {
+    const int row = threadIdx.x / kUnits, col = threadIdx.x % kUnits * kPer;
+    off = ((reverse ? kRows - 1 - row : row) * (uint32_t)s.t + col) * (uint32_t)sizeof(T);
+    if (col >= width) off = kOutside;
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t x, const Rows &s, bool reverse,
+                                       int n) {
+    const int row = threadIdx.x / kUnits;
+    const uint32_t step = kRows * (uint32_t)s.t * (uint32_t)sizeof(T);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      r[k] = __builtin_amdgcn_raw_buffer_load_b128(
+          x, row + k * kRows < n ? off : kOutside, (reverse ? N - 1 - k : k) * step, 0);
+  }
+  __device__ __forceinline__ void store(T *tile) const {
+    const int row = threadIdx.x / kUnits, granule = threadIdx.x % kUnits * (kPer / 4);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      *reinterpret_cast<u32x4 *>(tile + Tile<T, W>::at(row + k * kRows, granule)) = r[k];
+  }
 };
 
-// The first value column of a wave's columns, and the place of lane column c (0 .. 15) of
-// tile ct among them: with two tiles a lane's rows of both are eight consecutive columns.
+// a^e for e = 0 .. 64 as a sum of two floats: a chunk's a^64 meets X thousands of times,
+// and one float's rounding would be raised to that power.
+struct Powers {
+  float hi[kChunkT + 1], lo[kChunkT + 1];
+  f32x4 sum[kChunkT / 4];     // sum_scale a^(n - shift - j) of a chunk's n tokens, 0 behind them
+  float row[kChunkT];         // row_scale a^(i + shift)
+  float pair[kChunkT + 16];   // pair_scale a^(e) at e + 16, 0 for e < 0
+};
+__device__ __forceinline__ void power(double g, int e, float &hi, float &lo) {
+  const double d = e == 0 ? 1.0 : exp(g * e);   // 0^0 = 1
+  hi = (float)d;
+  lo = isfinite(hi) ? (float)(d - hi) : 0.f;
+}
+__device__ __forceinline__ void fill_powers(Powers &p, float g) {
+  if (threadIdx.x <= kChunkT) power(g, threadIdx.x, p.hi[threadIdx.x], p.lo[threadIdx.x]);
+}
+// The weights of a chunk's tokens in its sum (after fill_powers and a barrier).
+__device__ __forceinline__ void fill_sum(Powers &p, int n, int shift, float scale) {
+  if (threadIdx.x < kChunkT) {
+    const int e = n - shift - (int)threadIdx.x;
+    reinterpret_cast<float *>(p.sum)[threadIdx.x] = e >= 0 ? p.hi[max(e, 0)] * scale : 0.f;
+  }
+}
+// The weights of rows and pairs (likewise).
+__device__ __forceinline__ void fill_rows(Powers &p, const DecayScan &a) {
+  if (threadIdx.x < kChunkT) {
+    p.row[threadIdx.x] = p.hi[threadIdx.x + a.shift] * a.row_scale;
+    p.pair[threadIdx.x + 16] = p.hi[threadIdx.x] * a.pair_scale;
+  } else if (threadIdx.x < kChunkT + 16) {
+    p.pair[threadIdx.x - kChunkT] = 0.f;
+  }
+}
+
+// A lane's 4 NCT consecutive columns of an output row, rounded to T.
+template <typename T, int NCT>
+__device__ __forceinline__ void put_row(__amdgpu_buffer_rsrc_t x, uint32_t off, uint32_t soff,
+                                        const f32x4 (&v)[NCT]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[ct]), x, off + 16 * ct,
+                                             soff, 0);
+  } else if constexpr (NCT == 2) {
+    __builtin_amdgcn_raw_buffer_store_b128(
+        __builtin_bit_cast(u32x4, Mma<bf16>::pack(v[0], v[1])), x, off, soff, 0);
+  } else {
+    bf16x4 b;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = (bf16)v[0][j];
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, b), x, off, soff, 0);
+  }
+}
+
+// X's tiles of one wave: [k rows / 16][its value columns / 16][a lane's four k rows].
+template <int KD, int NCT>
+struct State {
+  float x[KD / 16][NCT][4];
+};
+// Column c (0 .. 15) of a wave's tile ct among the wave's value columns: with two tiles, a
+// lane's accumulator rows of both are eight consecutive columns.
 template <int NCT>
 __device__ __forceinline__ int value_col(int ct, int c) {
   return NCT == 2 ? perm_col(ct, c) : c;
 }
+__device__ __forceinline__ void put(float (&x)[4], f32x4 v) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = v[j];
+}
+__device__ __forceinline__ f32x4 get(const float (&x)[4]) { return f32x4{x[0], x[1], x[2], x[3]}; }
 
 // Slice partials in the workspace: the accumulators as they are, 16 bytes per lane.
 template <int KD, int NW, int NCT>
 __device__ __forceinline__ size_t part_at(const DecayScan &a, int bh, int seg, int slice, int nb,
                                           int ct) {
-  const int nslice = (a.vd + 16 * NW * NCT - 1) / (16 * NW * NCT);
+  constexpr int VS = 16 * NW * NCT;
+  const int nslice = (a.vd + VS - 1) / VS;
   const size_t x = ((size_t)bh * (a.nseg - 1) + seg) * nslice + slice;
-  return x * (KD * 16 * NW * NCT) +
-         4 * ((size_t)(((threadIdx.x >> 6) * (KD / 16) + nb) * NCT + ct) * 64 + lane_id());
+  return x * (KD * VS) + 4 * (((wave_id() * (KD / 16) + nb) * NCT + ct) * 64 + lane_id());
+}
+
+// Four k rows of one column of a state in its own layout.
+__device__ __forceinline__ f32x4 read_state(const DecayScan &a, int bh, int kc, int vc) {
+  f32x4 x{0.f, 0.f, 0.f, 0.f};
+  if (vc < a.vd && kc < a.kd) {
+    const float *p = a.x_in + (size_t)bh * a.kd * a.vd;
+    if (a.x_t) {
+      x = *reinterpret_cast<const f32x4 *>(p + (size_t)vc * a.kd + kc);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = p[(size_t)(kc + j) * a.vd + vc];
+    }
+  }
+  return x;
 }
 
 template <int KD, int NW, int NCT>
 __device__ __forceinline__ void load_state(const DecayScan &a, const Item &it,
                                            State<KD, NCT> &s) {
-  const int w = threadIdx.x >> 6, l = lane_id(), g = l >> 4, c = l & 15;
+  const int l = lane_id(), w0 = 16 * NCT * (NW * it.slice + wave_id());
 #pragma unroll
   for (int nb = 0; nb < KD / 16; ++nb)
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
-      f32x4 x{0.f, 0.f, 0.f, 0.f};
-      if (it.seg > 0) {
-        x = *reinterpret_cast<const f32x4 *>(
-            a.part + part_at<KD, NW, NCT>(a, it.bh, it.seg - 1, it.slice, nb, ct));
-      } else if (a.x_in) {
-        const int vc = 16 * NW * NCT * it.slice + 16 * NCT * w + value_col<NCT>(ct, c);
-        const int kc = perm_col(nb, 4 * g);
-        if (vc < a.vd && kc < a.kd) {
-          const float *p = a.x_in + (size_t)it.bh * a.kd * a.vd;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            x[j] = a.x_t ? p[(size_t)vc * a.kd + kc + j] : p[(size_t)(kc + j) * a.vd + vc];
-        }
-      }
-      s.x[nb][ct] = x;
+      if (it.seg > 0)
+        put(s.x[nb][ct], *reinterpret_cast<const f32x4 *>(a.part + part_at<KD, NW, NCT>(
+                             a, it.bh, it.seg - 1, it.slice, nb, ct)));
+      else if (a.x_in)
+        put(s.x[nb][ct], read_state(a, it.bh, 16 * nb + 4 * (l >> 4),
+                                    w0 + value_col<NCT>(ct, l & 15)));
+      else
+        put(s.x[nb][ct], f32x4{0.f, 0.f, 0.f, 0.f});
     }
 }
 
 template <int KD, int NW, int NCT>
 __device__ __forceinline__ void store_state(const DecayScan &a, const Item &it,
                                             const State<KD, NCT> &s) {
-  const int w = threadIdx.x >> 6, l = lane_id(), g = l >> 4, c = l & 15;
+  const int l = lane_id(), w0 = 16 * NCT * (NW * it.slice + wave_id());
 #pragma unroll
   for (int nb = 0; nb < KD / 16; ++nb)
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
-      const int vc = 16 * NW * NCT * it.slice + 16 * NCT * w + value_col<NCT>(ct, c);
-      const int kc = perm_col(nb, 4 * g);
+      const int kc = 16 * nb + 4 * (l >> 4), vc = w0 + value_col<NCT>(ct, l & 15);
       if (vc < a.vd && kc < a.kd) {
         float *p = a.x_out + (size_t)it.bh * a.kd * a.vd;
+        if (a.x_t) {
+          *reinterpret_cast<f32x4 *>(p + (size_t)vc * a.kd + kc) = get(s.x[nb][ct]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          p[a.x_t ? (size_t)vc * a.kd + kc + j : (size_t)(kc + j) * a.vd + vc] = s.x[nb][ct][j];
+          for (int j = 0; j < 4; ++j) p[(size_t)(kc + j) * a.vd + vc] = s.x[nb][ct][j];
+        }
       }
     }
 }
 
-// X <- a^n X + sum_scale K^T diag(a^(n - shift - j)) V of a chunk with n tokens. vt: the
-// wave's value columns transposed, tokens in chained order.
+// The wave's value columns of a chunk, transposed: tokens in chained order.
+template <typename T, int NW, int NCT>
+__device__ __forceinline__ void load_values(const T *Vs, typename Mma<T>::frag (&vt)[NCT][2]) {
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+      vt[ct][m] = Tile<T, 16 * NW * NCT>::trans(Vs, 4 * NCT * wave_id() + ct, NCT, m);
+}
+
+// X <- a^n X + K^T diag(pw.sum) V of a chunk with n tokens.
 template <typename T, int KD, int NCT>
 __device__ __forceinline__ void update_state(State<KD, NCT> &s, const T *Ks,
                                              const typename Mma<T>::frag (&vt)[NCT][2],
-                                             const Powers &pw, int n, int shift,
-                                             float sum_scale) {
+                                             const Powers &pw, int n) {
   using P = Mma<T>;
   constexpr int N = kSumTerms<T>;
   const int g = lane_id() >> 4;
   typename P::frag vw[2][NCT][N];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    float wt[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int e = n - shift - (32 * m + 16 * (i >> 2) + 4 * g + (i & 3));
-      wt[i] = e >= 0 ? pw.hi[max(e, 0)] * sum_scale : 0.f;
-    }
+    const f32x4 w0 = pw.sum[8 * m + g], w1 = pw.sum[8 * m + 4 + g];
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
       float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = to_f32(vt[ct][m][i]) * wt[i];
+      for (int i = 0; i < 4; ++i) {
+        x[i] = to_f32(vt[ct][m][i]) * w0[i];
+        x[4 + i] = to_f32(vt[ct][m][4 + i]) * w1[i];
+      }
       split8<N>(x, vw[m][ct]);
     }
   }
@@ -272,59 +378,55 @@ __device__ __forceinline__ void update_state(State<KD, NCT> &s, const T *Ks,
     for (int ct = 0; ct < NCT; ++ct) u[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const auto kt = load_tr(Ks, KD + kPad<T>, m, perm_col(nb, 0), 8);
+      const auto kt = Tile<T, KD>::trans(Ks, 4 * nb, 1, m);
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct)
+      for (int t = N - 1; t >= 0; --t)
 #pragma unroll
-        for (int t = N - 1; t >= 0; --t) u[ct] = P::mma(kt, vw[m][ct][t], u[ct]);
+        for (int ct = 0; ct < NCT; ++ct) u[ct] = P::mma(kt, vw[m][ct][t], u[ct]);
     }
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float x = s.x[nb][ct][j];
-        s.x[nb][ct][j] = fmaf(x, hi, fmaf(x, lo, u[ct][j]));
+        // x hi + (x lo + u), the outer step in place: left to itself the compiler forms
+        // it in u's register and copies every element of X back, one instruction in three
+        float &x = s.x[nb][ct][j];
+        const float low = fmaf(x, lo, u[ct][j]);
+        asm("v_fma_f32 %0, %0, %1, %2" : "+v"(x) : "v"(hi), "v"(low));
       }
+    if (nb & 1) __builtin_amdgcn_sched_barrier(0);
   }
-}
-
-template <typename T, int NW, int NCT>
-__device__ __forceinline__ void load_values(const T *Vs, typename Mma<T>::frag (&vt)[NCT][2]) {
-  const int w = threadIdx.x >> 6;
-#pragma unroll
-  for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-      vt[ct][m] = load_tr(Vs, 16 * NW * NCT + kPad<T>, m,
-                          16 * NCT * w + value_col<NCT>(ct, 0), NCT == 2 ? 8 : 4);
 }
 
 // The sums of one segment of 64 * chunks tokens, from X = 0.
 template <typename T, int KD, int NW, int NCT>
 __global__ __launch_bounds__(64 * NW) void k_decay_sums(DecayScan a) {
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT;
-  __shared__ __align__(16) T Ks[kChunkT * (KD + kPad<T>)];
-  __shared__ __align__(16) T Vs[kChunkT * (VS + kPad<T>)];
+  __shared__ __align__(16) T Ks[kChunkT * KD];
+  __shared__ __align__(16) T Vs[kChunkT * VS];
   __shared__ Powers pw;
   const int nslice = (a.vd + VS - 1) / VS;
   const Item it = item_of(a, xcd_item(blockIdx.x, gridDim.x), nslice, a.nseg - 1);
   if (it.seg >= last_seg(a, it.len)) return;   // X_n comes from the scan
-  fill_powers(pw, a.log_decay[it.h]);
   const int v0 = VS * it.slice;
-  const int64_t sgn = a.reverse ? -1 : 1;
+  Staged<T, KD, NT> kr;
+  Staged<T, VS, NT> vr;
+  kr.start(a.ks, a.reverse, a.kd);
+  vr.start(a.vs, a.reverse, a.vd - v0);
+  const auto fetch = [&](int c) {
+    const int r = it.first + c;
+    kr.load(chunk_rows<T>(a.k, a.ks, it, 0, a.reverse, r), a.ks, a.reverse, kChunkT);
+    vr.load(chunk_rows<T>(a.v, a.vs, it, v0, a.reverse, r), a.vs, a.reverse, kChunkT);
+  };
+  fetch(0);
+  fill_powers(pw, a.log_decay[it.h]);
+  __syncthreads();
+  fill_sum(pw, kChunkT, a.shift, a.sum_scale);
   State<KD, NCT> s;
 #pragma unroll
   for (int nb = 0; nb < KD / 16; ++nb)
 #pragma unroll
-    for (int ct = 0; ct < NCT; ++ct) s.x[nb][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Staged<T, KD, NT> kr;
-  Staged<T, VS, NT> vr;
-  const auto fetch = [&](int c) {
-    const int r = it.first + c, n = min(kChunkT, it.n - c);
-    kr.load(row_ptr<T>(a.k, a.ks, it, a.reverse, r), sgn * a.ks.t, n, a.kd);
-    vr.load(row_ptr<T>(a.v, a.vs, it, a.reverse, r) + v0, sgn * a.vs.t, n, a.vd - v0);
-  };
-  fetch(0);
+    for (int ct = 0; ct < NCT; ++ct) put(s.x[nb][ct], f32x4{0.f, 0.f, 0.f, 0.f});
   for (int c = 0; c < it.n; c += kChunkT) {
     kr.store(Ks);
     vr.store(Vs);
@@ -332,7 +434,7 @@ __global__ __launch_bounds__(64 * NW) void k_decay_sums(DecayScan a) {
     if (c + kChunkT < it.n) fetch(c + kChunkT);
     typename Mma<T>::frag vt[NCT][2];
     load_values<T, NW, NCT>(Vs, vt);
-    update_state<T, KD, NCT>(s, Ks, vt, pw, kChunkT, a.shift, a.sum_scale);
+    update_state<T, KD, NCT>(s, Ks, vt, pw, kChunkT);
     __syncthreads();
   }
 #pragma unroll
@@ -340,7 +442,7 @@ __global__ __launch_bounds__(64 * NW) void k_decay_sums(DecayScan a) {
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
       *reinterpret_cast<f32x4 *>(
-          a.part + part_at<KD, NW, NCT>(a, it.bh, it.seg, it.slice, nb, ct)) = s.x[nb][ct];
+          a.part + part_at<KD, NW, NCT>(a, it.bh, it.seg, it.slice, nb, ct)) = get(s.x[nb][ct]);
 }
 
 // part of a head's segments: X before segment s + 1 = a^seg_len (X before s) + sums of s,
@@ -350,23 +452,15 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayScan a) {
   constexpr int VS = 16 * NW * NCT, Q = KD * VS / 4;
   const int nslice = (a.vd + VS - 1) / VS;
   const int e = (blockIdx.x % (Q / 256)) * 256 + threadIdx.x;
-  const int id = blockIdx.x / (Q / 256);
-  const Item it = item_of(a, id, nslice, 1);
+  const Item it = item_of(a, blockIdx.x / (Q / 256), nslice, 1);
   const int last = last_seg(a, it.len);
   if (last == 0) return;
-  const int l = e & 63, g = l >> 4, c = l & 15;
-  const int ct = (e >> 6) % NCT, nb = (e >> 6) / NCT % (KD / 16), w = (e >> 6) / NCT / (KD / 16);
+  const int l = e & 63, ct = (e >> 6) % NCT, nb = (e >> 6) / NCT % (KD / 16);
+  const int w = (e >> 6) / NCT / (KD / 16);
   f32x4 x{0.f, 0.f, 0.f, 0.f};
-  if (a.x_in) {
-    const int vc = VS * it.slice + 16 * NCT * w + value_col<NCT>(ct, c);
-    const int kc = perm_col(nb, 4 * g);
-    if (vc < a.vd && kc < a.kd) {
-      const float *p = a.x_in + (size_t)it.bh * a.kd * a.vd;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        x[j] = a.x_t ? p[(size_t)vc * a.kd + kc + j] : p[(size_t)(kc + j) * a.vd + vc];
-    }
-  }
+  if (a.x_in)
+    x = read_state(a, it.bh, 16 * nb + 4 * (l >> 4),
+                   16 * NCT * (NW * it.slice + w) + value_col<NCT>(ct, l & 15));
   float hi, lo;
   power(a.log_decay[it.h], a.seg_len, hi, lo);
   f32x4 *p = reinterpret_cast<f32x4 *>(a.part) +
@@ -379,39 +473,76 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayScan a) {
   }
 }
 
+// Waves per SIMD that the register budget of the scan is set for.
+constexpr int scan_waves(int elt, int KD, int NCT) {
+  return elt == 2 && KD <= 128 && NCT == 1 ? 4 : KD == 256 && elt == 4 ? 1 : 2;
+}
+
 template <typename T, int KD, int NW, int NCT>
-__global__ __launch_bounds__(64 * NW) void k_decay_scan(DecayScan a) {
+__global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_decay_scan(DecayScan a) {
   using P = Mma<T>;
   using frag = typename P::frag;
-  constexpr int NT = 64 * NW, VS = 16 * NW * NCT, NP = KD / 32, LD = KD + kPad<T>;
-  __shared__ __align__(16) T Qs[kChunkT * LD];
-  __shared__ __align__(16) T Ks[kChunkT * LD];
-  __shared__ __align__(16) T Vs[kChunkT * (VS + kPad<T>)];
+  constexpr int NT = 64 * NW, VS = 16 * NW * NCT, NP = KD / 32;
+  __shared__ __align__(16) T Qs[kChunkT * KD];
+  __shared__ __align__(16) T Ks[kChunkT * KD];
+  __shared__ __align__(16) T Vs[kChunkT * VS];
+  // the pair weights as B operands: rows 16 i .. + 15, tokens 32 m .. + 31 in fragment
+  // first(i) + m
+  __shared__ __align__(16) frag Ps[6 * 64];
   __shared__ Powers pw;
+  const auto first = [](int i) { return (i >= 1) + (i >= 2) + 2 * (i >= 3); };
   const int nslice = (a.vd + VS - 1) / VS;
   const Item it = item_of(a, xcd_item(blockIdx.x, gridDim.x), nslice, a.nseg);
-  const int w = threadIdx.x >> 6, l = lane_id(), g = l >> 4, c16 = l & 15;
+  const int w = wave_id(), l = lane_id(), g = l >> 4, c16 = l & 15;
   const int v0 = VS * it.slice;
-  const int64_t sgn = a.reverse ? -1 : 1;
-  fill_powers(pw, a.log_decay[it.h]);
-  State<KD, NCT> s;
-  load_state<KD, NW, NCT>(a, it, s);
   Staged<T, KD, NT> qr, kr;
   Staged<T, VS, NT> vr;
+  qr.start(a.qs, a.reverse, a.kd);
+  kr.start(a.ks, a.reverse, a.kd);
+  vr.start(a.vs, a.reverse, a.vd - v0);
   const auto fetch = [&](int c) {
-    const int r = it.first + c, n = min(kChunkT, it.n - c);
-    qr.load(row_ptr<T>(a.q, a.qs, it, a.reverse, r), sgn * a.qs.t, n, a.kd);
-    kr.load(row_ptr<T>(a.k, a.ks, it, a.reverse, r), sgn * a.ks.t, n, a.kd);
-    vr.load(row_ptr<T>(a.v, a.vs, it, a.reverse, r) + v0, sgn * a.vs.t, n, a.vd - v0);
+    const int r = it.first + c, n = it.n - c;
+    qr.load(chunk_rows<T>(a.q, a.qs, it, 0, a.reverse, r), a.qs, a.reverse, n);
+    kr.load(chunk_rows<T>(a.k, a.ks, it, 0, a.reverse, r), a.ks, a.reverse, n);
+    vr.load(chunk_rows<T>(a.v, a.vs, it, v0, a.reverse, r), a.vs, a.reverse, n);
   };
   if (it.n > 0) fetch(0);
+  State<KD, NCT> s;
+  load_state<KD, NW, NCT>(a, it, s);
+  fill_powers(pw, a.log_decay[it.h]);
+  for (int i = threadIdx.x; i < 6 * 64; i += NT) Ps[i] = P::splat(0.f);   // j > i stays 0
+  __syncthreads();
+  fill_rows(pw, a);
+  // a lane's outputs: row c16 of a block, 4 NCT columns
+  const int vc = 16 * NCT * w + 4 * NCT * g;
+  const uint32_t ooff = v0 + vc < a.vd ? ((a.reverse ? 15 - c16 : c16) * (uint32_t)a.os.t + vc) *
+                                             (uint32_t)sizeof(T)
+                                       : kOutside;
   for (int c = 0; c < it.n; c += kChunkT) {
     const int n = min(kChunkT, it.n - c);
     qr.store(Qs);
     kr.store(Ks);
     vr.store(Vs);
+    if (c == 0 || n < kChunkT) fill_sum(pw, n, a.shift, a.sum_scale);
     __syncthreads();
     if (c + kChunkT < it.n) fetch(c + kChunkT);
+
+    // D o K Q^T, the ten 16 x 16 tiles with j <= i shared out over the waves
+    for (int t = w; t < 10; t += NW) {
+      const int ib = (t >= 1) + (t >= 3) + (t >= 6), jb = t - ib * (ib + 1) / 2;
+      const int e = 16 * (ib - jb) + c16 - 4 * g;
+      float wt[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) wt[j] = pw.pair[16 + e - j];
+      f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        x = P::mma(Tile<T, KD>::rows(Ks, jb, p), Tile<T, KD>::rows(Qs, ib, p), x);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = e >= j ? x[j] * wt[j] : 0.f;   // (an Inf of j > i goes)
+      T *pp = reinterpret_cast<T *>(&Ps[(first(ib) + (jb >> 1)) * 64 + l]);
+      store4(pp + 4 * (jb & 1), x);
+    }
 
     // X^T Q^T
     f32x4 o[4][NCT];
@@ -421,78 +552,45 @@ __global__ __launch_bounds__(64 * NW) void k_decay_scan(DecayScan a) {
       for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      frag xf[NCT][kStateTerms<T>];
+      frag xf[NCT];
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) {
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[j] = s.x[2 * p][ct][j];
-          x[4 + j] = s.x[2 * p + 1][ct][j];
-        }
-        split8<kStateTerms<T>>(x, xf[ct]);
-      }
+      for (int ct = 0; ct < NCT; ++ct)
+        xf[ct] = P::pack(get(s.x[2 * p][ct]), get(s.x[2 * p + 1][ct]));
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) {
-        const frag qf = load_frag<T>(&Qs[(16 * ib + c16) * LD + 32 * p + 8 * g]);
+        const frag qf = Tile<T, KD>::rows(Qs, ib, p);
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-          for (int t = kStateTerms<T> - 1; t >= 0; --t) o[ib][ct] = P::mma(xf[ct][t], qf, o[ib][ct]);
+        for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(xf[ct], qf, o[ib][ct]);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int ib = 0; ib < 4; ++ib) {
-      const float f = pw.hi[16 * ib + c16 + a.shift] * a.row_scale;
+      const float f = pw.row[16 * ib + c16];
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[ib][ct][j] *= f;
     }
-
-    // + V^T (D o K Q^T), the pairs j <= i
     frag vt[NCT][2];
     load_values<T, NW, NCT>(Vs, vt);
+    __syncthreads();
+
+    // + V^T (D o K Q^T)
+    const auto rows = chunk_rows<T>(a.o, a.os, it, v0, a.reverse, it.first + c);
 #pragma unroll
     for (int ib = 0; ib < 4; ++ib) {
-      frag qf[NP];
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-        qf[p] = load_frag<T>(&Qs[(16 * ib + c16) * LD + 32 * p + 8 * g]);
 #pragma unroll
       for (int m = 0; m <= ib / 2; ++m) {
-        f32x4 pt[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int jb = 2 * m + h;
-          f32x4 x{0.f, 0.f, 0.f, 0.f};
-          if (jb <= ib) {
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-              x = P::mma(load_frag<T>(&Ks[(16 * jb + c16) * LD + 32 * p + 8 * g]), qf[p], x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int e = 16 * (ib - jb) + c16 - 4 * g - j;
-              x[j] = e >= 0 ? x[j] * (pw.hi[max(e, 0)] * a.pair_scale) : 0.f;
-            }
-          }
-          pt[h] = x;
-        }
-        const frag pf = P::pack(pt[0], pt[1]);
+        const frag pf = Ps[(first(ib) + m) * 64 + l];
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(vt[ct][m], pf, o[ib][ct]);
       }
-      const int i = 16 * ib + c16;
-      if (i < n) {
-        T *op = const_cast<T *>(row_ptr<T>(a.o, a.os, it, a.reverse, it.first + c + i));
-        const int vc = v0 + 16 * NCT * w + 4 * NCT * g;
-        if (vc < a.vd) {
-          if constexpr (NCT == 2) store8(op + vc, o[ib][0], o[ib][1]);
-          else store4(op + vc, o[ib][0]);
-        }
-      }
+      put_row<T, NCT>(rows, 16 * ib + c16 < n ? ooff : kOutside,
+                      16 * (a.reverse ? 3 - ib : ib) * (uint32_t)a.os.t * (uint32_t)sizeof(T),
+                      o[ib]);
     }
-    update_state<T, KD, NCT>(s, Ks, vt, pw, n, a.shift, a.sum_scale);
+    update_state<T, KD, NCT>(s, Ks, vt, pw, n);
     __syncthreads();
   }
 
@@ -512,24 +610,27 @@ enum class Which { Sums, Prefix, Scan };
 
 template <typename T, int KD, int NW, int NCT>
 hipError_t launch(const DecayScan &a, Which which, hipStream_t st) {
+  constexpr int VS = 16 * NW * NCT;
   const int nslice = decay_slices(a.kd, a.vd);
   if (which == Which::Sums) {
     k_decay_sums<T, KD, NW, NCT><<<a.BH * (a.nseg - 1) * nslice, 64 * NW, 0, st>>>(a);
   } else if (which == Which::Prefix) {
-    k_decay_prefix<KD, NW, NCT>
-        <<<a.BH * nslice * (KD * 16 * NW * NCT / 4 / 256), 256, 0, st>>>(a);
+    k_decay_prefix<KD, NW, NCT><<<a.BH * nslice * (KD * VS / 4 / 256), 256, 0, st>>>(a);
   } else {
     k_decay_scan<T, KD, NW, NCT><<<a.BH * a.nseg * nslice, 64 * NW, 0, st>>>(a);
   }
   return hipGetLastError();
 }
 
+// fp32 inputs keep one value tile per wave, in twice as many waves: their operands take
+// twice the registers.
 template <typename T>
 hipError_t dispatch(const DecayScan &a, Which which, hipStream_t st) {
+  constexpr int NW = sizeof(T) == 2 ? 4 : 8, NCT = 8 / NW;
   const bool wide = decay_slice(a.kd, a.vd) == 128;
-  if (a.kd <= 64) return wide ? launch<T, 64, 4, 2>(a, which, st) : launch<T, 64, 2, 2>(a, which, st);
+  if (a.kd <= 64) return wide ? launch<T, 64, NW, NCT>(a, which, st) : launch<T, 64, 4, 1>(a, which, st);
   if (a.kd <= 128)
-    return wide ? launch<T, 128, 4, 2>(a, which, st) : launch<T, 128, 2, 2>(a, which, st);
+    return wide ? launch<T, 128, NW, NCT>(a, which, st) : launch<T, 128, 4, 1>(a, which, st);
   return launch<T, 256, 4, 1>(a, which, st);
 }
 
@@ -546,8 +647,8 @@ int decay_slice(int kd, int vd) { return kd > 128 || vd <= 64 ? 64 : 128; }
 hipError_t launch_decay_sums(const DecayScan &a, Dt dt, hipStream_t st) {
   return dispatch(a, dt, Which::Sums, st);
 }
-hipError_t launch_decay_prefix(const DecayScan &a, hipStream_t st) {
-  return dispatch(a, Dt::F32, Which::Prefix, st);
+hipError_t launch_decay_prefix(const DecayScan &a, Dt dt, hipStream_t st) {
+  return dispatch(a, dt, Which::Prefix, st);
 }
 hipError_t launch_decay_scan(const DecayScan &a, Dt dt, hipStream_t st) {
   return dispatch(a, dt, Which::Scan, st);

@@ -48,7 +48,7 @@ inline size_t decay_slice_floats(int kd, int vd) {
 // The sums of every segment but the last, in part.
 hipError_t launch_decay_sums(const DecayScan &a, Dt dt, hipStream_t st);
 // part: from each segment's sums to X before the segment that follows it.
-hipError_t launch_decay_prefix(const DecayScan &a, hipStream_t st);
+hipError_t launch_decay_prefix(const DecayScan &a, Dt dt, hipStream_t st);
 // The rows, each segment from the X before it.
 hipError_t launch_decay_scan(const DecayScan &a, Dt dt, hipStream_t st);
 

@@ -61,6 +61,8 @@ favor_status device_result(hipError_t e, const char *what) {
 
 constexpr int kMaxL = 1 << 30;
 constexpr int64_t kMaxStride = (int64_t)1 << 46;   // element offsets stay within 64 bits
+// the kernels reach a chunk's 64 rows by 32-bit offsets
+constexpr int64_t kMaxTokenBytes = 1 << 25;
 enum Op { kOpForward = 0, kOpBackward = 1, kOpStep = 2 };
 
 struct Tensor {
@@ -84,6 +86,8 @@ favor_status check_strides(const favor_decay_desc *g, const Tensor &t, int op) {
     if (stride[i] % unit != 0)
       return fail(FAVOR_ERR_INVALID_ARGUMENT,
                   "strides of %s must be multiples of 16 bytes (%d elements)", t.name, unit);
+    if (i == 2 && stride[i] > kMaxTokenBytes / (16 / unit))
+      return fail(FAVOR_ERR_UNSUPPORTED, "the token stride of %s exceeds 2^25 bytes", t.name);
     if (stride[i] > kMaxStride / (size[i] - 1) || (reach += stride[i] * (size[i] - 1)) > kMaxStride)
       return fail(FAVOR_ERR_UNSUPPORTED, "%s reaches past 2^46 elements", t.name);
   }
@@ -203,7 +207,7 @@ favor_status run_scan(const DecayScan &a, favor::Dt dt, hipStream_t st, const ch
     }
     if (e != hipSuccess) return device_result(e, what);
     favor::LaunchTimer t(favor::kKerDecayPrefix, st);
-    e = favor::launch_decay_prefix(a, st);
+    e = favor::launch_decay_prefix(a, dt, st);
     if (e != hipSuccess) return device_result(e, what);
   }
   favor::LaunchTimer t(favor::kKerDecayScan, st);

@@ -122,6 +122,8 @@ def _desc(**kw):
     (dict(v=(1 << 45, 128, 512)), 0),
     (dict(v=(1 << 46, 128, 512)), 2),
     (dict(v=(1 << 62, 1 << 62, 1 << 62)), 2),
+    (dict(q=(64, 64, 1 << 24)), 0), (dict(q=(64, 64, (1 << 24) + 8)), 2),   # 2^25 bytes
+    (dict(q=(64, 64, 1 << 23), dtype=fv.F32), 0), (dict(q=(64, 64, (1 << 23) + 8), dtype=fv.F32), 2),
 ])
 def test_descriptor(kw, status):
     ops = (0, 1) if any(isinstance(x, tuple) for x in kw.values()) else (0, 1, 2)
