@@ -36,9 +36,9 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // An LDS tile of 64 rows and W columns, in granules of four elements. Granule c of a row
 // lies at place c ^ f(row), so that both ways of reading it meet each of the 64 banks once:
-//   rows():  16 rows at two granules (bf16, 8 bytes each) or at one (fp32, 16 bytes)
-//   trans(): eight rows by four granules (bf16), or one column of four rows by four
-//            granules (fp32)
+//   RowReader:   16 rows at two granules (bf16, 8 bytes each) or at one (fp32, 16 bytes)
+//   TransReader: eight rows by four granules (bf16), or one column of four rows by four
+//                granules (fp32)
 // bf16 pairs of granules stay together, so staging writes 16 bytes.
 template <typename T, int W>
 struct Tile {
@@ -50,69 +50,111 @@ struct Tile {
   static __device__ __forceinline__ int at(int row, int granule) {
     return row * W + 4 * (granule ^ f(row));
   }
-  // Operand fragment of rows 16 b .. + 15 over columns 32 p .. + 31, chained order.
-  static __device__ __forceinline__ typename Mma<T>::frag rows(const T *t, int b, int p) {
+  // granules the swizzle stays within: what lies above is a constant offset
+  static constexpr int kSpan = sizeof(T) == 4 || W == 64 ? 16 : 32;
+  static constexpr int kGranule = 4 * (int)sizeof(T);
+  static constexpr int kRow = W * (int)sizeof(T);
+};
+
+// LDS addresses as integers. A tile starts at a multiple of 256 bytes, so that a swizzled
+// place is a lane's own address with a constant exclusive-ored in: one register per way of
+// reading instead of one per place.
+using lds_t = uint32_t;
+__device__ __forceinline__ lds_t lds_of(const void *p) {
+  return (lds_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
+// Operand fragments of a tile's rows 16 b .. + 15 over columns 32 p .. + 31, chained order.
+template <typename T, int W>
+struct RowReader {
+  using L = Tile<T, W>;
+  lds_t base;
+  __device__ __forceinline__ explicit RowReader(lds_t tile) {
+    const int r = lane_id() & 15, g = lane_id() >> 4;
+    base = tile + r * L::kRow + (g ^ L::f(r)) * L::kGranule;
+  }
+  __device__ __forceinline__ typename Mma<T>::frag operator()(int b, int p) const {
     typedef T quad __attribute__((ext_vector_type(4)));
-    const int l = lane_id(), r = l & 15, g = l >> 4;
     // volatile: loads of two fragments are not to be merged into one wide load, whose
     // halves would then have to be moved
     using ldsq = const volatile __attribute__((address_space(3))) quad;
-    t += 16 * b * W;
-    const quad lo = *(ldsq *)(t + at(r, 8 * p + g));
-    const quad hi = *(ldsq *)(t + at(r, 8 * p + 4 + g));
+    const int over = (8 * p & ~(L::kSpan - 1)) * L::kGranule + 16 * b * L::kRow;
+    const int in = (8 * p & (L::kSpan - 1)) * L::kGranule;
+    const quad lo = *(ldsq *)((base ^ in) + over);
+    const quad hi = *(ldsq *)((base ^ (in + 4 * L::kGranule)) + over);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  // Operand fragment of the transpose: 16 columns (granules c0, c0 + step, ..) over rows
-  // 32 m .. + 31, chained order.
-  static __device__ __forceinline__ typename Mma<T>::frag trans(const T *t, int c0, int step,
-                                                                int m) {
-    const int l = lane_id(), c = l & 15, g = l >> 4;
-    t += 32 * m * W;
+};
+
+// Operand fragments of a tile's transpose: 16 columns over rows 32 m .. + 31, chained order.
+// The columns are the granules c0, c0 + STEP, c0 + 2 STEP and c0 + 3 STEP, c0 having none of
+// STEP's multiples' bits.
+template <typename T, int W, int STEP>
+struct TransReader {
+  using L = Tile<T, W>;
+  lds_t base;
+  __device__ __forceinline__ explicit TransReader(lds_t tile) {
+    const int c = lane_id() & 15, g = lane_id() >> 4;
+    if constexpr (sizeof(T) == 2) {
+      const int row = 4 * g + (c >> 2);
+      base = tile + row * L::kRow + ((STEP * (c & 3)) ^ L::f(row)) * L::kGranule;
+    } else {
+      base = tile + 4 * g * L::kRow + ((STEP * (c >> 2)) ^ L::f(4 * g)) * L::kGranule + 4 * (c & 3);
+    }
+  }
+  __device__ __forceinline__ typename Mma<T>::frag operator()(int c0, int m) const {
+    const int over = (c0 & ~(L::kSpan - 1)) * L::kGranule + 32 * m * L::kRow;
+    const int in = (c0 & (L::kSpan - 1)) * L::kGranule;
     if constexpr (sizeof(T) == 2) {
       using lds4 = __attribute__((address_space(3))) s16x4;
-      const T *p = t + at(4 * g + (c >> 2), c0 + step * (c & 3));
+      const lds_t p = (base ^ in) + over;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 16 * W));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 16 * L::kRow));
       struct Two { s16x4 a, b; };
       return __builtin_bit_cast(bf16x8, Two{lo, hi});
     } else {
+      using ldsf = const __attribute__((address_space(3))) float;
       f32x8 x;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const T *p = t + at(4 * g + i, c0 + step * (c >> 2)) + (c & 3);
-        x[i] = p[0];
-        x[4 + i] = p[16 * W];
+      for (int i = 0; i < 4; ++i) {   // f(4 g + i) = f(4 g) ^ i
+        const lds_t p = (base ^ (in ^ i * L::kGranule)) + over + i * L::kRow;
+        x[i] = *(ldsf *)p;
+        x[4 + i] = *(ldsf *)(p + 16 * L::kRow);
       }
       return x;
     }
   }
 };
 
-// Eight fp32 values as N operand fragments whose sum they are: all but the last term
-// truncated (no term of a finite value overflows, and the remainder is exact), the last
-// rounded.
+// Eight fp32 values as N operand fragments whose sum they are: each term rounded, and what
+// it leaves (exact) passed on. The dot product of a pair of terms with (-1, 0) or (0, -1)
+// takes one term from its value without unpacking it.
+// (These come from the arguments: the compiler writes (-1, 0) as an immediate that the
+// instruction takes for the float -1.)
 template <int N>
-__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&f)[N]) {
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&f)[N],
+                                       const uint32_t (&minus)[2]) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 first = __builtin_bit_cast(bf16x2, minus[0]);
+  const bf16x2 second = __builtin_bit_cast(bf16x2, minus[1]);
   float r[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = x[i];
 #pragma unroll
-  for (int n = 0; n + 1 < N; ++n) {
-    u32x4 w;
+  for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned a = __float_as_uint(r[2 * i]), b = __float_as_uint(r[2 * i + 1]);
-      w[i] = __builtin_amdgcn_perm(b, a, 0x07060302);
-      r[2 * i] -= __uint_as_float(a & 0xffff0000u);
-      r[2 * i + 1] -= __uint_as_float(b & 0xffff0000u);
+    for (int i = 0; i < 8; i += 2) {
+      const bf16x2 t = {(bf16)r[i], (bf16)r[i + 1]};
+      f[n][i] = t[0];
+      f[n][i + 1] = t[1];
+      if (n + 1 < N) {
+        r[i] = __builtin_amdgcn_fdot2_f32_bf16(t, first, r[i], false);
+        r[i + 1] = __builtin_amdgcn_fdot2_f32_bf16(t, second, r[i + 1], false);
+      }
     }
-    f[n] = __builtin_bit_cast(bf16x8, w);
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[N - 1][i] = (bf16)r[i];
 }
 template <int N>
-__device__ __forceinline__ void split8(const float (&x)[8], f32x8 (&f)[N]) {
+__device__ __forceinline__ void split8(const float (&x)[8], f32x8 (&f)[N], const uint32_t (&)[2]) {
   static_assert(N == 1, "fp32 operands are whole");
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[0][i] = x[i];
@@ -123,6 +165,22 @@ template <typename T> constexpr int kSumTerms = sizeof(T) == 2 ? 3 : 1;
 __device__ __forceinline__ int wave_id() {
   return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 }
+
+// a^64 for chunk after chunk as single floats whose products stay right: each is chosen so
+// that the product of all of them so far is a^(64 c) to one rounding. (One float's own
+// rounding would be raised to the number of chunks: 128 of them put X off by 4e-6; a
+// second float for its error costs one more operation on every element of X.)
+struct Carry {
+  double d, inv, err;   // a^64, its reciprocal, (a^(64 c) / product) - 1
+  __device__ __forceinline__ explicit Carry(float g)
+      : d(exp((double)g * kChunkT)), inv(d > 1e-30 && d < 1e30 ? 1.0 / d : 0.0), err(0.0) {}
+  __device__ __forceinline__ float next() {
+    const double t = fma(d, err, d);
+    const float f = (float)t;
+    err = inv > 0.0 ? (t - f) * inv : 0.0;
+    return f;
+  }
+};
 
 // What a workgroup works on.
 struct Item {
@@ -199,56 +257,53 @@ struct Staged {
   }
 };
 
-// a^e for e = 0 .. 64 as a sum of two floats: a chunk's a^64 meets X thousands of times,
-// and one float's rounding would be raised to that power.
+// a^e for e = 0 .. 64, and the weights made of them.
 struct Powers {
-  float hi[kChunkT + 1], lo[kChunkT + 1];
+  float a[kChunkT + 1];
   f32x4 sum[kChunkT / 4];     // sum_scale a^(n - shift - j) of a chunk's n tokens, 0 behind them
   float row[kChunkT];         // row_scale a^(i + shift)
   float pair[kChunkT + 16];   // pair_scale a^(e) at e + 16, 0 for e < 0
 };
-__device__ __forceinline__ void power(double g, int e, float &hi, float &lo) {
-  const double d = e == 0 ? 1.0 : exp(g * e);   // 0^0 = 1
-  hi = (float)d;
-  lo = isfinite(hi) ? (float)(d - hi) : 0.f;
-}
+__device__ __forceinline__ double power(double g, int e) { return e == 0 ? 1.0 : exp(g * e); }
 __device__ __forceinline__ void fill_powers(Powers &p, float g) {
-  if (threadIdx.x <= kChunkT) power(g, threadIdx.x, p.hi[threadIdx.x], p.lo[threadIdx.x]);
+  if (threadIdx.x <= kChunkT) p.a[threadIdx.x] = (float)power(g, threadIdx.x);   // 0^0 = 1
 }
 // The weights of a chunk's tokens in its sum (after fill_powers and a barrier).
 __device__ __forceinline__ void fill_sum(Powers &p, int n, int shift, float scale) {
   if (threadIdx.x < kChunkT) {
     const int e = n - shift - (int)threadIdx.x;
-    reinterpret_cast<float *>(p.sum)[threadIdx.x] = e >= 0 ? p.hi[max(e, 0)] * scale : 0.f;
+    reinterpret_cast<float *>(p.sum)[threadIdx.x] = e >= 0 ? p.a[max(e, 0)] * scale : 0.f;
   }
 }
 // The weights of rows and pairs (likewise).
 __device__ __forceinline__ void fill_rows(Powers &p, const DecayScan &a) {
   if (threadIdx.x < kChunkT) {
-    p.row[threadIdx.x] = p.hi[threadIdx.x + a.shift] * a.row_scale;
-    p.pair[threadIdx.x + 16] = p.hi[threadIdx.x] * a.pair_scale;
+    p.row[threadIdx.x] = p.a[threadIdx.x + a.shift] * a.row_scale;
+    p.pair[threadIdx.x + 16] = p.a[threadIdx.x] * a.pair_scale;
   } else if (threadIdx.x < kChunkT + 16) {
     p.pair[threadIdx.x - kChunkT] = 0.f;
   }
 }
 
-// A lane's 4 NCT consecutive columns of an output row, rounded to T.
+// A lane's 4 NCT consecutive columns of an output row, rounded to T. (No scalar offset: the
+// compiler takes it that a 16-byte store with one needs no wait before its data registers
+// are written again, and lanes 12 .. 15 then stored what came next.)
 template <typename T, int NCT>
-__device__ __forceinline__ void put_row(__amdgpu_buffer_rsrc_t x, uint32_t off, uint32_t soff,
+__device__ __forceinline__ void put_row(__amdgpu_buffer_rsrc_t x, uint32_t off,
                                         const f32x4 (&v)[NCT]) {
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
       __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[ct]), x, off + 16 * ct,
-                                             soff, 0);
+                                             0, 0);
   } else if constexpr (NCT == 2) {
     __builtin_amdgcn_raw_buffer_store_b128(
-        __builtin_bit_cast(u32x4, Mma<bf16>::pack(v[0], v[1])), x, off, soff, 0);
+        __builtin_bit_cast(u32x4, Mma<bf16>::pack(v[0], v[1])), x, off, 0, 0);
   } else {
     bf16x4 b;
 #pragma unroll
     for (int j = 0; j < 4; ++j) b[j] = (bf16)v[0][j];
-    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, b), x, off, soff, 0);
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, b), x, off, 0, 0);
   }
 }
 
@@ -335,24 +390,21 @@ __device__ __forceinline__ void store_state(const DecayScan &a, const Item &it,
 }
 
 // The wave's value columns of a chunk, transposed: tokens in chained order.
-template <typename T, int NW, int NCT>
-__device__ __forceinline__ void load_values(const T *Vs, typename Mma<T>::frag (&vt)[NCT][2]) {
+template <typename T, int VS, int NCT>
+__device__ __forceinline__ void load_values(lds_t Vs, typename Mma<T>::frag (&vt)[NCT][2]) {
+  const TransReader<T, VS, NCT> values(Vs);
 #pragma unroll
   for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-      vt[ct][m] = Tile<T, 16 * NW * NCT>::trans(Vs, 4 * NCT * wave_id() + ct, NCT, m);
+    for (int m = 0; m < 2; ++m) vt[ct][m] = values(4 * NCT * wave_id() + ct, m);
 }
 
-// X <- a^n X + K^T diag(pw.sum) V of a chunk with n tokens.
-template <typename T, int KD, int NCT>
-__device__ __forceinline__ void update_state(State<KD, NCT> &s, const T *Ks,
-                                             const typename Mma<T>::frag (&vt)[NCT][2],
-                                             const Powers &pw, int n) {
-  using P = Mma<T>;
-  constexpr int N = kSumTerms<T>;
+// diag(pw.sum) V in operand terms.
+template <typename T, int NCT>
+__device__ __forceinline__ void weigh_values(
+    typename Mma<T>::frag (&vw)[2][NCT][kSumTerms<T>],
+    const typename Mma<T>::frag (&vt)[NCT][2], const Powers &pw, const uint32_t (&minus)[2]) {
   const int g = lane_id() >> 4;
-  typename P::frag vw[2][NCT][N];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     const f32x4 w0 = pw.sum[8 * m + g], w1 = pw.sum[8 * m + 4 + g];
@@ -364,13 +416,21 @@ __device__ __forceinline__ void update_state(State<KD, NCT> &s, const T *Ks,
         x[i] = to_f32(vt[ct][m][i]) * w0[i];
         x[4 + i] = to_f32(vt[ct][m][4 + i]) * w1[i];
       }
-      split8<N>(x, vw[m][ct]);
+      split8<kSumTerms<T>>(x, vw[m][ct], minus);
     }
   }
+}
+
+// X <- carry X + K^T (diag(pw.sum) V).
+template <typename T, int KD, int NCT>
+__device__ __forceinline__ void update_state(
+    State<KD, NCT> &s, lds_t Ks, const typename Mma<T>::frag (&vw)[2][NCT][kSumTerms<T>],
+    float carry) {
+  using P = Mma<T>;
+  const TransReader<T, KD, 1> keys(Ks);
   // The chunk's sum starts from zero and joins X in one rounded step: the bf16 matrix
   // core cuts off what its accumulator cannot hold, always downwards, which over the
   // chunks of a long memory (8192 positive terms, a = 1) put X off by 6e-6.
-  const float hi = pw.hi[n], lo = pw.lo[n];
 #pragma unroll
   for (int nb = 0; nb < KD / 16; ++nb) {
     f32x4 u[NCT];
@@ -378,32 +438,27 @@ __device__ __forceinline__ void update_state(State<KD, NCT> &s, const T *Ks,
     for (int ct = 0; ct < NCT; ++ct) u[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const auto kt = Tile<T, KD>::trans(Ks, 4 * nb, 1, m);
+      const auto kt = keys(4 * nb, m);
 #pragma unroll
-      for (int t = N - 1; t >= 0; --t)
+      for (int t = kSumTerms<T> - 1; t >= 0; --t)
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) u[ct] = P::mma(kt, vw[m][ct][t], u[ct]);
     }
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // x hi + (x lo + u), the outer step in place: left to itself the compiler forms
-        // it in u's register and copies every element of X back, one instruction in three
-        float &x = s.x[nb][ct][j];
-        const float low = fmaf(x, lo, u[ct][j]);
-        asm("v_fma_f32 %0, %0, %1, %2" : "+v"(x) : "v"(hi), "v"(low));
-      }
+      for (int j = 0; j < 4; ++j)
+        s.x[nb][ct][j] = fmaf(s.x[nb][ct][j], carry, u[ct][j]);
     if (nb & 1) __builtin_amdgcn_sched_barrier(0);
   }
 }
 
 // The sums of one segment of 64 * chunks tokens, from X = 0.
 template <typename T, int KD, int NW, int NCT>
-__global__ __launch_bounds__(64 * NW) void k_decay_sums(DecayScan a) {
+__global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayScan a) {
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT;
-  __shared__ __align__(16) T Ks[kChunkT * KD];
-  __shared__ __align__(16) T Vs[kChunkT * VS];
+  __shared__ __align__(256) T Ks[kChunkT * KD];
+  __shared__ __align__(256) T Vs[kChunkT * VS];
   __shared__ Powers pw;
   const int nslice = (a.vd + VS - 1) / VS;
   const Item it = item_of(a, xcd_item(blockIdx.x, gridDim.x), nslice, a.nseg - 1);
@@ -427,14 +482,18 @@ __global__ __launch_bounds__(64 * NW) void k_decay_sums(DecayScan a) {
   for (int nb = 0; nb < KD / 16; ++nb)
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) put(s.x[nb][ct], f32x4{0.f, 0.f, 0.f, 0.f});
+  Carry carry(a.log_decay[it.h]);
   for (int c = 0; c < it.n; c += kChunkT) {
     kr.store(Ks);
     vr.store(Vs);
     __syncthreads();
     if (c + kChunkT < it.n) fetch(c + kChunkT);
     typename Mma<T>::frag vt[NCT][2];
-    load_values<T, NW, NCT>(Vs, vt);
-    update_state<T, KD, NCT>(s, Ks, vt, pw, kChunkT);
+    const lds_t zero = c & a.zero;
+    load_values<T, VS, NCT>(lds_of(Vs) + zero, vt);
+    typename Mma<T>::frag vw[2][NCT][kSumTerms<T>];
+    weigh_values<T, NCT>(vw, vt, pw, a.minus);
+    update_state<T, KD, NCT>(s, lds_of(Ks) + zero, vw, carry.next());
     __syncthreads();
   }
 #pragma unroll
@@ -461,8 +520,9 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayScan a) {
   if (a.x_in)
     x = read_state(a, it.bh, 16 * nb + 4 * (l >> 4),
                    16 * NCT * (NW * it.slice + w) + value_col<NCT>(ct, l & 15));
-  float hi, lo;
-  power(a.log_decay[it.h], a.seg_len, hi, lo);
+  // a^seg_len as two floats: it meets X once per segment
+  const double d = power(a.log_decay[it.h], a.seg_len);
+  const float hi = (float)d, lo = isfinite(hi) ? (float)(d - hi) : 0.f;
   f32x4 *p = reinterpret_cast<f32x4 *>(a.part) +
              ((size_t)it.bh * (a.nseg - 1) * nslice + it.slice) * Q + e;
   for (int s = 0; s < last; ++s, p += (size_t)nslice * Q) {
@@ -483,9 +543,9 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   using P = Mma<T>;
   using frag = typename P::frag;
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT, NP = KD / 32;
-  __shared__ __align__(16) T Qs[kChunkT * KD];
-  __shared__ __align__(16) T Ks[kChunkT * KD];
-  __shared__ __align__(16) T Vs[kChunkT * VS];
+  __shared__ __align__(256) T Qs[kChunkT * KD];
+  __shared__ __align__(256) T Ks[kChunkT * KD];
+  __shared__ __align__(256) T Vs[kChunkT * VS];
   // the pair weights as B operands: rows 16 i .. + 15, tokens 32 m .. + 31 in fragment
   // first(i) + m
   __shared__ __align__(16) frag Ps[6 * 64];
@@ -513,11 +573,13 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   for (int i = threadIdx.x; i < 6 * 64; i += NT) Ps[i] = P::splat(0.f);   // j > i stays 0
   __syncthreads();
   fill_rows(pw, a);
-  // a lane's outputs: row c16 of a block, 4 NCT columns
+  // a lane's outputs: row c16 of a block (in reversed order from the chunk's last block
+  // down), 4 NCT columns
   const int vc = 16 * NCT * w + 4 * NCT * g;
-  const uint32_t ooff = v0 + vc < a.vd ? ((a.reverse ? 15 - c16 : c16) * (uint32_t)a.os.t + vc) *
-                                             (uint32_t)sizeof(T)
-                                       : kOutside;
+  const uint32_t ostep = (a.reverse ? -16u : 16u) * (uint32_t)a.os.t * (uint32_t)sizeof(T);
+  const uint32_t ooff = ((a.reverse ? kChunkT - 1 - c16 : c16) * (uint32_t)a.os.t + vc) *
+                  (uint32_t)sizeof(T);
+  Carry carry(a.log_decay[it.h]);
   for (int c = 0; c < it.n; c += kChunkT) {
     const int n = min(kChunkT, it.n - c);
     qr.store(Qs);
@@ -526,6 +588,9 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
     if (c == 0 || n < kChunkT) fill_sum(pw, n, a.shift, a.sum_scale);
     __syncthreads();
     if (c + kChunkT < it.n) fetch(c + kChunkT);
+
+    const lds_t zero = c & a.zero;
+    const RowReader<T, KD> queries(lds_of(Qs) + zero), keys(lds_of(Ks) + zero);
 
     // D o K Q^T, the ten 16 x 16 tiles with j <= i shared out over the waves
     for (int t = w; t < 10; t += NW) {
@@ -537,7 +602,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int p = 0; p < NP; ++p)
-        x = P::mma(Tile<T, KD>::rows(Ks, jb, p), Tile<T, KD>::rows(Qs, ib, p), x);
+        x = P::mma(keys(jb, p), queries(ib, p), x);
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = e >= j ? x[j] * wt[j] : 0.f;   // (an Inf of j > i goes)
       T *pp = reinterpret_cast<T *>(&Ps[(first(ib) + (jb >> 1)) * 64 + l]);
@@ -558,7 +623,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
         xf[ct] = P::pack(get(s.x[2 * p][ct]), get(s.x[2 * p + 1][ct]));
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) {
-        const frag qf = Tile<T, KD>::rows(Qs, ib, p);
+        const frag qf = queries(ib, p);
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(xf[ct], qf, o[ib][ct]);
       }
@@ -572,8 +637,8 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[ib][ct][j] *= f;
     }
-    frag vt[NCT][2];
-    load_values<T, NW, NCT>(Vs, vt);
+    frag vt[NCT][2], vw[2][NCT][kSumTerms<T>];
+    load_values<T, VS, NCT>(lds_of(Vs) + zero, vt);
     __syncthreads();
 
     // + V^T (D o K Q^T)
@@ -586,11 +651,10 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(vt[ct][m], pf, o[ib][ct]);
       }
-      put_row<T, NCT>(rows, 16 * ib + c16 < n ? ooff : kOutside,
-                      16 * (a.reverse ? 3 - ib : ib) * (uint32_t)a.os.t * (uint32_t)sizeof(T),
-                      o[ib]);
+      put_row<T, NCT>(rows, 16 * ib + c16 < n && v0 + vc < a.vd ? ooff + ib * ostep : kOutside, o[ib]);
     }
-    update_state<T, KD, NCT>(s, Ks, vt, pw, n);
+    weigh_values<T, NCT>(vw, vt, pw, a.minus);
+    update_state<T, KD, NCT>(s, lds_of(Ks) + zero, vw, n == kChunkT ? carry.next() : pw.a[n]);
     __syncthreads();
   }
 

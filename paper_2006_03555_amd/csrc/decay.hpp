@@ -32,6 +32,8 @@ struct DecayScan {
   int seg_len, nseg;       // segments of seg_len rows (a multiple of 64)
   int reverse, shift;
   float pair_scale, row_scale, sum_scale;
+  int zero = 0;   // the loops' addresses depend on it: they are formed anew, not kept
+  uint32_t minus[2] = {0x0000bf80u, 0xbf800000u};   // bf16 pairs (-1, 0) and (0, -1)
 };
 
 // Columns of v that one workgroup takes, and slices of them; floats of one slice's X in

@@ -106,6 +106,32 @@ def test_forward(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dk,dv", [(128, 128), (88, 128), (256, 88), (64, 64)])
+def test_many_heads(dk, dv, dtype):
+    """Every compute unit busy with several workgroups: each element of each head against
+    the same heads run a few at a time. (A wide store whose registers were written again
+    too early went wrong here in some lanes, and only under load.)"""
+    import torch
+    fv = _fv()
+    x = _inputs(5, 21, 174, dk, dv, dtype, 6)
+    q, k, v, do = (to_dev(x[n], dtype) for n in ("q", "k", "v", "do"))
+    g, S = to_dev(x["g"]), to_dev(x["S"])
+    for _ in range(3):
+        out = fv.attn_decay(q, k, v, g, state_in=S)
+        grads = fv.attn_decay_backward(q, k, v, g, do, state_in=S)
+        for b in range(5):
+            s = slice(b, b + 1)
+            few = [fv.attn_decay(q[s], k[s], v[s], g, state_in=S[s])]
+            few += fv.attn_decay_backward(q[s], k[s], v[s], g, do[s], state_in=S[s])
+            for t, r in zip((out, *grads), few):
+                assert torch.equal(t[s], r)
+    y = _abs(x)
+    ref, _ = decay.attn(x["q"], x["k"], x["v"], x["g"], 1.0, state=x["S"])
+    mag, _ = decay.attn(y["q"], y["k"], y["v"], x["g"], 1.0, state=y["S"])
+    _near(out, ref, mag, dk, 174, dtype, "out")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("shape", SHAPES)
 def test_backward(shape, dtype):
     fv = _fv()
