@@ -166,18 +166,29 @@ __device__ __forceinline__ int wave_id() {
   return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 }
 
-// a^64 for chunk after chunk as single floats whose products stay right: each is chosen so
-// that the product of all of them so far is a^(64 c) to one rounding. (One float's own
-// rounding would be raised to the number of chunks: 128 of them put X off by 4e-6; a
-// second float for its error costs one more operation on every element of X.)
+// The value of lane 0, as a scalar.
+__device__ __forceinline__ float uniform(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+
+// a^64 for chunk after chunk as single floats whose products stay right: what the products
+// so far lack (relative to a^(64 c)) goes into the next one. (One float's own rounding
+// would be raised to the number of chunks: 128 of them put X off by 4e-6; a second float
+// for its error costs one more operation on every element of X.)
 struct Carry {
-  double d, inv, err;   // a^64, its reciprocal, (a^(64 c) / product) - 1
-  __device__ __forceinline__ explicit Carry(float g)
-      : d(exp((double)g * kChunkT)), inv(d > 1e-30 && d < 1e30 ? 1.0 / d : 0.0), err(0.0) {}
+  float one, lack, inv;   // a^64 rounded, what the rounding left relative to it, 1 / one
+  float err;              // (a^(64 c) / product) - 1
+  __device__ __forceinline__ explicit Carry(float g) : err(0.f) {
+    const double d = exp((double)g * kChunkT);
+    one = uniform((float)d);
+    const bool plain = one > 1e-30f && one < 1e30f;
+    inv = uniform(plain ? 1.f / one : 0.f);
+    lack = uniform(plain ? (float)((d - one) / d) : 0.f);
+  }
   __device__ __forceinline__ float next() {
-    const double t = fma(d, err, d);
-    const float f = (float)t;
-    err = inv > 0.0 ? (t - f) * inv : 0.0;
+    err += lack;
+    const float f = fmaf(one, err, one);
+    err -= (f - one) * inv;
     return f;
   }
 };
@@ -189,6 +200,14 @@ struct Item {
   int first;  // the segment's first row (in the scan's order)
   int n;      // its tokens
 };
+
+// The scan of a workgroup: scans that run together take turns, so that those that read the
+// same rows read them at about the same time.
+__device__ __forceinline__ const DecayScan &scan_of(const DecayPass &pass, int &id) {
+  const int r = pass.n > 1 ? id % pass.n : 0;
+  id = pass.n > 1 ? id / pass.n : id;
+  return pass.scan[r];
+}
 
 __device__ __forceinline__ Item item_of(const DecayScan &a, int id, int nslice, int nseg) {
   Item it;
@@ -324,69 +343,60 @@ __device__ __forceinline__ void put(float (&x)[4], f32x4 v) {
 }
 __device__ __forceinline__ f32x4 get(const float (&x)[4]) { return f32x4{x[0], x[1], x[2], x[3]}; }
 
-// Slice partials in the workspace: the accumulators as they are, 16 bytes per lane.
-template <int KD, int NW, int NCT>
-__device__ __forceinline__ size_t part_at(const DecayScan &a, int bh, int seg, int slice, int nb,
-                                          int ct) {
-  constexpr int VS = 16 * NW * NCT;
-  const int nslice = (a.vd + VS - 1) / VS;
-  const size_t x = ((size_t)bh * (a.nseg - 1) + seg) * nslice + slice;
-  return x * (KD * VS) + 4 * (((wave_id() * (KD / 16) + nb) * NCT + ct) * 64 + lane_id());
-}
-
-// Four k rows of one column of a state in its own layout.
-__device__ __forceinline__ f32x4 read_state(const DecayScan &a, int bh, int kc, int vc) {
+// X of one head at p ([kd][vd], or transposed), four k rows of one column at a time.
+__device__ __forceinline__ f32x4 read_state(const DecayScan &a, const float *p, int kc, int vc) {
   f32x4 x{0.f, 0.f, 0.f, 0.f};
   if (vc < a.vd && kc < a.kd) {
-    const float *p = a.x_in + (size_t)bh * a.kd * a.vd;
     if (a.x_t) {
-      x = *reinterpret_cast<const f32x4 *>(p + (size_t)vc * a.kd + kc);
+      x = *reinterpret_cast<const f32x4 *>(p + vc * a.kd + kc);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = p[(size_t)(kc + j) * a.vd + vc];
+      for (int j = 0; j < 4; ++j) x[j] = p[(kc + j) * a.vd + vc];
     }
   }
   return x;
+}
+__device__ __forceinline__ void write_state(const DecayScan &a, float *p, int kc, int vc,
+                                            const float (&x)[4]) {
+  if (vc < a.vd && kc < a.kd) {
+    if (a.x_t) {
+      *reinterpret_cast<f32x4 *>(p + vc * a.kd + kc) = get(x);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[(kc + j) * a.vd + vc] = x[j];
+    }
+  }
+}
+// The sums of a segment, and later X before the one behind it.
+__device__ __forceinline__ float *part_of(const DecayScan &a, int bh, int seg) {
+  return a.part + ((size_t)bh * (a.nseg - 1) + seg) * (a.kd * a.vd);
 }
 
 template <int KD, int NW, int NCT>
 __device__ __forceinline__ void load_state(const DecayScan &a, const Item &it,
                                            State<KD, NCT> &s) {
   const int l = lane_id(), w0 = 16 * NCT * (NW * it.slice + wave_id());
+  const float *p = it.seg > 0 ? part_of(a, it.bh, it.seg - 1)
+                   : a.x_in   ? a.x_in + (size_t)it.bh * (a.kd * a.vd)
+                              : nullptr;
 #pragma unroll
   for (int nb = 0; nb < KD / 16; ++nb)
 #pragma unroll
-    for (int ct = 0; ct < NCT; ++ct) {
-      if (it.seg > 0)
-        put(s.x[nb][ct], *reinterpret_cast<const f32x4 *>(a.part + part_at<KD, NW, NCT>(
-                             a, it.bh, it.seg - 1, it.slice, nb, ct)));
-      else if (a.x_in)
-        put(s.x[nb][ct], read_state(a, it.bh, 16 * nb + 4 * (l >> 4),
-                                    w0 + value_col<NCT>(ct, l & 15)));
-      else
-        put(s.x[nb][ct], f32x4{0.f, 0.f, 0.f, 0.f});
-    }
+    for (int ct = 0; ct < NCT; ++ct)
+      put(s.x[nb][ct], p ? read_state(a, p, 16 * nb + 4 * (l >> 4),
+                                      w0 + value_col<NCT>(ct, l & 15))
+                         : f32x4{0.f, 0.f, 0.f, 0.f});
 }
 
 template <int KD, int NW, int NCT>
-__device__ __forceinline__ void store_state(const DecayScan &a, const Item &it,
+__device__ __forceinline__ void store_state(const DecayScan &a, const Item &it, float *p,
                                             const State<KD, NCT> &s) {
   const int l = lane_id(), w0 = 16 * NCT * (NW * it.slice + wave_id());
 #pragma unroll
   for (int nb = 0; nb < KD / 16; ++nb)
 #pragma unroll
-    for (int ct = 0; ct < NCT; ++ct) {
-      const int kc = 16 * nb + 4 * (l >> 4), vc = w0 + value_col<NCT>(ct, l & 15);
-      if (vc < a.vd && kc < a.kd) {
-        float *p = a.x_out + (size_t)it.bh * a.kd * a.vd;
-        if (a.x_t) {
-          *reinterpret_cast<f32x4 *>(p + (size_t)vc * a.kd + kc) = get(s.x[nb][ct]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) p[(size_t)(kc + j) * a.vd + vc] = s.x[nb][ct][j];
-        }
-      }
-    }
+    for (int ct = 0; ct < NCT; ++ct)
+      write_state(a, p, 16 * nb + 4 * (l >> 4), w0 + value_col<NCT>(ct, l & 15), s.x[nb][ct]);
 }
 
 // The wave's value columns of a chunk, transposed: tokens in chained order.
@@ -455,13 +465,14 @@ __device__ __forceinline__ void update_state(
 
 // The sums of one segment of 64 * chunks tokens, from X = 0.
 template <typename T, int KD, int NW, int NCT>
-__global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayScan a) {
+__global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT;
   __shared__ __align__(256) T Ks[kChunkT * KD];
   __shared__ __align__(256) T Vs[kChunkT * VS];
   __shared__ Powers pw;
-  const int nslice = (a.vd + VS - 1) / VS;
-  const Item it = item_of(a, xcd_item(blockIdx.x, gridDim.x), nslice, a.nseg - 1);
+  int id = xcd_item(blockIdx.x, gridDim.x);
+  const DecayScan &a = scan_of(pass, id);
+  const Item it = item_of(a, id, (a.vd + VS - 1) / VS, a.nseg - 1);
   if (it.seg >= last_seg(a, it.len)) return;   // X_n comes from the scan
   const int v0 = VS * it.slice;
   Staged<T, KD, NT> kr;
@@ -496,40 +507,37 @@ __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayScan a) {
     update_state<T, KD, NCT>(s, lds_of(Ks) + zero, vw, carry.next());
     __syncthreads();
   }
-#pragma unroll
-  for (int nb = 0; nb < KD / 16; ++nb)
-#pragma unroll
-    for (int ct = 0; ct < NCT; ++ct)
-      *reinterpret_cast<f32x4 *>(
-          a.part + part_at<KD, NW, NCT>(a, it.bh, it.seg, it.slice, nb, ct)) = get(s.x[nb][ct]);
+  store_state<KD, NW, NCT>(a, it, part_of(a, it.bh, it.seg), s);
 }
 
 // part of a head's segments: X before segment s + 1 = a^seg_len (X before s) + sums of s,
-// one accumulator quadruple per thread, in the slices' own order.
-template <int KD, int NW, int NCT>
-__global__ __launch_bounds__(256) void k_decay_prefix(DecayScan a) {
-  constexpr int VS = 16 * NW * NCT, Q = KD * VS / 4;
-  const int nslice = (a.vd + VS - 1) / VS;
-  const int e = (blockIdx.x % (Q / 256)) * 256 + threadIdx.x;
-  const Item it = item_of(a, blockIdx.x / (Q / 256), nslice, 1);
+// four elements per thread.
+__global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
+  int id = blockIdx.y;
+  const DecayScan &a = scan_of(pass, id);
+  const int e = blockIdx.x * 256 + threadIdx.x, n = a.kd * a.vd / 4;
+  const Item it = item_of(a, id, 1, 1);
   const int last = last_seg(a, it.len);
-  if (last == 0) return;
-  const int l = e & 63, ct = (e >> 6) % NCT, nb = (e >> 6) / NCT % (KD / 16);
-  const int w = (e >> 6) / NCT / (KD / 16);
+  if (e >= n || last == 0) return;
   f32x4 x{0.f, 0.f, 0.f, 0.f};
-  if (a.x_in)
-    x = read_state(a, it.bh, 16 * nb + 4 * (l >> 4),
-                   16 * NCT * (NW * it.slice + w) + value_col<NCT>(ct, l & 15));
+  if (a.x_in) x = reinterpret_cast<const f32x4 *>(a.x_in)[(size_t)it.bh * n + e];
   // a^seg_len as two floats: it meets X once per segment
   const double d = power(a.log_decay[it.h], a.seg_len);
   const float hi = (float)d, lo = isfinite(hi) ? (float)(d - hi) : 0.f;
-  f32x4 *p = reinterpret_cast<f32x4 *>(a.part) +
-             ((size_t)it.bh * (a.nseg - 1) * nslice + it.slice) * Q + e;
-  for (int s = 0; s < last; ++s, p += (size_t)nslice * Q) {
-    const f32x4 u = *p;
+  f32x4 *p = reinterpret_cast<f32x4 *>(part_of(a, it.bh, 0)) + e;
+  constexpr int kAhead = 4;   // loads in flight
+  for (int s = 0; s < last; s += kAhead, p += kAhead * n) {
+    f32x4 u[kAhead];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = fmaf(x[j], hi, fmaf(x[j], lo, u[j]));
-    *p = x;
+    for (int k = 0; k < kAhead; ++k)
+      if (s + k < last) u[k] = p[k * n];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (s + k < last) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = fmaf(x[j], hi, fmaf(x[j], lo, u[k][j]));
+        p[k * n] = x;
+      }
   }
 }
 
@@ -539,7 +547,7 @@ constexpr int scan_waves(int elt, int KD, int NCT) {
 }
 
 template <typename T, int KD, int NW, int NCT>
-__global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_decay_scan(DecayScan a) {
+__global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_decay_scan(DecayPass pass) {
   using P = Mma<T>;
   using frag = typename P::frag;
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT, NP = KD / 32;
@@ -551,8 +559,9 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   __shared__ __align__(16) frag Ps[6 * 64];
   __shared__ Powers pw;
   const auto first = [](int i) { return (i >= 1) + (i >= 2) + 2 * (i >= 3); };
-  const int nslice = (a.vd + VS - 1) / VS;
-  const Item it = item_of(a, xcd_item(blockIdx.x, gridDim.x), nslice, a.nseg);
+  int id = xcd_item(blockIdx.x, gridDim.x);
+  const DecayScan &a = scan_of(pass, id);
+  const Item it = item_of(a, id, (a.vd + VS - 1) / VS, a.nseg);
   const int w = wave_id(), l = lane_id(), g = l >> 4, c16 = l & 15;
   const int v0 = VS * it.slice;
   Staged<T, KD, NT> qr, kr;
@@ -651,14 +660,15 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(vt[ct][m], pf, o[ib][ct]);
       }
-      put_row<T, NCT>(rows, 16 * ib + c16 < n && v0 + vc < a.vd ? ooff + ib * ostep : kOutside, o[ib]);
+      put_row<T, NCT>(rows, 16 * ib + c16 < n && v0 + vc < a.vd ? ooff + zero + ib * ostep : kOutside, o[ib]);
     }
     weigh_values<T, NCT>(vw, vt, pw, a.minus);
     update_state<T, KD, NCT>(s, lds_of(Ks) + zero, vw, n == kChunkT ? carry.next() : pw.a[n]);
     __syncthreads();
   }
 
-  if (a.x_out && it.seg == last_seg(a, it.len)) store_state<KD, NW, NCT>(a, it, s);
+  if (a.x_out && it.seg == last_seg(a, it.len))
+    store_state<KD, NW, NCT>(a, it, a.x_out + (size_t)it.bh * (a.kd * a.vd), s);
   // the rows of the segment past the sequence's end
   const int end = min(a.L, it.first + a.seg_len);
   constexpr int kPer = 16 / (int)sizeof(T), kUnits = VS / kPer;
@@ -670,36 +680,28 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   }
 }
 
-enum class Which { Sums, Prefix, Scan };
-
 template <typename T, int KD, int NW, int NCT>
-hipError_t launch(const DecayScan &a, Which which, hipStream_t st) {
-  constexpr int VS = 16 * NW * NCT;
-  const int nslice = decay_slices(a.kd, a.vd);
-  if (which == Which::Sums) {
-    k_decay_sums<T, KD, NW, NCT><<<a.BH * (a.nseg - 1) * nslice, 64 * NW, 0, st>>>(a);
-  } else if (which == Which::Prefix) {
-    k_decay_prefix<KD, NW, NCT><<<a.BH * nslice * (KD * VS / 4 / 256), 256, 0, st>>>(a);
-  } else {
-    k_decay_scan<T, KD, NW, NCT><<<a.BH * a.nseg * nslice, 64 * NW, 0, st>>>(a);
-  }
+hipError_t launch(const DecayPass &pass, bool sums, hipStream_t st) {
+  const DecayScan &a = pass.scan[0];
+  const int heads = pass.n * a.BH * decay_slices(a.kd, a.vd);
+  if (sums)
+    k_decay_sums<T, KD, NW, NCT><<<heads * (a.nseg - 1), 64 * NW, 0, st>>>(pass);
+  else
+    k_decay_scan<T, KD, NW, NCT><<<heads * a.nseg, 64 * NW, 0, st>>>(pass);
   return hipGetLastError();
 }
 
 // fp32 inputs keep one value tile per wave, in twice as many waves: their operands take
 // twice the registers.
 template <typename T>
-hipError_t dispatch(const DecayScan &a, Which which, hipStream_t st) {
+hipError_t dispatch(const DecayPass &p, bool sums, hipStream_t st) {
   constexpr int NW = sizeof(T) == 2 ? 4 : 8, NCT = 8 / NW;
-  const bool wide = decay_slice(a.kd, a.vd) == 128;
-  if (a.kd <= 64) return wide ? launch<T, 64, NW, NCT>(a, which, st) : launch<T, 64, 4, 1>(a, which, st);
-  if (a.kd <= 128)
-    return wide ? launch<T, 128, NW, NCT>(a, which, st) : launch<T, 128, 4, 1>(a, which, st);
-  return launch<T, 256, 4, 1>(a, which, st);
-}
-
-hipError_t dispatch(const DecayScan &a, Dt dt, Which which, hipStream_t st) {
-  return dt == Dt::BF16 ? dispatch<bf16>(a, which, st) : dispatch<float>(a, which, st);
+  const int kd = p.scan[0].kd;
+  const bool wide = decay_slice(kd, p.scan[0].vd) == 128;
+  if (kd <= 64) return wide ? launch<T, 64, NW, NCT>(p, sums, st) : launch<T, 64, 4, 1>(p, sums, st);
+  if (kd <= 128)
+    return wide ? launch<T, 128, NW, NCT>(p, sums, st) : launch<T, 128, 4, 1>(p, sums, st);
+  return launch<T, 256, 4, 1>(p, sums, st);
 }
 
 }  // namespace
@@ -708,14 +710,16 @@ hipError_t dispatch(const DecayScan &a, Dt dt, Which which, hipStream_t st) {
 // leave room for the operands in registers.
 int decay_slice(int kd, int vd) { return kd > 128 || vd <= 64 ? 64 : 128; }
 
-hipError_t launch_decay_sums(const DecayScan &a, Dt dt, hipStream_t st) {
-  return dispatch(a, dt, Which::Sums, st);
+hipError_t launch_decay_sums(const DecayPass &p, Dt dt, hipStream_t st) {
+  return dt == Dt::BF16 ? dispatch<bf16>(p, true, st) : dispatch<float>(p, true, st);
 }
-hipError_t launch_decay_prefix(const DecayScan &a, Dt dt, hipStream_t st) {
-  return dispatch(a, dt, Which::Prefix, st);
+hipError_t launch_decay_prefix(const DecayPass &p, hipStream_t st) {
+  const int n = p.scan[0].kd * p.scan[0].vd / 4;
+  k_decay_prefix<<<dim3((n + 255) / 256, p.n * p.scan[0].BH), 256, 0, st>>>(p);
+  return hipGetLastError();
 }
-hipError_t launch_decay_scan(const DecayScan &a, Dt dt, hipStream_t st) {
-  return dispatch(a, dt, Which::Scan, st);
+hipError_t launch_decay_scan(const DecayPass &p, Dt dt, hipStream_t st) {
+  return dt == Dt::BF16 ? dispatch<bf16>(p, false, st) : dispatch<float>(p, false, st);
 }
 
 }  // namespace favor

@@ -17,17 +17,18 @@ struct Rows {
 //   X_n = a^n X_0 + sum_s sum_scale a^(n - shift - s) k_s v_s^T
 // The forward pass is (q, k, v) with shift 1, X the state after the last token; dQ is
 // (dout, V, K) on the transposed state; dV is (K, Q, dout) and dK (V, dout, Q) in
-// reversed order with shift 0, X the state's gradient with its decay applied.
+// reversed order with shift 0, X the state's gradient with its decay applied. X_0, X_n
+// and part may be transposed ([vd][kd]), so that scans on X and on X^T share them.
 struct DecayScan {
   const void *q, *k, *v;   // kd, kd and vd columns
   void *o;                 // vd columns
   Rows qs, ks, vs, os;
   const float *log_decay;  // [H]
   const int32_t *lengths;  // [B], or null: every sequence has L tokens
-  const float *x_in;       // X_0 [BH][kd][vd] (x_t: [BH][vd][kd]), or null for zeros
-  float *x_out;            // X_n in the same layout, or null
-  float *part;             // [BH][nseg - 1][slices][X of a slice]: sums, then prefixes
-  int x_t;
+  const float *x_in;       // X_0 [BH][kd][vd], or null for zeros
+  float *x_out;            // X_n, or null
+  float *part;             // [BH][nseg - 1][X]: the segments' sums, then X behind each
+  int x_t;                 // x_in, x_out and part hold [vd][kd]
   int BH, H, L, kd, vd;
   int seg_len, nseg;       // segments of seg_len rows (a multiple of 64)
   int reverse, shift;
@@ -36,23 +37,25 @@ struct DecayScan {
   uint32_t minus[2] = {0x0000bf80u, 0xbf800000u};   // bf16 pairs (-1, 0) and (0, -1)
 };
 
-// Columns of v that one workgroup takes, and slices of them; floats of one slice's X in
-// the workspace.
+// Scans launched together: the same kd, vd, heads and segments. At most three.
+struct DecayPass {
+  DecayScan scan[3];
+  int n;
+};
+
+// Columns of v that one workgroup takes, and slices of them.
 int decay_slice(int kd, int vd);
 inline int decay_slices(int kd, int vd) {
   const int s = decay_slice(kd, vd);
   return (vd + s - 1) / s;
 }
-inline size_t decay_slice_floats(int kd, int vd) {
-  return (size_t)(kd <= 64 ? 64 : kd <= 128 ? 128 : 256) * decay_slice(kd, vd);
-}
 
 // The sums of every segment but the last, in part.
-hipError_t launch_decay_sums(const DecayScan &a, Dt dt, hipStream_t st);
+hipError_t launch_decay_sums(const DecayPass &p, Dt dt, hipStream_t st);
 // part: from each segment's sums to X before the segment that follows it.
-hipError_t launch_decay_prefix(const DecayScan &a, Dt dt, hipStream_t st);
+hipError_t launch_decay_prefix(const DecayPass &p, hipStream_t st);
 // The rows, each segment from the X before it.
-hipError_t launch_decay_scan(const DecayScan &a, Dt dt, hipStream_t st);
+hipError_t launch_decay_scan(const DecayPass &p, Dt dt, hipStream_t st);
 
 // One token of B sequences on the states [n_slots][H][dk][dv], in place.
 struct DecayStep {

@@ -151,41 +151,29 @@ favor::Dt dt_of(const favor_decay_desc *g) {
 constexpr int kTargetWorkgroups = 512;
 constexpr int kMinRows = 256;
 
-void plan(DecayScan &a) {
-  const int tiles = std::max(1, (a.L + 63) / 64);
-  const int slices = favor::decay_slices(a.kd, a.vd);
-  const int have = a.BH * slices;
+void plan(const favor_decay_desc *g, int kd, int vd, int &seg_len, int &nseg) {
+  const int tiles = std::max(1, (g->L + 63) / 64);
+  const int have = g->B * g->H * favor::decay_slices(kd, vd);
   int want = (kTargetWorkgroups + have - 1) / have;
   want = std::max(1, std::min(want, tiles / (kMinRows / 64)));
   const int per = (tiles + want - 1) / want;
-  a.seg_len = 64 * per;
-  a.nseg = (tiles + per - 1) / per;
+  seg_len = 64 * per;
+  nseg = (tiles + per - 1) / per;
 }
 
-size_t part_bytes(const DecayScan &a) {
-  return round_up((size_t)a.BH * (a.nseg - 1) * favor::decay_slices(a.kd, a.vd) *
-                      favor::decay_slice_floats(a.kd, a.vd) * sizeof(float),
-                  256);
+// Floats of one scan's segment states.
+size_t part_floats(const favor_decay_desc *g, int nseg) {
+  return (size_t)g->B * g->H * (nseg - 1) * g->dk * g->dv;
 }
 
-// A scan's shape (its tensors come later).
-DecayScan shape_of(const favor_decay_desc *g, bool swapped) {
-  DecayScan a{};
-  a.BH = g->B * g->H;
-  a.H = g->H;
-  a.L = g->L;
-  a.kd = swapped ? g->dv : g->dk;
-  a.vd = swapped ? g->dk : g->dv;
-  plan(a);
-  return a;
-}
-
-// Workspace of a call: the forward pass has one scan, the backward pass dV like it and dQ
-// and dK on the transposed state. They run one after another in the same memory.
+// Workspace: the segment states of the forward pass's scan, or of the backward pass's two
+// (S for dQ, its gradient R for dK and dV). The backward scans on [dv][dk] and [dk][dv]
+// share one plan.
 size_t workspace_of(const favor_decay_desc *g, int op) {
   if ((long long)g->B * g->H == 0 || g->L == 0) return 0;
-  const size_t n = part_bytes(shape_of(g, false));
-  return op == kOpBackward ? std::max(n, part_bytes(shape_of(g, true))) : n;
+  int seg_len, nseg;
+  plan(g, g->dk, g->dv, seg_len, nseg);
+  return round_up(part_floats(g, nseg) * sizeof(float) * (op == kOpBackward ? 2 : 1), 256);
 }
 
 favor_status check_workspace(const void *ws, size_t bytes, size_t need) {
@@ -198,21 +186,52 @@ favor_status check_workspace(const void *ws, size_t bytes, size_t need) {
   return FAVOR_OK;
 }
 
-favor_status run_scan(const DecayScan &a, favor::Dt dt, hipStream_t st, const char *what) {
-  hipError_t e = hipSuccess;
-  if (a.nseg > 1) {
-    {
-      favor::LaunchTimer t(favor::kKerDecaySums, st);
-      e = favor::launch_decay_sums(a, dt, st);
-    }
-    if (e != hipSuccess) return device_result(e, what);
-    favor::LaunchTimer t(favor::kKerDecayPrefix, st);
-    e = favor::launch_decay_prefix(a, dt, st);
-    if (e != hipSuccess) return device_result(e, what);
+// A scan of g: kd, vd (exchanged on the transposed state), its segments and the arguments
+// that all have in common.
+DecayScan scan_of(const favor_decay_desc *g, bool swapped, const float *log_decay,
+                  const int32_t *lengths) {
+  DecayScan a{};
+  a.log_decay = log_decay;
+  a.lengths = lengths;
+  a.BH = g->B * g->H;
+  a.H = g->H;
+  a.L = g->L;
+  a.kd = swapped ? g->dv : g->dk;
+  a.vd = swapped ? g->dk : g->dv;
+  a.x_t = swapped;
+  plan(g, g->dk, g->dv, a.seg_len, a.nseg);
+  a.pair_scale = g->scale;
+  return a;
+}
+
+// Forward order: the scale on the rows; reversed: on the sums, so that X takes the
+// gradient of a state as it is.
+void forward_order(DecayScan &a, float scale) {
+  a.shift = 1;
+  a.row_scale = scale;
+  a.sum_scale = 1.f;
+}
+void reversed_order(DecayScan &a, float scale) {
+  a.reverse = 1;
+  a.row_scale = 1.f;
+  a.sum_scale = scale;
+}
+
+favor_status run_sums(const favor::DecayPass &p, favor::Dt dt, hipStream_t st, const char *what) {
+  if (p.scan[0].nseg <= 1) return ok();
+  hipError_t e;
+  {
+    favor::LaunchTimer t(favor::kKerDecaySums, st);
+    e = favor::launch_decay_sums(p, dt, st);
   }
+  if (e != hipSuccess) return device_result(e, what);
+  favor::LaunchTimer t(favor::kKerDecayPrefix, st);
+  return device_result(favor::launch_decay_prefix(p, st), what);
+}
+
+favor_status run_scan(const favor::DecayPass &p, favor::Dt dt, hipStream_t st, const char *what) {
   favor::LaunchTimer t(favor::kKerDecayScan, st);
-  e = favor::launch_decay_scan(a, dt, st);
-  return device_result(e, what);
+  return device_result(favor::launch_decay_scan(p, dt, st), what);
 }
 
 }  // namespace
@@ -247,7 +266,10 @@ favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q, const vo
     return fail(FAVOR_ERR_INVALID_ARGUMENT, "out must not be an input");
   if (!heads || (!work && !state_out)) return ok();
   FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g, kOpForward)));
-  DecayScan a = shape_of(g, false);
+  favor::DecayPass p{};
+  p.n = 1;
+  DecayScan &a = p.scan[0];
+  a = scan_of(g, false, log_decay, lengths);
   a.q = Q;
   a.k = K;
   a.v = V;
@@ -256,15 +278,12 @@ favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q, const vo
   a.ks = rows_of(g, g->k, g->dk);
   a.vs = rows_of(g, g->v, g->dv);
   a.os = rows_of(g, g->out, g->dv);
-  a.log_decay = log_decay;
-  a.lengths = lengths;
   a.x_in = state_in;
   a.x_out = state_out;
   a.part = static_cast<float *>(ws);
-  a.shift = 1;
-  a.pair_scale = a.row_scale = g->scale;
-  a.sum_scale = 1.f;
-  return run_scan(a, dt_of(g), stream, "favor_attn_decay");
+  forward_order(a, g->scale);
+  FAVOR_TRY(run_sums(p, dt_of(g), stream, "favor_attn_decay segment sums"));
+  return run_scan(p, dt_of(g), stream, "favor_attn_decay");
 }
 
 favor_status favor_attn_decay_backward(const favor_decay_desc *g, const void *Q, const void *K,
@@ -293,60 +312,48 @@ favor_status favor_attn_decay_backward(const favor_decay_desc *g, const void *Q,
   const favor::Dt dt = dt_of(g);
   const Rows qs = rows_of(g, g->q, g->dk), ks = rows_of(g, g->k, g->dk),
              vs = rows_of(g, g->v, g->dv), ds = rows_of(g, g->grad_out, g->dv);
-  const auto scan = [&](bool swapped) {
-    DecayScan a = shape_of(g, swapped);
-    a.log_decay = log_decay;
-    a.lengths = lengths;
-    a.part = static_cast<float *>(ws);
-    a.x_t = swapped;
-    a.pair_scale = g->scale;
-    return a;
-  };
-  if (work) {
-    DecayScan a = scan(true);   // dQ: queries dout, keys V, values K
-    a.q = dout;
-    a.k = V;
-    a.v = K;
-    a.o = dQ;
-    a.qs = ds;
-    a.ks = vs;
-    a.vs = ks;
-    a.os = rows_of(g, g->grad_q, g->dk);
-    a.x_in = state_in;
-    a.shift = 1;
-    a.row_scale = g->scale;
-    a.sum_scale = 1.f;
-    FAVOR_TRY(run_scan(a, dt, stream, "favor_attn_decay_backward dQ"));
-    a = scan(true);             // dK: queries V, keys dout, values Q, from the last token
-    a.q = V;
-    a.k = dout;
-    a.v = Q;
-    a.o = dK;
-    a.qs = vs;
-    a.ks = ds;
-    a.vs = qs;
-    a.os = rows_of(g, g->grad_k, g->dk);
-    a.x_in = dstate_out;
-    a.reverse = 1;
-    a.row_scale = 1.f;
-    a.sum_scale = g->scale;
-    FAVOR_TRY(run_scan(a, dt, stream, "favor_attn_decay_backward dK"));
-  }
-  DecayScan a = scan(false);    // dV: queries K, keys Q, values dout, from the last token
-  a.q = K;
-  a.k = Q;
-  a.v = dout;
-  a.o = dV;
-  a.qs = ks;
-  a.ks = qs;
-  a.vs = ds;
-  a.os = rows_of(g, g->grad_v, g->dv);
-  a.x_in = dstate_out;
-  a.x_out = dstate_in;
-  a.reverse = 1;
-  a.row_scale = 1.f;
-  a.sum_scale = g->scale;
-  return run_scan(a, dt, stream, "favor_attn_decay_backward dV");
+  // dQ: queries dout, keys V, values K, on S^T; dK: queries V, keys dout, values Q, on R^T;
+  // dV: queries K, keys Q, values dout, on R
+  DecayScan dq = scan_of(g, true, log_decay, lengths), dk = dq;
+  DecayScan dv = scan_of(g, false, log_decay, lengths);
+  dq.q = dk.k = dv.v = dout;
+  dq.qs = dk.ks = dv.vs = ds;
+  dq.k = dk.q = V;
+  dq.ks = dk.qs = vs;
+  dq.v = dv.q = K;
+  dq.vs = dv.qs = ks;
+  dk.v = dv.k = Q;
+  dk.vs = dv.ks = qs;
+  dq.o = dQ;
+  dk.o = dK;
+  dv.o = dV;
+  dq.os = rows_of(g, g->grad_q, g->dk);
+  dk.os = rows_of(g, g->grad_k, g->dk);
+  dv.os = rows_of(g, g->grad_v, g->dv);
+  dq.x_in = state_in;
+  dk.x_in = dv.x_in = dstate_out;
+  dv.x_out = dstate_in;
+  dq.part = static_cast<float *>(ws);
+  dk.part = dv.part = dq.part + part_floats(g, dq.nseg);
+  forward_order(dq, g->scale);
+  reversed_order(dk, g->scale);
+  reversed_order(dv, g->scale);
+  // S of the segments from (K, V) and R from (Q, dout), both [dk][dv]
+  DecayScan s = dv;
+  s.k = K;
+  s.ks = ks;
+  s.v = V;
+  s.vs = vs;
+  s.x_in = state_in;
+  s.part = dq.part;
+  s.reverse = 0;
+  forward_order(s, g->scale);
+  FAVOR_TRY(run_sums({{s, dv}, 2}, dt, stream, "favor_attn_decay_backward segment sums"));
+  if (!work) return run_scan({{dv}, 1}, dt, stream, "favor_attn_decay_backward state gradient");
+  if (g->dk == g->dv)
+    return run_scan({{dk, dv, dq}, 3}, dt, stream, "favor_attn_decay_backward gradients");
+  FAVOR_TRY(run_scan({{dk, dq}, 2}, dt, stream, "favor_attn_decay_backward dK, dQ"));
+  return run_scan({{dv}, 1}, dt, stream, "favor_attn_decay_backward dV");
 }
 
 favor_status favor_attn_decay_step(const favor_decay_desc *g, const void *Q, const void *K,
