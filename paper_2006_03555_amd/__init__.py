@@ -541,18 +541,20 @@ def library_loaded_from():
 
 # ------------------------------------------------- linear attention with a decay per head
 def _require_here(*ts):
-    """The kernels run on the current device and read raw addresses there."""
-    here = None
+    """The kernels run on the current device and read raw addresses there. Returns that
+    device's number (-1 without a tensor)."""
+    here = -1
     for t in ts:
         if t is None:
             continue
-        if not t.is_cuda:
+        dev = t.get_device()
+        if dev < 0:
             raise FavorError(1, "tensors must be GPU tensors")
-        if here is None:
+        if here < 0:
             here = _torch().cuda.current_device()
-        if t.device.index != here:
-            raise FavorError(1, f"a tensor is on device {t.device.index}, the current device is "
-                                f"{here}")
+        if dev != here:
+            raise FavorError(1, f"a tensor is on device {dev}, the current device is {here}")
+    return here
 
 
 def _require_whole(*ts):
@@ -561,11 +563,15 @@ def _require_whole(*ts):
             raise FavorError(1, "states, decays, lengths and slots must be contiguous")
 
 
-def _row_strides(t, name):
-    """(batch, head, token) strides of [B, H, L, d] rows (token: any for [B, H, d]).
-    Dimensions of one element have no stride; d stands in for it, since three zeros
-    mean the contiguous layout."""
-    shape, s = t.shape, t.stride()
+def _like(t):
+    """What a call's plan depends on of one tensor."""
+    return None if t is None else (t.shape, t.dtype, t.stride())
+
+
+def _row_strides(shape, s, name):
+    """(batch, head, token) strides of [B, H, L, d] rows (token: any for [B, H, d]) of a
+    tensor with strides s. Dimensions of one element have no stride; d stands in for it,
+    since three zeros mean the contiguous layout."""
     d = shape[-1]
     if d > 1 and s[-1] != 1:
         raise FavorError(1, f"rows of {name} must be contiguous")
@@ -577,50 +583,75 @@ def _row_strides(t, name):
     return got
 
 
-_DECAY_STRIDES = ("q", "k", "v", "out", "grad_out", "grad_q", "grad_k", "grad_v")
-
-
 class _DecayCall:
-    """A decay descriptor with its by-reference argument and workspace sizes (see _Call)."""
-    __slots__ = ("g", "ref", "sizes")
+    """A decay descriptor with its by-reference argument and workspace size."""
+    __slots__ = ("g", "ref", "workspace")
 
-    def __init__(self, g):
+    def __init__(self, g, backward=None):
         self.g = g
         self.ref = ctypes.byref(g)
-        self.sizes = [None, None]
+        self.workspace = 0 if backward is None else decay_workspace_size(g, backward)
 
-    def workspace(self, backward):
-        n = self.sizes[backward]
-        if n is None:
-            n = self.sizes[backward] = decay_workspace_size(self.g, backward)
-        return n
+
+def _require_shape(like, shape, dtype, name):
+    if like is not None and (like[0] != shape or like[1] != dtype):
+        raise FavorError(1, f"{name} must be {tuple(shape)} {dtype}, got {tuple(like[0])} "
+                            f"{like[1]}")
 
 
 @functools.lru_cache(maxsize=256)
-def _decay_call(B, H, L, dk, dv, code, scale, strides):
-    return _DecayCall(make_decay_desc(B, H, L, dk, dv, code, scale,
-                                      **dict(zip(_DECAY_STRIDES, strides))))
+def _decay_plan(backward, q, k, v, rows, log_decay, lengths, states, scale):
+    """The _DecayCall of a forward (False), backward (True) or single-token (None) call, its
+    tensors' shapes and types checked. Every argument is made of _like()'s plain values, so
+    a program that makes the same call again pays for one look into the cache.
 
-
-def _decay_shapes(Q, K, V, log_decay, dims):
+    rows: (name, descriptor field, which of "qkv" it is shaped like, _like()) of the others.
+    """
     torch = _torch()
-    if Q.dim() != dims or V.dim() != dims:
-        want = "[B, H, L, d]" if dims == 4 else "[B, H, d]"
-        raise FavorError(1, f"inputs must be {want}, got {tuple(Q.shape)} and {tuple(V.shape)}")
-    if Q.shape[-1] == 0 or V.shape[-1] == 0:
+    dims = 3 if backward is None else 4
+    if len(q[0]) != dims or len(v[0]) != dims:
+        want = "[B, H, d]" if dims == 3 else "[B, H, L, d]"
+        raise FavorError(1, f"inputs must be {want}, got {tuple(q[0])} and {tuple(v[0])}")
+    B, H = q[0][:2]
+    L = 1 if backward is None else q[0][2]
+    dk, dv = q[0][-1], v[0][-1]
+    if dk == 0 or dv == 0:
         raise FavorError(1, "dk and dv must be positive")
-    _require_like(K, Q.shape, Q.dtype, "K")
-    _require_like(V, Q.shape[:-1] + V.shape[-1:], Q.dtype, "V")
-    _require_like(log_decay, (Q.shape[1],), torch.float32, "log_decay")
+    dtype = q[1]
+    _require_shape(k, q[0], dtype, "K")
+    _require_shape(v, q[0][:-1] + (dv,), dtype, "V")
+    _require_shape(log_decay, (H,), torch.float32, "log_decay")
+    _require_shape(lengths, (B,), torch.int32, "slots" if backward is None else "lengths")
+    strides = {n: _row_strides(t[0], t[2], n.upper()) for n, t in (("q", q), ("k", k), ("v", v))}
+    like = {"q": q, "k": k, "v": v}
+    for name, field, of, t in rows:
+        _require_shape(t, like[of][0], dtype, name)
+        if t is not None:
+            strides[field] = _row_strides(t[0], t[2], name)
+    for name, t in states:
+        if t is not None:
+            n = t[0][0] if backward is None and len(t[0]) == 4 else B
+            _require_shape(t, (n, H, dk, dv), torch.float32, name)
+    return _DecayCall(make_decay_desc(B, H, L, dk, dv, _dtype_code(dtype), scale, **strides),
+                      backward)
 
 
 def _decay_workspace(n, workspace):
-    if n == 0 and workspace is None:
-        return None, 0
     if workspace is not None:
         _require_here(workspace)
         _require_whole(workspace)
+    elif n == 0:
+        return None, 0
     return _workspace_of(n, workspace)
+
+
+def _stream_on(device, stream):
+    """As _stream, where the current device is already known (-1: it is not)."""
+    if stream is None and device >= 0:
+        raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(device)
+    return _stream(stream)
 
 
 @_on_stream
@@ -637,27 +668,21 @@ def attn_decay(Q, K, V, log_decay, scale=1.0, lengths=None, state_in=None, retur
     given), or (out, state_out) when return_state is true.
     """
     torch = _torch()
-    _decay_shapes(Q, K, V, log_decay, 4)
-    B, H, L, dk = Q.shape
-    dv = V.shape[3]
-    sshape = (B, H, dk, dv)
     if out is None:
         out = torch.empty_like(V)
+    c = _decay_plan(False, _like(Q), _like(K), _like(V), (("out", "out", "v", _like(out)),),
+                    _like(log_decay), _like(lengths),
+                    (("state_in", _like(state_in)), ("state_out", _like(state_out))),
+                    float(scale))
     if return_state and state_out is None:
-        state_out = torch.empty(sshape, dtype=torch.float32, device=Q.device)
-    _require_like(out, V.shape, V.dtype, "out")
-    _require_like(lengths, (B,), torch.int32, "lengths")
-    _require_like(state_in, sshape, torch.float32, "state_in")
-    _require_like(state_out, sshape, torch.float32, "state_out")
-    _require_here(Q, K, V, log_decay, lengths, out, state_in, state_out)
+        g = c.g
+        state_out = torch.empty((g.B, g.H, g.dk, g.dv), dtype=torch.float32, device=Q.device)
+    here = _require_here(Q, K, V, log_decay, lengths, out, state_in, state_out)
     _require_whole(log_decay, lengths, state_in, state_out)
-    c = _decay_call(B, H, L, dk, dv, _dtype_code(Q.dtype), float(scale),
-                    (_row_strides(Q, "Q"), _row_strides(K, "K"), _row_strides(V, "V"),
-                     _row_strides(out, "out")))
-    ws, nbytes = _decay_workspace(c.workspace(0), workspace)
+    ws, nbytes = _decay_workspace(c.workspace, workspace)
     _check(lib().favor_attn_decay(c.ref, _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay),
                                   _ptr(lengths), _ptr(out), _ptr(state_in), _ptr(state_out),
-                                  _ptr(ws), nbytes, _stream(stream)))
+                                  _ptr(ws), nbytes, _stream_on(here, stream)))
     return (out, state_out) if return_state else out
 
 
@@ -672,35 +697,25 @@ def attn_decay_backward(Q, K, V, log_decay, dout, scale=1.0, lengths=None, state
     Returns (dQ, dK, dV), or (dQ, dK, dV, dstate_in) when return_state_grad is true.
     """
     torch = _torch()
-    _decay_shapes(Q, K, V, log_decay, 4)
-    B, H, L, dk = Q.shape
-    dv = V.shape[3]
-    sshape = (B, H, dk, dv)
-    grads = []
-    for name, t, x in (("dQ", dQ, Q), ("dK", dK, K), ("dV", dV, V)):
-        if t is None:
-            t = torch.empty_like(x)
-        _require_like(t, x.shape, x.dtype, name)
-        grads.append(t)
-    dQ, dK, dV = grads
+    dQ, dK, dV = (torch.empty_like(x) if t is None else t
+                  for t, x in ((dQ, Q), (dK, K), (dV, V)))
+    c = _decay_plan(True, _like(Q), _like(K), _like(V),
+                    (("dout", "grad_out", "v", _like(dout)), ("dQ", "grad_q", "q", _like(dQ)),
+                     ("dK", "grad_k", "k", _like(dK)), ("dV", "grad_v", "v", _like(dV))),
+                    _like(log_decay), _like(lengths),
+                    (("state_in", _like(state_in)), ("dstate_out", _like(dstate_out)),
+                     ("dstate_in", _like(dstate_in))), float(scale))
     if return_state_grad and dstate_in is None:
-        dstate_in = torch.empty(sshape, dtype=torch.float32, device=Q.device)
-    _require_like(dout, V.shape, V.dtype, "dout")
-    _require_like(lengths, (B,), torch.int32, "lengths")
-    for name, t in (("state_in", state_in), ("dstate_out", dstate_out),
-                    ("dstate_in", dstate_in)):
-        _require_like(t, sshape, torch.float32, name)
-    _require_here(Q, K, V, log_decay, lengths, dout, dQ, dK, dV, state_in, dstate_out, dstate_in)
+        g = c.g
+        dstate_in = torch.empty((g.B, g.H, g.dk, g.dv), dtype=torch.float32, device=Q.device)
+    here = _require_here(Q, K, V, log_decay, lengths, dout, dQ, dK, dV, state_in, dstate_out,
+                         dstate_in)
     _require_whole(log_decay, lengths, state_in, dstate_out, dstate_in)
-    c = _decay_call(B, H, L, dk, dv, _dtype_code(Q.dtype), float(scale),
-                    (_row_strides(Q, "Q"), _row_strides(K, "K"), _row_strides(V, "V"), (0, 0, 0),
-                     _row_strides(dout, "dout"), _row_strides(dQ, "dQ"), _row_strides(dK, "dK"),
-                     _row_strides(dV, "dV")))
-    ws, nbytes = _decay_workspace(c.workspace(1), workspace)
+    ws, nbytes = _decay_workspace(c.workspace, workspace)
     _check(lib().favor_attn_decay_backward(
         c.ref, _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(lengths), _ptr(state_in),
         _ptr(dout), _ptr(dstate_out), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(dstate_in), _ptr(ws),
-        nbytes, _stream(stream)))
+        nbytes, _stream_on(here, stream)))
     return (dQ, dK, dV, dstate_in) if return_state_grad else (dQ, dK, dV)
 
 
@@ -714,25 +729,16 @@ def attn_decay_step(q, k, v, log_decay, state, scale=1.0, slots=None, out=None, 
     its own index); one outside 0 .. n - 1 is padding and gives out = 0. Returns out
     [B, H, dv].
     """
-    torch = _torch()
-    _decay_shapes(q, k, v, log_decay, 3)
-    B, H, dk = q.shape
-    dv = v.shape[2]
-    if state.dim() != 4:
-        raise FavorError(1, f"state must be [n, H, dk, dv], got {tuple(state.shape)}")
-    _require_like(state, (state.shape[0], H, dk, dv), torch.float32, "state")
-    _require_like(slots, (B,), torch.int32, "slots")
     if out is None:
-        out = torch.empty((B, H, dv), dtype=v.dtype, device=v.device)
-    _require_like(out, v.shape, v.dtype, "out")
-    _require_here(q, k, v, log_decay, state, slots, out)
+        out = _torch().empty_like(v, memory_format=_torch().contiguous_format)
+    c = _decay_plan(None, _like(q), _like(k), _like(v), (("out", "out", "v", _like(out)),),
+                    _like(log_decay), _like(slots), (("state", _like(state)),), float(scale))
+    here = _require_here(q, k, v, log_decay, state, slots, out)
     _require_whole(log_decay, state, slots)
-    c = _decay_call(B, H, 1, dk, dv, _dtype_code(q.dtype), float(scale),
-                    (_row_strides(q, "q"), _row_strides(k, "k"), _row_strides(v, "v"),
-                     _row_strides(out, "out")))
-    _check(lib().favor_attn_decay_step(c.ref, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay),
-                                       _ptr(slots), state.shape[0], _ptr(state), _ptr(out),
-                                       _stream(stream)))
+    _check(lib().favor_attn_decay_step(c.ref, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                       log_decay.data_ptr(), _ptr(slots), state.shape[0],
+                                       state.data_ptr(), out.data_ptr(),
+                                       _stream_on(here, stream)))
     return out
 
 
@@ -752,14 +758,13 @@ def dropout(x, p, seed=0, offset=0, residual=None, out=None, rng=None, stream=No
     _require_like(out, x.shape, x.dtype, "out")
     if rng is not None and (rng.shape != (2,) or rng.dtype not in (torch.int64, torch.uint64)):
         raise FavorError(1, f"rng must be two 64-bit words, got {tuple(rng.shape)} {rng.dtype}")
-    _require_here(x, residual, out, rng)
+    here = _require_here(x, residual, out, rng)
     _require_cuda(x, residual, out, rng)
-    for name, v in (("seed", seed), ("offset", offset)):
-        if not 0 <= operator.index(v) < 1 << 64:
-            raise FavorError(1, f"{name} must be a 64-bit unsigned number, got {v}")
+    if not (0 <= operator.index(seed) < 1 << 64 and 0 <= operator.index(offset) < 1 << 64):
+        raise FavorError(1, f"seed and offset are 64-bit unsigned numbers, got {seed}, {offset}")
     _check(lib().favor_dropout(_ptr(x), _ptr(residual), _ptr(out), x.numel(),
                                _dtype_code(x.dtype), float(p), seed, offset, _ptr(rng),
-                               _stream(stream)))
+                               _stream_on(here, stream)))
     return out
 
 

@@ -278,7 +278,10 @@ def test_binding_refusals():
 
 def test_binding_strides():
     import torch
-    rows = fv._row_strides
+
+    def rows(t, name):
+        return fv._row_strides(t.shape, t.stride(), name)
+
     x = torch.zeros(2, 5, 3, 8)
     assert rows(x, "x") == (120, 24, 8)
     assert rows(x.transpose(1, 2), "x") == (120, 8, 24)
