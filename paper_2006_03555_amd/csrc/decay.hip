@@ -266,7 +266,7 @@ struct Staged {
 #pragma unroll
     for (int k = 0; k < N; ++k)
       r[k] = __builtin_amdgcn_raw_buffer_load_b128(
-          x, row + k * kRows < n ? off : kOutside, (reverse ? N - 1 - k : k) * step, 0);
+          x, row < n - k * kRows ? off : kOutside, (reverse ? N - 1 - k : k) * step, 0);
   }
   __device__ __forceinline__ void store(T *tile) const {
     const int row = threadIdx.x / kUnits, granule = threadIdx.x % kUnits * (kPer / 4);
@@ -343,60 +343,73 @@ __device__ __forceinline__ void put(float (&x)[4], f32x4 v) {
 }
 __device__ __forceinline__ f32x4 get(const float (&x)[4]) { return f32x4{x[0], x[1], x[2], x[3]}; }
 
-// X of one head at p ([kd][vd], or transposed), four k rows of one column at a time.
-__device__ __forceinline__ f32x4 read_state(const DecayScan &a, const float *p, int kc, int vc) {
-  f32x4 x{0.f, 0.f, 0.f, 0.f};
-  if (vc < a.vd && kc < a.kd) {
-    if (a.x_t) {
-      x = *reinterpret_cast<const f32x4 *>(p + vc * a.kd + kc);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = p[(kc + j) * a.vd + vc];
-    }
-  }
-  return x;
-}
-__device__ __forceinline__ void write_state(const DecayScan &a, float *p, int kc, int vc,
-                                            const float (&x)[4]) {
-  if (vc < a.vd && kc < a.kd) {
-    if (a.x_t) {
-      *reinterpret_cast<f32x4 *>(p + vc * a.kd + kc) = get(x);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[(kc + j) * a.vd + vc] = x[j];
-    }
-  }
-}
 // The sums of a segment, and later X before the one behind it.
 __device__ __forceinline__ float *part_of(const DecayScan &a, int bh, int seg) {
   return a.part + ((size_t)bh * (a.nseg - 1) + seg) * (a.kd * a.vd);
 }
 
+// X of one head in memory ([kd][vd], or transposed): four k rows of one column at a time,
+// without branches (null reads as zeros).
+struct StateRows {
+  __amdgpu_buffer_rsrc_t rows;
+  int kd, vd;
+  bool x_t;
+  __device__ __forceinline__ StateRows(const DecayScan &a, const float *p)
+      : rows(__builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p), 0, p ? kOutside : 0,
+                                               0x00020000)),
+        kd(a.kd), vd(a.vd), x_t(a.x_t) {}
+  __device__ __forceinline__ uint32_t at(int kc, int vc) const {
+    return vc < vd && kc < kd ? 4 * (uint32_t)(x_t ? vc * kd + kc : kc * vd + vc) : kOutside;
+  }
+  __device__ __forceinline__ void read(float (&x)[4], int kc, int vc) const {
+    const uint32_t off = at(kc, vc);
+    if (x_t) {
+      put(x, __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, off, 0, 0)));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rows, off, 4 * j * vd, 0));
+    }
+  }
+  __device__ __forceinline__ void write(const float (&x)[4], int kc, int vc) const {
+    const uint32_t off = at(kc, vc);
+    if (x_t) {
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, get(x)), rows, off, 0, 0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[j]), rows, off, 4 * j * vd, 0);
+    }
+  }
+};
+
 template <int KD, int NW, int NCT>
 __device__ __forceinline__ void load_state(const DecayScan &a, const Item &it,
                                            State<KD, NCT> &s) {
   const int l = lane_id(), w0 = 16 * NCT * (NW * it.slice + wave_id());
-  const float *p = it.seg > 0 ? part_of(a, it.bh, it.seg - 1)
-                   : a.x_in   ? a.x_in + (size_t)it.bh * (a.kd * a.vd)
-                              : nullptr;
+  const StateRows rows(a, it.seg > 0 ? part_of(a, it.bh, it.seg - 1)
+                          : a.x_in   ? a.x_in + (size_t)it.bh * (a.kd * a.vd)
+                                     : nullptr);
 #pragma unroll
-  for (int nb = 0; nb < KD / 16; ++nb)
+  for (int nb = 0; nb < KD / 16; ++nb) {
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
-      put(s.x[nb][ct], p ? read_state(a, p, 16 * nb + 4 * (l >> 4),
-                                      w0 + value_col<NCT>(ct, l & 15))
-                         : f32x4{0.f, 0.f, 0.f, 0.f});
+      rows.read(s.x[nb][ct], 16 * nb + 4 * (l >> 4), w0 + value_col<NCT>(ct, l & 15));
+  }
 }
 
 template <int KD, int NW, int NCT>
 __device__ __forceinline__ void store_state(const DecayScan &a, const Item &it, float *p,
                                             const State<KD, NCT> &s) {
   const int l = lane_id(), w0 = 16 * NCT * (NW * it.slice + wave_id());
+  const StateRows rows(a, p);
 #pragma unroll
-  for (int nb = 0; nb < KD / 16; ++nb)
+  for (int nb = 0; nb < KD / 16; ++nb) {
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
-      write_state(a, p, 16 * nb + 4 * (l >> 4), w0 + value_col<NCT>(ct, l & 15), s.x[nb][ct]);
+      rows.write(s.x[nb][ct], 16 * nb + 4 * (l >> 4), w0 + value_col<NCT>(ct, l & 15));
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 // The wave's value columns of a chunk, transposed: tokens in chained order.
@@ -459,7 +472,8 @@ __device__ __forceinline__ void update_state(
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         s.x[nb][ct][j] = fmaf(s.x[nb][ct][j], carry, u[ct][j]);
-    if (nb & 1) __builtin_amdgcn_sched_barrier(0);
+    // so many tiles' operands at a time as registers are left for
+    if (nb % (NCT == 2 ? 2 : 8) == (NCT == 2 ? 1 : 7)) __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -525,7 +539,7 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
   const double d = power(a.log_decay[it.h], a.seg_len);
   const float hi = (float)d, lo = isfinite(hi) ? (float)(d - hi) : 0.f;
   f32x4 *p = reinterpret_cast<f32x4 *>(part_of(a, it.bh, 0)) + e;
-  constexpr int kAhead = 4;   // loads in flight
+  constexpr int kAhead = 16;   // loads in flight
   for (int s = 0; s < last; s += kAhead, p += kAhead * n) {
     f32x4 u[kAhead];
 #pragma unroll
@@ -569,13 +583,18 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   qr.start(a.qs, a.reverse, a.kd);
   kr.start(a.ks, a.reverse, a.kd);
   vr.start(a.vs, a.reverse, a.vd - v0);
+  const auto fetch_q = [&](int c) {
+    qr.load(chunk_rows<T>(a.q, a.qs, it, 0, a.reverse, it.first + c), a.qs, a.reverse, it.n - c);
+  };
   const auto fetch = [&](int c) {
     const int r = it.first + c, n = it.n - c;
-    qr.load(chunk_rows<T>(a.q, a.qs, it, 0, a.reverse, r), a.qs, a.reverse, n);
     kr.load(chunk_rows<T>(a.k, a.ks, it, 0, a.reverse, r), a.ks, a.reverse, n);
     vr.load(chunk_rows<T>(a.v, a.vs, it, v0, a.reverse, r), a.vs, a.reverse, n);
   };
-  if (it.n > 0) fetch(0);
+  if (it.n > 0) {
+    fetch_q(0);
+    fetch(0);
+  }
   State<KD, NCT> s;
   load_state<KD, NW, NCT>(a, it, s);
   fill_powers(pw, a.log_decay[it.h]);
@@ -596,7 +615,14 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
     vr.store(Vs);
     if (c == 0 || n < kChunkT) fill_sum(pw, n, a.shift, a.sum_scale);
     __syncthreads();
-    if (c + kChunkT < it.n) fetch(c + kChunkT);
+    // At 256 k columns the next queries wait until the pairs' operands leave registers free.
+    // (Their fetch has no condition, which would keep the old rows in registers until then;
+    // behind the last chunk it reads nothing.)
+    constexpr bool kLateQ = KD == 256;
+    if (kLateQ || c + kChunkT < it.n) {
+      if (!kLateQ) fetch_q(c + kChunkT);
+      fetch(c + kChunkT);
+    }
 
     const lds_t zero = c & a.zero;
     const RowReader<T, KD> queries(lds_of(Qs) + zero), keys(lds_of(Ks) + zero);
@@ -610,8 +636,10 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       for (int j = 0; j < 4; ++j) wt[j] = pw.pair[16 + e - j];
       f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
+      for (int p = 0; p < NP; ++p) {
         x = P::mma(keys(jb, p), queries(ib, p), x);
+        if (p % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // not all operands at once
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = e >= j ? x[j] * wt[j] : 0.f;   // (an Inf of j > i goes)
       T *pp = reinterpret_cast<T *>(&Ps[(first(ib) + (jb >> 1)) * 64 + l]);
@@ -638,6 +666,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    if (kLateQ) fetch_q(c + kChunkT);
 #pragma unroll
     for (int ib = 0; ib < 4; ++ib) {
       const float f = pw.row[16 * ib + c16];
@@ -660,7 +689,8 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(vt[ct][m], pf, o[ib][ct]);
       }
-      put_row<T, NCT>(rows, 16 * ib + c16 < n && v0 + vc < a.vd ? ooff + zero + ib * ostep : kOutside, o[ib]);
+      put_row<T, NCT>(rows, c16 < n - 16 * ib && vc < a.vd - v0 ? ooff + zero + ib * ostep : kOutside,
+                      o[ib]);
     }
     weigh_values<T, NCT>(vw, vt, pw, a.minus);
     update_state<T, KD, NCT>(s, lds_of(Ks) + zero, vw, n == kChunkT ? carry.next() : pw.a[n]);
@@ -683,7 +713,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
 template <typename T, int KD, int NW, int NCT>
 hipError_t launch(const DecayPass &pass, bool sums, hipStream_t st) {
   const DecayScan &a = pass.scan[0];
-  const int heads = pass.n * a.BH * decay_slices(a.kd, a.vd);
+  const int heads = pass.n * a.BH * ((a.vd + a.slice - 1) / a.slice);
   if (sums)
     k_decay_sums<T, KD, NW, NCT><<<heads * (a.nseg - 1), 64 * NW, 0, st>>>(pass);
   else
@@ -697,7 +727,7 @@ template <typename T>
 hipError_t dispatch(const DecayPass &p, bool sums, hipStream_t st) {
   constexpr int NW = sizeof(T) == 2 ? 4 : 8, NCT = 8 / NW;
   const int kd = p.scan[0].kd;
-  const bool wide = decay_slice(kd, p.scan[0].vd) == 128;
+  const bool wide = p.scan[0].slice == 128;
   if (kd <= 64) return wide ? launch<T, 64, NW, NCT>(p, sums, st) : launch<T, 64, 4, 1>(p, sums, st);
   if (kd <= 128)
     return wide ? launch<T, 128, NW, NCT>(p, sums, st) : launch<T, 128, 4, 1>(p, sums, st);
@@ -705,10 +735,6 @@ hipError_t dispatch(const DecayPass &p, bool sums, hipStream_t st) {
 }
 
 }  // namespace
-
-// 64 columns for narrow values, and with more than 128 k columns, whose X would not
-// leave room for the operands in registers.
-int decay_slice(int kd, int vd) { return kd > 128 || vd <= 64 ? 64 : 128; }
 
 hipError_t launch_decay_sums(const DecayPass &p, Dt dt, hipStream_t st) {
   return dt == Dt::BF16 ? dispatch<bf16>(p, true, st) : dispatch<float>(p, true, st);

@@ -31,24 +31,18 @@ struct DecayScan {
   int x_t;                 // x_in, x_out and part hold [vd][kd]
   int BH, H, L, kd, vd;
   int seg_len, nseg;       // segments of seg_len rows (a multiple of 64)
+  int slice;               // columns of v that one workgroup takes: 64, or 128 (kd <= 128)
   int reverse, shift;
   float pair_scale, row_scale, sum_scale;
   int zero = 0;   // the loops' addresses depend on it: they are formed anew, not kept
   uint32_t minus[2] = {0x0000bf80u, 0xbf800000u};   // bf16 pairs (-1, 0) and (0, -1)
 };
 
-// Scans launched together: the same kd, vd, heads and segments. At most three.
+// Scans launched together: the same kd, vd, slices, heads and segments. At most three.
 struct DecayPass {
   DecayScan scan[3];
   int n;
 };
-
-// Columns of v that one workgroup takes, and slices of them.
-int decay_slice(int kd, int vd);
-inline int decay_slices(int kd, int vd) {
-  const int s = decay_slice(kd, vd);
-  return (vd + s - 1) / s;
-}
 
 // The sums of every segment but the last, in part.
 hipError_t launch_decay_sums(const DecayPass &p, Dt dt, hipStream_t st);

@@ -146,20 +146,52 @@ favor::Dt dt_of(const favor_decay_desc *g) {
   return raw_enum(&g->dtype) == FAVOR_BF16 ? favor::Dt::BF16 : favor::Dt::F32;
 }
 
-// Segments of one scan with kd k columns and vd value columns: enough workgroups for two
-// on each of the 256 compute units, of at least 256 rows each.
-constexpr int kTargetWorkgroups = 512;
-constexpr int kMinRows = 256;
+// How a scan with kd k columns and vd value columns is cut: its value columns into slices,
+// one per workgroup, and its rows into segments. A call of several segments runs a pass
+// for their sums and one that chains them first, so K and V are read twice.
+struct Cut {
+  int slice;
+  int seg_len, nseg;
+};
 
-void plan(const favor_decay_desc *g, int kd, int vd, int &seg_len, int &nseg) {
+// Whole calls in us (one to eight chunks of 64 rows per segment; a chunk takes a workgroup
+// that has a compute unit for itself 2.4 us at 64 x 64 bf16, 4 at 128 x 128, 6 and 12 in fp32):
+//   Long sequences: segments for 512 workgroups, two on each of the 256 compute units, as
+//   long as they have 256 rows.
+//   Shorter ones: as many segments as it takes for 256 workgroups, of one chunk at least,
+//   from four chunks on. B1 H8, with 256-row segments / with this: bf16 64 x 64 L512
+//   22.5 / 13.6, L4096 25.3 / 22.2; 128 x 128 L1024 40.2 / 24.0; fp32 128 x 128 L512
+//   79.9 / 25.4, L4096 87.7 / 66.6. For 512 workgroups instead: bf16 64 x 64 L4096 28.4,
+//   fp32 128 x 128 L2048 42.8 -> 50.4. Two chunks apart: bf16 64 x 64 L128 8.9 / 13.4.
+//   Slices of 64 value columns for wider values while the chunks are few: twice as many
+//   workgroups, each with half the work per chunk and the pair weights to itself. B1 H8
+//   128 x 128, slices of 128 / 64: bf16 L128 15.8 / 11.9, L4096 39.4 / 38.3, B2 H16 L16384
+//   215 / 217; fp32 L2048 45.5 / 42.8, L4096 62.1 / 66.6. With more than 128 k columns X
+//   leaves room for no more.
+constexpr int kFullWorkgroups = 512, kMinRows = 256;
+constexpr int kSomeWorkgroups = 256, kMinSplitTiles = 4;
+constexpr int kNarrowTiles = 512, kNarrowTilesF32 = 256;
+
+// scans: how many run together on g's heads.
+Cut cut_of(const favor_decay_desc *g, int kd, int vd, int scans) {
   const int tiles = std::max(1, (g->L + 63) / 64);
-  const int have = g->B * g->H * favor::decay_slices(kd, vd);
-  int want = (kTargetWorkgroups + have - 1) / have;
-  want = std::max(1, std::min(want, tiles / (kMinRows / 64)));
+  const int heads = g->B * g->H * scans;
+  const bool few = (long long)heads * tiles * ((vd + 127) / 128) <=
+                   (raw_enum(&g->dtype) == FAVOR_BF16 ? kNarrowTiles : kNarrowTilesF32);
+  Cut c;
+  c.slice = kd > 128 || vd <= 64 || few ? 64 : 128;
+  const int have = heads * ((vd + c.slice - 1) / c.slice);
+  const int full = std::min(kFullWorkgroups / have, tiles / (kMinRows / 64));
+  const int some = tiles < kMinSplitTiles ? 1 : std::min(kSomeWorkgroups / have, tiles);
+  const int want = std::max(1, std::max(full, some));
   const int per = (tiles + want - 1) / want;
-  seg_len = 64 * per;
-  nseg = (tiles + per - 1) / per;
+  c.seg_len = 64 * per;
+  c.nseg = (tiles + per - 1) / per;
+  return c;
 }
+
+// The backward pass sums for two scans and then runs three; its segments are cut for two.
+constexpr int kBackwardScans = 2;
 
 // Floats of one scan's segment states.
 size_t part_floats(const favor_decay_desc *g, int nseg) {
@@ -171,9 +203,7 @@ size_t part_floats(const favor_decay_desc *g, int nseg) {
 // share one plan.
 size_t workspace_of(const favor_decay_desc *g, int op) {
   if ((long long)g->B * g->H == 0 || g->L == 0) return 0;
-  int seg_len, nseg;
-  plan(g, g->dk, g->dv, seg_len, nseg);
-  return round_up(part_floats(g, nseg) * sizeof(float) * (op == kOpBackward ? 2 : 1), 256);
+  return round_up(part_floats(g, cut_of(g, g->dk, g->dv, op == kOpBackward ? kBackwardScans : 1).nseg) * sizeof(float) * (op == kOpBackward ? 2 : 1), 256);
 }
 
 favor_status check_workspace(const void *ws, size_t bytes, size_t need) {
@@ -188,7 +218,7 @@ favor_status check_workspace(const void *ws, size_t bytes, size_t need) {
 
 // A scan of g: kd, vd (exchanged on the transposed state), its segments and the arguments
 // that all have in common.
-DecayScan scan_of(const favor_decay_desc *g, bool swapped, const float *log_decay,
+DecayScan scan_of(const favor_decay_desc *g, bool swapped, int scans, const float *log_decay,
                   const int32_t *lengths) {
   DecayScan a{};
   a.log_decay = log_decay;
@@ -199,7 +229,10 @@ DecayScan scan_of(const favor_decay_desc *g, bool swapped, const float *log_deca
   a.kd = swapped ? g->dv : g->dk;
   a.vd = swapped ? g->dk : g->dv;
   a.x_t = swapped;
-  plan(g, g->dk, g->dv, a.seg_len, a.nseg);
+  const Cut c = cut_of(g, g->dk, g->dv, scans);
+  a.seg_len = c.seg_len;
+  a.nseg = c.nseg;
+  a.slice = cut_of(g, a.kd, a.vd, scans).slice;
   a.pair_scale = g->scale;
   return a;
 }
@@ -269,7 +302,7 @@ favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q, const vo
   favor::DecayPass p{};
   p.n = 1;
   DecayScan &a = p.scan[0];
-  a = scan_of(g, false, log_decay, lengths);
+  a = scan_of(g, false, 1, log_decay, lengths);
   a.q = Q;
   a.k = K;
   a.v = V;
@@ -314,8 +347,8 @@ favor_status favor_attn_decay_backward(const favor_decay_desc *g, const void *Q,
              vs = rows_of(g, g->v, g->dv), ds = rows_of(g, g->grad_out, g->dv);
   // dQ: queries dout, keys V, values K, on S^T; dK: queries V, keys dout, values Q, on R^T;
   // dV: queries K, keys Q, values dout, on R
-  DecayScan dq = scan_of(g, true, log_decay, lengths), dk = dq;
-  DecayScan dv = scan_of(g, false, log_decay, lengths);
+  DecayScan dq = scan_of(g, true, kBackwardScans, log_decay, lengths), dk = dq;
+  DecayScan dv = scan_of(g, false, kBackwardScans, log_decay, lengths);
   dq.q = dk.k = dv.v = dout;
   dq.qs = dk.ks = dv.vs = ds;
   dq.k = dk.q = V;

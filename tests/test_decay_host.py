@@ -190,7 +190,7 @@ def _backward(g, ws=A, n=1 << 40, **kw):
 def test_backward_refusals():
     g = _desc(L=100000, B=1)
     need = fv.decay_workspace_size(g, True)
-    assert need >= fv.decay_workspace_size(g)
+    assert need > 0 and need % 256 == 0
     for name in ("Q", "K", "V", "log_decay", "dout", "dQ", "dK", "dV"):
         assert _backward(g, **{name: NUL}) == 1, name
         assert name in fv.last_error()
