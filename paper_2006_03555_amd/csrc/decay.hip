@@ -343,21 +343,20 @@ __device__ __forceinline__ void put(float (&x)[4], f32x4 v) {
 }
 __device__ __forceinline__ f32x4 get(const float (&x)[4]) { return f32x4{x[0], x[1], x[2], x[3]}; }
 
-// The sums of a segment, and later X before the one behind it.
+// X before a segment; until the prefix pass, the sums of the segment in front of it.
 __device__ __forceinline__ float *part_of(const DecayScan &a, int bh, int seg) {
-  return a.part + ((size_t)bh * (a.nseg - 1) + seg) * (a.kd * a.vd);
+  return a.part + ((size_t)bh * a.nseg + seg) * (a.kd * a.vd);
 }
 
 // X of one head in memory ([kd][vd], or transposed): four k rows of one column at a time,
-// without branches (null reads as zeros).
+// without branches. Null has no rows: it reads as zeros.
 struct StateRows {
   __amdgpu_buffer_rsrc_t rows;
   int kd, vd;
   bool x_t;
   __device__ __forceinline__ StateRows(const DecayScan &a, const float *p)
-      : rows(__builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p), 0, p ? kOutside : 0,
-                                               0x00020000)),
-        kd(a.kd), vd(a.vd), x_t(a.x_t) {}
+      : rows(__builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p), 0, kOutside, 0x00020000)),
+        kd(p ? a.kd : 0), vd(a.vd), x_t(a.x_t) {}
   __device__ __forceinline__ uint32_t at(int kc, int vc) const {
     return vc < vd && kc < kd ? 4 * (uint32_t)(x_t ? vc * kd + kc : kc * vd + vc) : kOutside;
   }
@@ -387,9 +386,11 @@ template <int KD, int NW, int NCT>
 __device__ __forceinline__ void load_state(const DecayScan &a, const Item &it,
                                            State<KD, NCT> &s) {
   const int l = lane_id(), w0 = 16 * NCT * (NW * it.slice + wave_id());
-  const StateRows rows(a, it.seg > 0 ? part_of(a, it.bh, it.seg - 1)
-                          : a.x_in   ? a.x_in + (size_t)it.bh * (a.kd * a.vd)
-                                     : nullptr);
+  // With several segments X_0 too comes from the workspace: the caller's may already hold
+  // X_n, where they are the same.
+  const float *p = a.x_in ? a.x_in + (size_t)it.bh * (a.kd * a.vd) : nullptr;
+  if (a.nseg > 1 && (it.seg > 0 || p)) p = part_of(a, it.bh, it.seg);
+  const StateRows rows(a, p);
 #pragma unroll
   for (int nb = 0; nb < KD / 16; ++nb) {
 #pragma unroll
@@ -521,24 +522,26 @@ __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
     update_state<T, KD, NCT>(s, lds_of(Ks) + zero, vw, carry.next());
     __syncthreads();
   }
-  store_state<KD, NW, NCT>(a, it, part_of(a, it.bh, it.seg), s);
+  store_state<KD, NW, NCT>(a, it, part_of(a, it.bh, it.seg + 1), s);
 }
 
-// part of a head's segments: X before segment s + 1 = a^seg_len (X before s) + sums of s,
-// four elements per thread.
+// part of a head's segments: X_0, then X before segment s + 1 = a^seg_len (X before s) + sums
+// of s, four elements per thread.
 __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
   int id = blockIdx.y;
   const DecayScan &a = scan_of(pass, id);
   const int e = blockIdx.x * 256 + threadIdx.x, n = a.kd * a.vd / 4;
   const Item it = item_of(a, id, 1, 1);
   const int last = last_seg(a, it.len);
-  if (e >= n || last == 0) return;
+  if (e >= n) return;
   f32x4 x{0.f, 0.f, 0.f, 0.f};
   if (a.x_in) x = reinterpret_cast<const f32x4 *>(a.x_in)[(size_t)it.bh * n + e];
   // a^seg_len as two floats: it meets X once per segment
   const double d = power(a.log_decay[it.h], a.seg_len);
   const float hi = (float)d, lo = isfinite(hi) ? (float)(d - hi) : 0.f;
   f32x4 *p = reinterpret_cast<f32x4 *>(part_of(a, it.bh, 0)) + e;
+  *p = x;
+  p += n;
   constexpr int kAhead = 16;   // loads in flight
   for (int s = 0; s < last; s += kAhead, p += kAhead * n) {
     f32x4 u[kAhead];

@@ -27,7 +27,7 @@ struct DecayScan {
   const int32_t *lengths;  // [B], or null: every sequence has L tokens
   const float *x_in;       // X_0 [BH][kd][vd], or null for zeros
   float *x_out;            // X_n, or null
-  float *part;             // [BH][nseg - 1][X]: the segments' sums, then X behind each
+  float *part;             // nseg > 1: [BH][nseg][X], X before each segment (first their sums)
   int x_t;                 // x_in, x_out and part hold [vd][kd]
   int BH, H, L, kd, vd;
   int seg_len, nseg;       // segments of seg_len rows (a multiple of 64)

@@ -195,7 +195,7 @@ constexpr int kBackwardScans = 2;
 
 // Floats of one scan's segment states.
 size_t part_floats(const favor_decay_desc *g, int nseg) {
-  return (size_t)g->B * g->H * (nseg - 1) * g->dk * g->dv;
+  return nseg > 1 ? (size_t)g->B * g->H * nseg * g->dk * g->dv : 0;
 }
 
 // Workspace: the segment states of the forward pass's scan, or of the backward pass's two
@@ -383,7 +383,9 @@ favor_status favor_attn_decay_backward(const favor_decay_desc *g, const void *Q,
   forward_order(s, g->scale);
   FAVOR_TRY(run_sums({{s, dv}, 2}, dt, stream, "favor_attn_decay_backward segment sums"));
   if (!work) return run_scan({{dv}, 1}, dt, stream, "favor_attn_decay_backward state gradient");
-  if (g->dk == g->dv)
+  // dV leaves the incoming state's gradient, where dK may still be reading the outgoing one's
+  const bool apart = dstate_in && dstate_in == dstate_out && dv.nseg == 1;
+  if (g->dk == g->dv && !apart)
     return run_scan({{dk, dv, dq}, 3}, dt, stream, "favor_attn_decay_backward gradients");
   FAVOR_TRY(run_scan({{dk, dq}, 2}, dt, stream, "favor_attn_decay_backward dK, dQ"));
   return run_scan({{dv}, 1}, dt, stream, "favor_attn_decay_backward dV");
