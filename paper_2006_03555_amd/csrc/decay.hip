@@ -14,15 +14,24 @@
 // adjacent tiles of X (rows k, columns v) are in chained order the A operand of
 // O^T = X^T Q^T, and those of P^T = K Q^T (rows j, columns i) the B operand of V^T P^T.
 // Only V^T and K^T need a transpose; bf16 tiles get it from the LDS transpose read. Each
-// wave holds all of X's rows for 16 value columns; P^T is shared out over the waves and
-// passes through LDS.
+// wave holds all of X's rows for 16 or 32 value columns; P^T is shared out over the waves
+// and passes through LDS.
 //
 // Precision (bf16): X, and all sums, are fp32. The weighted values diag(a^(..)) V enter
-// K^T V as three bf16 terms (24 bits: exact), so X is as exact as fp32 inputs would make
-// it. X enters Q X and the pair weights enter P V as one term each: the two parts of an
-// output, whose roundings are independent, together add one rounding to the output's own
-// (errors against 64 bits 1.4 times a correctly rounded output's at most). A second term
-// of X took 32 of 176 matrix and 160 of 744 vector instructions of a chunk.
+// K^T V as three bf16 terms (24 bits: exact) where the call returns X, which is then as exact
+// as fp32 inputs would make it. Where X only feeds outputs, which take it as one bf16 term,
+// two terms do: they leave at most 2^-16 of each product (2.6e-6 of X by its norm, against
+// 1.6e-3 from its rounding); 65536 x 16 heads of 128 x 128 in 346 instead of 376 us, a
+// training step of 4 x 4096 x 16 in 332 instead of 362. X enters Q X and the pair weights
+// enter P V as one term each: the two parts of an output, whose roundings are independent,
+// together add one rounding to the output's own (errors against 64 bits 1.4 times a
+// correctly rounded output's at most). A second term of X: 421 against 399 us.
+//
+// Bound (128 x 128, bf16): the bytes, and the power that the arithmetic takes. 512 heads x
+// 2048 rows, one segment each, move 1.07 GB in 288 us when the call is repeated; a few calls
+// on a cool card take a sixth less, at 2.4 GHz. The memory traffic by itself takes 243 us
+// (4.4 TB/s), the arithmetic by itself 250. At 64 x 64 it is the bytes, 4.6 TB/s; in fp32 the
+// matrix instructions, 300 of 320 us at 256 heads x 1024 rows of 128 x 128.
 #include "decay.hpp"
 #include "tile_common.hpp"
 
@@ -159,7 +168,10 @@ __device__ __forceinline__ void split8(const float (&x)[8], f32x8 (&f)[N], const
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[0][i] = x[i];
 }
-template <typename T> constexpr int kSumTerms = sizeof(T) == 2 ? 3 : 1;
+// Terms of the weighted values: all of them where X leaves the call.
+template <typename T> constexpr int sum_terms(bool whole) {
+  return sizeof(T) == 4 ? 1 : whole ? 3 : 2;
+}
 
 // The wave's number, as a scalar.
 __device__ __forceinline__ int wave_id() {
@@ -434,10 +446,10 @@ __device__ __forceinline__ void load_values(lds_t Vs, typename Mma<T>::frag (&vt
     for (int m = 0; m < 2; ++m) vt[ct][m] = values(4 * NCT * wave_id() + ct, m);
 }
 
-// diag(pw.sum) V in operand terms.
-template <typename T, int NCT>
+// diag(pw.sum) V in N operand terms.
+template <typename T, int NCT, int N>
 __device__ __forceinline__ void weigh_values(
-    typename Mma<T>::frag (&vw)[2][NCT][kSumTerms<T>],
+    typename Mma<T>::frag (&vw)[2][NCT][N],
     const typename Mma<T>::frag (&vt)[NCT][2], const Powers &pw, const uint32_t (&minus)[2]) {
   const int g = lane_id() >> 4;
 #pragma unroll
@@ -451,15 +463,15 @@ __device__ __forceinline__ void weigh_values(
         x[i] = to_f32(vt[ct][m][i]) * w0[i];
         x[4 + i] = to_f32(vt[ct][m][4 + i]) * w1[i];
       }
-      split8<kSumTerms<T>>(x, vw[m][ct], minus);
+      split8<N>(x, vw[m][ct], minus);
     }
   }
 }
 
 // X <- carry X + K^T (diag(pw.sum) V).
-template <typename T, int KD, int NCT>
+template <typename T, int KD, int NCT, int N>
 __device__ __forceinline__ void update_state(
-    State<KD, NCT> &s, lds_t Ks, const typename Mma<T>::frag (&vw)[2][NCT][kSumTerms<T>],
+    State<KD, NCT> &s, lds_t Ks, const typename Mma<T>::frag (&vw)[2][NCT][N],
     float carry) {
   using P = Mma<T>;
   const TransReader<T, KD, 1> keys(Ks);
@@ -475,7 +487,7 @@ __device__ __forceinline__ void update_state(
     for (int m = 0; m < 2; ++m) {
       const auto kt = keys(4 * nb, m);
 #pragma unroll
-      for (int t = kSumTerms<T> - 1; t >= 0; --t)
+      for (int t = N - 1; t >= 0; --t)
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) u[ct] = P::mma(kt, vw[m][ct][t], u[ct]);
     }
@@ -489,8 +501,21 @@ __device__ __forceinline__ void update_state(
   }
 }
 
+// Wave priority by the chunk's number, lower as it rises (from 3 to 0, over and over): of two
+// workgroups on a compute unit the one behind goes first. With equal priorities the older
+// one always does, ends early and leaves the other alone (512 heads x 2048 rows of
+// 128 x 128: 207 and 238 us after their common start; with this 226 and 229).
+__device__ __forceinline__ void take_turns(int chunk) {
+  switch (chunk & 3) {
+    case 0: __builtin_amdgcn_s_setprio(3); break;
+    case 1: __builtin_amdgcn_s_setprio(2); break;
+    case 2: __builtin_amdgcn_s_setprio(1); break;
+    default: __builtin_amdgcn_s_setprio(0);
+  }
+}
+
 // The sums of one segment of 64 * chunks tokens, from X = 0.
-template <typename T, int KD, int NW, int NCT>
+template <typename T, int KD, int NW, int NCT, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT;
   // two buffers where two workgroups still share the unit: one barrier per chunk then
@@ -523,6 +548,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
     for (int ct = 0; ct < NCT; ++ct) put(s.x[nb][ct], f32x4{0.f, 0.f, 0.f, 0.f});
   Carry carry(a.log_decay[it.h], it.n > kChunkT);
   for (int c = 0; c < it.n; c += kChunkT) {
+    take_turns(c / kChunkT);
     const int buf = NB == 2 ? (c / kChunkT) & 1 : 0;
     kr.store(Ks[buf]);
     vr.store(Vs[buf]);
@@ -531,9 +557,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
     typename Mma<T>::frag vt[NCT][2];
     const lds_t zero = c & a.zero;
     load_values<T, VS, NCT>(lds_of(Vs[buf]) + zero, vt);
-    typename Mma<T>::frag vw[2][NCT][kSumTerms<T>];
-    weigh_values<T, NCT>(vw, vt, pw, a.minus);
-    update_state<T, KD, NCT>(s, lds_of(Ks[buf]) + zero, vw, carry.next());
+    typename Mma<T>::frag vw[2][NCT][sum_terms<T>(WHOLE)];
+    weigh_values<T>(vw, vt, pw, a.minus);
+    update_state<T>(s, lds_of(Ks[buf]) + zero, vw, carry.next());
     if (NB == 1) __syncthreads();
   }
   store_state<KD, NW, NCT>(a, it, part_of(a, it.bh, it.seg + 1), s);
@@ -577,7 +603,7 @@ constexpr int scan_waves(int elt, int KD, int NCT) {
   return elt == 2 && KD <= 128 && NCT == 1 ? 4 : KD == 256 && elt == 4 ? 1 : 2;
 }
 
-template <typename T, int KD, int NW, int NCT>
+template <typename T, int KD, int NW, int NCT, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_decay_scan(DecayPass pass) {
   using P = Mma<T>;
   using frag = typename P::frag;
@@ -626,6 +652,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
                   (uint32_t)sizeof(T);
   Carry carry(a.log_decay[it.h], it.n > kChunkT);
   for (int c = 0; c < it.n; c += kChunkT) {
+    if (pass.n == 1) take_turns(c / kChunkT);
     const int n = min(kChunkT, it.n - c);
     qr.store(Qs);
     kr.store(Ks);
@@ -692,7 +719,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[ib][ct][j] *= f;
     }
-    frag vt[NCT][2], vw[2][NCT][kSumTerms<T>];
+    frag vt[NCT][2], vw[2][NCT][sum_terms<T>(WHOLE)];
     load_values<T, VS, NCT>(lds_of(Vs) + zero, vt);
     __syncthreads();
 
@@ -709,8 +736,8 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       put_row<T, NCT>(rows, c16 < n - 16 * ib && vc < a.vd - v0 ? ooff + zero + ib * ostep : kOutside,
                       o[ib]);
     }
-    weigh_values<T, NCT>(vw, vt, pw, a.minus);
-    update_state<T, KD, NCT>(s, lds_of(Ks) + zero, vw, n == kChunkT ? carry.next() : pw.a[n]);
+    weigh_values<T>(vw, vt, pw, a.minus);
+    update_state<T>(s, lds_of(Ks) + zero, vw, n == kChunkT ? carry.next() : pw.a[n]);
     __syncthreads();
   }
 
@@ -727,35 +754,44 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   }
 }
 
-template <typename T, int KD, int NW, int NCT>
+template <typename T, int KD, int NW, int NCT, bool WHOLE>
 hipError_t launch(const DecayPass &pass, bool sums, hipStream_t st) {
   const DecayScan &a = pass.scan[0];
   const int heads = pass.n * a.BH * ((a.vd + a.slice - 1) / a.slice);
   if (sums)
-    k_decay_sums<T, KD, NW * NCT, 1><<<heads * (a.nseg - 1), 64 * NW * NCT, 0, st>>>(pass);
+    k_decay_sums<T, KD, NW * NCT, 1, WHOLE><<<heads * (a.nseg - 1), 64 * NW * NCT, 0, st>>>(pass);
   else
-    k_decay_scan<T, KD, NW, NCT><<<heads * a.nseg, 64 * NW, 0, st>>>(pass);
+    k_decay_scan<T, KD, NW, NCT, WHOLE><<<heads * a.nseg, 64 * NW, 0, st>>>(pass);
   return hipGetLastError();
 }
 
 // fp32 inputs keep one value tile per wave, in twice as many waves: their operands take
 // twice the registers. So do the sums, which have registers to spare: two buffers and eight
 // waves against one and four, ragged prompts of 6 x 1999 rows 96.4 -> 93.0 us.
-template <typename T>
+template <typename T, bool WHOLE>
 hipError_t dispatch(const DecayPass &p, bool sums, hipStream_t st) {
   constexpr int NW = sizeof(T) == 2 ? 4 : 8, NCT = 8 / NW;
   const int kd = p.scan[0].kd;
   const bool wide = p.scan[0].slice == 128;
-  if (kd <= 64) return wide ? launch<T, 64, NW, NCT>(p, sums, st) : launch<T, 64, 4, 1>(p, sums, st);
+  if (kd <= 64)
+    return wide ? launch<T, 64, NW, NCT, WHOLE>(p, sums, st)
+                : launch<T, 64, 4, 1, WHOLE>(p, sums, st);
   if (kd <= 128)
-    return wide ? launch<T, 128, NW, NCT>(p, sums, st) : launch<T, 128, 4, 1>(p, sums, st);
-  return launch<T, 256, 4, 1>(p, sums, st);
+    return wide ? launch<T, 128, NW, NCT, WHOLE>(p, sums, st)
+                : launch<T, 128, 4, 1, WHOLE>(p, sums, st);
+  return launch<T, 256, 4, 1, WHOLE>(p, sums, st);
+}
+hipError_t dispatch(const DecayPass &p, Dt dt, bool sums, hipStream_t st) {
+  if (dt == Dt::F32) return dispatch<float, true>(p, sums, st);
+  for (int i = 0; i < p.n; ++i)
+    if (p.scan[i].x_out) return dispatch<bf16, true>(p, sums, st);
+  return dispatch<bf16, false>(p, sums, st);
 }
 
 }  // namespace
 
 hipError_t launch_decay_sums(const DecayPass &p, Dt dt, hipStream_t st) {
-  return dt == Dt::BF16 ? dispatch<bf16>(p, true, st) : dispatch<float>(p, true, st);
+  return dispatch(p, dt, true, st);
 }
 hipError_t launch_decay_prefix(const DecayPass &p, hipStream_t st) {
   const int n = p.scan[0].kd * p.scan[0].vd / 4;
@@ -763,7 +799,7 @@ hipError_t launch_decay_prefix(const DecayPass &p, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_decay_scan(const DecayPass &p, Dt dt, hipStream_t st) {
-  return dt == Dt::BF16 ? dispatch<bf16>(p, false, st) : dispatch<float>(p, false, st);
+  return dispatch(p, dt, false, st);
 }
 
 }  // namespace favor

@@ -4,8 +4,10 @@ Bounds, per element, with A the same formula on absolute values (what the sums a
   fp32: products over dk, pairs over a chunk's 64 tokens and one carry per chunk, each sum
         off by at most its number of additions times 2^-24 A, and four roundings of
         weights: (dk + 64 + 4 chunks + 16) 2^-24 A.
-  bf16: the output's rounding 2^-8 |o|, the pair weights' 2^-8 A, and the fp32 bound; the
-        state's two bf16 terms leave 2^-16 A. States are fp32 sums of exact products.
+  bf16: the output's rounding 2^-8 |o|, the pair weights' 2^-8 A or the state's (each
+        enters as one bf16 term, and A is the sum of both parts), the state's products'
+        2^-16 A and the fp32 bound. A state that is returned is the fp32 sum of exact
+        products.
 A gradient is the same scan with the columns' roles exchanged, so the bound's width is
 the larger of dk and dv."""
 import numpy as np
