@@ -27,11 +27,13 @@
 // together add one rounding to the output's own (errors against 64 bits 1.4 times a
 // correctly rounded output's at most). A second term of X: 421 against 399 us.
 //
-// Bound (128 x 128, bf16): the bytes, and the power that the arithmetic takes. 512 heads x
-// 2048 rows, one segment each, move 1.07 GB in 288 us when the call is repeated; a few calls
-// on a cool card take a sixth less, at 2.4 GHz. The memory traffic by itself takes 243 us
-// (4.4 TB/s), the arithmetic by itself 250. At 64 x 64 it is the bytes, 4.6 TB/s; in fp32 the
-// matrix instructions, 300 of 320 us at 256 heads x 1024 rows of 128 x 128.
+// Bound: the bytes, and at 128 x 128 in bf16 the power that the arithmetic takes. 512 segments
+// of 2048 rows (65536 x 16 heads, 1.07 GB) take 224 us (4.8 TB/s) while the clock is at 2.4
+// GHz and 264 in a long run, which lowers it. 512 heads x 2048 rows in a long run: 280 us;
+// 217 with every chunk's rows from the cache, 221 with the traffic only. At 64 x 64 the scan
+// moves 4.6 TB/s, at 256 x 64 4.4. fp32 is bound by a chunk's chain of products: 256 heads x
+// 1024 rows of 128 x 128 327 us, 308 without the traffic. Calls of few heads read K and V
+// twice, once for the segments' sums.
 #include "decay.hpp"
 #include "tile_common.hpp"
 
@@ -504,7 +506,9 @@ __device__ __forceinline__ void update_state(
 // Wave priority by the chunk's number, lower as it rises (from 3 to 0, over and over): of two
 // workgroups on a compute unit the one behind goes first. With equal priorities the older
 // one always does, ends early and leaves the other alone (512 heads x 2048 rows of
-// 128 x 128: 207 and 238 us after their common start; with this 226 and 229).
+// 128 x 128: 207 and 238 us after their common start; with this 226 and 229). Scans that run
+// together read the same rows when they happen to keep pace and are better left alone: a
+// training step of 4 x 4096 x 16 heads 331 us, with turns 345.
 __device__ __forceinline__ void take_turns(int chunk) {
   switch (chunk & 3) {
     case 0: __builtin_amdgcn_s_setprio(3); break;
@@ -514,7 +518,8 @@ __device__ __forceinline__ void take_turns(int chunk) {
   }
 }
 
-// The sums of one segment of 64 * chunks tokens, from X = 0.
+// The sums of one segment of 64 * chunks tokens, from X = 0. Bound by the bytes of K and V:
+// those of 65536 x 16 heads of 128 x 128 (540 MB with the sums) in 110 us, 4.9 TB/s.
 template <typename T, int KD, int NW, int NCT, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT;
@@ -566,7 +571,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
 }
 
 // part of a head's segments: X_0, then X before segment s + 1 = a^seg_len (X before s) + sums
-// of s, four elements per thread.
+// of s, four elements per thread. Bound by the bytes: 16 heads x 32 states of 128 x 128 read
+// and written (67 MB) in 13 us, 5.1 TB/s. (Two elements per thread and twice as many loads
+// ahead: calls 1 to 5 us longer.)
 __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
   int id = blockIdx.y;
   const DecayScan &a = scan_of(pass, id);

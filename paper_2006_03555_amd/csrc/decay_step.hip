@@ -7,6 +7,9 @@
 // KB at 128 x 128) and everything else is small. A workgroup takes one (sequence, head);
 // a thread owns four value columns of every n-th row, so the state moves in 16-byte
 // units, whole rows at a time; the threads' parts of o are summed in a fixed order.
+// 1024 sequences x 16 heads at 128 x 128 (2.1 GB) take 412 us, 5.2 TB/s (a copy on this card:
+// 4.95); 48 sequences, whose states stay in the memory-side cache, 16 us, 6.2 TB/s. One
+// sequence of 8 heads takes 4 us, most of it the launch and one round of loads.
 #include "decay.hpp"
 #include "favor_common.hpp"
 
