@@ -393,8 +393,9 @@ FAVOR_API size_t favor_decay_workspace_size(const favor_decay_desc *g, int backw
 
 /*
  * favor_attn_decay - the chunked form, for prompts and training. state_in (nullable): S
- * before the first token; state_out (nullable; may be state_in): S after each sequence's
- * last one, so a sequence can be processed in pieces. Deterministic (no atomics).
+ * before the first token; state_out (nullable; may be state_in, and must not overlap it
+ * otherwise): S after each sequence's last one, so a sequence can be processed in pieces.
+ * Deterministic (no atomics).
  */
 FAVOR_API favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q,
                                         const void *K, const void *V, const float *log_decay,
@@ -409,8 +410,8 @@ FAVOR_API favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q
  *   dk_j = scale sum_{i >= j} a^(i-j) (dout_i . v_j) q_i + a^(n-1-j) dS_out v_j
  *   dv_j = scale sum_{i >= j} a^(i-j) (q_i . k_j) dout_i + a^(n-1-j) dS_out^T k_j
  *   dS_in = a^n dS_out + scale sum_i a^(i+1) q_i dout_i^T
- * dstate_in (nullable; may be dstate_out) receives the gradient of state_in. Nothing from
- * the forward call is needed. log_decay receives no gradient. For a broadcast input every
+ * dstate_in (nullable; may be dstate_out; overlaps neither it nor state_in otherwise)
+ * receives the gradient of state_in. Nothing from the forward call is needed. log_decay receives no gradient. For a broadcast input every
  * head (or batch entry) gets its own gradient, to be summed by the caller. Deterministic.
  */
 FAVOR_API favor_status favor_attn_decay_backward(
@@ -440,7 +441,8 @@ FAVOR_API favor_status favor_validate_decay_desc(const favor_decay_desc *g, int 
 /*
  * favor_dropout - y_n = residual_n + [bits_n >= t] x_n / (1 - t / 2^16) with t = p 2^16
  * rounded to the nearest (ties to even): p is taken to 16 bits, and p >= 1 - 2^-17 drops
- * everything. residual nullable (0); y may be x or residual. x, residual, y: n elements
+ * everything. residual nullable (0); y may be x or residual, and overlaps
+ * neither otherwise. x, residual, y: n elements
  * of dtype, contiguous, 16-byte aligned. A dropped element is 0 whatever x holds.
  *
  * bits_n is 16-bit piece n % 8 of Philox4x32-10 (Salmon et al., SC'11) with key (seed low,

@@ -54,6 +54,19 @@ favor_status check_optional(const void *p, const char *name, size_t align = 16) 
   return check_ptr(p, name, p != nullptr, align);
 }
 
+// An output that is written while an input of the same size is read: the two may be one
+// where `same` says so (each element is then read first), and must not overlap otherwise.
+favor_status check_apart(const void *out, const char *name, const void *in, const char *other,
+                         int64_t bytes, bool same) {
+  if (!out || !in || (out == in && same)) return FAVOR_OK;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(out), b = reinterpret_cast<uintptr_t>(in);
+  if ((a > b ? a - b : b - a) >= (uint64_t)bytes) return FAVOR_OK;
+  return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s overlaps %s", name, other);
+}
+int64_t state_bytes(const favor_decay_desc *g) {
+  return (int64_t)sizeof(float) * g->B * g->H * g->dk * g->dv;
+}
+
 favor_status device_result(hipError_t e, const char *what) {
   if (e != hipSuccess) return fail(FAVOR_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
   return ok();
@@ -297,6 +310,7 @@ favor_status favor_attn_decay(const favor_decay_desc *g, const void *Q, const vo
   FAVOR_TRY(check_optional(state_out, "state_out"));
   if (work && (out == Q || out == K || out == V))
     return fail(FAVOR_ERR_INVALID_ARGUMENT, "out must not be an input");
+  FAVOR_TRY(check_apart(state_out, "state_out", state_in, "state_in", state_bytes(g), true));
   if (!heads || (!work && !state_out)) return ok();
   FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g, kOpForward)));
   favor::DecayPass p{};
@@ -340,6 +354,8 @@ favor_status favor_attn_decay_backward(const favor_decay_desc *g, const void *Q,
       for (int i = 0; i < o; ++i)
         if (ptrs[o] == ptrs[i])
           return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s must not be %s", names[o], names[i]);
+  FAVOR_TRY(check_apart(dstate_in, "dstate_in", dstate_out, "dstate_out", state_bytes(g), true));
+  FAVOR_TRY(check_apart(dstate_in, "dstate_in", state_in, "state_in", state_bytes(g), false));
   if (!heads || (!work && !dstate_in)) return ok();
   FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g, kOpBackward)));
   const favor::Dt dt = dt_of(g);
@@ -451,6 +467,9 @@ favor_status favor_dropout(const void *x, const void *residual, void *y, int64_t
   FAVOR_TRY(check_ptr(y, "y", n > 0));
   FAVOR_TRY(check_optional(residual, "residual"));
   FAVOR_TRY(check_optional(rng, "rng", 8));
+  const int64_t bytes = n * (dt == FAVOR_BF16 ? 2 : 4);
+  FAVOR_TRY(check_apart(y, "y", x, "x", bytes, true));
+  FAVOR_TRY(check_apart(y, "y", residual, "residual", bytes, true));
   if (n == 0) return ok();
   favor::Dropout a{};
   a.x = x;

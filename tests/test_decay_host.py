@@ -293,3 +293,25 @@ def test_binding_strides():
         rows(x[..., ::2], "x")
     with pytest.raises(fv.FavorError, match="broadcast"):
         rows(x[:1, :1, :1].expand(2, 4, 3, 8), "x")
+
+
+def test_overlaps_are_refused():
+    """A state or a dropout's output written over part of what the same call still reads."""
+    g = _desc()
+    size = 4 * g.B * g.H * g.dk * g.dv
+    at = 1 << 24
+    for by in (16, size // 2, size - 16):
+        for lo, hi in ((at, at + by), (at + by, at)):
+            assert _forward(g, state_in=P(lo), state_out=P(hi)) == 1, by
+            assert "state_out overlaps state_in" in fv.last_error()
+            assert _backward(g, dstate_out=P(lo), dstate_in=P(hi)) == 1, by
+            assert "dstate_in overlaps dstate_out" in fv.last_error()
+            assert _backward(g, state_in=P(lo), dstate_in=P(hi)) == 1, by
+            assert "dstate_in overlaps state_in" in fv.last_error()
+    assert _backward(g, state_in=P(at), dstate_in=P(at)) == 1
+    for name in ("x", "residual"):
+        kw = {"x": P(1 << 28), "residual": P(1 << 28), name: P(at)}
+        for dtype, n in ((fv.BF16, 2), (fv.F32, 4)):
+            assert _drop(y=P(at + 16), dtype=dtype, n=1000, **kw) == 1
+            assert f"y overlaps {name}" in fv.last_error()
+            assert _drop(y=P(at), dtype=dtype, n=1000, **{**kw, name: P(at + 1000 * n // 16 * 16 - 16)}) == 1
