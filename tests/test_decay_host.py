@@ -2,6 +2,9 @@
 quadratic form, differences, published generator vectors), the C ABI's and the binding's
 refusals."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -9,6 +12,8 @@ import pytest
 import paper_2006_03555_amd as fv
 from oracle import decay
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM_INCLUDE = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
 P = ctypes.c_void_p
 A, NUL = P(1 << 20), P(0)   # an aligned address, never dereferenced
 
@@ -315,3 +320,32 @@ def test_overlaps_are_refused():
             assert _drop(y=P(at + 16), dtype=dtype, n=1000, **kw) == 1
             assert f"y overlaps {name}" in fv.last_error()
             assert _drop(y=P(at), dtype=dtype, n=1000, **{**kw, name: P(at + 1000 * n // 16 * 16 - 16)}) == 1
+
+
+# ------------------------------------------------------------------ under sanitizers
+@pytest.fixture(scope="module")
+def fuzzer(tmp_path_factory):
+    gxx = shutil.which("g++")
+    if gxx is None or not os.path.isdir(os.path.join(ROCM_INCLUDE, "hip")):
+        pytest.skip("needs g++ and the HIP headers")
+    csrc = "paper_2006_03555_amd/csrc"
+    sources = ["tests/host/fuzz_decay.cpp", "tests/host/stubs.cpp", f"{csrc}/decay_api.cpp",
+               f"{csrc}/favor_api.cpp", f"{csrc}/timing.cpp"]
+    exe = str(tmp_path_factory.mktemp("host") / "fuzz_decay")
+    r = subprocess.run([gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined",
+                        "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer",
+                        "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INCLUDE, "-I", f"{ROOT}/include",
+                        *[os.path.join(ROOT, x) for x in sources], "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    return exe
+
+
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_calls_fuzzed_under_sanitizers(fuzzer, seed):
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=1",
+               UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
+    r = subprocess.run([fuzzer, str(seed), "20000"], capture_output=True, text=True, env=env,
+                       timeout=300)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
+    assert " 0 failures" in r.stdout
