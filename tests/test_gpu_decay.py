@@ -6,7 +6,8 @@ Bounds, per element, with A the same formula on absolute values (what the sums a
         weights: (dk + 64 + 4 chunks + 16) 2^-24 A.
   bf16: the output's rounding 2^-8 |o|, the pair weights' 2^-8 A or the state's (each
         enters as one bf16 term, and A is the sum of both parts), the state's products'
-        2^-16 A and the fp32 bound. A state that is returned is the fp32 sum of exact
+        2^-16 A (two terms, each off by at most 2^-8 of what it stands for) and the
+        fp32 bound. A state that is returned is the fp32 sum of exact
         products.
 A gradient is the same scan with the columns' roles exchanged, so the bound's width is
 the larger of dk and dv."""
@@ -105,6 +106,30 @@ def test_forward(shape, dtype):
     ref, _ = decay.attn(x["q"], x["k"], x["v"], x["g"], 1.0)
     mag, _ = decay.attn(y["q"], y["k"], y["v"], x["g"], 1.0)
     _near(fv.attn_decay(q, k, v, g), ref, mag, dk, L, dtype, "out without a state")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(1, 2, 1, 64, 64), (2, 3, 130, 64, 128), (1, 2, 700, 72, 40),
+                                   (1, 3, 500, 256, 64), (1, 2, 1999, 128, 128)])
+def test_states_in_but_none_out(shape, dtype):
+    """A state and a state's gradient come in, none is returned: the calls whose states only
+    feed rows."""
+    fv = _fv()
+    B, H, L, dk, dv = shape
+    x = _inputs(*shape, dtype, 3 * sum(shape))
+    y = _abs(x)
+    q, k, v, do = (_laid_out(x[n], dtype, "blhd") for n in ("q", "k", "v", "do"))
+    g, S, G = to_dev(x["g"]), to_dev(x["S"]), to_dev(x["G"])
+    ref, _ = decay.attn(x["q"], x["k"], x["v"], x["g"], 0.3, state=x["S"])
+    mag, _ = decay.attn(y["q"], y["k"], y["v"], x["g"], 0.3, state=y["S"])
+    _near(fv.attn_decay(q, k, v, g, 0.3, state_in=S), ref, mag, dk, L, dtype, "out")
+    ref = decay.attn_backward(x["q"], x["k"], x["v"], x["g"], x["do"], 0.3, state=x["S"],
+                              dstate=x["G"])
+    mag = decay.attn_backward(y["q"], y["k"], y["v"], x["g"], y["do"], 0.3, state=y["S"],
+                              dstate=y["G"])
+    got = fv.attn_decay_backward(q, k, v, g, do, 0.3, state_in=S, dstate_out=G)
+    for t, r, m, n in zip(got, ref, mag, ("dQ", "dK", "dV")):
+        _near(t, r, m, max(dk, dv), L, dtype, n)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
