@@ -32,7 +32,7 @@
 // GHz and 264 in a long run, which lowers it. 512 heads x 2048 rows in a long run: 280 us;
 // 217 with every chunk's rows from the cache, 221 with the traffic only. At 64 x 64 the scan
 // moves 4.6 TB/s, at 256 x 64 4.4. fp32 is bound by a chunk's chain of products: 256 heads x
-// 1024 rows of 128 x 128 327 us, 308 without the traffic. Calls of few heads read K and V
+// 1024 rows of 128 x 128 (0.54 GB) 337 us, a twentieth less without the traffic. Calls of few heads read K and V
 // twice, once for the segments' sums.
 #include "decay.hpp"
 #include "tile_common.hpp"
@@ -498,8 +498,10 @@ __device__ __forceinline__ void update_state(
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         s.x[nb][ct][j] = fmaf(s.x[nb][ct][j], carry, u[ct][j]);
-    // so many tiles' operands at a time as registers are left for
-    if (nb % (NCT == 2 ? 2 : 8) == (NCT == 2 ? 1 : 7)) __builtin_amdgcn_sched_barrier(0);
+    // as many tiles' operands at a time as registers are left for (fp32, 256 heads x 1024 rows
+    // of 128 x 128: eight 349 us and a backward pass of 708, two 337 and 660)
+    constexpr int kGroup = NCT == 2 || sizeof(T) == 4 ? 2 : 8;
+    if (nb % kGroup == kGroup - 1) __builtin_amdgcn_sched_barrier(0);
   }
 }
 
