@@ -25,7 +25,8 @@
 // training step of 4 x 4096 x 16 in 332 instead of 362. X enters Q X and the pair weights
 // enter P V as one term each: the two parts of an output, whose roundings are independent,
 // together add one rounding to the output's own (errors against 64 bits 1.4 times a
-// correctly rounded output's at most). A second term of X: 421 against 399 us.
+// correctly rounded output's). A second term of X: 421 against 399 us; calls of few rows
+// take two of both.
 //
 // Bound: the bytes, and at 128 x 128 in bf16 the power that the arithmetic takes. 512 segments
 // of 2048 rows (65536 x 16 heads, 1.07 GB) take 224 us (4.8 TB/s) while the clock is at 2.4
@@ -607,12 +608,30 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
   }
 }
 
+// What the rounding of values to T leaves of them.
+template <typename T>
+__device__ __forceinline__ f32x4 rest(f32x4 x) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] -= to_f32((T)x[j]);
+  return x;
+}
+
+// Terms of the pair weights and of X in calls of few rows, whose sequences are one chunk each.
+// A weight's rounding is common to the elements of a row and does not average out over few
+// rows: with one term, outputs and gradients of one to five tokens were up to 2.1 times as far
+// off as rounded outputs are (by their norm; with two and in calls of more rows 1.48 times at
+// most). In us, one term / two: B1 H8 of 64 rows 6.9 / 7.0 at 64 x 64, 7.3 / 7.8 at 128 x 128,
+// B2 H16 10.0 / 11.1 at 256 x 256; many rows, which need it least, take longest: 2048 heads of
+// one token 33 / 45 at 128 x 128, 4096 of 64 tokens 70 / 108.
+constexpr int kFewRows = 1024;
+template <typename T> constexpr int kRowTerms = sizeof(T) == 2 ? 2 : 1;
+
 // Waves per SIMD that the register budget of the scan is set for.
 constexpr int scan_waves(int elt, int KD, int NCT) {
   return elt == 2 && KD <= 128 && NCT == 1 ? 4 : KD == 256 && elt == 4 ? 1 : 2;
 }
 
-template <typename T, int KD, int NW, int NCT, bool WHOLE>
+template <typename T, int KD, int NW, int NCT, bool WHOLE, int TERMS>
 __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_decay_scan(DecayPass pass) {
   using P = Mma<T>;
   using frag = typename P::frag;
@@ -622,7 +641,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   __shared__ __align__(256) T Vs[kChunkT * VS];
   // the pair weights as B operands: rows 16 i .. + 15, tokens 32 m .. + 31 in fragment
   // first(i) + m
-  __shared__ __align__(16) frag Ps[6 * 64];
+  __shared__ __align__(16) frag Ps[TERMS][6 * 64];
   __shared__ Powers pw;
   const auto first = [](int i) { return (i >= 1) + (i >= 2) + 2 * (i >= 3); };
   int id = xcd_item(blockIdx.x, gridDim.x);
@@ -650,7 +669,9 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   State<KD, NCT> s;
   load_state<KD, NW, NCT>(a, it, s);
   fill_powers(pw, a.log_decay[it.h]);
-  for (int i = threadIdx.x; i < 6 * 64; i += NT) Ps[i] = P::splat(0.f);   // j > i stays 0
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t)
+    for (int i = threadIdx.x; i < 6 * 64; i += NT) Ps[t][i] = P::splat(0.f);   // j > i stays 0
   __syncthreads();
   fill_rows(pw, a);
   // a lane's outputs: row c16 of a block (in reversed order from the chunk's last block
@@ -695,8 +716,12 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = e >= j ? x[j] * wt[j] : 0.f;   // (an Inf of j > i goes)
-      T *pp = reinterpret_cast<T *>(&Ps[(first(ib) + (jb >> 1)) * 64 + l]);
-      store4(pp + 4 * (jb & 1), x);
+#pragma unroll
+      for (int u = 0; u < TERMS; ++u) {
+        T *pp = reinterpret_cast<T *>(&Ps[u][(first(ib) + (jb >> 1)) * 64 + l]);
+        store4(pp + 4 * (jb & 1), x);
+        x = rest<T>(x);
+      }
     }
 
     // X^T Q^T
@@ -707,15 +732,24 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      frag xf[NCT];
+      frag xf[TERMS][NCT];
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct)
-        xf[ct] = P::pack(get(s.x[2 * p][ct]), get(s.x[2 * p + 1][ct]));
+      for (int ct = 0; ct < NCT; ++ct) {
+        f32x4 x0 = get(s.x[2 * p][ct]), x1 = get(s.x[2 * p + 1][ct]);
+#pragma unroll
+        for (int u = 0; u < TERMS; ++u) {
+          xf[u][ct] = P::pack(x0, x1);
+          x0 = rest<T>(x0);
+          x1 = rest<T>(x1);
+        }
+      }
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) {
         const frag qf = queries(ib, p);
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(xf[ct], qf, o[ib][ct]);
+        for (int u = TERMS - 1; u >= 0; --u)
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(xf[u][ct], qf, o[ib][ct]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -738,9 +772,12 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
     for (int ib = 0; ib < 4; ++ib) {
 #pragma unroll
       for (int m = 0; m <= ib / 2; ++m) {
-        const frag pf = Ps[(first(ib) + m) * 64 + l];
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(vt[ct][m], pf, o[ib][ct]);
+        for (int u = TERMS - 1; u >= 0; --u) {
+          const frag pf = Ps[u][(first(ib) + m) * 64 + l];
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(vt[ct][m], pf, o[ib][ct]);
+        }
       }
       put_row<T, NCT>(rows, c16 < n - 16 * ib && vc < a.vd - v0 ? ooff + zero + ib * ostep : kOutside,
                       o[ib]);
@@ -769,8 +806,10 @@ hipError_t launch(const DecayPass &pass, bool sums, hipStream_t st) {
   const int heads = pass.n * a.BH * ((a.vd + a.slice - 1) / a.slice);
   if (sums)
     k_decay_sums<T, KD, NW * NCT, 1, WHOLE><<<heads * (a.nseg - 1), 64 * NW * NCT, 0, st>>>(pass);
+  else if (sizeof(T) == 2 && a.L <= kChunkT && a.BH * a.L <= kFewRows)
+    k_decay_scan<T, KD, NW, NCT, true, kRowTerms<T>><<<heads, 64 * NW, 0, st>>>(pass);
   else
-    k_decay_scan<T, KD, NW, NCT, WHOLE><<<heads * a.nseg, 64 * NW, 0, st>>>(pass);
+    k_decay_scan<T, KD, NW, NCT, WHOLE, 1><<<heads * a.nseg, 64 * NW, 0, st>>>(pass);
   return hipGetLastError();
 }
 

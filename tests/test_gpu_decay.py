@@ -132,6 +132,36 @@ def test_states_in_but_none_out(shape, dtype):
         _near(t, r, m, max(dk, dv), L, dtype, n)
 
 
+@pytest.mark.parametrize("state", [False, True])
+@pytest.mark.parametrize("L,dk,dv", [(1, 128, 184), (4, 128, 248), (3, 256, 56), (64, 64, 64),
+                                     (17, 16, 128)])
+def test_few_rows_in_bf16(L, dk, dv, state):
+    """Rows too few for the roundings of pair weights and states to average out: both come in
+    two terms, so that an output's own rounding is what is left. Element by element: 2^-8 for
+    that rounding; 2^-16 of A for the pair weights, the states and the products in a state;
+    (dk + 64 + 4 + 16) 2^-24 A <= 340 2^-24 A for the fp32 sums."""
+    fv = _fv()
+    x = _inputs(3, 2, L, dk, dv, "bf16", L + dk)
+    x["g"][:] = -1 / 32
+    q, k, v, do = (to_dev(x[n], "bf16") for n in ("q", "k", "v", "do"))
+    g, S, G = to_dev(x["g"]), to_dev(x["S"]), to_dev(x["G"])
+    kw = dict(state=x["S"]) if state else {}
+    kd = dict(kw, dstate=x["G"]) if state else {}
+    ref = [decay.attn(x["q"], x["k"], x["v"], x["g"], 0.5, **kw)[0],
+           *decay.attn_backward(x["q"], x["k"], x["v"], x["g"], x["do"], 0.5, **kd)[:3]]
+    got = [fv.attn_decay(q, k, v, g, 0.5, state_in=S if state else None),
+           *fv.attn_decay_backward(q, k, v, g, do, 0.5, state_in=S if state else None,
+                                   dstate_out=G if state else None)]
+    y = _abs(x)
+    ky = dict(state=y["S"]) if state else {}
+    kyd = dict(ky, dstate=y["G"]) if state else {}
+    mag = [decay.attn(y["q"], y["k"], y["v"], x["g"], 0.5, **ky)[0],
+           *decay.attn_backward(y["q"], y["k"], y["v"], x["g"], y["do"], 0.5, **kyd)[:3]]
+    for t, r, m, n in zip(got, ref, mag, ("out", "dQ", "dK", "dV")):
+        tol = 2.0 ** -8 * np.abs(r) * (1 + 2.0 ** -8) + (3 * 2.0 ** -16 + 340 * 2.0 ** -24) * m
+        assert (np.abs(_host(t) - r) <= tol).all(), (n, state)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("dk,dv", [(128, 128), (88, 128), (256, 88), (64, 64)])
 def test_many_heads(dk, dv, dtype):
