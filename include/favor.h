@@ -365,8 +365,10 @@ FAVOR_API favor_status favor_attn_both_backward(const favor_desc *g, const void 
  * Supported: dk and dv multiples of 8 up to 256; dtype (inputs, out, gradients) F32 or
  * BF16; 0 <= L <= 2^30; B*H <= 65535. F32 uses fp32 matrix cores, BF16 bf16 ones with
  * fp32 sums; states are fp32 throughout, and one that a call returns is as exact for BF16
- * inputs as for F32 ones. (A BF16 call that returns none takes its products to 16 bits:
- * the last bits of its outputs may differ from those of one that does.)
+ * inputs as for F32 ones. In BF16 pair weights and states enter the products of a row to
+ * 16 bits, so that the row's own rounding is what it is off by, whatever its batch. (The
+ * products in a state that the call does not return are taken to 16 bits too: the last bits
+ * of such a call's outputs may differ from those of one that returns it.)
  *
  * lengths [B] int32 (nullable, device): sequence b has its first lengths[b] tokens
  * (values outside 0 .. L are taken as 0 or L), and rows behind them are padding: their

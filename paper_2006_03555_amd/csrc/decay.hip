@@ -19,14 +19,13 @@
 //
 // Precision (bf16): X, and all sums, are fp32. The weighted values diag(a^(..)) V enter
 // K^T V as three bf16 terms (24 bits: exact) where the call returns X, which is then as exact
-// as fp32 inputs would make it. Where X only feeds outputs, which take it as one bf16 term,
-// two terms do: they leave at most 2^-16 of each product (2.6e-6 of X by its norm, against
-// 1.6e-3 from its rounding); 65536 x 16 heads of 128 x 128 in 346 instead of 376 us, a
-// training step of 4 x 4096 x 16 in 332 instead of 362. X enters Q X and the pair weights
-// enter P V as one term each: the two parts of an output, whose roundings are independent,
-// together add one rounding to the output's own (errors against 64 bits 1.4 times a
-// correctly rounded output's). A second term of X: 421 against 399 us; calls of few rows
-// take two of both.
+// as fp32 inputs would make it. Where X only feeds outputs, two terms do: they leave at most
+// 2^-16 of each product (2.6e-6 of X by its norm). X in Q X and the pair weights in P V are
+// two terms each, in every call: what they leave, 2^-16, is far below the output's own
+// rounding, so that a row is as near as a rounded one can be, whatever batch it is in. With
+// one term, 2^-8 off, errors by norm are 1.4 times a correctly rounded output's and those of
+// single rows, whose few weights do not average out, up to 2.1 times; 65536 x 16 heads of 128 x 128
+// took 359 us instead of 385 and a training step of 4 x 4096 x 16 333 instead of 368.
 //
 // Bound: the bytes, and at 128 x 128 in bf16 the power that the arithmetic takes. 512 segments
 // of 2048 rows (65536 x 16 heads, 1.07 GB) take 224 us (4.8 TB/s) while the clock is at 2.4
@@ -608,40 +607,42 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
   }
 }
 
-// What the rounding of values to T leaves of them.
-template <typename T>
-__device__ __forceinline__ f32x4 rest(f32x4 x) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] -= to_f32((T)x[j]);
-  return x;
-}
-
-// Terms of the pair weights and of X in calls of few rows, whose sequences are one chunk each.
-// A weight's rounding is common to the elements of a row and does not average out over few
-// rows: with one term, outputs and gradients of one to five tokens were up to 2.1 times as far
-// off as rounded outputs are (by their norm; with two and in calls of more rows 1.48 times at
-// most). In us, one term / two: B1 H8 of 64 rows 6.9 / 7.0 at 64 x 64, 7.3 / 7.8 at 128 x 128,
-// B2 H16 10.0 / 11.1 at 256 x 256; many rows, which need it least, take longest: 2048 heads of
-// one token 33 / 45 at 128 x 128, 4096 of 64 tokens 70 / 108.
-constexpr int kFewRows = 1024;
+// Terms of the pair weights and of X (see above).
 template <typename T> constexpr int kRowTerms = sizeof(T) == 2 ? 2 : 1;
+
+// Four pair weights as a first term and what it leaves. The first keeps within bf16's range,
+// so that a weight past it ends as Inf, not as Inf - Inf.
+__device__ __forceinline__ f32x4 first_term(f32x4 x) {
+  f32x4 t;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    t[j] = to_f32((bf16)__builtin_amdgcn_fmed3f(x[j], -0x1.fep127f, 0x1.fep127f));
+  return t;
+}
 
 // Waves per SIMD that the register budget of the scan is set for.
 constexpr int scan_waves(int elt, int KD, int NCT) {
   return elt == 2 && KD <= 128 && NCT == 1 ? 4 : KD == 256 && elt == 4 ? 1 : 2;
 }
 
-template <typename T, int KD, int NW, int NCT, bool WHOLE, int TERMS>
+template <typename T, int KD, int NW, int NCT, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_decay_scan(DecayPass pass) {
   using P = Mma<T>;
   using frag = typename P::frag;
-  constexpr int NT = 64 * NW, VS = 16 * NW * NCT, NP = KD / 32;
+  constexpr int NT = 64 * NW, VS = 16 * NW * NCT, NP = KD / 32, TERMS = kRowTerms<T>;
   __shared__ __align__(256) T Qs[kChunkT * KD];
   __shared__ __align__(256) T Ks[kChunkT * KD];
   __shared__ __align__(256) T Vs[kChunkT * VS];
   // the pair weights as B operands: rows 16 i .. + 15, tokens 32 m .. + 31 in fragment
-  // first(i) + m
-  __shared__ __align__(16) frag Ps[TERMS][6 * 64];
+  // first(i) + m. Second terms behind the first ones; at 256 k columns, where that would
+  // leave no room for a second workgroup on the unit, in the values' place once they are read
+  // (4 x 8192 x 8 heads of 256 x 64: 137 instead of 168 us).
+  constexpr bool kTight = TERMS == 2 && KD == 256;
+  static_assert(!kTight || sizeof(Vs) >= 6 * 64 * sizeof(frag), "room for the second terms");
+  __shared__ __align__(16) frag Ps[kTight ? 1 : TERMS][6 * 64];
+  const auto pairs_of = [&](int term) {
+    return kTight && term == 1 ? reinterpret_cast<frag *>(Vs) : Ps[term];
+  };
   __shared__ Powers pw;
   const auto first = [](int i) { return (i >= 1) + (i >= 2) + 2 * (i >= 3); };
   int id = xcd_item(blockIdx.x, gridDim.x);
@@ -670,7 +671,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   load_state<KD, NW, NCT>(a, it, s);
   fill_powers(pw, a.log_decay[it.h]);
 #pragma unroll
-  for (int t = 0; t < TERMS; ++t)
+  for (int t = 0; t < (kTight ? 1 : TERMS); ++t)
     for (int i = threadIdx.x; i < 6 * 64; i += NT) Ps[t][i] = P::splat(0.f);   // j > i stays 0
   __syncthreads();
   fill_rows(pw, a);
@@ -702,27 +703,35 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
     const RowReader<T, KD> queries(lds_of(Qs) + zero), keys(lds_of(Ks) + zero);
 
     // D o K Q^T, the ten 16 x 16 tiles with j <= i shared out over the waves
-    for (int t = w; t < 10; t += NW) {
-      const int ib = (t >= 1) + (t >= 3) + (t >= 6), jb = t - ib * (ib + 1) / 2;
-      const int e = 16 * (ib - jb) + c16 - 4 * g;
-      float wt[4];
+    const auto pairs = [&] {
+      for (int t = w; t < 10; t += NW) {
+        const int ib = (t >= 1) + (t >= 3) + (t >= 6), jb = t - ib * (ib + 1) / 2;
+        const int e = 16 * (ib - jb) + c16 - 4 * g;
+        float wt[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) wt[j] = pw.pair[16 + e - j];
-      f32x4 x{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < 4; ++j) wt[j] = pw.pair[16 + e - j];
+        f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        x = P::mma(keys(jb, p), queries(ib, p), x);
-        if (p % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // not all operands at once
+        for (int p = 0; p < NP; ++p) {
+          x = P::mma(keys(jb, p), queries(ib, p), x);
+          if (p % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // not all operands at once
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = e >= j ? x[j] * wt[j] : 0.f;   // (an Inf of j > i goes)
+        const auto put = [&](int term, int half, f32x4 y) {
+          store4(reinterpret_cast<T *>(pairs_of(term) + (first(ib) + (jb >> 1)) * 64 + l) + 4 * half, y);
+        };
+        if constexpr (TERMS == 1) {
+          put(0, jb & 1, x);
+        } else {
+          const f32x4 x0 = first_term(x);
+          put(0, jb & 1, x0);
+          put(1, jb & 1, x - x0);
+          if (kTight && ib == jb && !(jb & 1)) put(1, 1, f32x4{0.f, 0.f, 0.f, 0.f});   // j > i
+        }
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = e >= j ? x[j] * wt[j] : 0.f;   // (an Inf of j > i goes)
-#pragma unroll
-      for (int u = 0; u < TERMS; ++u) {
-        T *pp = reinterpret_cast<T *>(&Ps[u][(first(ib) + (jb >> 1)) * 64 + l]);
-        store4(pp + 4 * (jb & 1), x);
-        x = rest<T>(x);
-      }
-    }
+    };
+    if (!kTight) pairs();
 
     // X^T Q^T
     f32x4 o[4][NCT];
@@ -732,16 +741,16 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      frag xf[TERMS][NCT];
+      frag xf[NCT][TERMS];
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct) {
-        f32x4 x0 = get(s.x[2 * p][ct]), x1 = get(s.x[2 * p + 1][ct]);
+        float x[8];
 #pragma unroll
-        for (int u = 0; u < TERMS; ++u) {
-          xf[u][ct] = P::pack(x0, x1);
-          x0 = rest<T>(x0);
-          x1 = rest<T>(x1);
+        for (int j = 0; j < 4; ++j) {
+          x[j] = s.x[2 * p][ct][j];
+          x[4 + j] = s.x[2 * p + 1][ct][j];
         }
+        split8(x, xf[ct], a.minus);
       }
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) {
@@ -749,11 +758,11 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
 #pragma unroll
         for (int u = TERMS - 1; u >= 0; --u)
 #pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(xf[u][ct], qf, o[ib][ct]);
+          for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(xf[ct][u], qf, o[ib][ct]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (kLateQ) fetch_q(c + kChunkT);
+    if (kLateQ && !kTight) fetch_q(c + kChunkT);
 #pragma unroll
     for (int ib = 0; ib < 4; ++ib) {
       const float f = pw.row[16 * ib + c16];
@@ -765,6 +774,11 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
     frag vt[NCT][2], vw[2][NCT][sum_terms<T>(WHOLE)];
     load_values<T, VS, NCT>(lds_of(Vs) + zero, vt);
     __syncthreads();
+    if (kTight) {
+      pairs();
+      fetch_q(c + kChunkT);   // (in front of the pairs: 150 us)
+      __syncthreads();
+    }
 
     // + V^T (D o K Q^T)
     const auto rows = chunk_rows<T>(a.o, a.os, it, v0, a.reverse, it.first + c);
@@ -774,7 +788,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
       for (int m = 0; m <= ib / 2; ++m) {
 #pragma unroll
         for (int u = TERMS - 1; u >= 0; --u) {
-          const frag pf = Ps[u][(first(ib) + m) * 64 + l];
+          const frag pf = pairs_of(u)[(first(ib) + m) * 64 + l];
 #pragma unroll
           for (int ct = 0; ct < NCT; ++ct) o[ib][ct] = P::mma(vt[ct][m], pf, o[ib][ct]);
         }
@@ -806,10 +820,8 @@ hipError_t launch(const DecayPass &pass, bool sums, hipStream_t st) {
   const int heads = pass.n * a.BH * ((a.vd + a.slice - 1) / a.slice);
   if (sums)
     k_decay_sums<T, KD, NW * NCT, 1, WHOLE><<<heads * (a.nseg - 1), 64 * NW * NCT, 0, st>>>(pass);
-  else if (sizeof(T) == 2 && a.L <= kChunkT && a.BH * a.L <= kFewRows)
-    k_decay_scan<T, KD, NW, NCT, true, kRowTerms<T>><<<heads, 64 * NW, 0, st>>>(pass);
   else
-    k_decay_scan<T, KD, NW, NCT, WHOLE, 1><<<heads * a.nseg, 64 * NW, 0, st>>>(pass);
+    k_decay_scan<T, KD, NW, NCT, WHOLE><<<heads * a.nseg, 64 * NW, 0, st>>>(pass);
   return hipGetLastError();
 }
 
