@@ -351,8 +351,10 @@ FAVOR_API favor_status favor_attn_both_backward(const favor_desc *g, const void 
  * are, for instance as favor_feature_map wrote them):
  *   S_t = a_h S_{t-1} + k_t v_t^T,   out_t = scale q_t^T S_t,   a_h = exp(log_decay[h]),
  * that is out_i = scale (sum_{j <= i} a^(i-j) (q_i . k_j) v_j + a^(i+1) q_i^T S_in).
- * log_decay [H] fp32: at most 0; 0 keeps everything, -Inf only the token itself. (A
- * positive value grows as the formula says.)
+ * log_decay [H] fp32: 0 keeps everything, -Inf only the token itself. A positive value
+ * grows as the formula says up to 1.38 (while a^64, and scale a^64, are in fp32's range; in
+ * sequences of fewer tokens, a^L); beyond it results may be Inf or NaN where the formula
+ * is finite.
  *
  * Layouts: Q, K [B][H][L][dk], V, out [B][H][L][dv] with rows of contiguous elements and
  * any strides between them, in elements (favor_strides; all three 0 = the contiguous

@@ -303,11 +303,12 @@ struct Powers {
   float row[kChunkT];         // row_scale a^(i + shift)
   float pair[kChunkT + 16];   // pair_scale a^(e) at e + 16, 0 for e < 0
 };
-// a^e = exp(g e) to about one rounding: g e as a sum of two floats, 0^0 = 1.
+// a^e = exp(g e) to about one rounding: g e as a sum of two floats, 0^0 = 1. (0 and Inf, past
+// the range on either side, stay: the second float may be NaN there.)
 __device__ __forceinline__ float power(float g, int e) {
   const float x = g * (float)e, low = fmaf(g, (float)e, -x);
   const float y = expf(x);
-  return e == 0 ? 1.f : isfinite(x) ? fmaf(y, low, y) : y;
+  return e == 0 ? 1.f : y > 0.f && y < INFINITY ? fmaf(y, low, y) : y;
 }
 __device__ __forceinline__ void fill_powers(Powers &p, float g) {
   if (threadIdx.x <= kChunkT) p.a[threadIdx.x] = power(g, threadIdx.x);
@@ -585,9 +586,12 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
   if (e >= n) return;
   f32x4 x{0.f, 0.f, 0.f, 0.f};
   if (a.x_in) x = reinterpret_cast<const f32x4 *>(a.x_in)[(size_t)it.bh * n + e];
-  // a^seg_len as two floats: it meets X once per segment
-  const double d = exp((double)a.log_decay[it.h] * a.seg_len);
-  const float hi = (float)d, lo = isfinite(hi) ? (float)(d - hi) : 0.f;
+  // a^seg_len, which meets X once per segment, as two floats and a power of two: where it
+  // is past fp32's range, its product with X need not be (2^400 takes any X but 0 past it)
+  const double t = (double)a.log_decay[it.h] * a.seg_len * 1.4426950408889634074;
+  const int two = t > -400. ? t < 400. ? (int)floor(t) : 400 : -400;
+  const double d = exp2((t < 400. || t != t ? t : 400.) - two);
+  const float hi = (float)d, lo = (float)(d - hi);
   f32x4 *p = reinterpret_cast<f32x4 *>(part_of(a, it.bh, 0)) + e;
   *p = x;
   p += n;
@@ -601,7 +605,10 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
     for (int k = 0; k < kAhead; ++k)
       if (s + k < last) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = fmaf(x[j], hi, fmaf(x[j], lo, u[k][j]));
+        for (int j = 0; j < 4; ++j) {
+          const float y = ldexpf(x[j], two);
+          x[j] = fmaf(y, hi, fmaf(y, lo, u[k][j]));
+        }
         p[k * n] = x;
       }
   }
