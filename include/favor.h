@@ -426,8 +426,10 @@ FAVOR_API favor_status favor_attn_decay_backward(
 
 /*
  * favor_attn_decay_step - the recurrent form, for single tokens: Q, K [B][H][dk], V, out
- * [B][H][dv] (g->L and the token strides are not read), and the states state
- * [n_slots][H][dk][dv] updated in place. slots [B] int32 (nullable, device): the place of
+ * [B][H][dv], and the states state [n_slots][H][dk][dv] updated in place. g->L has no effect
+ * (it must be in its range). Nor have token strides, except that a tensor whose three strides
+ * are 0 is contiguous: one row for every sequence and head has batch = head = 0 and a token
+ * stride that is not 0. slots [B] int32 (nullable, device): the place of
  * each sequence's state, NULL: state b is sequence b's (n_slots >= B). A sequence with a
  * place outside 0 .. n_slots - 1 (padding of a captured batch) has no state and out = 0.
  * Sequences that name the same place take their turns in order, as tokens of one sequence.

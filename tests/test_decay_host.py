@@ -157,6 +157,17 @@ def test_unknown_operation_and_null_descriptor():
     assert fv.lib().favor_decay_workspace_size(None, 0) == 0
 
 
+def test_single_tokens_and_the_token_stride():
+    """Three zeros are the contiguous layout, also of an output; with a token stride, zeros are
+    one row for all, which an output may not be. L has its range and no effect."""
+    for s, status in (((0, 0, 0), 0), ((0, 0, 8), 1), ((0, 0, -3), 1), ((4 * 128, 128, 0), 0),
+                      ((4 * 128, 128, 5), 0), ((0, 128, 1), 1), ((128, 0, 1), 1)):
+        assert fv.validate_decay_desc(_desc(out=s), 2) == status, s
+        assert fv.validate_decay_desc(_desc(q=s, k=s, v=s), 2) == 0, s   # (an input may)
+    for L, status in ((0, 0), (1 << 30, 0), (-1, 1), ((1 << 30) + 1, 2)):
+        assert fv.validate_decay_desc(_desc(L=L), 2) == status
+
+
 # ------------------------------------------------------------------ calls
 def _forward(g, ptrs=None, ws=A, n=1 << 40, **kw):
     p = dict(Q=A, K=A, V=A, log_decay=A, lengths=NUL, out=P(1 << 21), state_in=NUL,
