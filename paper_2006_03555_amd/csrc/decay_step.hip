@@ -28,7 +28,11 @@ __global__ __launch_bounds__(kStepThreads) void k_decay_step(DecayStep a) {
   const int tid = threadIdx.x;
   const int units = a.dv / 4, groups = kStepThreads / units;
   const int unit = tid % units, group = tid / units;
-  const float lam = expf(a.log_decay[h]);
+  // a as two floats: one's rounding, the same at every token, would add up over a long memory
+  // (8192 tokens: states up to 1.3e-4 off instead of 1.5e-5 at most; 48 sequences 18.4 us
+  // instead of 18.2)
+  const double decay = exp((double)a.log_decay[h]);
+  const float lam = (float)decay, low = lam < INFINITY ? (float)(decay - lam) : 0.f;
   for (int b = blockIdx.x / a.H; b < a.B;) {
     // sequences that share a place take their turns in order, by the first one's
     // workgroup: find an earlier one (this workgroup has nothing to do) and the next
@@ -70,7 +74,7 @@ __global__ __launch_bounds__(kStepThreads) void k_decay_step(DecayStep a) {
         const float kr = qk[1][r], qr = qk[0][r];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          s[j] = fmaf(s[j], lam, kr * v[j]);
+          s[j] = fmaf(s[j], lam, fmaf(s[j], low, kr * v[j]));
           o[j] = fmaf(qr, s[j], o[j]);
         }
         sp[(size_t)r * units] = s;
