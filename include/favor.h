@@ -376,7 +376,8 @@ FAVOR_API favor_status favor_attn_both_backward(const favor_desc *g, const void 
  * (values outside 0 .. L are taken as 0 or L), and rows behind them are padding: their
  * inputs are not read, their rows of out and of the gradients are written as zeros. A
  * NaN or infinity in a token reaches the results of its own chunk of 64 tokens and of
- * those behind it (in a gradient, before it).
+ * those behind it (dK, dV and dS_in: before it); in BF16 an infinity in a value or a state
+ * may arrive there as NaN.
  */
 typedef struct {
   int64_t batch, head, token;

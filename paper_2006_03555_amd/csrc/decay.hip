@@ -20,20 +20,19 @@
 // Precision (bf16): X, and all sums, are fp32. The weighted values diag(a^(..)) V enter
 // K^T V as three bf16 terms (24 bits: exact) where the call returns X, which is then as exact
 // as fp32 inputs would make it. Where X only feeds outputs, two terms do: they leave at most
-// 2^-16 of each product (2.6e-6 of X by its norm). X in Q X and the pair weights in P V are
-// two terms each, in every call: what they leave, 2^-16, is far below the output's own
-// rounding, so that a row is as near as a rounded one can be, whatever batch it is in. With
-// one term, 2^-8 off, errors by norm are 1.4 times a correctly rounded output's and those of
-// single rows, whose few weights do not average out, up to 2.1 times; 65536 x 16 heads of 128 x 128
-// took 359 us instead of 385 and a training step of 4 x 4096 x 16 333 instead of 368.
+// 2^-16 of each product (2.6e-6 of X by its norm; 65536 x 16 heads of 128 x 128 in 380
+// instead of 407 us, a training step of 4 x 4096 x 16 in 364 instead of 401). X in Q X and
+// the pair weights in P V are two terms each, in every call: what they leave, 2^-16, is far
+// below the output's own rounding, so that a row is as near as a rounded one can be, whatever
+// batch it is in. With one term, 2^-8 off, errors by norm are 1.4 times a correctly rounded
+// output's and those of single rows, whose few weights do not average out, up to 2.1 times;
+// the same calls then take 358 and 328 us.
 //
 // Bound: the bytes, and at 128 x 128 in bf16 the power that the arithmetic takes. 512 segments
-// of 2048 rows (65536 x 16 heads, 1.07 GB) take 224 us (4.8 TB/s) while the clock is at 2.4
-// GHz and 264 in a long run, which lowers it. 512 heads x 2048 rows in a long run: 280 us;
-// 217 with every chunk's rows from the cache, 221 with the traffic only. At 64 x 64 the scan
-// moves 4.6 TB/s, at 256 x 64 4.4. fp32 is bound by a chunk's chain of products: 256 heads x
-// 1024 rows of 128 x 128 (0.54 GB) 337 us, a twentieth less without the traffic. Calls of few heads read K and V
-// twice, once for the segments' sums.
+// of 2048 rows (65536 x 16 heads, 1.07 GB) take 250 us (4.3 TB/s), but 302 in the first tens
+// of calls of a run, while the clock settles; 512 heads x 2048 rows 254. At 64 x 64 the scan moves 4.6 TB/s, at 256 x 64 4.5. fp32 is bound by a
+// chunk's chain of products: 256 heads x 1024 rows of 128 x 128 (0.54 GB) 337 us. Calls of few
+// heads read K and V twice, once for the segments' sums.
 #include "decay.hpp"
 #include "tile_common.hpp"
 
@@ -374,8 +373,8 @@ __device__ __forceinline__ float *part_of(const DecayScan &a, int bh, int seg) {
   return a.part + ((size_t)bh * a.nseg + seg) * (a.kd * a.vd);
 }
 
-// X of one head in memory ([kd][vd], or transposed): four k rows of one column at a time,
-// without branches. Null has no rows: it reads as zeros.
+// X of one head in memory ([kd][vd], or transposed): four k rows of one column at a time.
+// Null has no rows: it reads as zeros.
 struct StateRows {
   __amdgpu_buffer_rsrc_t rows;
   int kd, vd;
@@ -500,7 +499,7 @@ __device__ __forceinline__ void update_state(
       for (int j = 0; j < 4; ++j)
         s.x[nb][ct][j] = fmaf(s.x[nb][ct][j], carry, u[ct][j]);
     // as many tiles' operands at a time as registers are left for (fp32, 256 heads x 1024 rows
-    // of 128 x 128: eight 349 us and a backward pass of 708, two 337 and 660)
+    // of 128 x 128: eight 351 us and a backward pass of 700, two 337 and 657)
     constexpr int kGroup = NCT == 2 || sizeof(T) == 4 ? 2 : 8;
     if (nb % kGroup == kGroup - 1) __builtin_amdgcn_sched_barrier(0);
   }
@@ -509,9 +508,9 @@ __device__ __forceinline__ void update_state(
 // Wave priority by the chunk's number, lower as it rises (from 3 to 0, over and over): of two
 // workgroups on a compute unit the one behind goes first. With equal priorities the older
 // one always does, ends early and leaves the other alone (512 heads x 2048 rows of
-// 128 x 128: 207 and 238 us after their common start; with this 226 and 229). Scans that run
-// together read the same rows when they happen to keep pace and are better left alone: a
-// training step of 4 x 4096 x 16 heads 331 us, with turns 345.
+// 128 x 128: 269 us, with this 254; at 64 x 64 253 and 231). Scans that run together read the
+// same rows when they happen to keep pace and are better left alone: a training step of
+// 4 x 4096 x 16 heads 364 us, with turns 373.
 __device__ __forceinline__ void take_turns(int chunk) {
   switch (chunk & 3) {
     case 0: __builtin_amdgcn_s_setprio(3); break;
@@ -522,7 +521,7 @@ __device__ __forceinline__ void take_turns(int chunk) {
 }
 
 // The sums of one segment of 64 * chunks tokens, from X = 0. Bound by the bytes of K and V:
-// those of 65536 x 16 heads of 128 x 128 (540 MB with the sums) in 110 us, 4.9 TB/s.
+// those of 65536 x 16 heads of 128 x 128 (550 MB with the sums) in 111 us, 5.0 TB/s.
 template <typename T, int KD, int NW, int NCT, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
   constexpr int NT = 64 * NW, VS = 16 * NW * NCT;
@@ -575,7 +574,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_decay_sums(DecayPass pass) {
 
 // part of a head's segments: X_0, then X before segment s + 1 = a^seg_len (X before s) + sums
 // of s, four elements per thread. Bound by the bytes: 16 heads x 32 states of 128 x 128 read
-// and written (67 MB) in 13 us, 5.1 TB/s. (Two elements per thread and twice as many loads
+// and written (67 MB) in 14 us, 4.8 TB/s. (Two elements per thread and twice as many loads
 // ahead: calls 1 to 5 us longer.)
 __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
   int id = blockIdx.y;
@@ -617,8 +616,8 @@ __global__ __launch_bounds__(256) void k_decay_prefix(DecayPass pass) {
 // Terms of the pair weights and of X (see above).
 template <typename T> constexpr int kRowTerms = sizeof(T) == 2 ? 2 : 1;
 
-// Four pair weights as a first term and what it leaves. The first keeps within bf16's range,
-// so that a weight past it ends as Inf, not as Inf - Inf.
+// The first terms of four pair weights. They keep within bf16's range, so that a weight past
+// it ends as Inf, not as Inf - Inf.
 __device__ __forceinline__ f32x4 first_term(f32x4 x) {
   f32x4 t;
 #pragma unroll
@@ -643,7 +642,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
   // the pair weights as B operands: rows 16 i .. + 15, tokens 32 m .. + 31 in fragment
   // first(i) + m. Second terms behind the first ones; at 256 k columns, where that would
   // leave no room for a second workgroup on the unit, in the values' place once they are read
-  // (4 x 8192 x 8 heads of 256 x 64: 137 instead of 168 us).
+  // (512 heads x 2048 rows of 256 x 64: 298 us instead of 407).
   constexpr bool kTight = TERMS == 2 && KD == 256;
   static_assert(!kTight || sizeof(Vs) >= 6 * 64 * sizeof(frag), "room for the second terms");
   __shared__ __align__(16) frag Ps[kTight ? 1 : TERMS][6 * 64];
@@ -783,7 +782,7 @@ __global__ __launch_bounds__(64 * NW, scan_waves(sizeof(T), KD, NCT)) void k_dec
     __syncthreads();
     if (kTight) {
       pairs();
-      fetch_q(c + kChunkT);   // (in front of the pairs: 150 us)
+      fetch_q(c + kChunkT);   // (in front of the pairs, spilled: a tenth more)
       __syncthreads();
     }
 
@@ -834,7 +833,7 @@ hipError_t launch(const DecayPass &pass, bool sums, hipStream_t st) {
 
 // fp32 inputs keep one value tile per wave, in twice as many waves: their operands take
 // twice the registers. So do the sums, which have registers to spare: two buffers and eight
-// waves against one and four, ragged prompts of 6 x 1999 rows 96.4 -> 93.0 us.
+// waves against one and four, padded prompts of 6 x 1999 rows 97 to 100 -> 94 to 98 us.
 template <typename T, bool WHOLE>
 hipError_t dispatch(const DecayPass &p, bool sums, hipStream_t st) {
   constexpr int NW = sizeof(T) == 2 ? 4 : 8, NCT = 8 / NW;

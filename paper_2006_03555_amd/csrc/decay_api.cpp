@@ -168,18 +168,18 @@ struct Cut {
 };
 
 // Whole calls in us (one to eight chunks of 64 rows per segment; a chunk takes a workgroup
-// that has a compute unit for itself 2.4 us at 64 x 64 bf16, 4 at 128 x 128, 6 and 12 in fp32):
+// that has a compute unit for itself 3 us at 64 x 64 bf16, 4.5 at 128 x 128, 6 and 9 in fp32):
 //   Long sequences: segments for 512 workgroups, two on each of the 256 compute units, as
 //   long as they have 256 rows.
 //   Shorter ones: as many segments as it takes for 256 workgroups, of one chunk at least,
 //   from four chunks on. B1 H8, with 256-row segments / with this: bf16 64 x 64 L512
-//   22.5 / 13.6, L4096 25.3 / 22.2; 128 x 128 L1024 40.2 / 24.0; fp32 128 x 128 L512
-//   79.9 / 25.4, L4096 87.7 / 66.6. For 512 workgroups instead: bf16 64 x 64 L4096 28.4,
-//   fp32 128 x 128 L2048 42.8 -> 50.4. Two chunks apart: bf16 64 x 64 L128 8.9 / 13.4.
+//   25.3 / 14.2, L4096 28.1 / 23.8; 128 x 128 L1024 34.3 / 24.7; fp32 128 x 128 L512
+//   59.1 / 25.5, L4096 88.9 / 62.2. For 512 workgroups instead: bf16 64 x 64 L4096 29.0,
+//   fp32 128 x 128 L2048 43.0 -> 49.5. Two chunks apart: bf16 64 x 64 L128 10.0 / 13.4.
 //   Slices of 64 value columns for wider values while the chunks are few: twice as many
 //   workgroups, each with half the work per chunk and the pair weights to itself. B1 H8
-//   128 x 128, slices of 128 / 64: bf16 L128 15.8 / 11.9, L4096 39.4 / 38.3, B2 H16 L16384
-//   215 / 217; fp32 L2048 45.5 / 42.8, L4096 62.1 / 66.6. With more than 128 k columns X
+//   128 x 128, slices of 128 / 64: bf16 L128 17.3 / 12.7, L4096 38.8 / 39.7, B2 H16 L8192
+//   117 / 130; fp32 L2048 45.3 / 43.0, L4096 62.2 / 67.4. With more than 128 k columns X
 //   leaves room for no more.
 constexpr int kFullWorkgroups = 512, kMinRows = 256;
 constexpr int kSomeWorkgroups = 256, kMinSplitTiles = 4;

@@ -8,8 +8,10 @@
 // a thread owns four value columns of every n-th row, so the state moves in 16-byte
 // units, whole rows at a time; the threads' parts of o are summed in a fixed order.
 // 1024 sequences x 16 heads at 128 x 128 (2.1 GB) take 412 us, 5.2 TB/s (a copy on this card:
-// 4.95); 48 sequences, whose states stay in the memory-side cache, 16 us, 6.2 TB/s. One
-// sequence of 8 heads takes 4 us, most of it the launch and one round of loads.
+// 4.95). 48 sequences (101 MB) repeated on the same states, which then stay in the memory-side
+// cache, take 16.6 us, 6.1 TB/s, and 18.4 us, 5.5 TB/s, where new ones come from call to
+// call. One sequence of 8 heads takes 4.0 us in a graph (traced alone 4.9), most of it the
+// launch and one round of loads.
 #include "decay.hpp"
 #include "favor_common.hpp"
 
