@@ -464,6 +464,191 @@ FAVOR_API favor_status favor_dropout(const void *x, const void *residual, void *
                                      favor_dtype dtype, double p, uint64_t seed,
                                      uint64_t offset, const uint64_t *rng, hipStream_t stream);
 
+/*
+ * Short causal convolution, one filter per channel (the step in front of a selective scan):
+ *   u_t = bias + sum_{j < width} w[j] x_{t - width + 1 + j},   y_t = u_t, or u_t sigmoid(u_t)
+ * with the inputs before the first token from a state (zeros without one).
+ *
+ * Layouts: x, y [B][L][D] with rows of D contiguous elements and any strides between them, in
+ * elements (favor_strides, head unused; all three 0 = contiguous), multiples of 16 bytes, so
+ * that halves of one projection and transposed batches need no copy; outputs' rows must not
+ * share elements, and outputs must not overlap inputs. weight [D][width] and bias [D]
+ * (nullable) fp32. States [B][width - 1][D] in dtype, contiguous: the last width - 1 inputs,
+ * the oldest first.
+ *
+ * Supported: width 2 to 8; D a multiple of 8 up to 65536; dtype (x, y, states and their
+ * gradients) F32 or BF16, sums in fp32; 0 <= L <= 2^30, B <= 65535. lengths [B] int32
+ * (nullable, device): as for favor_attn_decay: rows behind a sequence are not read and their
+ * rows of y and dx are written as zeros.
+ */
+typedef struct {
+  int32_t B, L, D, width;
+  favor_dtype dtype;
+  int32_t silu;                      /* 0: y = u */
+  favor_strides x, y;
+  favor_strides grad_y, grad_x;      /* read by the backward pass only */
+} favor_conv_desc;
+
+/* state_in (nullable), state_out (nullable; may be state_in, and overlaps it not otherwise). */
+FAVOR_API favor_status favor_conv(const favor_conv_desc *g, const void *x, const float *weight,
+                                  const float *bias, const int32_t *lengths, void *y,
+                                  const void *state_in, void *state_out, hipStream_t stream);
+
+/*
+ * Gradients from dy and dstate_out (nullable: zeros) of x, weight [D][width], bias (dbias
+ * nullable) and state_in (dstate_in nullable; overlaps neither state nor dstate_out).
+ * Nothing from the forward call is needed. Deterministic. Workspace:
+ * favor_conv_workspace_size(g) bytes, 256-byte aligned; its contents do not matter.
+ */
+FAVOR_API favor_status favor_conv_backward(const favor_conv_desc *g, const void *x,
+                                           const float *weight, const float *bias,
+                                           const int32_t *lengths, const void *state_in,
+                                           const void *dy, const void *dstate_out, void *dx,
+                                           float *dweight, float *dbias, void *dstate_in,
+                                           void *ws, size_t ws_bytes, hipStream_t stream);
+FAVOR_API size_t favor_conv_workspace_size(const favor_conv_desc *g);
+
+/*
+ * One token of B sequences: x, y [B][D] (batch strides; L has no effect) and the states
+ * [n_slots][width - 1][D], updated in place. slots as for favor_attn_decay_step: a place
+ * outside 0 .. n_slots - 1 is padding and gives y = 0, sequences that name the same place
+ * take their turns in order.
+ */
+FAVOR_API favor_status favor_conv_step(const favor_conv_desc *g, const void *x,
+                                       const float *weight, const float *bias,
+                                       const int32_t *slots, int32_t n_slots, void *state,
+                                       void *y, hipStream_t stream);
+
+/*
+ * Selective state space scan, per channel d (in group g = d / (D / groups)) and state n:
+ *   s_t = softplus(dt_t + dt_bias_d)   (softplus = 0: dt_t + dt_bias_d)
+ *   h_t[n] = exp(s_t A[d][n]) h_{t-1}[n] + s_t x_t B_t[g][n]
+ *   y_t = (sum_n C_t[g][n] h_t[n] + skip_d x_t) silu(z_t)
+ * without the terms of a NULL dt_bias, skip or z.
+ *
+ * Layouts: x, dt, z, y [B][L][D] as for favor_conv; B, C [B][L][groups][N] with N contiguous
+ * elements and any strides in elements (head: the group's), not aligned. A [D][N], skip and
+ * dt_bias [D] fp32. States [B][D][N] fp32, contiguous.
+ *
+ * Supported: N from 1 to 256; D up to 65536 with D / groups a multiple of 8; dtype (x, dt, B,
+ * C, z, y and their gradients) F32 or BF16; 0 <= L <= 2^30, B <= 65535. Steps, states and sums
+ * are fp32 for both. A is meant to be negative; for a positive one exp(A times the steps of
+ * any 128 tokens) has to be in fp32's range, and A must be finite. lengths as for favor_conv
+ * (B's and C's padding is not read either, its gradients are zeros). A NaN or infinity reaches
+ * the results of its own channel (in B or C: of its group) from its token on, and gradients as the
+ * formulas carry it; in the backward pass it may reach all of its chunk of 128 tokens.
+ */
+typedef struct {
+  int32_t B, L, D, N, groups;
+  favor_dtype dtype;
+  int32_t softplus;
+  favor_strides x, dt, b, c, z, y;
+  favor_strides grad_y, grad_x, grad_dt, grad_b, grad_c, grad_z;   /* backward pass only */
+} favor_scan_desc;
+
+/* Bytes of device workspace for favor_selective_scan (backward = 0) or its backward pass (1),
+ * 256-byte aligned; 0 if none is needed or g is invalid. Its contents do not matter. */
+FAVOR_API size_t favor_scan_workspace_size(const favor_scan_desc *g, int backward);
+
+/* state_in (nullable), state_out (nullable; may be state_in, and overlaps it not otherwise):
+ * the state before the first and after each sequence's last token. Deterministic. */
+FAVOR_API favor_status favor_selective_scan(const favor_scan_desc *g, const void *x,
+                                            const void *dt, const float *A, const void *Bm,
+                                            const void *C, const float *skip, const void *z,
+                                            const float *dt_bias, const int32_t *lengths,
+                                            void *y, const float *state_in, float *state_out,
+                                            void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Gradients from dy and dstate_out (nullable: zeros): with e_t = dy_t silu(z_t), and
+ * q_t = exp(s_t A) (C_t e_t + q_{t+1}) from the right (q behind the last token: dstate_out),
+ *   dC = sum_d e h,  dB = sum_d (C e + q_{t+1}) s x,  dA = sum s_t q_t h_{t-1},  dstate_in = q_0
+ *   ds = sum_n A q_t h_{t-1} + x sum_n (C e + q_{t+1}) B,  ddt = ds softplus'(dt + dt_bias)
+ *   dx = s sum_n (C e + q_{t+1}) B + skip e,  dz = dy (C h + skip x) silu'(z),  dskip = sum e x
+ * and ddt_bias = sum ddt. dskip, dz and ddt_bias are required where skip, z and dt_bias are
+ * given, and not written otherwise. dstate_in (nullable) may be dstate_out, and overlaps
+ * neither it nor state_in otherwise. Nothing from the forward call is needed. Deterministic.
+ */
+FAVOR_API favor_status favor_selective_scan_backward(
+    const favor_scan_desc *g, const void *x, const void *dt, const float *A, const void *Bm,
+    const void *C, const float *skip, const void *z, const float *dt_bias,
+    const int32_t *lengths, const float *state_in, const void *dy, const float *dstate_out,
+    void *dx, void *ddt, float *dA, void *dB, void *dC, float *dskip, void *dz,
+    float *ddt_bias, float *dstate_in, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* One token of B sequences: x, dt, z, y [B][D], Bm, C [B][groups][N] (token strides and L have
+ * no effect), the states [n_slots][D][N] updated in place; slots as for favor_conv_step. */
+FAVOR_API favor_status favor_selective_scan_step(const favor_scan_desc *g, const void *x,
+                                                 const void *dt, const float *A, const void *Bm,
+                                                 const void *C, const float *skip, const void *z,
+                                                 const float *dt_bias, const int32_t *slots,
+                                                 int32_t n_slots, float *state, void *y,
+                                                 hipStream_t stream);
+
+/* Host-only validation of a descriptor (op: 0 forward, 1 backward, 2 single tokens). */
+FAVOR_API favor_status favor_validate_conv_desc(const favor_conv_desc *g, int op);
+FAVOR_API favor_status favor_validate_scan_desc(const favor_scan_desc *g, int op);
+
+/*
+ * Beam search's choice of the next tokens: for each of B entries the n best of the K V
+ * continuations by
+ *   score(k, v) = scores[k] + x[k][v] - log sum_u exp x[k][u]
+ * in falling order: out_scores [B][n] fp32, parent [B][n] (the beam k) and token [B][n] int32.
+ * Ties go to the lower beam, then in one beam to the higher logit and the lower token. Sums of
+ * exponentials are fp32 per lane and joined in 64 bits; scores are compared in 64 bits.
+ *
+ * logits [B][K][V] of dtype, V contiguous, strides in elements (both 0 = contiguous), not
+ * aligned: any V and slices of a padded vocabulary. scores [B][K] fp32. ended [B][K] bytes
+ * (nullable): a beam that has ended (not 0) offers only itself, with end_token and its own
+ * score, and its logits are not read. end_token < 0: there is none (then ended must be NULL).
+ * Only finite scores are offered: a beam of score -Inf, a token of logit -Inf and a beam with a
+ * NaN or +Inf among its logits (whose sum is no number) offer nothing. Where fewer than n are
+ * offered the rest has score -Inf, parent 0 and token end_token (0 without one).
+ *
+ * Supported: K and n up to 64, V from 1 to 2^30, B K <= 65535. Workspace:
+ * favor_beam_workspace_size(g) bytes, 256-byte aligned; its contents do not matter.
+ */
+typedef struct {
+  int32_t B, K, V, n;
+  favor_dtype dtype;
+  int64_t batch_stride, beam_stride;
+  int32_t end_token;
+} favor_beam_desc;
+
+FAVOR_API favor_status favor_validate_beam_desc(const favor_beam_desc *g);   /* host only */
+FAVOR_API size_t favor_beam_workspace_size(const favor_beam_desc *g);
+FAVOR_API favor_status favor_beam_select(const favor_beam_desc *g, const void *logits,
+                                         const float *scores, const uint8_t *ended,
+                                         float *out_scores, int32_t *parent, int32_t *token,
+                                         void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * The states of pools (of favor_attn_decay_step, favor_conv_step, favor_selective_scan_step)
+ * behind the chosen beams: beam j of entry b continues beam parent[b][j], whose state is at
+ * place slots[b][parent[b][j]] of every pool (slots NULL: b K + the beam). A beam's first
+ * child takes its place as it is; its other children, in order, take the places of the
+ * entry's beams without children, in order, and the states are copied there, in place. So only
+ * the states of dead beams are written, and new_slots [B][K] holds the same places as slots in
+ * another order. A beam whose parent is outside 0 .. K - 1 takes a free place and its state
+ * stays what it was there. Nothing is copied from or to places outside 0 .. n_slots - 1.
+ * The places inside the pools that one call names must differ. new_slots must not overlap
+ * slots or parent.
+ *
+ * pools: n_pools host descriptions, read during the call: data (16-byte aligned),
+ * bytes_per_slot (a multiple of 16, up to 2^34) and n_slots. K <= 64, B K <= 65535. Up to 64
+ * pools are one launch.
+ */
+typedef struct {
+  void *data;
+  int64_t bytes_per_slot;
+  int32_t n_slots;
+} favor_beam_pool;
+
+FAVOR_API favor_status favor_beam_reorder(int32_t B, int32_t K, const int32_t *parent,
+                                          const int32_t *slots, int32_t *new_slots,
+                                          const favor_beam_pool *pools, int32_t n_pools,
+                                          hipStream_t stream);
+
 /* Host-only validation of a descriptor for an operation (0 feature map,
  * 1 bidirectional, 2 causal, 3 both, 4 bidirectional backward, 5 causal
  * backward, 6 backward of both directions); launches nothing and touches no

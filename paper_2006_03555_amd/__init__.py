@@ -27,6 +27,9 @@ from ._lib import (  # noqa: F401
     FavorDesc, FavorError, FavorLibraryMissing, lib, lib_path, make_desc, status_string,
     validate_desc, workspace_size, last_error, timing_enable, timing_reset, timing_read,
     FavorDecayDesc, decay_workspace_size, make_decay_desc, validate_decay_desc,
+    FavorBeamDesc, FavorBeamPool, FavorConvDesc, FavorScanDesc, beam_workspace_size,
+    conv_workspace_size, make_beam_desc, make_conv_desc, make_scan_desc, scan_workspace_size,
+    validate_beam_desc, validate_conv_desc, validate_scan_desc,
 )
 
 __all__ = [
@@ -36,6 +39,12 @@ __all__ = [
     "attn_both_noalloc", "noalloc_scratch_bytes",
     "attn_decay", "attn_decay_backward", "attn_decay_step", "decay_workspace_size",
     "make_decay_desc", "validate_decay_desc", "dropout", "dropout_backward",
+    "causal_conv", "causal_conv_backward", "causal_conv_step", "conv_workspace_size",
+    "make_conv_desc", "validate_conv_desc",
+    "selective_scan", "selective_scan_backward", "selective_scan_step", "scan_workspace_size",
+    "make_scan_desc", "validate_scan_desc",
+    "beam_select", "beam_reorder", "beam_workspace_size", "make_beam_desc",
+    "validate_beam_desc",
     "validate_desc", "FavorError", "FavorLibraryMissing", "lib", "lib_path",
 ]
 
@@ -771,3 +780,378 @@ def dropout(x, p, seed=0, offset=0, residual=None, out=None, rng=None, stream=No
 def dropout_backward(dout, p, seed=0, offset=0, dx=None, rng=None, stream=None):
     """The gradient of dropout's x (its residual's is dout): the same mask on dout."""
     return dropout(dout, p, seed, offset, out=dx, rng=rng, stream=stream)
+
+
+# ------------------------------------------------- short convolution and selective scan
+class _Planned:
+    """A descriptor with its by-reference argument and workspace size."""
+    __slots__ = ("g", "ref", "workspace")
+
+    def __init__(self, g, workspace):
+        self.g = g
+        self.ref = ctypes.byref(g)
+        self.workspace = workspace
+
+
+def _token_rows(like, name):
+    """(batch, unused, token) strides of [B, L, D] (or [B, D]) rows; see _row_strides."""
+    return _row_strides((like[0][0], 1) + tuple(like[0][1:]),
+                        (like[2][0], 0) + tuple(like[2][1:]), name)
+
+
+def _group_rows(like, name):
+    """(batch, group, token) strides of [B, L, G, N] (or [B, G, N]) rows."""
+    shape, s = like[0], like[2]
+    if len(shape) == 3:
+        return _row_strides(shape, s, name)
+    return _row_strides((shape[0], shape[2], shape[1], shape[3]), (s[0], s[2], s[1], s[3]), name)
+
+
+def _require_dims(like, dims, want, name):
+    if len(like[0]) != dims:
+        raise FavorError(1, f"{name} must be {want}, got {tuple(like[0])}")
+
+
+def _require_state(name, like, shape, dtype, pool):
+    """A state of every sequence; pool: of any number of places."""
+    if like is not None:
+        _require_dims(like, len(shape), f"of {len(shape)} dimensions", name)
+        _require_shape(like, (like[0][0],) + shape[1:] if pool else shape, dtype, name)
+
+
+@functools.lru_cache(maxsize=256)
+def _conv_plan(op, x, weight, bias, lengths, rows, states, silu):
+    """The _Planned call of a forward (0), backward (1) or single-token (2) convolution, its tensors'
+    shapes and types checked; every argument is made of _like()'s plain values."""
+    torch = _torch()
+    _require_dims(x, 2 if op == 2 else 3, "[B, D]" if op == 2 else "[B, L, D]", "x")
+    _require_dims(weight, 2, "[D, width]", "weight")
+    B, D, L = x[0][0], x[0][-1], 1 if op == 2 else x[0][1]
+    width = weight[0][1]
+    _require_shape(weight, (D, width), torch.float32, "weight")
+    _require_shape(bias, (D,), torch.float32, "bias")
+    _require_shape(lengths, (B,), torch.int32, "slots" if op == 2 else "lengths")
+    strides = {"x": _token_rows(x, "x")}
+    for name, field, t in rows:
+        if field is None:
+            _require_shape(t, (D, width) if name == "dweight" else (D,), torch.float32, name)
+        else:
+            _require_shape(t, x[0], x[1], name)
+            strides[field] = _token_rows(t, name)
+    for name, t in states:
+        _require_state(name, t, (B, width - 1, D), x[1], op == 2)
+    g = make_conv_desc(B, L, D, width, _dtype_code(x[1]), silu, **strides)
+    _check(validate_conv_desc(g, op))
+    return _Planned(g, conv_workspace_size(g) if op == 1 else 0)
+
+
+@_on_stream
+def causal_conv(x, weight, bias=None, silu=False, lengths=None, state_in=None,
+                return_state=False, out=None, state_out=None, stream=None):
+    """Short causal convolution, one filter per channel (favor_conv):
+    y_t = act(bias + sum_j weight[:, j] x_{t - width + 1 + j}).
+
+    x [B, L, D]: bfloat16 or float32, rows contiguous, any other strides (a half of a
+    projection); D a multiple of 8. weight [D, width] (2 to 8 taps) and bias [D] float32;
+    silu: y = u sigmoid(u). lengths [B] int32: tokens of each right-padded sequence. States
+    [B, width - 1, D] in x's type: the last inputs. Returns y [B, L, D] (contiguous unless
+    given), or (y, state_out) when return_state is true.
+    """
+    torch = _torch()
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    c = _conv_plan(0, _like(x), _like(weight), _like(bias), _like(lengths),
+                   (("out", "y", _like(out)),),
+                   (("state_in", _like(state_in)), ("state_out", _like(state_out))), bool(silu))
+    if return_state and state_out is None:
+        g = c.g
+        state_out = torch.empty((g.B, g.width - 1, g.D), dtype=x.dtype, device=x.device)
+    here = _require_here(x, weight, bias, lengths, out, state_in, state_out)
+    _require_whole(weight, bias, lengths, state_in, state_out)
+    _check(lib().favor_conv(c.ref, _ptr(x), _ptr(weight), _ptr(bias), _ptr(lengths), _ptr(out),
+                            _ptr(state_in), _ptr(state_out), _stream_on(here, stream)))
+    return (out, state_out) if return_state else out
+
+
+@_on_stream
+def causal_conv_backward(x, weight, dout, bias=None, silu=False, lengths=None, state_in=None,
+                         dstate_out=None, return_state_grad=False, dx=None, dweight=None,
+                         dbias=None, dstate_in=None, workspace=None, stream=None):
+    """Gradients of causal_conv (favor_conv_backward) from dout and dstate_out (default zeros).
+
+    Returns (dx, dweight, dbias), or (dx, dweight, dbias, dstate_in) when return_state_grad is
+    true; dbias is None without a bias.
+    """
+    torch = _torch()
+    if dx is None:
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+    if dweight is None:
+        dweight = torch.empty_like(weight)
+    if bias is None:
+        dbias = None
+    elif dbias is None:
+        dbias = torch.empty_like(bias)
+    c = _conv_plan(1, _like(x), _like(weight), _like(bias), _like(lengths),
+                   (("dout", "grad_y", _like(dout)), ("dx", "grad_x", _like(dx)),
+                    ("dweight", None, _like(dweight)), ("dbias", None, _like(dbias))),
+                   (("state_in", _like(state_in)), ("dstate_out", _like(dstate_out)),
+                    ("dstate_in", _like(dstate_in))), bool(silu))
+    if return_state_grad and dstate_in is None:
+        g = c.g
+        dstate_in = torch.empty((g.B, g.width - 1, g.D), dtype=x.dtype, device=x.device)
+    here = _require_here(x, weight, bias, lengths, dout, dx, dweight, dbias, state_in, dstate_out,
+                         dstate_in)
+    _require_whole(weight, bias, lengths, dweight, dbias, state_in, dstate_out, dstate_in)
+    ws, nbytes = _decay_workspace(c.workspace, workspace)
+    _check(lib().favor_conv_backward(
+        c.ref, _ptr(x), _ptr(weight), _ptr(bias), _ptr(lengths), _ptr(state_in), _ptr(dout),
+        _ptr(dstate_out), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dstate_in), _ptr(ws), nbytes,
+        _stream_on(here, stream)))
+    return (dx, dweight, dbias, dstate_in) if return_state_grad else (dx, dweight, dbias)
+
+
+@_on_stream
+def causal_conv_step(x, weight, state, bias=None, silu=False, slots=None, out=None, stream=None):
+    """The next token of B sequences (favor_conv_step): x [B, D], state [n, width - 1, D] (the
+    last inputs) updated in place. slots [B] int32: the place of each sequence's state
+    (default: its own index); one outside 0 .. n - 1 is padding and gives y = 0. Returns
+    y [B, D].
+    """
+    if out is None:
+        out = _torch().empty_like(x, memory_format=_torch().contiguous_format)
+    c = _conv_plan(2, _like(x), _like(weight), _like(bias), _like(slots),
+                   (("out", "y", _like(out)),), (("state", _like(state)),), bool(silu))
+    here = _require_here(x, weight, bias, state, slots, out)
+    _require_whole(weight, bias, state, slots)
+    _check(lib().favor_conv_step(c.ref, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(slots),
+                                 state.shape[0], state.data_ptr(), out.data_ptr(),
+                                 _stream_on(here, stream)))
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def _scan_plan(op, x, A, params, b, c, rows, lengths, states, softplus):
+    """As _conv_plan, of a selective scan. params: (name, _like()) of [D] ones; rows: (name,
+    field, which of "x" and "b" it is shaped like, _like())."""
+    torch = _torch()
+    _require_dims(x, 2 if op == 2 else 3, "[B, D]" if op == 2 else "[B, L, D]", "x")
+    _require_dims(A, 2, "[D, N]", "A")
+    lead, D, N = x[0][:-1], x[0][-1], A[0][1]
+    if op == 2:
+        _require_dims(b, 3, "[B, groups, N]", "B")
+    else:
+        _require_dims(b, 4, "[B, L, groups, N]", "B")
+    groups = b[0][-2]
+    _require_shape(A, (D, N), torch.float32, "A")
+    for name, t in params:
+        _require_shape(t, (D, N) if name == "dA" else (D,), torch.float32, name)
+    _require_shape(b, lead + (groups, N), x[1], "B")
+    _require_shape(c, b[0], x[1], "C")
+    _require_shape(lengths, lead[:1], torch.int32, "slots" if op == 2 else "lengths")
+    strides = {"x": _token_rows(x, "x"), "b": _group_rows(b, "B"), "c": _group_rows(c, "C")}
+    for name, field, of, t in rows:
+        if t is None:
+            continue
+        _require_shape(t, x[0] if of == "x" else b[0], x[1], name)
+        strides[field] = _token_rows(t, name) if of == "x" else _group_rows(t, name)
+    for name, t in states:
+        _require_state(name, t, (lead[0], D, N), torch.float32, op == 2)
+    g = make_scan_desc(lead[0], 1 if op == 2 else lead[1], D, N, _dtype_code(x[1]), groups,
+                       softplus, **strides)
+    _check(validate_scan_desc(g, op))
+    return _Planned(g, 0 if op == 2 else scan_workspace_size(g, op == 1))
+
+
+@_on_stream
+def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, lengths=None,
+                   state_in=None, return_state=False, out=None, state_out=None, workspace=None,
+                   stream=None):
+    """Selective state space scan (favor_selective_scan): with s = softplus(dt + dt_bias),
+    h_t = exp(s_t A) h_{t-1} + s_t x_t B_t and y_t = (C_t h_t + D x_t) silu(z_t).
+
+    x, dt, z [B, L, D]: bfloat16 or float32, rows contiguous, any other strides; B, C
+    [B, L, groups, N] of the same type (channel d reads group d / (D / groups)), N up to 256;
+    D / groups a multiple of 8. A [D, N], D and dt_bias [D] float32; D, z and dt_bias may be
+    left out, softplus=False takes s = dt + dt_bias. lengths [B] int32: tokens of each
+    right-padded sequence. States [B, D, N] float32. Returns y [B, L, D] (contiguous unless
+    given), or (y, state_out) when return_state is true.
+    """
+    torch = _torch()
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    c = _scan_plan(0, _like(x), _like(A), (("D", _like(D)), ("dt_bias", _like(dt_bias))),
+                   _like(B), _like(C),
+                   (("dt", "dt", "x", _like(dt)), ("z", "z", "x", _like(z)),
+                    ("out", "y", "x", _like(out))), _like(lengths),
+                   (("state_in", _like(state_in)), ("state_out", _like(state_out))),
+                   bool(softplus))
+    if return_state and state_out is None:
+        g = c.g
+        state_out = torch.empty((g.B, g.D, g.N), dtype=torch.float32, device=x.device)
+    here = _require_here(x, dt, A, B, C, D, z, dt_bias, lengths, out, state_in, state_out)
+    _require_whole(A, D, dt_bias, lengths, state_in, state_out)
+    ws, nbytes = _decay_workspace(c.workspace, workspace)
+    _check(lib().favor_selective_scan(
+        c.ref, _ptr(x), _ptr(dt), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z), _ptr(dt_bias),
+        _ptr(lengths), _ptr(out), _ptr(state_in), _ptr(state_out), _ptr(ws), nbytes,
+        _stream_on(here, stream)))
+    return (out, state_out) if return_state else out
+
+
+@_on_stream
+def selective_scan_backward(x, dt, A, B, C, dout, D=None, z=None, dt_bias=None, softplus=True,
+                            lengths=None, state_in=None, dstate_out=None,
+                            return_state_grad=False, dx=None, ddt=None, dA=None, dB=None, dC=None,
+                            dD=None, dz=None, ddt_bias=None, dstate_in=None, workspace=None,
+                            stream=None):
+    """Gradients of selective_scan (favor_selective_scan_backward) from dout and dstate_out
+    (default zeros).
+
+    Returns (dx, ddt, dA, dB, dC, dD, dz, ddt_bias), followed by dstate_in when
+    return_state_grad is true; dD, dz and ddt_bias are None where D, z and dt_bias are.
+    """
+    torch = _torch()
+    whole = torch.contiguous_format
+    dx, ddt, dB, dC = (torch.empty_like(like, memory_format=whole) if t is None else t
+                       for t, like in ((dx, x), (ddt, dt), (dB, B), (dC, C)))
+    dA = torch.empty_like(A) if dA is None else dA
+    dD, dz, ddt_bias = (None if like is None else
+                        torch.empty_like(like, memory_format=whole) if t is None else t
+                        for t, like in ((dD, D), (dz, z), (ddt_bias, dt_bias)))
+    c = _scan_plan(1, _like(x), _like(A),
+                   (("D", _like(D)), ("dt_bias", _like(dt_bias)), ("dA", _like(dA)),
+                    ("dD", _like(dD)), ("ddt_bias", _like(ddt_bias))), _like(B), _like(C),
+                   (("dt", "dt", "x", _like(dt)), ("z", "z", "x", _like(z)),
+                    ("dout", "grad_y", "x", _like(dout)), ("dx", "grad_x", "x", _like(dx)),
+                    ("ddt", "grad_dt", "x", _like(ddt)), ("dz", "grad_z", "x", _like(dz)),
+                    ("dB", "grad_b", "b", _like(dB)), ("dC", "grad_c", "b", _like(dC))),
+                   _like(lengths),
+                   (("state_in", _like(state_in)), ("dstate_out", _like(dstate_out)),
+                    ("dstate_in", _like(dstate_in))), bool(softplus))
+    if return_state_grad and dstate_in is None:
+        g = c.g
+        dstate_in = torch.empty((g.B, g.D, g.N), dtype=torch.float32, device=x.device)
+    here = _require_here(x, dt, A, B, C, D, z, dt_bias, lengths, state_in, dout, dstate_out, dx,
+                         ddt, dA, dB, dC, dD, dz, ddt_bias, dstate_in)
+    _require_whole(A, D, dt_bias, lengths, state_in, dstate_out, dA, dD, ddt_bias, dstate_in)
+    ws, nbytes = _decay_workspace(c.workspace, workspace)
+    _check(lib().favor_selective_scan_backward(
+        c.ref, _ptr(x), _ptr(dt), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z), _ptr(dt_bias),
+        _ptr(lengths), _ptr(state_in), _ptr(dout), _ptr(dstate_out), _ptr(dx), _ptr(ddt), _ptr(dA),
+        _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dz), _ptr(ddt_bias), _ptr(dstate_in), _ptr(ws), nbytes,
+        _stream_on(here, stream)))
+    grads = (dx, ddt, dA, dB, dC, dD, dz, ddt_bias)
+    return grads + (dstate_in,) if return_state_grad else grads
+
+
+@_on_stream
+def selective_scan_step(x, dt, A, B, C, state, D=None, z=None, dt_bias=None, softplus=True,
+                        slots=None, out=None, stream=None):
+    """The next token of B sequences (favor_selective_scan_step): x, dt, z [B, D], B, C
+    [B, groups, N], state [n, D, N] float32 updated in place; slots as for causal_conv_step.
+    Returns y [B, D].
+    """
+    if out is None:
+        out = _torch().empty_like(x, memory_format=_torch().contiguous_format)
+    c = _scan_plan(2, _like(x), _like(A), (("D", _like(D)), ("dt_bias", _like(dt_bias))),
+                   _like(B), _like(C),
+                   (("dt", "dt", "x", _like(dt)), ("z", "z", "x", _like(z)),
+                    ("out", "y", "x", _like(out))), _like(slots), (("state", _like(state)),),
+                   bool(softplus))
+    here = _require_here(x, dt, A, B, C, D, z, dt_bias, state, slots, out)
+    _require_whole(A, D, dt_bias, state, slots)
+    _check(lib().favor_selective_scan_step(
+        c.ref, x.data_ptr(), dt.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(D),
+        _ptr(z), _ptr(dt_bias), _ptr(slots), state.shape[0], state.data_ptr(), out.data_ptr(),
+        _stream_on(here, stream)))
+    return out
+
+
+# ----------------------------------------------------------------------------- beam search
+@functools.lru_cache(maxsize=256)
+def _beam_plan(logits, scores, ended, outs, n, end_token):
+    torch = _torch()
+    _require_dims(logits, 3, "[B, K, V]", "logits")
+    B, K, V = logits[0]
+    if V > 1 and logits[2][2] != 1:
+        raise FavorError(1, "rows of logits must be contiguous")
+    _require_shape(scores, (B, K), torch.float32, "scores")
+    if ended is not None and (ended[0] != (B, K) or ended[1] not in (torch.bool, torch.uint8)):
+        raise FavorError(1, f"ended must be {(B, K)} bool or uint8, got {tuple(ended[0])} "
+                            f"{ended[1]}")
+    for (name, t), dtype in zip(outs, (torch.float32, torch.int32, torch.int32)):
+        _require_shape(t, (B, n), dtype, name)
+    batch, beam = (logits[2][i] if logits[0][i] > 1 else V for i in range(2))
+    if batch == 0 and beam == 0:
+        raise FavorError(1, "logits is one row broadcast to all")
+    g = make_beam_desc(B, K, V, n, _dtype_code(logits[1]), batch, beam, end_token)
+    _check(validate_beam_desc(g))
+    return _Planned(g, beam_workspace_size(g))
+
+
+@_on_stream
+def beam_select(logits, scores, n=None, ended=None, end_token=-1, out_scores=None, parent=None,
+                token=None, workspace=None, stream=None):
+    """The best n (default K) continuations of each entry's K beams (favor_beam_select) by
+    scores[b, k] + log_softmax(logits[b, k])[v].
+
+    logits [B, K, V] (bfloat16 or float32, V contiguous, any other strides and alignment),
+    scores [B, K] float32. ended [B, K] (bool or uint8): beams that stay as they are, with
+    end_token. Ties go to the lower beam and token. Returns (scores [B, n] float32 in falling
+    order, parent [B, n] int32, token [B, n] int32); where fewer can be chosen the rest has
+    the score -inf, parent 0 and end_token (0 without one).
+    """
+    torch = _torch()
+    if n is None:
+        n = logits.shape[1] if logits.dim() == 3 else 1
+    n = operator.index(n)
+    if logits.dim() == 3:
+        shape, dev = (logits.shape[0], max(n, 0)), logits.device
+        if out_scores is None:
+            out_scores = torch.empty(shape, dtype=torch.float32, device=dev)
+        if parent is None:
+            parent = torch.empty(shape, dtype=torch.int32, device=dev)
+        if token is None:
+            token = torch.empty(shape, dtype=torch.int32, device=dev)
+    c = _beam_plan(_like(logits), _like(scores), _like(ended),
+                   (("out_scores", _like(out_scores)), ("parent", _like(parent)),
+                    ("token", _like(token))), n, operator.index(end_token))
+    here = _require_here(logits, scores, ended, out_scores, parent, token)
+    _require_whole(scores, ended, out_scores, parent, token)
+    ws, nbytes = _decay_workspace(c.workspace, workspace)
+    _check(lib().favor_beam_select(c.ref, _ptr(logits), _ptr(scores), _ptr(ended),
+                                   _ptr(out_scores), _ptr(parent), _ptr(token), _ptr(ws), nbytes,
+                                   _stream_on(here, stream)))
+    return out_scores, parent, token
+
+
+@_on_stream
+def beam_reorder(parent, slots, pools, new_slots=None, stream=None):
+    """Moves the states of pools behind chosen beams, in place (favor_beam_reorder): beam j of
+    entry b continues beam parent[b, j], whose state is at slots[b, parent[b, j]] of every pool
+    (slots None: b K + the beam). A beam's first child keeps its place, the others get copies
+    in the places of beams without children.
+
+    parent, slots [B, K] int32 (the valid places all different), pools: contiguous tensors
+    [n, ...] whose entries are multiples of 16 bytes, such as the states of attn_decay_step,
+    causal_conv_step and selective_scan_step. Returns the new slots [B, K].
+    """
+    torch = _torch()
+    if parent.dim() != 2:
+        raise FavorError(1, f"parent must be [B, K], got {tuple(parent.shape)}")
+    if new_slots is None:
+        new_slots = torch.empty_like(parent, memory_format=torch.contiguous_format)
+    for name, t in (("parent", parent), ("slots", slots), ("new_slots", new_slots)):
+        _require_like(t, parent.shape, torch.int32, name)
+    here = _require_here(parent, slots, new_slots, *pools)
+    _require_whole(parent, slots, new_slots)
+    table = (FavorBeamPool * len(pools))()
+    for row, p in zip(table, pools):
+        if p.dim() < 1 or not p.is_contiguous():
+            raise FavorError(1, "pools must be contiguous tensors [n, ...]")
+        n = p.shape[0]
+        row.data, row.n_slots = p.data_ptr(), n
+        row.bytes_per_slot = p.numel() // n * p.element_size() if n else 0
+    _check(lib().favor_beam_reorder(parent.shape[0], parent.shape[1], _ptr(parent), _ptr(slots),
+                                    _ptr(new_slots), table, len(pools), _stream_on(here, stream)))
+    return new_slots

@@ -59,6 +59,38 @@ class FavorDecayDesc(ctypes.Structure):
     ]
 
 
+class FavorConvDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("L", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("width", ctypes.c_int32), ("dtype", ctypes.c_int), ("silu", ctypes.c_int32),
+        ("x", FavorStrides), ("y", FavorStrides), ("grad_y", FavorStrides),
+        ("grad_x", FavorStrides),
+    ]
+
+
+class FavorScanDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("L", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("N", ctypes.c_int32), ("groups", ctypes.c_int32), ("dtype", ctypes.c_int),
+        ("softplus", ctypes.c_int32),
+        *((n, FavorStrides) for n in ("x", "dt", "b", "c", "z", "y", "grad_y", "grad_x",
+                                      "grad_dt", "grad_b", "grad_c", "grad_z")),
+    ]
+
+
+class FavorBeamDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("K", ctypes.c_int32), ("V", ctypes.c_int32),
+        ("n", ctypes.c_int32), ("dtype", ctypes.c_int), ("batch_stride", ctypes.c_int64),
+        ("beam_stride", ctypes.c_int64), ("end_token", ctypes.c_int32),
+    ]
+
+
+class FavorBeamPool(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("bytes_per_slot", ctypes.c_int64),
+                ("n_slots", ctypes.c_int32)]
+
+
 def lib_path():
     return os.environ.get("FAVOR_LIBRARY", os.path.join(_HERE, "libfavor.so"))
 
@@ -76,6 +108,7 @@ def lib():
     vp, i32, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
     dp = ctypes.POINTER(FavorDesc)
     ddp, i64 = ctypes.POINTER(FavorDecayDesc), ctypes.c_int64
+    cdp, sdp, bdp = (ctypes.POINTER(d) for d in (FavorConvDesc, FavorScanDesc, FavorBeamDesc))
     sig = {
         "favor_orf_draw": (ctypes.c_int, [u64, i32, i32, i32, ctypes.c_int, vp, vp, vp]),
         "favor_feature_map": (ctypes.c_int, [dp, vp, vp, vp, vp, vp]),
@@ -112,6 +145,21 @@ def lib():
         "favor_validate_decay_desc": (ctypes.c_int, [ddp, ctypes.c_int]),
         "favor_dropout": (ctypes.c_int, [vp, vp, vp, i64, ctypes.c_int, ctypes.c_double, u64, u64,
                                          vp, vp]),
+        "favor_conv": (ctypes.c_int, [cdp, *[vp] * 8]),
+        "favor_conv_backward": (ctypes.c_int, [cdp, *[vp] * 12, sz, vp]),
+        "favor_conv_workspace_size": (sz, [cdp]),
+        "favor_conv_step": (ctypes.c_int, [cdp, vp, vp, vp, vp, i32, vp, vp, vp]),
+        "favor_validate_conv_desc": (ctypes.c_int, [cdp, ctypes.c_int]),
+        "favor_scan_workspace_size": (sz, [sdp, ctypes.c_int]),
+        "favor_selective_scan": (ctypes.c_int, [sdp, *[vp] * 13, sz, vp]),
+        "favor_selective_scan_backward": (ctypes.c_int, [sdp, *[vp] * 22, sz, vp]),
+        "favor_selective_scan_step": (ctypes.c_int, [sdp, *[vp] * 9, i32, vp, vp, vp]),
+        "favor_validate_scan_desc": (ctypes.c_int, [sdp, ctypes.c_int]),
+        "favor_beam_workspace_size": (sz, [bdp]),
+        "favor_validate_beam_desc": (ctypes.c_int, [bdp]),
+        "favor_beam_select": (ctypes.c_int, [bdp, *[vp] * 7, sz, vp]),
+        "favor_beam_reorder": (ctypes.c_int, [i32, i32, vp, vp, vp,
+                                              ctypes.POINTER(FavorBeamPool), i32, vp]),
         "favor_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "favor_last_error": (ctypes.c_char_p, []),
         "favor_abi_version": (i32, []),
@@ -175,6 +223,56 @@ def validate_decay_desc(g, op):
 
 def decay_workspace_size(g, backward=False):
     return lib().favor_decay_workspace_size(ctypes.byref(g), 1 if backward else 0)
+
+
+def _strided(g, strides):
+    for name, s in strides.items():
+        setattr(g, name, FavorStrides(*s))
+    return g
+
+
+def make_conv_desc(B, L, D, width, dtype, silu=False, **strides):
+    """Descriptor of the short convolution; strides: (batch, unused, token) element strides by
+    field (x, y, grad_y, grad_x), those not given contiguous."""
+    return _strided(FavorConvDesc(B, L, D, width, dtype, 1 if silu else 0), strides)
+
+
+def make_scan_desc(B, L, D, N, dtype, groups=1, softplus=True, **strides):
+    """Descriptor of the selective scan; strides: (batch, group, token) element strides by
+    field (x, dt, b, c, z, y and grad_y, grad_x, grad_dt, grad_b, grad_c, grad_z; the group's
+    is read for b and c only), those not given contiguous."""
+    return _strided(FavorScanDesc(B, L, D, N, groups, dtype, 1 if softplus else 0), strides)
+
+
+def make_beam_desc(B, K, V, n, dtype, batch_stride=0, beam_stride=0, end_token=-1):
+    """Descriptor of the beam selection; strides in elements, both 0: contiguous."""
+    return FavorBeamDesc(B, K, V, n, dtype, batch_stride, beam_stride, end_token)
+
+
+def validate_conv_desc(g, op):
+    """op: 0 forward, 1 backward, 2 single tokens."""
+    return lib().favor_validate_conv_desc(ctypes.byref(g), op)
+
+
+def validate_scan_desc(g, op):
+    """op: 0 forward, 1 backward, 2 single tokens."""
+    return lib().favor_validate_scan_desc(ctypes.byref(g), op)
+
+
+def validate_beam_desc(g):
+    return lib().favor_validate_beam_desc(ctypes.byref(g))
+
+
+def conv_workspace_size(g):
+    return lib().favor_conv_workspace_size(ctypes.byref(g))
+
+
+def scan_workspace_size(g, backward=False):
+    return lib().favor_scan_workspace_size(ctypes.byref(g), 1 if backward else 0)
+
+
+def beam_workspace_size(g):
+    return lib().favor_beam_workspace_size(ctypes.byref(g))
 
 
 def backward_workspace_size(g, causal):

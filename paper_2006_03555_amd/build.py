@@ -21,7 +21,9 @@ ARCH = "gfx950"
 
 SOURCES = ["orf_draw.hip", "feature_map.hip", "bidir.hip", "causal.hip", "backward.hip",
            "feature_scan.hip", "backward_f32.hip", "noalloc.hip", "probe.hip", "favor_api.cpp", "timing.cpp",
-           "decay.hip", "decay_step.hip", "dropout.hip", "decay_api.cpp"]
+           "decay.hip", "decay_step.hip", "dropout.hip", "decay_api.cpp",
+           "conv.hip", "scan.hip", "scan_backward.hip", "scan_step.hip", "beam.hip",
+           "recurrent_api.cpp"]
 
 # Packed fp32 arithmetic is disabled for all device code (no v_pk_*_f32).
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

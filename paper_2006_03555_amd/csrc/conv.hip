@@ -1,0 +1,376 @@
+// conv.hip - short causal convolution, one filter of `width` taps per channel, with an
+// optional bias and SiLU:
+//
+//   u_t = bias + sum_j w[j] x_{t - W + 1 + j},   y_t = u_t or u_t sigmoid(u_t)
+//   g_t = dy_t (dy/du)(u_t),  dx_t = sum_j w[j] g_{t + W - 1 - j},
+//   dw[j] = sum_t g_t x_{t - W + 1 + j},  dbias = sum_t g_t
+//
+// Bound by the bytes: an input is read once and an output written once, with 2 W operations
+// between them. A thread owns 16 bytes of neighbouring channels and a run of tokens, so the
+// window of the last W - 1 inputs moves through its registers, and only the run's W - 1 first
+// inputs are read twice. Everything is fp32 between load and store.
+#include "recurrent.hpp"
+#include "vec_rows.hpp"
+
+namespace favor {
+namespace {
+
+constexpr int kConvThreads = 256;
+constexpr int kAhead = 4;   // rows in flight
+
+// Token t of one sequence: x for t >= 0, the carried inputs before it.
+template <typename T, int V>
+__device__ __forceinline__ void input_row(RowVec<T, V> &r, const T *x, int64_t stride,
+                                          const T *state, int64_t D, int W, int t, int n) {
+  if (t >= n) r.zero();
+  else if (t >= 0) r.load(x + t * stride);
+  else if (state) r.load(state + (W - 1 + t) * D);
+  else r.zero();
+}
+
+template <typename T, int W, int V>
+__global__ __launch_bounds__(kConvThreads) void k_conv(Conv a) {
+  const int units = a.D / V;
+  const int64_t id = (int64_t)blockIdx.x * kConvThreads + threadIdx.x;
+  const int run = (int)(id / units), unit = (int)(id - (int64_t)run * units);
+  const int t0 = run * a.run, b = blockIdx.y;
+  if (t0 >= max(a.L, 1)) return;
+  const int c = unit * V;
+  const int n = clamped_length(a.lengths, b, a.L);
+  const T *x = static_cast<const T *>(a.x) + b * a.xs.b + c;
+  T *y = static_cast<T *>(a.y) + b * a.ys.b + c;
+  const T *state =
+      a.state_in ? static_cast<const T *>(a.state_in) + (int64_t)b * (W - 1) * a.D + c : nullptr;
+  float w[V][W], bias[V], win[W - 1][V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[i][j] = a.w[(int64_t)(c + i) * W + j];
+    bias[i] = a.bias ? a.bias[c + i] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < W - 1; ++i) {
+    RowVec<T, V> r;
+    input_row<T, V>(r, x, a.xs.t, state, a.D, W, t0 - (W - 1) + i, n);
+    r.get(win[i]);
+  }
+  if (run == 0 && a.state_out) {
+    // the inputs after the last token; all are read before the first is written, since
+    // state_out may be state_in (whose readers are all in run 0: a run has W - 1 tokens)
+    RowVec<T, V> r[W - 1];
+    T *so = static_cast<T *>(a.state_out) + (int64_t)b * (W - 1) * a.D + c;
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i)
+      input_row<T, V>(r[i], x, a.xs.t, state, a.D, W, n - (W - 1) + i, n);
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {
+      float v[V];
+      r[i].get(v);
+      store_row<V>(so + (int64_t)i * a.D, v);
+    }
+  }
+  const int t1 = min(t0 + a.run, a.L);
+  for (int t = t0; t < t1; t += kAhead) {
+    RowVec<T, V> r[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (t + i < min(n, t1)) r[i].load(x + (t + i) * a.xs.t);
+      else r[i].zero();
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (t + i >= t1) break;
+      float v[V], u[V];
+      r[i].get(v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        u[k] = bias[k];
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) u[k] = fmaf(w[k][j], win[j][k], u[k]);
+        u[k] = fmaf(w[k][W - 1], v[k], u[k]);
+        if (a.silu) u[k] *= sigmoid(u[k]);
+        if (t + i >= n) u[k] = 0.f;
+      }
+      store_row<V>(y + (t + i) * a.ys.t, u);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) win[j][k] = win[j + 1][k];
+        win[W - 2][k] = v[k];
+      }
+    }
+  }
+}
+
+// A workgroup takes `units_wide` neighbouring units by 256 / units_wide runs, and sums the
+// filters' gradients of its runs in LDS.
+constexpr int kBackWide = 16;
+template <typename T> constexpr int back_vec(int W) {
+  return sizeof(T) == 2 && W <= 4 ? 8 : 4;   // more taps of more channels spill
+}
+constexpr int kBackRun = 32;
+
+template <typename T, int W, int V>
+__global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide, int tiles) {
+  __shared__ float sums[(W + 1) * V][kConvThreads + 1];
+  const int units = a.D / V, tid = threadIdx.x;
+  const int tile = blockIdx.x % tiles, block = blockIdx.x / tiles;
+  const int unit = tile * wide + tid % wide;
+  const int high = kConvThreads / wide;
+  const int b = blockIdx.y;
+  const int run = block * high + tid / wide;
+  const int64_t t0w = (int64_t)run * kBackRun;
+  const bool live = unit < units && t0w < max(a.L, 1);
+  float dw[W][V], db[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    db[k] = 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) dw[j][k] = 0.f;
+  }
+  if (live) {
+    const int t0 = (int)t0w, c = unit * V;
+    const int n = clamped_length(a.lengths, b, a.L);
+    const T *x = static_cast<const T *>(a.x) + b * a.xs.b + c;
+    const T *dy = static_cast<const T *>(a.dy) + b * a.dys.b + c;
+    T *dx = static_cast<T *>(a.dx) + b * a.dxs.b + c;
+    const int64_t at_state = (int64_t)b * (W - 1) * a.D + c;
+    const T *state = a.state_in ? static_cast<const T *>(a.state_in) + at_state : nullptr;
+    const T *dso = a.dstate_out ? static_cast<const T *>(a.dstate_out) + at_state : nullptr;
+    T *dsi = a.dstate_in ? static_cast<T *>(a.dstate_in) + at_state : nullptr;
+    float w[W][V], bias[V], win[W][V], g[W][V];   // g[j]: of token t - W + 1 + j
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        w[j][k] = a.w[(int64_t)(c + k) * W + j];
+        g[j][k] = 0.f;
+      }
+      bias[k] = a.bias ? a.bias[c + k] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {
+      RowVec<T, V> r;
+      input_row<T, V>(r, x, a.xs.t, state, a.D, W, t0 - (W - 1) + i, n);
+      r.get(win[i + 1]);
+    }
+    // dx of token s needs g up to s + W - 1: the run's last tokens read W - 1 rows past it
+    const int end = min(t0 + kBackRun, a.L) + W - 1;
+    for (int t = t0; t < end; t += kAhead) {
+      RowVec<T, V> rx[kAhead], rd[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (t + i < min(n, end)) {
+          rx[i].load(x + (t + i) * a.xs.t);
+          rd[i].load(dy + (t + i) * a.dys.t);
+        } else {
+          rx[i].zero();
+          rd[i].zero();
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int tt = t + i;
+        if (tt >= end) break;
+        float d[V], o[V];
+        rd[i].get(d);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+#pragma unroll
+          for (int j = 0; j < W - 1; ++j) {
+            win[j][k] = win[j + 1][k];
+            g[j][k] = g[j + 1][k];
+          }
+        }
+        rx[i].get(win[W - 1]);
+        const bool inside = tt < n, own = inside && tt < t0 + kBackRun;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          if (a.silu) {
+            float u = bias[k];
+#pragma unroll
+            for (int j = 0; j < W; ++j) u = fmaf(w[j][k], win[j][k], u);
+            const float s = sigmoid(u);
+            d[k] *= s * fmaf(u, 1.f - s, 1.f);
+          }
+          g[W - 1][k] = inside ? d[k] : 0.f;
+          if (own) {
+            db[k] += d[k];
+#pragma unroll
+            for (int j = 0; j < W; ++j) dw[j][k] = fmaf(d[k], win[j][k], dw[j][k]);
+          }
+          o[k] = 0.f;
+#pragma unroll
+          for (int j = 0; j < W; ++j) o[k] = fmaf(w[W - 1 - j][k], g[j][k], o[k]);
+        }
+        const int s = tt - (W - 1);   // dx of this token is complete
+        if (s < t0 && (run > 0 || !dsi)) continue;
+        if (dso && s < n && s >= n - (W - 1)) {
+          RowVec<T, V> r;
+          float v[V];
+          r.load(dso + (int64_t)(s - n + W - 1) * a.D);
+          r.get(v);
+#pragma unroll
+          for (int k = 0; k < V; ++k) o[k] += v[k];
+        }
+        if (s >= 0) {
+          if (s >= n) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) o[k] = 0.f;
+          }
+          store_row<V>(dx + s * a.dxs.t, o);
+        } else {
+          store_row<V>(dsi + (int64_t)(s + W - 1) * a.D, o);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) sums[j * V + k][tid] = dw[j][k];
+    sums[W * V + k][tid] = db[k];
+  }
+  __syncthreads();
+  const int64_t row = (int64_t)b * (gridDim.x / tiles) + block;
+  for (int i = tid; i < wide * (W + 1) * V; i += kConvThreads) {
+    const int j = i / (wide * V), ck = i - j * wide * V;   // tap, channel of the tile
+    const int u = ck / V, k = ck - u * V;
+    const int c = (tile * wide + u) * V + k;
+    if (c >= a.D) continue;
+    float s = 0.f;
+    for (int r = 0; r < high; ++r) s += sums[j * V + k][r * wide + u];
+    a.part[(row * (W + 1) + j) * a.D + c] = s;
+  }
+}
+
+// Sums of part's rows: 64 columns by 16 row lanes of a workgroup, joined in a fixed order.
+constexpr int kSumCols = 64, kSumLanes = 16;
+__global__ __launch_bounds__(kSumCols *kSumLanes) void k_conv_sums(Conv a, int rows) {
+  __shared__ float part[kSumLanes][kSumCols];
+  const int64_t cols = (int64_t)(a.width + 1) * a.D;
+  const int64_t col = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
+  const int lane = threadIdx.x / kSumCols;
+  float s = 0.f;
+  if (col < cols)
+#pragma unroll 8
+    for (int r = lane; r < rows; r += kSumLanes) s += a.part[r * cols + col];
+  part[lane][threadIdx.x % kSumCols] = s;
+  __syncthreads();
+  if (lane || col >= cols) return;
+  for (int i = 1; i < kSumLanes; ++i) s += part[i][threadIdx.x];
+  const int j = (int)(col / a.D), c = (int)(col - (int64_t)j * a.D);
+  if (j < a.width) a.dw[(int64_t)c * a.width + j] = s;
+  else if (a.dbias) a.dbias[c] = s;
+}
+
+// One token of B sequences, the last inputs in a pool: bound by the launch and one round of
+// loads. A thread owns four channels of one sequence.
+template <typename T>
+__global__ __launch_bounds__(kConvThreads) void k_conv_step(Conv a) {
+  __shared__ int next;
+  constexpr int V = 4;
+  const int W = a.width, c = (blockIdx.x * kConvThreads + threadIdx.x) * V;
+  const int first = blockIdx.y;
+  for (int b = first; b < a.B;) {
+    int slot = b, after = a.B;
+    if (a.slots) {
+      slot = a.slots[b];
+      if (slot >= 0 && slot < a.n_slots) {
+        after = next_turn<kConvThreads>(a.slots, a.B, b, first, slot, &next);
+        if (after < 0) return;
+      }
+    }
+    const bool live = slot >= 0 && slot < a.n_slots;   // others have no state: y = 0
+    if (c < a.D) {
+      float u[V] = {0.f, 0.f, 0.f, 0.f}, v[V];
+      if (live) {
+        T *state = static_cast<T *>(a.state_out) + (int64_t)slot * (W - 1) * a.D + c;
+        RowVec<T, V> r, rx;
+        rx.load(static_cast<const T *>(a.x) + b * a.xs.b + c);
+        if (a.bias)
+#pragma unroll
+          for (int k = 0; k < V; ++k) u[k] = a.bias[c + k];
+        for (int j = 0; j < W; ++j) {
+          if (j < W - 1) r.load(state + (int64_t)j * a.D);
+          else r = rx;
+          r.get(v);
+#pragma unroll
+          for (int k = 0; k < V; ++k) u[k] = fmaf(a.w[(int64_t)(c + k) * W + j], v[k], u[k]);
+          if (j > 0) store_row<V>(state + (int64_t)(j - 1) * a.D, v);
+        }
+        if (a.silu)
+#pragma unroll
+          for (int k = 0; k < V; ++k) u[k] *= sigmoid(u[k]);
+      }
+      store_row<V>(static_cast<T *>(a.y) + b * a.ys.b + c, u);
+    }
+    b = after;
+  }
+}
+
+template <typename T, int W>
+hipError_t launch_w(const Conv &a, hipStream_t st) {
+  constexpr int V = 16 / sizeof(T);
+  const int64_t runs = a.L > 0 ? (a.L + a.run - 1) / a.run : 1;
+  const int64_t threads = runs * (a.D / V);
+  const dim3 grid((unsigned)((threads + kConvThreads - 1) / kConvThreads), a.B);
+  k_conv<T, W, V><<<grid, kConvThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+int back_units_wide(int units) {
+  int wide = 1;
+  while (wide < kBackWide && wide < units) wide *= 2;
+  return wide;
+}
+
+template <typename T, int W>
+hipError_t launch_back_w(const Conv &a, hipStream_t st) {
+  constexpr int V = back_vec<T>(W);
+  const int units = a.D / V, wide = back_units_wide(units);
+  const int tiles = (units + wide - 1) / wide;
+  const int blocks = conv_part_rows(1, a.L, a.D, W, sizeof(T) == 2 ? Dt::BF16 : Dt::F32);
+  k_conv_backward<T, W, V><<<dim3(tiles * blocks, a.B), kConvThreads, 0, st>>>(a, wide, tiles);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int conv_part_rows(int B, int L, int D, int width, Dt dt) {
+  const int V = dt == Dt::BF16 ? back_vec<bf16>(width) : back_vec<float>(width);
+  const int tokens = kBackRun * (kConvThreads / back_units_wide(D / V));
+  return B * (L > 0 ? (L + tokens - 1) / tokens : 1);
+}
+
+#define FAVOR_BY_WIDTH(fn)                                           \
+  switch (a.width) {                                                 \
+    case 2: return dt == Dt::BF16 ? fn<bf16, 2>(a, st) : fn<float, 2>(a, st); \
+    case 3: return dt == Dt::BF16 ? fn<bf16, 3>(a, st) : fn<float, 3>(a, st); \
+    case 4: return dt == Dt::BF16 ? fn<bf16, 4>(a, st) : fn<float, 4>(a, st); \
+    case 5: return dt == Dt::BF16 ? fn<bf16, 5>(a, st) : fn<float, 5>(a, st); \
+    case 6: return dt == Dt::BF16 ? fn<bf16, 6>(a, st) : fn<float, 6>(a, st); \
+    case 7: return dt == Dt::BF16 ? fn<bf16, 7>(a, st) : fn<float, 7>(a, st); \
+    case 8: return dt == Dt::BF16 ? fn<bf16, 8>(a, st) : fn<float, 8>(a, st); \
+  }                                                                  \
+  return hipErrorInvalidValue;
+
+hipError_t launch_conv(const Conv &a, Dt dt, hipStream_t st) { FAVOR_BY_WIDTH(launch_w) }
+hipError_t launch_conv_backward(const Conv &a, Dt dt, hipStream_t st) {
+  FAVOR_BY_WIDTH(launch_back_w)
+}
+
+hipError_t launch_conv_sums(const Conv &a, int rows, hipStream_t st) {
+  const int64_t cols = (int64_t)(a.width + 1) * a.D;
+  k_conv_sums<<<(unsigned)((cols + kSumCols - 1) / kSumCols), kSumCols * kSumLanes, 0, st>>>(a, rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_conv_step(const Conv &a, Dt dt, hipStream_t st) {
+  const dim3 grid((a.D / 4 + kConvThreads - 1) / kConvThreads, a.B);
+  if (dt == Dt::BF16) k_conv_step<bf16><<<grid, kConvThreads, 0, st>>>(a);
+  else k_conv_step<float><<<grid, kConvThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace favor

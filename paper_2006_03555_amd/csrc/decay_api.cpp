@@ -5,75 +5,22 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
-#include <cstring>
 
 #include "../../include/favor.h"
 #include "decay.hpp"
+#include "host_checks.hpp"
 
 namespace {
 
 using favor::DecayScan;
 using favor::Rows;
 
-favor_status fail(favor_status st, const char *fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  return favor::report(st, buf);
-}
-favor_status ok() { return favor::report(FAVOR_OK, ""); }
+using namespace favor::host;
 
-#define FAVOR_TRY(expr)                \
-  do {                                 \
-    favor_status st__ = (expr);        \
-    if (st__ != FAVOR_OK) return st__; \
-  } while (0)
-
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-// The integer in an enum-typed field (a C caller may store any int there).
-int raw_enum(const void *p) {
-  int v;
-  std::memcpy(&v, p, sizeof v);
-  return v;
-}
-
-favor_status check_ptr(const void *p, const char *name, bool needed, size_t align = 16) {
-  if (!needed) return FAVOR_OK;
-  if (!p) return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s is NULL", name);
-  if (!aligned(p, align))
-    return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s is not %zu-byte aligned", name, align);
-  return FAVOR_OK;
-}
-favor_status check_optional(const void *p, const char *name, size_t align = 16) {
-  return check_ptr(p, name, p != nullptr, align);
-}
-
-// An output that is written while an input of the same size is read: the two may be one
-// where `same` says so (each element is then read first), and must not overlap otherwise.
-favor_status check_apart(const void *out, const char *name, const void *in, const char *other,
-                         int64_t bytes, bool same) {
-  if (!out || !in || (out == in && same)) return FAVOR_OK;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(out), b = reinterpret_cast<uintptr_t>(in);
-  if ((a > b ? a - b : b - a) >= (uint64_t)bytes) return FAVOR_OK;
-  return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s overlaps %s", name, other);
-}
 int64_t state_bytes(const favor_decay_desc *g) {
   return (int64_t)sizeof(float) * g->B * g->H * g->dk * g->dv;
 }
 
-favor_status device_result(hipError_t e, const char *what) {
-  if (e != hipSuccess) return fail(FAVOR_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
-  return ok();
-}
-
-constexpr int kMaxL = 1 << 30;
-constexpr int64_t kMaxStride = (int64_t)1 << 46;   // element offsets stay within 64 bits
 // the kernels reach a chunk's 64 rows by 32-bit offsets
 constexpr int64_t kMaxTokenBytes = 1 << 25;
 enum Op { kOpForward = 0, kOpBackward = 1, kOpStep = 2 };
@@ -85,38 +32,10 @@ struct Tensor {
   bool out;
 };
 
-// Strides of one tensor; dimensions of size 1 or less have none.
 favor_status check_strides(const favor_decay_desc *g, const Tensor &t, int op) {
   const int64_t size[3] = {g->B, g->H, op == kOpStep ? 1 : g->L};
-  const int64_t stride[3] = {t.s->batch, t.s->head, t.s->token};
   const int unit = raw_enum(&g->dtype) == FAVOR_BF16 ? 8 : 4;
-  if (!stride[0] && !stride[1] && !stride[2]) return FAVOR_OK;   // contiguous
-  int64_t reach = 0;
-  for (int i = 0; i < 3; ++i) {
-    if (size[i] <= 1) continue;
-    if (stride[i] < 0)
-      return fail(FAVOR_ERR_INVALID_ARGUMENT, "a stride of %s is negative", t.name);
-    if (stride[i] % unit != 0)
-      return fail(FAVOR_ERR_INVALID_ARGUMENT,
-                  "strides of %s must be multiples of 16 bytes (%d elements)", t.name, unit);
-    if (i == 2 && stride[i] > kMaxTokenBytes / (16 / unit))
-      return fail(FAVOR_ERR_UNSUPPORTED, "the token stride of %s exceeds 2^25 bytes", t.name);
-    if (stride[i] > kMaxStride / (size[i] - 1) || (reach += stride[i] * (size[i] - 1)) > kMaxStride)
-      return fail(FAVOR_ERR_UNSUPPORTED, "%s reaches past 2^46 elements", t.name);
-  }
-  if (!t.out) return FAVOR_OK;
-  // rows written must not share elements: taken by stride, each dimension steps over
-  // everything inside it
-  int at[3] = {0, 1, 2};
-  std::sort(at, at + 3, [&](int i, int j) { return stride[i] < stride[j]; });
-  int64_t inner = t.d;
-  for (int i : at) {
-    if (size[i] <= 1) continue;
-    if (stride[i] < inner)
-      return fail(FAVOR_ERR_INVALID_ARGUMENT, "rows of %s overlap", t.name);
-    inner += stride[i] * (size[i] - 1);
-  }
-  return FAVOR_OK;
+  return check_rows(t.name, *t.s, size, t.d, unit, kMaxTokenBytes / (16 / unit), t.out);
 }
 
 favor_status validate(const favor_decay_desc *g, int op) {
@@ -217,16 +136,6 @@ size_t part_floats(const favor_decay_desc *g, int nseg) {
 size_t workspace_of(const favor_decay_desc *g, int op) {
   if ((long long)g->B * g->H == 0 || g->L == 0) return 0;
   return round_up(part_floats(g, cut_of(g, g->dk, g->dv, op == kOpBackward ? kBackwardScans : 1).nseg) * sizeof(float) * (op == kOpBackward ? 2 : 1), 256);
-}
-
-favor_status check_workspace(const void *ws, size_t bytes, size_t need) {
-  if (need == 0) return FAVOR_OK;
-  if (!ws) return fail(FAVOR_ERR_INVALID_ARGUMENT, "workspace is NULL");
-  if (!aligned(ws, 256))
-    return fail(FAVOR_ERR_INVALID_ARGUMENT, "workspace is not 256-byte aligned");
-  if (bytes < need)
-    return fail(FAVOR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu bytes, need %zu", bytes, need);
-  return FAVOR_OK;
 }
 
 // A scan of g: kd, vd (exchanged on the transposed state), its segments and the arguments

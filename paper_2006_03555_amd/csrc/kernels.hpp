@@ -199,6 +199,18 @@ enum KernelId {
   kKerDecayScan,
   kKerDecayStep,
   kKerDropout,
+  kKerConv,
+  kKerConvBwd,
+  kKerConvStep,
+  kKerScanSums,
+  kKerScanPrefix,
+  kKerScan,
+  kKerScanBwd,
+  kKerScanStep,
+  kKerColumnSums,
+  kKerBeamPieces,
+  kKerBeamMerge,
+  kKerBeamReorder,
   kNumKernels
 };
 const char *kernel_name(int k);

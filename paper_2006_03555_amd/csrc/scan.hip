@@ -1,0 +1,233 @@
+// scan.hip - selective state space scan over a sequence, forward: per channel d and state n
+//
+//   s_t = softplus(dt_t + bias_d),  h_t = exp(s_t A_dn) h_{t-1} + s_t x_t B_t[n],
+//   y_t = (sum_n C_t[n] h_t[n] + skip_d x_t) silu(z_t)
+//
+// Bound by the vector unit: each (token, channel, state) takes a product and an exponential
+// (two issue slots), the input's product, the recurrence once inside the lane and once from
+// its true state, and the output's sum; B and C are read from LDS for two channels at a time.
+// Nothing of size tokens x channels x states leaves the registers.
+#include "scan_common.hpp"
+
+namespace favor {
+namespace {
+
+// Channels per lane: a workgroup's 8 waves take 32 * kCh channels.
+template <int kCh> constexpr int kWide = 4 * kScanWaves * kCh;
+
+// One (chunk, n) step of kCh channels: a = 2^(s A), S and P of the lane, the row's scan.
+// kOut: y += C h; h of the row's last lane goes back to `carry`.
+template <int kCh, bool kOut>
+__device__ __forceinline__ void forward_state(const float (&s)[kCh][8], const float (&sx)[kCh][8],
+                                              const float (&ssum)[kCh], const float *Bv,
+                                              const float *Cv, const float *A2, float *carry,
+                                              int tl, float (&y)[kCh][8]) {
+  float a[kCh][8], bx[kCh][8], S[kCh], P[kCh], h[kCh];
+#pragma unroll
+  for (int i = 0; i < kCh; ++i) {
+    const float A = A2[4 * i];
+    h[i] = carry[4 * i];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      a[i][j] = exp2_hw(s[i][j] * A);
+      bx[i][j] = sx[i][j] * Bv[j];
+    }
+    S[i] = tl == 0 ? h[i] : 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) S[i] = fmaf(a[i][j], S[i], bx[i][j]);
+    P[i] = exp2_hw(ssum[i] * A);
+  }
+  if constexpr (kCh == 2) row_scan2<false>(S[0], P[0], h[0], S[1], P[1], h[1]);
+  else row_scan<false>(S[0], P[0], h[0]);
+#pragma unroll
+  for (int i = 0; i < kCh; ++i) {
+    if constexpr (kOut) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[i] = fmaf(a[i][j], h[i], bx[i][j]);
+        y[i][j] = fmaf(Cv[j], h[i], y[i][j]);
+      }
+    }
+    if (tl == 15) carry[4 * i] = S[i];
+  }
+}
+
+// kOut: the rows y and the state after the last token. Otherwise the sums of the segments.
+template <typename T, int kCh, bool kOut>
+__global__ __launch_bounds__(kScanThreads) void k_scan(Scan a) {
+  constexpr int W = kWide<kCh>;
+  extern __shared__ __align__(16) float lds[];
+  float *ts = lds, *tb = ts + W * kTok, *tc = tb + kStates * kTok;
+  float *tA = tc + (kOut ? kStates * kTok : 0), *th = tA + a.N * W;
+  T *tx = reinterpret_cast<T *>(th + a.N * W);
+  const ScanPlace p = scan_place(a, W);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
+  const int cl = 4 * kCh * wave + lane / 16;   // this lane's first channel; the next is 4 on
+  const int64_t DN = (int64_t)a.D * a.N, at_part = ((int64_t)p.b * a.nseg + p.seg) * DN;
+  load_channels<W>(a.A, p, a.N, 0, a.N, kLog2e, tA);
+  const float *h0 = nullptr;
+  if (kOut && a.nseg > 1) h0 = a.part + at_part;
+  else if (kOut && a.h_in) h0 = a.h_in + p.b * DN;
+  load_channels<W>(h0, p, a.N, 0, a.N, 1.f, th);
+  float seg_steps[kCh] = {};
+  const int first = p.seg * a.chunks, last = min(first + a.chunks, (a.L + kTok - 1) / kTok);
+  for (int chunk = first; chunk < last; ++chunk) {
+    const int64_t t0 = (int64_t)chunk * kTok;
+    const bool some = t0 < p.n;
+    if (!some && !kOut) break;
+    __syncthreads();   // the last chunk's rows have been read
+    if (some) {
+      load_steps<T, W>(a, p, t0, ts, tx);
+      float s[kCh][8], sx[kCh][8], ssum[kCh], y[kCh][8];
+      for (int n0 = 0; n0 < a.N; n0 += kStates) {
+        const int count = min(kStates, a.N - n0);
+        if (n0) __syncthreads();   // the last states' B and C have been read
+        load_states<T>(a.b, a.bs, p, t0, n0, count, tb);
+        if (kOut) load_states<T>(a.c, a.cs, p, t0, n0, count, tc);
+        __syncthreads();
+        if (n0 == 0) {
+#pragma unroll
+          for (int i = 0; i < kCh; ++i) {
+            lane_tokens(ts, cl + 4 * i, tl, s[i]);
+            lane_tokens(tx, cl + 4 * i, tl, sx[i]);
+            ssum[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              sx[i][j] *= s[i][j];
+              ssum[i] += s[i][j];
+              y[i][j] = 0.f;
+            }
+            if (!kOut) seg_steps[i] += ssum[i];
+          }
+        }
+        for (int n = 0; n < count; ++n) {
+          float Bv[8], Cv[8];
+          load8(tb + n * kTok + 8 * tl, Bv);
+          if (kOut) load8(tc + n * kTok + 8 * tl, Cv);
+          const int at = (n0 + n) * W + cl;
+          forward_state<kCh, kOut>(s, sx, ssum, Bv, Cv, tA + at, th + at, tl, y);
+        }
+      }
+      if (kOut) {
+#pragma unroll
+        for (int i = 0; i < kCh; ++i)   // in place of the lane's own steps
+          store8_lds(ts + tile_at<float>(cl + 4 * i, kLaneTok * tl), y[i]);
+        __syncthreads();
+      }
+    }
+    if (!kOut) continue;
+    constexpr int units = W / 8;
+    for (int i = threadIdx.x; i < kTok * units; i += kScanThreads) {
+      const int u = i % units, t = i / units, c = p.c0 + 8 * u;
+      if (t0 + t >= a.L || c >= p.cend) continue;
+      float y[8], z[8];
+      if (t0 + t < p.n) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          y[k] = ts[tile_at<float>(8 * u + k, t)];
+          if (a.skip) y[k] = fmaf(a.skip[c + k], to_f32(tx[tile_at<T>(8 * u + k, t)]), y[k]);
+        }
+        if (a.z) {
+          RowVec<T, 8> r;
+          r.load(static_cast<const T *>(a.z) + p.b * a.zs.b + (t0 + t) * a.zs.t + c);
+          r.get(z);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] *= z[k] * sigmoid(z[k]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = 0.f;
+      }
+      store_row<8>(static_cast<T *>(a.y) + p.b * a.ys.b + (t0 + t) * a.ys.t + c, y);
+    }
+  }
+  __syncthreads();
+  if (kOut) {
+    if (a.h_out && p.seg == a.nseg - 1) store_channels<W>(a.h_out + p.b * DN, p, a.N, 0, a.N, th);
+  } else {
+    store_channels<W>(a.part + at_part, p, a.N, 0, a.N, th);
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) {
+      const float total = row_sum(seg_steps[i]);
+      const int c = p.c0 + cl + 4 * i;
+      if (tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
+    }
+  }
+}
+
+// One thread per (sequence, channel, state): the states before each segment from the
+// segments' sums; kRight: behind each segment, from the last.
+constexpr int kPrefixThreads = 256;
+template <bool kRight>
+__device__ __forceinline__ void chain(const Scan &a, float *part, float h, float A2, int64_t at, int64_t at_s) {
+  const int64_t DN = (int64_t)a.D * a.N;
+  constexpr int kAhead = 8;
+  for (int i = 0; i < a.nseg; i += kAhead) {
+    float S[kAhead], s[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i + j >= a.nseg) break;
+      const int k = kRight ? a.nseg - 1 - i - j : i + j;
+      S[j] = part[at + k * DN];
+      s[j] = a.steps[at_s + (int64_t)k * a.D];
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i + j >= a.nseg) break;
+      const int k = kRight ? a.nseg - 1 - i - j : i + j;
+      part[at + k * DN] = h;
+      h = fmaf(exp2_hw(s[j] * A2), h, S[j]);
+    }
+  }
+  if (kRight) {
+    if (a.dh_in) a.dh_in[at - (int64_t)blockIdx.y * (a.nseg - 1) * DN] = h;
+  }
+}
+
+template <bool kBackward> __global__ __launch_bounds__(kPrefixThreads) void k_scan_prefix(Scan a) {
+  const int64_t DN = (int64_t)a.D * a.N, i = (int64_t)blockIdx.x * kPrefixThreads + threadIdx.x;
+  if (i >= DN) return;
+  const int b = blockIdx.y;
+  const float A2 = kLog2e * a.A[i];
+  const int64_t at = (int64_t)b * a.nseg * DN + i, at_s = (int64_t)b * a.nseg * a.D + i / a.N;
+  if (kBackward && blockIdx.z) chain<true>(a, a.part_r, a.dh_out ? a.dh_out[b * DN + i] : 0.f, A2, at, at_s);
+  else chain<false>(a, a.part, a.h_in ? a.h_in[b * DN + i] : 0.f, A2, at, at_s);
+}
+
+template <typename T, int kCh, bool kOut> hipError_t launch_as(const Scan &a, hipStream_t st) {
+  constexpr int W = kWide<kCh>;
+  const size_t lds = sizeof(float) * (W * kTok + (kOut ? 2 : 1) * kStates * kTok + 2 * (size_t)a.N * W) +
+                     sizeof(T) * W * kTok;
+  const auto kernel = k_scan<T, kCh, kOut>;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  const int tiles = a.G * ((a.D / a.G + W - 1) / W);
+  kernel<<<dim3((unsigned)(tiles * a.nseg), a.B), kScanThreads, lds, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_scan(const Scan &a, Dt dt, int tile, hipStream_t st) {
+  if (tile == kWide<2>)
+    return dt == Dt::BF16 ? launch_as<bf16, 2, true>(a, st) : launch_as<float, 2, true>(a, st);
+  return dt == Dt::BF16 ? launch_as<bf16, 1, true>(a, st) : launch_as<float, 1, true>(a, st);
+}
+
+hipError_t launch_scan_sums(const Scan &a, Dt dt, int tile, hipStream_t st) {
+  if (tile == kWide<2>)
+    return dt == Dt::BF16 ? launch_as<bf16, 2, false>(a, st) : launch_as<float, 2, false>(a, st);
+  return dt == Dt::BF16 ? launch_as<bf16, 1, false>(a, st) : launch_as<float, 1, false>(a, st);
+}
+
+hipError_t launch_scan_prefix(const Scan &a, bool backward, hipStream_t st) {
+  const unsigned blocks = (unsigned)(((int64_t)a.D * a.N + kPrefixThreads - 1) / kPrefixThreads);
+  if (backward) k_scan_prefix<true><<<dim3(blocks, a.B, 2), kPrefixThreads, 0, st>>>(a);
+  else k_scan_prefix<false><<<dim3(blocks, a.B), kPrefixThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace favor

@@ -1,0 +1,416 @@
+// scan_backward.hip - gradients of the selective scan. With a_t = exp(s_t A) and
+// e_t = dy_t silu(z_t), per channel and state
+//
+//   g_t = C_t e_t + q_{t+1},  q_t = a_t g_t        (from the last token back; q_L = dh_out)
+//   dC_t = sum_d e_t h_t,  dB_t = sum_d g_t s_t x_t,  dA = sum_t s_t q_t h_{t-1},
+//   d(s x)_t = sum_n g_t B_t,  ds_t = sum_n A q_t h_{t-1} + x_t d(s x)_t,  dx_t = s_t d(s x)_t + skip e_t
+//
+// Every chunk of 128 tokens is a workgroup of its own: a first pass takes each chunk's sums of
+// h (from the left) and of q (from the right), a second chains them, and the third recomputes
+// h and q inside the chunk from the two states around it. Bound by the vector unit: about 23
+// issue slots per (token, channel, state) in the third pass. dB and dC are sums over channels: a
+// lane adds its two, the wave's four rows are joined by exchanging halves and rows (each exchange
+// leaves half as many values), and the waves add into LDS in turns, wave w at state i + w, so
+// that the order is fixed. What the workgroups of a group of channels leave is added up last.
+#include "scan_common.hpp"
+
+namespace favor {
+namespace {
+
+constexpr int W = kScanBackTile;
+constexpr int kCh = 2;
+static_assert(W == 4 * kScanWaves * kCh, "a workgroup's channels");
+
+// e = dy silu(z) of the tile's tokens, zeros behind the sequence and the group.
+template <typename T>
+__device__ __forceinline__ void gated(const Scan &a, const ScanPlace &p, int64_t t, int c, float *e, float *z) {
+  RowVec<T, 8> r;
+  r.load(static_cast<const T *>(a.dy) + p.b * a.dys.b + t * a.dys.t + c);
+  r.get(e);
+  if (!a.z) return;
+  r.load(static_cast<const T *>(a.z) + p.b * a.zs.b + t * a.zs.t + c);
+  r.get(z);
+}
+template <typename T>
+__device__ __forceinline__ void load_gated(const Scan &a, const ScanPlace &p, int64_t t0, float *te) {
+  for (int i = threadIdx.x; i < kTok * (W / 8); i += kScanThreads) {
+    const int u = i % (W / 8), t = i / (W / 8), c = p.c0 + 8 * u;
+    float e[8], z[8];
+    if (t0 + t < p.n && c < p.cend) {
+      gated<T>(a, p, t0 + t, c, e, z);
+      if (a.z)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] *= z[k] * sigmoid(z[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) e[k] = 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) te[tile_at<float>(8 * u + k, t)] = e[k];
+  }
+}
+
+template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_parts(Scan a) {
+  extern __shared__ __align__(16) float lds[];
+  float *ts = lds, *te = ts + W * kTok, *tb = te + W * kTok, *tc = tb + kStates * kTok;
+  float *tA = tc + kStates * kTok, *th = tA + kStates * W, *tq = th + kStates * W;
+  T *tx = reinterpret_cast<T *>(tq + kStates * W);
+  const ScanPlace p = scan_place(a, W);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
+  const int cl = 4 * kCh * wave + lane / 16;
+  const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
+  const int64_t t0 = (int64_t)p.seg * kTok;
+  load_steps<T, W>(a, p, t0, ts, tx);
+  load_gated<T>(a, p, t0, te);
+  float s[kCh][8], sx[kCh][8], e[kCh][8], ssum[kCh];
+  for (int n0 = 0; n0 < a.N; n0 += kStates) {
+    const int count = min(kStates, a.N - n0);
+    load_states<T>(a.b, a.bs, p, t0, n0, count, tb);
+    load_states<T>(a.c, a.cs, p, t0, n0, count, tc);
+    load_channels<W>(a.A, p, a.N, n0, count, kLog2e, tA);
+    __syncthreads();
+    if (n0 == 0) {
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) {
+        lane_tokens(ts, cl + 4 * i, tl, s[i]);
+        lane_tokens(tx, cl + 4 * i, tl, sx[i]);
+        lane_tokens(te, cl + 4 * i, tl, e[i]);
+        ssum[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sx[i][j] *= s[i][j];
+          ssum[i] += s[i][j];
+        }
+        const float total = row_sum(ssum[i]);
+        const int c = p.c0 + cl + 4 * i;
+        if (tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
+      }
+    }
+    for (int n = 0; n < count; ++n) {
+      float Bv[8], Cv[8], S[kCh], Q[kCh], P[kCh], P2[kCh], h[kCh], q[kCh];
+      load8(tb + n * kTok + kLaneTok * tl, Bv);
+      load8(tc + n * kTok + kLaneTok * tl, Cv);
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) {
+        const float A = tA[n * W + cl + 4 * i];
+        float at[8];
+        S[i] = Q[i] = h[i] = q[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          at[j] = exp2_hw(s[i][j] * A);
+          S[i] = fmaf(at[j], S[i], sx[i][j] * Bv[j]);
+        }
+#pragma unroll
+        for (int j = 7; j >= 0; --j) Q[i] = at[j] * fmaf(e[i][j], Cv[j], Q[i]);
+        P[i] = P2[i] = exp2_hw(ssum[i] * A);
+      }
+      row_scan2<false>(S[0], P[0], h[0], S[1], P[1], h[1]);
+      row_scan2<true>(Q[0], P2[0], q[0], Q[1], P2[1], q[1]);
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) {
+        if (tl == 15) th[n * W + cl + 4 * i] = S[i];
+        if (tl == 0) tq[n * W + cl + 4 * i] = Q[i];
+      }
+    }
+    __syncthreads();
+    store_channels<W>(a.part + at_part, p, a.N, n0, count, th);
+    store_channels<W>(a.part_r + at_part, p, a.N, n0, count, tq);
+  }
+}
+
+// The sums of 16 values over the wave's four rows of lanes; row r keeps values 4 r' .. 4 r' + 3
+// of (v: first eight, then the others): rows 0, 1 the first eight's halves, rows 2, 3 the
+// others'.
+__device__ __forceinline__ f32x4 join_rows(const float (&v)[8], const float (&w)[8]) {
+  float x[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[j]), __float_as_uint(w[j]), false, false);
+    x[j] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  f32x4 o;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[j]), __float_as_uint(x[j + 4]), false, false);
+    o[j] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return o;
+}
+
+template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_backward(Scan a) {
+  extern __shared__ __align__(16) float lds[];
+  float *ts = lds, *tx = ts + W * kTok, *te = tx + W * kTok;
+  float *tb = te + W * kTok, *tc = tb + kStates * kTok;
+  float *tlow = tc + kStates * kTok;   // dB, then dC
+  float *tA = tlow + 2 * kStates * kTok, *th = tA + kStates * W, *tq = th + kStates * W;
+  const ScanPlace p = scan_place(a, W);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
+  const int cl = 4 * kCh * wave + lane / 16;
+  const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
+  const int64_t at_sum = ((int64_t)p.b * a.nseg + p.seg) * a.D;
+  const int64_t t0 = (int64_t)p.seg * kTok;
+  const bool some = t0 < p.n;
+  float s[kCh][8], sx[kCh][8], e[kCh][8], ds[kCh][8], dsx[kCh][8], y[kCh][8], ssum[kCh];
+  if (some) {
+    load_steps<T, W>(a, p, t0, ts, tx);
+    load_gated<T>(a, p, t0, te);
+  }
+  for (int n0 = 0; n0 < a.N; n0 += kStates) {
+    const int count = min(kStates, a.N - n0);
+    if (!some) {
+      for (int i = threadIdx.x; i < W * kStates; i += kScanThreads) th[i] = 0.f;
+    } else {
+      load_states<T>(a.b, a.bs, p, t0, n0, count, tb);
+      load_states<T>(a.c, a.cs, p, t0, n0, count, tc);
+      for (int i = threadIdx.x + count * W; i < kStates * W; i += kScanThreads) tA[i] = th[i] = tq[i] = 0.f;
+      load_channels<W>(a.A, p, a.N, n0, count, 1.f, tA);
+      load_channels<W>(a.part + at_part, p, a.N, n0, count, 1.f, th);
+      load_channels<W>(a.part_r + at_part, p, a.N, n0, count, 1.f, tq);
+      __syncthreads();
+      if (n0 == 0) {
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) {
+          float skip = 0.f;
+          lane_tokens(ts, cl + 4 * i, tl, s[i]);
+          lane_tokens(tx, cl + 4 * i, tl, sx[i]);
+          lane_tokens(te, cl + 4 * i, tl, e[i]);
+          ssum[i] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            skip = fmaf(e[i][j], sx[i][j], skip);
+            sx[i][j] *= s[i][j];
+            ssum[i] += s[i][j];
+            ds[i][j] = dsx[i][j] = y[i][j] = 0.f;
+          }
+          if (a.dskip) {
+            const float total = row_sum(skip);
+            const int c = p.c0 + cl + 4 * i;
+            if (tl == 15 && c < p.cend) a.part_d[at_sum + c] = total;
+          }
+        }
+      }
+      const int each = (count + kScanWaves - 1) / kScanWaves;   // states of a wave's turn
+      for (int turn = 0; turn < kScanWaves; ++turn) {
+        for (int k = 0; k < each; ++k) {
+          const int n = ((turn + wave) % kScanWaves) * each + k;
+          float Bv[8], Cv[8], dB[8], dC[8];
+          load8(tb + n * kTok + kLaneTok * tl, Bv);
+          load8(tc + n * kTok + kLaneTok * tl, Cv);
+#pragma unroll
+          for (int i = 0; i < kCh; ++i) {
+            const int at_c = n * W + cl + 4 * i;
+            const float A = tA[at_c], A2 = kLog2e * A;
+            float h = th[at_c], q = tq[at_c], at[8], bx[8], ce[8];
+            float S = tl == 0 ? h : 0.f, Q = tl == 15 ? q : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              at[j] = exp2_hw(s[i][j] * A2);
+              bx[j] = sx[i][j] * Bv[j];
+              ce[j] = e[i][j] * Cv[j];
+              S = fmaf(at[j], S, bx[j]);
+            }
+#pragma unroll
+            for (int j = 7; j >= 0; --j) Q = at[j] * (ce[j] + Q);
+            float P = exp2_hw(ssum[i] * A2), P2 = P;
+            row_scan<false>(S, P, h);
+            row_scan<true>(Q, P2, q);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float before = h;
+              h = fmaf(at[j], h, bx[j]);
+              dC[j] = i ? fmaf(e[i][j], h, dC[j]) : e[i][j] * h;
+              y[i][j] = fmaf(Cv[j], h, y[i][j]);
+              bx[j] = before;
+            }
+            float dA = 0.f;
+#pragma unroll
+            for (int j = 7; j >= 0; --j) {
+              const float g = ce[j] + q;
+              q = at[j] * g;
+              dB[j] = i ? fmaf(g, sx[i][j], dB[j]) : g * sx[i][j];
+              dsx[i][j] = fmaf(g, Bv[j], dsx[i][j]);
+              const float u = q * bx[j];
+              ds[i][j] = fmaf(A, u, ds[i][j]);
+              dA = fmaf(s[i][j], u, dA);
+            }
+            dA = row_sum(dA);
+            if (tl == 15) th[at_c] = dA;   // h before the chunk has been read
+          }
+          f32x4 low = join_rows(dB, dC);
+          f32x4 *to = reinterpret_cast<f32x4 *>(tlow + (lane / 32 * kStates + n) * kTok + kLaneTok * tl +
+                                                (lane / 16 % 2) * 4);
+          if (turn) low += *to;
+          *to = low;
+        }
+        __syncthreads();
+      }
+      for (int i = threadIdx.x; i < kTok * kStates; i += kScanThreads) {
+        const int n = i % kStates, t = i / kStates;
+        if (n >= count || t0 + t >= p.n) continue;
+        const int64_t at = ((((int64_t)p.tile * a.B + p.b) * a.L + t0 + t) * a.G + p.g) * a.N + n0 + n;
+        a.part_b[at] = tlow[n * kTok + t];
+        a.part_c[at] = tlow[(kStates + n) * kTok + t];
+      }
+    }
+    if (!some) __syncthreads();
+    store_channels<W>(a.part_a + at_part, p, a.N, n0, count, th);
+    __syncthreads();
+  }
+  if (some) {
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) {   // in place of what only this lane has read
+      const int at = tile_at<float>(cl + 4 * i, kLaneTok * tl);
+      store8_lds(ts + at, ds[i]);
+      store8_lds(tx + at, dsx[i]);
+      store8_lds(te + at, y[i]);
+    }
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < kTok * (W / 8); i += kScanThreads) {
+    const int u = i % (W / 8), t = i / (W / 8), c = p.c0 + 8 * u;
+    const int64_t tt = t0 + t;
+    const bool row = tt < a.L && c < p.cend, live = tt < p.n && c < p.cend;
+    float dx[8], ddt[8], dz[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dx[k] = ddt[k] = dz[k] = 0.f;
+    if (live) {
+      RowVec<T, 8> r;
+      float x[8], raw[8], do_[8], z[8];
+      r.load(static_cast<const T *>(a.x) + p.b * a.xs.b + tt * a.xs.t + c);
+      r.get(x);
+      r.load(static_cast<const T *>(a.dt) + p.b * a.dts.b + tt * a.dts.t + c);
+      r.get(raw);
+      gated<T>(a, p, tt, c, do_, z);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int at = tile_at<float>(8 * u + k, t);
+        const float v = a.bias ? raw[k] + a.bias[c + k] : raw[k], skip = a.skip ? a.skip[c + k] : 0.f;
+        const float step = a.softplus ? softplus(v) : v;
+        float ek = do_[k];
+        if (a.z) {
+          const float k1 = sigmoid(z[k]);
+          ek *= z[k] * k1;
+          dz[k] = do_[k] * fmaf(skip, x[k], te[at]) * (k1 * fmaf(z[k], 1.f - k1, 1.f));
+        }
+        const float d = tx[at];
+        dx[k] = fmaf(step, d, skip * ek);
+        ddt[k] = fmaf(x[k], d, ts[at]);
+        if (a.softplus) ddt[k] *= sigmoid(v);
+      }
+    }
+    if (a.dbias && some)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) ts[tile_at<float>(8 * u + k, t)] = ddt[k];
+    if (!row) continue;
+    store_row<8>(static_cast<T *>(a.dx) + p.b * a.dxs.b + tt * a.dxs.t + c, dx);
+    store_row<8>(static_cast<T *>(a.ddt) + p.b * a.ddts.b + tt * a.ddts.t + c, ddt);
+    if (a.z) store_row<8>(static_cast<T *>(a.dz) + p.b * a.dzs.b + tt * a.dzs.t + c, dz);
+  }
+  if (some && !a.dbias) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kCh; ++i) {
+    float v[8], total = 0.f;
+    const int c = p.c0 + cl + 4 * i;
+    if (some) {
+      lane_tokens(ts, cl + 4 * i, tl, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) total += v[j];
+      total = row_sum(total);
+    }
+    if (tl != 15 || c >= p.cend) continue;
+    if (a.dbias) a.part_s[at_sum + c] = total;
+    if (a.dskip && !some) a.part_d[at_sum + c] = 0.f;
+  }
+}
+
+// dB and dC: over the workgroups of a group of channels.
+constexpr int kLowThreads = 256;
+template <typename T> __global__ __launch_bounds__(kLowThreads) void k_scan_low(Scan a, int tiles) {
+  const int64_t GN = (int64_t)a.G * a.N, per = (int64_t)a.L * GN;
+  const int64_t i = (int64_t)blockIdx.x * kLowThreads + threadIdx.x;
+  if (i >= per) return;
+  const int b = blockIdx.y;
+  const int t = (int)(i / GN), gn = (int)(i - t * GN), g = gn / a.N, n = gn - g * a.N;
+  const float *part = blockIdx.z ? a.part_c : a.part_b;
+  float sum = 0.f;
+  if (t < clamped_length(a.lengths, b, a.L))
+#pragma unroll 8
+    for (int k = 0; k < tiles; ++k) sum += part[((int64_t)k * a.B + b) * per + i];
+  const Rows &r = blockIdx.z ? a.dcs : a.dbs;
+  static_cast<T *>(blockIdx.z ? a.dc : a.db)[b * r.b + g * r.h + t * r.t + n] = from_f32<T>(sum);
+}
+
+// dA, dskip and dbias: over sequences and chunks. 64 columns by 16 row lanes, joined in order.
+constexpr int kSumCols = 64, kSumLanes = 16;
+__global__ __launch_bounds__(kSumCols *kSumLanes) void k_scan_params(Scan a, int rows) {
+  __shared__ float part[kSumLanes][kSumCols];
+  const int64_t DN = (int64_t)a.D * a.N;
+  const int lane = threadIdx.x / kSumCols;
+  int64_t col = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
+  const float *src = a.part_a;
+  float *dst = a.dA;
+  int64_t cols = DN;
+  if (col >= DN) {
+    col -= DN;
+    cols = a.D;
+    src = a.part_d;
+    dst = a.dskip;
+    if (col >= a.D) {
+      col -= a.D;
+      src = a.part_s;
+      dst = a.dbias;
+    }
+  }
+  const bool live = col < cols && dst;
+  float s = 0.f;
+  if (live)
+#pragma unroll 8
+    for (int r = lane; r < rows; r += kSumLanes) s += src[r * cols + col];
+  part[lane][threadIdx.x % kSumCols] = s;
+  __syncthreads();
+  if (lane || !live) return;
+  for (int i = 1; i < kSumLanes; ++i) s += part[i][threadIdx.x];
+  dst[col] = s;
+}
+
+template <typename K> hipError_t launch_tiles(K kernel, const Scan &a, size_t lds, hipStream_t st) {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  const int tiles = a.G * ((a.D / a.G + W - 1) / W);
+  kernel<<<dim3((unsigned)(tiles * a.nseg), a.B), kScanThreads, lds, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st) {
+  const size_t lds = sizeof(float) * (2 * W * kTok + 2 * kStates * kTok + 3 * kStates * W) +
+                     (dt == Dt::BF16 ? 2 : 4) * W * kTok;
+  return dt == Dt::BF16 ? launch_tiles(k_scan_parts<bf16>, a, lds, st)
+                        : launch_tiles(k_scan_parts<float>, a, lds, st);
+}
+
+hipError_t launch_scan_backward(const Scan &a, Dt dt, hipStream_t st) {
+  const size_t lds = sizeof(float) * (3 * W * kTok + 4 * kStates * kTok + 3 * kStates * W);
+  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, lds, st)
+                        : launch_tiles(k_scan_backward<float>, a, lds, st);
+}
+
+hipError_t launch_scan_backward_sums(const Scan &a, Dt dt, hipStream_t st) {
+  const int64_t low = (int64_t)a.L * a.G * a.N;
+  if (low > 0) {
+    const int tiles = (a.D / a.G + W - 1) / W;
+    const dim3 grid((unsigned)((low + kLowThreads - 1) / kLowThreads), a.B, 2);
+    if (dt == Dt::BF16) k_scan_low<bf16><<<grid, kLowThreads, 0, st>>>(a, tiles);
+    else k_scan_low<float><<<grid, kLowThreads, 0, st>>>(a, tiles);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int64_t cols = (int64_t)a.D * a.N + 2 * a.D;
+  k_scan_params<<<(unsigned)((cols + kSumCols - 1) / kSumCols), kSumCols * kSumLanes, 0, st>>>(a, a.B * a.nseg);
+  return hipGetLastError();
+}
+
+}  // namespace favor

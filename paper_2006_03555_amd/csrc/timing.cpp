@@ -27,7 +27,11 @@ const char *const kNames[kNumKernels] = {"k_orf_draw",   "k_feature_map", "k_ksi
                                          "k_causal",     "k_sum_splits",  "k_bwd_dq",
                                          "k_kside_agg",  "k_suffix_scan", "k_bwd_dkv",
                                          "k_decay_sums", "k_decay_prefix", "k_decay_scan",
-                                         "k_decay_step", "k_dropout"};
+                                         "k_decay_step", "k_dropout",     "k_conv",
+                                         "k_conv_backward", "k_conv_step", "k_scan_sums",
+                                         "k_scan_prefix", "k_scan",       "k_scan_backward",
+                                         "k_scan_step",  "k_column_sums", "k_beam_pieces",
+                                         "k_beam_merge", "k_beam_reorder"};
 
 hipEvent_t take_event() {
   if (!g_pool.empty()) {

@@ -1,0 +1,310 @@
+"""The selective scan on the GPU against the fp64 oracle, each element within the first-order
+bound that the oracle carries through the same recurrences."""
+import numpy as np
+import pytest
+
+from helpers import to_dev, to_host, torch_dtype
+from oracle import recurrent as rec
+from test_gpu_conv import _round, near
+
+pytestmark = pytest.mark.gpu
+GRADS = ("dx", "ddt", "dA", "dB", "dC", "dD", "dz", "ddt_bias", "dstate")
+PARAMS = ("dA", "dD", "ddt_bias", "dstate")
+
+
+def _fv():
+    import paper_2006_03555_amd as fv
+    return fv
+
+
+def inputs(B, L, D, N, G, dtype, seed, skip=True, z=True, bias=True, state=True, soft=True):
+    r = np.random.default_rng(seed)
+    f32 = lambda v: v.astype(np.float32)
+    draw = lambda *s: _round(r.standard_normal(s), dtype)
+    dt = draw(B, L, D)
+    if not soft:
+        dt = _round(np.abs(dt) * 0.1, dtype)
+    return dict(x=draw(B, L, D), dt=dt, A=f32(-np.exp(r.uniform(-3, 1.5, (D, N)))),
+                Bm=draw(B, L, G, N), C=draw(B, L, G, N),
+                skip=f32(r.standard_normal(D)) if skip else None, z=draw(B, L, D) if z else None,
+                bias=f32(r.uniform(-4, 0, D) if soft else r.uniform(0, 0.1, D)) if bias else None,
+                state=f32(r.standard_normal((B, D, N))) if state else None, dy=draw(B, L, D),
+                dstate=f32(r.standard_normal((B, D, N))) if state else None)
+
+
+def dev(i, dtype):
+    own = ("x", "dt", "Bm", "C", "z", "dy")
+    return {k: None if v is None else to_dev(v, dtype if k in own else "f32") for k, v in i.items()}
+
+
+def forward(t, **kw):
+    return _fv().selective_scan(t["x"], t["dt"], t["A"], t["Bm"], t["C"], t["skip"], t["z"], t["bias"],
+                                state_in=t["state"], return_state=True, **kw)
+
+
+def backward(t, **kw):
+    return _fv().selective_scan_backward(
+        t["x"], t["dt"], t["A"], t["Bm"], t["C"], t["dy"], t["skip"], t["z"], t["bias"],
+        state_in=t["state"], dstate_out=t["dstate"], return_state_grad=True, **kw)
+
+
+def _args(i):
+    return [i[k] for k in ("x", "dt", "A", "Bm", "C")]
+
+
+def _opts(i, soft, lengths):
+    return dict(skip=i["skip"], z=i["z"], bias=i["bias"], soft=soft, lengths=lengths, state=i["state"])
+
+
+def check(i, dtype, got, grads, soft=True, lengths=None):
+    y, s = got
+    ref, sref = rec.scan(*_args(i), **_opts(i, soft, lengths))
+    refs = rec.scan_backward(*_args(i), i["dy"], dstate=i["dstate"], **_opts(i, soft, lengths))
+    units = rec.scan_bounds(*_args(i), i["dy"], dstate=i["dstate"], **_opts(i, soft, lengths))
+    near(y, ref, units[0], dtype, "y")
+    near(s, sref, units[1], "f32", "state")
+    for g, r, u, name in zip(grads, refs, units[2:], GRADS):
+        assert (g is None) == (r is None), name
+        if g is not None:
+            near(g, r, u, "f32" if name in PARAMS else dtype, name)
+
+
+SHAPES = [  # B, L, D, N, G
+    (1, 1, 8, 1, 1), (2, 3, 16, 4, 2), (1, 8, 24, 16, 1), (1, 127, 8, 16, 1), (2, 128, 72, 5, 1),
+    (1, 129, 40, 16, 1), (1, 385, 136, 16, 1), (3, 200, 48, 24, 3), (1, 150, 16, 64, 2),
+    (1, 140, 8, 130, 1), (1, 131, 8, 256, 1), (1, 700, 64, 16, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,L,D,N,G", SHAPES)
+def test_forward_and_backward(B, L, D, N, G, dtype):
+    i = inputs(B, L, D, N, G, dtype, 3 * L + N)
+    t = dev(i, dtype)
+    check(i, dtype, forward(t), backward(t))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("skip,z,bias,state,soft", [
+    (0, 0, 0, 0, 1), (1, 0, 0, 1, 0), (0, 1, 1, 0, 0), (0, 0, 1, 1, 1), (1, 1, 0, 0, 1)])
+def test_without_parts(skip, z, bias, state, soft, dtype):
+    i = inputs(2, 133, 24, 7, 1, dtype, 17, skip, z, bias, state, soft)
+    t = dev(i, dtype)
+    check(i, dtype, forward(t, softplus=bool(soft)), backward(t, softplus=bool(soft)), bool(soft))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_padded_batch(dtype):
+    """Lengths of 0 and 1, at chunk borders and out of range; padding that is NaN or Inf."""
+    import torch
+    B, L = 7, 300
+    lengths = [300, 0, 1, 128, 129, -3, 999]
+    i = inputs(B, L, 16, 9, 2, dtype, 5)
+    t = dev(i, dtype)
+    n = np.clip(lengths, 0, L)
+    for b in range(B):
+        for k in ("x", "dt", "Bm", "C", "z", "dy"):
+            t[k][b, n[b]:] = float("nan") if b % 2 else float("inf")
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    got, grads = forward(t, lengths=lens), backward(t, lengths=lens)
+    check(i, dtype, got, grads, True, lengths)
+    for b in range(B):
+        for v in (got[0], grads[0], grads[1], grads[3], grads[4], grads[6]):
+            assert not v[b, n[b]:].any()
+        if n[b] == 0:
+            assert torch.equal(got[1][b], t["state"][b]) and torch.equal(grads[8][b], t["dstate"][b])
+
+
+def test_strides_and_untouched_neighbours():
+    """Slices of projections in and out, groups in another order, broadcast inputs."""
+    import torch
+    fv = _fv()
+    B, L, D, N, G = 2, 140, 32, 8, 2
+    i = inputs(B, L, D, N, G, "bf16", 23)
+    t = dev(i, "bf16")
+    want, wants = forward(t), backward(t)
+    both = torch.full((B, L, 2 * D), 3.0, device="cuda", dtype=torch.bfloat16)
+    both[..., :D], both[..., D:] = t["x"], t["z"]
+    odd = 2 * G * N + 5   # B and C behind five others: not aligned
+    low = torch.full((B, L, odd), 3.0, device="cuda", dtype=torch.bfloat16)
+    bc = low[..., 5:].unflatten(-1, (2, N, G)).transpose(-1, -2)
+    bc[:, :, 0], bc[:, :, 1] = t["Bm"], t["C"]
+    # a group's states must be contiguous
+    with pytest.raises(fv.FavorError, match="contiguous"):
+        fv.selective_scan(t["x"], t["dt"], t["A"], bc[:, :, 0], bc[:, :, 1])
+    bc = low[..., 5:].unflatten(-1, (2, G, N))
+    bc[:, :, 0], bc[:, :, 1] = t["Bm"], t["C"]
+    u = dict(t, x=both[..., :D], z=both[..., D:], Bm=bc[:, :, 0], C=bc[:, :, 1])
+    out = torch.full((B, L, 3 * D), 7.0, device="cuda", dtype=torch.bfloat16)
+    got = forward(u, out=out[..., D:2 * D])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert (out[..., :D] == 7).all() and (out[..., 2 * D:] == 7).all()
+    dboth = torch.full((B, L, 3 * D), 7.0, device="cuda", dtype=torch.bfloat16)
+    dlow = torch.full((B, L, odd), 7.0, device="cuda", dtype=torch.bfloat16)
+    dbc = dlow[..., 5:].unflatten(-1, (2, G, N))
+    grads = backward(u, dx=dboth[..., :D], dz=dboth[..., D:2 * D], dB=dbc[:, :, 0], dC=dbc[:, :, 1])
+    for a, b in zip(grads, wants):
+        assert torch.equal(a, b)
+    assert (dboth[..., 2 * D:] == 7).all() and (dlow[..., :5] == 7).all()
+    still = dict(t, Bm=t["Bm"][:, :1].expand(B, L, G, N), x=t["x"][:1].expand(B, L, D))
+    plain = {k: None if v is None else v.contiguous() for k, v in still.items()}
+    for a, b in zip((*forward(still), *backward(still)), (*forward(plain), *backward(plain))):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pieces_and_states_in_place(dtype):
+    """Two pieces whose state goes on in place, forward and back, against the whole's oracle."""
+    B, L, L1 = 2, 300, 170
+    i = inputs(B, L, 40, 16, 1, dtype, 31)
+    t = dev(i, dtype)
+    cut = lambda d, s: {k: v[:, s] if k in ("x", "dt", "Bm", "C", "z", "dy") else v for k, v in d.items()}
+    a, b = cut(t, slice(0, L1)), cut(t, slice(L1, L))
+    s = t["state"].clone()
+    middle = None
+    ya, _ = forward(dict(a, state=s), state_out=s)
+    middle = s.clone()
+    yb, end = forward(dict(b, state=s), state_out=s)
+    q = t["dstate"].clone()
+    gb = backward(dict(b, state=middle, dstate=q), dstate_in=q)
+    ga = backward(dict(a, dstate=q), dstate_in=q)
+    import torch
+    grads = []
+    for k, name in enumerate(GRADS):
+        if name == "dstate":
+            grads.append(q)
+        elif name in PARAMS:
+            grads.append(ga[k] + gb[k])
+        else:
+            grads.append(torch.cat((ga[k], gb[k]), 1))
+    check(i, dtype, (torch.cat((ya, yb), 1), end), grads)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,N,G", [(8, 1, 1), (24, 5, 3), (72, 16, 1), (16, 64, 2), (8, 131, 1),
+                                   (16, 256, 1)])
+def test_single_tokens(D, N, G, dtype):
+    """Tokens one by one on a pool against the stretch; absent sequences and shared places."""
+    import torch
+    fv = _fv()
+    T = 6
+    i = inputs(4, T, D, N, G, dtype, 41)
+    t = dev(i, dtype)
+    ref, end = rec.scan(*_args(i), **_opts(i, True, None))
+    units = rec.scan_bounds(*_args(i), i["dy"], dstate=i["dstate"], **_opts(i, True, None))
+    pool = torch.full((6, D, N), 9.0, device="cuda")
+    places = [4, 0, 5, 2]
+    pool[places] = t["state"]
+    slots = torch.tensor(places[:1] + [-1] + places[1:] + [6], dtype=torch.int32, device="cuda")
+    live = [0, 2, 3, 4]
+
+    def spread(v, k):
+        w = torch.zeros((6,) + v.shape[2:], device="cuda", dtype=torch_dtype(dtype))
+        w[live] = v[:, k]
+        return w
+
+    for k in range(T):
+        y = fv.selective_scan_step(spread(t["x"], k), spread(t["dt"], k), t["A"], spread(t["Bm"], k),
+                                   spread(t["C"], k), pool, t["skip"], spread(t["z"], k), t["bias"],
+                                   slots=slots)
+        near(y[live], ref[:, k], units[0][:, k], dtype, f"token {k}")
+        assert not y[1].any() and not y[5].any()
+    near(pool[places], end, units[1], "f32", "states")
+    assert (pool[[1, 3]] == 9).all()
+    pool[3] = t["state"][0]
+    order = [(0, 0), (1, 0), (0, 1), (0, 2)]
+    row = lambda v: torch.stack([v[b, k] for b, k in order])
+    y = fv.selective_scan_step(row(t["x"]), row(t["dt"]), t["A"], row(t["Bm"]), row(t["C"]), pool,
+                               t["skip"], row(t["z"]), t["bias"],
+                               slots=torch.tensor([3, 1, 3, 3], dtype=torch.int32, device="cuda"))
+    near(y[[0, 2, 3]], ref[0, :3], units[0][0, :3], dtype, "turns")
+
+
+def test_extreme_steps():
+    """Steps of 0 and of many units, a decay of exp(-1e4), one of exp(-0)."""
+    i = inputs(1, 260, 16, 4, 1, "f32", 51)
+    i["dt"][0, :, 0] = -200.0      # softplus 0 in fp32: the state stays
+    i["dt"][0, :, 1] = 60.0        # everything is forgotten at every token
+    i["dt"][0, 100:110, 2] = 90.0
+    i["A"][3] = -1e4
+    i["A"][4] = -0.0
+    t = dev(i, "f32")
+    check(i, "f32", forward(t), backward(t))
+
+
+def test_empty_calls():
+    import torch
+    fv = _fv()
+    i = inputs(2, 4, 8, 3, 1, "f32", 1)
+    t = dev(i, "f32")
+    for k in ("x", "dt", "Bm", "C", "z", "dy"):
+        t[k] = t[k][:, :0].contiguous()
+    y, s = forward(t)
+    assert y.shape == (2, 0, 8) and torch.equal(s, t["state"])
+    g = backward(t)
+    assert torch.equal(g[8], t["dstate"])
+    for k in (2, 5, 7):
+        assert not g[k].any()
+    none = {k: v if v is None or k in ("A", "skip", "bias") else v[:0] for k, v in t.items()}
+    assert forward(none)[0].shape == (0, 0, 8)
+    _ = fv
+
+
+def test_not_a_number_stays_in_its_channel():
+    import torch
+    i = inputs(2, 300, 24, 16, 1, "f32", 61)
+    t = dev(i, "f32")
+    want, grads = forward(t), backward(t)
+    u = dict(t, x=t["x"].clone())
+    u["x"][0, 150, 5] = float("nan")
+    got = forward(u)
+    hit = torch.zeros((2, 300, 24), dtype=torch.bool, device="cuda")
+    hit[0, 150:, 5] = True
+    assert torch.equal(got[0].isnan(), hit)
+    assert torch.equal(got[0][~hit], want[0][~hit])
+    dx = backward(u)[0]
+    clean = torch.ones((2, 300, 24), dtype=torch.bool, device="cuda")
+    clean[0, :, 5] = False
+    assert torch.equal(dx[clean], grads[0][clean])
+
+
+def test_gradients_against_differences():
+    i = inputs(1, 40, 8, 6, 1, "f32", 71)
+    grads = backward(dev(i, "f32"))
+    r = np.random.default_rng(2)
+    names = ("x", "dt", "A", "Bm", "C", "skip", "z", "bias", "state")
+    for k, g in zip(names, grads):
+        step = r.standard_normal(i[k].shape)
+        h = 1e-5
+
+        def loss(s):
+            j = {n: None if v is None else v.astype(np.float64) for n, v in i.items()}
+            j[k] = j[k] + s * step
+            y, end = rec.scan(*_args(j), **_opts(j, True, None))
+            return (y * j["dy"]).sum() + (end * j["dstate"]).sum()
+
+        want = (loss(h) - loss(-h)) / (2 * h)
+        assert abs((to_host(g) * step).sum() - want) < 2e-5 * np.abs(to_host(g) * step).sum(), k
+
+
+@pytest.mark.parametrize("B,L,D,N", [(1, 4099, 64, 16), (2, 1999, 1000, 24), (1, 20000, 8, 8)])
+def test_long_and_wide(B, L, D, N):
+    """Sequences of many segments and chunks, by norm: fp32 against fp64 on sampled channels."""
+    i = inputs(B, L, D, N, 1, "f32", 81)
+    t = dev(i, "f32")
+    got, grads = forward(t), backward(t)
+    c = [0, D // 2, D - 1] if D > 8 else list(range(D))
+    j = {k: None if v is None else
+         v[..., c] if k in ("x", "dt", "skip", "z", "bias", "dy") else
+         v[c] if k == "A" else v[:, c] if k in ("state", "dstate") else v for k, v in i.items()}
+    ref = rec.scan(*_args(j), **_opts(j, True, None))
+    refs = rec.scan_backward(*_args(j), j["dy"], dstate=j["dstate"], **_opts(j, True, None))
+    pick = lambda v, name: to_host(v[c] if name in ("dA", "dD", "ddt_bias") else
+                                   v[:, c] if name in ("dstate", "state") else v[..., c])
+    for g, r, name in zip((*got, *grads), (*ref, *refs), ("y", "state") + GRADS):
+        if name in ("dB", "dC") and len(c) < D:
+            continue   # sums over all channels
+        err = np.linalg.norm(pick(g, name) - r) / np.linalg.norm(r) if name not in ("dB", "dC") else (
+            np.linalg.norm(to_host(g) - r) / np.linalg.norm(r))
+        # a few dozen roundings of 2^-24 that do not conspire
+        assert err < 40 * 2.0 ** -24, (name, err)
