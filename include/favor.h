@@ -527,8 +527,8 @@ FAVOR_API favor_status favor_conv_step(const favor_conv_desc *g, const void *x,
  * without the terms of a NULL dt_bias, skip or z.
  *
  * Layouts: x, dt, z, y [B][L][D] as for favor_conv; B, C [B][L][groups][N] with N contiguous
- * elements and any strides in elements (head: the group's), not aligned. A [D][N], skip and
- * dt_bias [D] fp32. States [B][D][N] fp32, contiguous.
+ * elements and any strides in elements (head: the group's), not aligned; tokens of all of them
+ * at most 2^25 bytes apart. A [D][N], skip and dt_bias [D] fp32. States [B][D][N] fp32, contiguous.
  *
  * Supported: N from 1 to 256; D up to 65536 with D / groups a multiple of 8; dtype (x, dt, B,
  * C, z, y and their gradients) F32 or BF16; 0 <= L <= 2^30, B <= 65535. Steps, states and sums

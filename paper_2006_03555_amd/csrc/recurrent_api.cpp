@@ -18,6 +18,8 @@ using namespace favor::host;
 enum Op { kOpForward = 0, kOpBackward = 1, kOpStep = 2 };
 constexpr int kMaxD = 65536, kMaxB = 65535;
 constexpr int64_t kMaxBlocks = 0x7fffffff;
+// the scan reaches a chunk's 128 rows by 32-bit offsets
+constexpr int64_t kMaxTokenBytes = 1 << 25;
 
 Dt dt_of(const favor_dtype &d) { return raw_enum(&d) == FAVOR_BF16 ? Dt::BF16 : Dt::F32; }
 int bytes_of(const favor_dtype &d) { return dt_of(d) == Dt::BF16 ? 2 : 4; }
@@ -159,7 +161,8 @@ favor_status validate(const favor_scan_desc *g, int op) {
     if (i == 5 ? op == kOpBackward : i > 5 && op != kOpBackward) continue;
     const int64_t size[3] = {g->B, ts[i].low ? g->groups : 1, op == kOpStep ? 1 : g->L};
     FAVOR_TRY(check_rows(ts[i].name, *ts[i].s, size, ts[i].low ? g->N : g->D,
-                         ts[i].low ? 1 : 16 / bytes_of(g->dtype), 0, ts[i].out));
+                         ts[i].low ? 1 : 16 / bytes_of(g->dtype), kMaxTokenBytes / bytes_of(g->dtype),
+                         ts[i].out));
   }
   if ((int64_t)tiles_of(g, favor::kScanBackTile) * chunks_of(g) > kMaxBlocks ||
       (int64_t)g->L * g->groups * g->N / 256 > kMaxBlocks)
@@ -171,10 +174,10 @@ favor_status validate(const favor_scan_desc *g, int op) {
 struct ScanCut {
   int tile, chunks, nseg;
 };
-constexpr int kScanBlocks = 512;
+constexpr int kScanBlocks = 2048;
 ScanCut cut_of(const favor_scan_desc *g) {
   ScanCut c;
-  c.tile = g->N <= 128 ? 64 : 32;
+  c.tile = 32;
   const int chunks = chunks_of(g);
   const int64_t blocks = (int64_t)g->B * tiles_of(g, c.tile);
   const int want = (int)std::min<int64_t>(std::max(chunks, 1), std::max<int64_t>(1, kScanBlocks / blocks));
@@ -470,7 +473,7 @@ favor_status favor_selective_scan(const favor_scan_desc *g, const void *x, const
     hipError_t e;
     {
       favor::LaunchTimer t(favor::kKerScanSums, stream);
-      e = favor::launch_scan_sums(a, type, c.tile, stream);
+      e = favor::launch_scan_sums(a, type, g->N <= 128 ? 64 : 32, stream);
     }
     if (e != hipSuccess) return device_result(e, "favor_selective_scan segment sums");
     favor::LaunchTimer t(favor::kKerScanPrefix, stream);

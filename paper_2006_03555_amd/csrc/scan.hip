@@ -17,20 +17,32 @@ template <int kCh> constexpr int kWide = 4 * kScanWaves * kCh;
 
 // One (chunk, n) step of kCh channels: a = 2^(s A), S and P of the lane, the row's scan.
 // kOut: y += C h; h of the row's last lane goes back to `carry`.
+template <int kCh, bool kOut> struct StateIn {   // what a step reads from LDS
+  float B[8], C[8], A[kCh], h[kCh];
+
+  __device__ __forceinline__ void load(const float *b, const float *c, const float *A2, const float *carry, int tl) {
+    lane_load(b, tl, B);
+    if (kOut) lane_load(c, tl, C);
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) {
+      A[i] = A2[4 * i];
+      h[i] = carry[4 * i];
+    }
+  }
+};
 template <int kCh, bool kOut>
 __device__ __forceinline__ void forward_state(const float (&s)[kCh][8], const float (&sx)[kCh][8],
-                                              const float (&ssum)[kCh], const float *Bv,
-                                              const float *Cv, const float *A2, float *carry,
-                                              int tl, float (&y)[kCh][8]) {
+                                              const float (&ssum)[kCh], const StateIn<kCh, kOut> &in,
+                                              float *carry, int tl, float (&y)[kCh][8]) {
   float a[kCh][8], bx[kCh][8], S[kCh], P[kCh], h[kCh];
 #pragma unroll
   for (int i = 0; i < kCh; ++i) {
-    const float A = A2[4 * i];
-    h[i] = carry[4 * i];
+    const float A = in.A[i];
+    h[i] = in.h[i];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       a[i][j] = exp2_hw(s[i][j] * A);
-      bx[i][j] = sx[i][j] * Bv[j];
+      bx[i][j] = sx[i][j] * in.B[j];
     }
     S[i] = tl == 0 ? h[i] : 0.f;
 #pragma unroll
@@ -45,7 +57,7 @@ __device__ __forceinline__ void forward_state(const float (&s)[kCh][8], const fl
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         h[i] = fmaf(a[i][j], h[i], bx[i][j]);
-        y[i][j] = fmaf(Cv[j], h[i], y[i][j]);
+        y[i][j] = fmaf(in.C[j], h[i], y[i][j]);
       }
     }
     if (tl == 15) carry[4 * i] = S[i];
@@ -54,98 +66,141 @@ __device__ __forceinline__ void forward_state(const float (&s)[kCh][8], const fl
 
 // kOut: the rows y and the state after the last token. Otherwise the sums of the segments.
 template <typename T, int kCh, bool kOut>
-__global__ __launch_bounds__(kScanThreads) void k_scan(Scan a) {
+__global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
   constexpr int W = kWide<kCh>;
   extern __shared__ __align__(16) float lds[];
-  float *ts = lds, *tb = ts + W * kTok, *tc = tb + kStates * kTok;
-  float *tA = tc + (kOut ? kStates * kTok : 0), *th = tA + a.N * W;
-  T *tx = reinterpret_cast<T *>(th + a.N * W);
+  float *tile = lds, *tb = tile + W * kTok, *tc = tb + kStates * kTok;
+  const int padded = (a.N + kStates - 1) / kStates * kStates;
+  float *tA = tc + (kOut ? kStates * kTok : 0), *th = tA + padded * W;
   const ScanPlace p = scan_place(a, W);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
   const int cl = 4 * kCh * wave + lane / 16;   // this lane's first channel; the next is 4 on
   const int64_t DN = (int64_t)a.D * a.N, at_part = ((int64_t)p.b * a.nseg + p.seg) * DN;
-  load_channels<W>(a.A, p, a.N, 0, a.N, kLog2e, tA);
   const float *h0 = nullptr;
   if (kOut && a.nseg > 1) h0 = a.part + at_part;
   else if (kOut && a.h_in) h0 = a.h_in + p.b * DN;
-  load_channels<W>(h0, p, a.N, 0, a.N, 1.f, th);
+  for (int n0 = 0; n0 < a.N; n0 += kStates) {
+    load_channels<W>(a.A, p, a.N, n0, min(kStates, a.N - n0), kLog2e, tA + n0 * W);
+    load_channels<W>(h0, p, a.N, n0, min(kStates, a.N - n0), 1.f, th + n0 * W);
+  }
   float seg_steps[kCh] = {};
   const int first = p.seg * a.chunks, last = min(first + a.chunks, (a.L + kTok - 1) / kTok);
   for (int chunk = first; chunk < last; ++chunk) {
     const int64_t t0 = (int64_t)chunk * kTok;
     const bool some = t0 < p.n;
     if (!some && !kOut) break;
-    __syncthreads();   // the last chunk's rows have been read
     if (some) {
-      load_steps<T, W>(a, p, t0, ts, tx);
       float s[kCh][8], sx[kCh][8], ssum[kCh], y[kCh][8];
+      States<T> low_b, low_c;
+      {
+        // everything is requested at once; the tile holds the steps, then s x, then y
+        Steps<T, W> steps;
+        float in[kLoads<W>][8], own[kLoads<W>][8];
+        steps.load(a, p, t0);
+        low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N));
+        if (kOut) low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N));
+#pragma unroll
+        for (int i = 0; i < kLoads<W>; ++i) steps.template get<true>(a, unit_of<W>(p, t0, i), i, own[i], in[i]);
+        __syncthreads();   // the last chunk's rows have been read
+#pragma unroll
+        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i), own[i]);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, s[i]);
+        low_b.put(tb, p, t0, min(kStates, a.N));
+        if (kOut) low_c.put(tc, p, t0, min(kStates, a.N));
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i), in[i]);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) {
+          tile_load(tile, cl + 4 * i, tl, sx[i]);
+          ssum[i] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            ssum[i] += s[i][j];
+            y[i][j] = 0.f;
+          }
+          if (!kOut) seg_steps[i] += ssum[i];
+        }
+      }
       for (int n0 = 0; n0 < a.N; n0 += kStates) {
         const int count = min(kStates, a.N - n0);
-        if (n0) __syncthreads();   // the last states' B and C have been read
-        load_states<T>(a.b, a.bs, p, t0, n0, count, tb);
-        if (kOut) load_states<T>(a.c, a.cs, p, t0, n0, count, tc);
-        __syncthreads();
-        if (n0 == 0) {
-#pragma unroll
-          for (int i = 0; i < kCh; ++i) {
-            lane_tokens(ts, cl + 4 * i, tl, s[i]);
-            lane_tokens(tx, cl + 4 * i, tl, sx[i]);
-            ssum[i] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              sx[i][j] *= s[i][j];
-              ssum[i] += s[i][j];
-              y[i][j] = 0.f;
-            }
-            if (!kOut) seg_steps[i] += ssum[i];
-          }
+        if (n0) {
+          low_b.load(a.b, a.bs, p, t0, n0, count);
+          if (kOut) low_c.load(a.c, a.cs, p, t0, n0, count);
+          __syncthreads();   // the last states' B and C have been read
+          low_b.put(tb, p, t0, count);
+          if (kOut) low_c.put(tc, p, t0, count);
+          __syncthreads();
         }
-        for (int n = 0; n < count; ++n) {
-          float Bv[8], Cv[8];
-          load8(tb + n * kTok + 8 * tl, Bv);
-          if (kOut) load8(tc + n * kTok + 8 * tl, Cv);
+        // each state's values are read while the one before it is computed
+        StateIn<kCh, kOut> even, odd;
+        const auto read = [&](StateIn<kCh, kOut> &in, int n) {
+          n = min(n, count - 1);
           const int at = (n0 + n) * W + cl;
-          forward_state<kCh, kOut>(s, sx, ssum, Bv, Cv, tA + at, th + at, tl, y);
+          in.load(tb + n * kTok, tc + n * kTok, tA + at, th + at, tl);
+        };
+        read(even, 0);
+        for (int n = 0; n < count; n += 2) {
+          float *carry = th + (n0 + n) * W + cl;
+          read(odd, n + 1);
+          forward_state<kCh, kOut>(s, sx, ssum, even, carry, tl, y);
+          if (n + 1 == count) break;
+          read(even, n + 2);
+          forward_state<kCh, kOut>(s, sx, ssum, odd, carry + W, tl, y);
         }
       }
       if (kOut) {
 #pragma unroll
-        for (int i = 0; i < kCh; ++i)   // in place of the lane's own steps
-          store8_lds(ts + tile_at<float>(cl + 4 * i, kLaneTok * tl), y[i]);
-        __syncthreads();
+        for (int i = 0; i < kCh; ++i) tile_store(tile, cl + 4 * i, tl, y[i]);
+      }
+    }
+    RowVec<T, 8> rx[kLoads<W>], rz[kLoads<W>];
+    if (kOut && some) {
+#pragma unroll
+      for (int i = 0; i < kLoads<W>; ++i) {
+        const Unit w = unit_of<W>(p, t0, i);
+        if (a.skip) rx[i] = get_row<T>(a.x, a.xs, p, t0, w);
+        if (a.z) rz[i] = get_row<T>(a.z, a.zs, p, t0, w);
       }
     }
     if (!kOut) continue;
-    constexpr int units = W / 8;
-    for (int i = threadIdx.x; i < kTok * units; i += kScanThreads) {
-      const int u = i % units, t = i / units, c = p.c0 + 8 * u;
-      if (t0 + t >= a.L || c >= p.cend) continue;
-      float y[8], z[8];
-      if (t0 + t < p.n) {
+    __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          y[k] = ts[tile_at<float>(8 * u + k, t)];
-          if (a.skip) y[k] = fmaf(a.skip[c + k], to_f32(tx[tile_at<T>(8 * u + k, t)]), y[k]);
+    for (int i = 0; i < kLoads<W>; ++i) {
+      const Unit w = unit_of<W>(p, t0, i);
+      if (w.t >= a.L - t0 || w.c >= p.cend) continue;
+      float y[8], v[8];
+      if (w.live) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = tile[tile_at(8 * w.u + k, w.t)];
+        if (a.skip) {
+          rx[i].get(v);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = fmaf(a.skip[w.c + k], v[k], y[k]);
         }
         if (a.z) {
-          RowVec<T, 8> r;
-          r.load(static_cast<const T *>(a.z) + p.b * a.zs.b + (t0 + t) * a.zs.t + c);
-          r.get(z);
+          rz[i].get(v);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] *= z[k] * sigmoid(z[k]);
+          for (int k = 0; k < 8; ++k) y[k] *= v[k] * sigmoid(v[k]);
         }
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) y[k] = 0.f;
       }
-      store_row<8>(static_cast<T *>(a.y) + p.b * a.ys.b + (t0 + t) * a.ys.t + c, y);
+      put_row<T>(a.y, a.ys, p, t0, w, y);
     }
   }
   __syncthreads();
-  if (kOut) {
-    if (a.h_out && p.seg == a.nseg - 1) store_channels<W>(a.h_out + p.b * DN, p, a.N, 0, a.N, th);
-  } else {
-    store_channels<W>(a.part + at_part, p, a.N, 0, a.N, th);
+  float *end = nullptr;
+  if (!kOut) end = a.part + at_part;
+  else if (a.h_out && p.seg == a.nseg - 1) end = a.h_out + p.b * DN;
+  if (end)
+    for (int n0 = 0; n0 < a.N; n0 += kStates)
+      store_channels<W>(end, p, a.N, n0, min(kStates, a.N - n0), th + n0 * W);
+  if (!kOut) {
 #pragma unroll
     for (int i = 0; i < kCh; ++i) {
       const float total = row_sum(seg_steps[i]);
@@ -196,8 +251,8 @@ template <bool kBackward> __global__ __launch_bounds__(kPrefixThreads) void k_sc
 
 template <typename T, int kCh, bool kOut> hipError_t launch_as(const Scan &a, hipStream_t st) {
   constexpr int W = kWide<kCh>;
-  const size_t lds = sizeof(float) * (W * kTok + (kOut ? 2 : 1) * kStates * kTok + 2 * (size_t)a.N * W) +
-                     sizeof(T) * W * kTok;
+  const size_t lds = sizeof(float) * (W * kTok + (kOut ? 2 : 1) * kStates * kTok +
+                                     2 * (size_t)((a.N + kStates - 1) / kStates * kStates) * W);
   const auto kernel = k_scan<T, kCh, kOut>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),

@@ -21,66 +21,100 @@ constexpr int W = kScanBackTile;
 constexpr int kCh = 2;
 static_assert(W == 4 * kScanWaves * kCh, "a workgroup's channels");
 
-// e = dy silu(z) of the tile's tokens, zeros behind the sequence and the group.
-template <typename T>
-__device__ __forceinline__ void gated(const Scan &a, const ScanPlace &p, int64_t t, int c, float *e, float *z) {
-  RowVec<T, 8> r;
-  r.load(static_cast<const T *>(a.dy) + p.b * a.dys.b + t * a.dys.t + c);
-  r.get(e);
-  if (!a.z) return;
-  r.load(static_cast<const T *>(a.z) + p.b * a.zs.b + t * a.zs.t + c);
-  r.get(z);
-}
-template <typename T>
-__device__ __forceinline__ void load_gated(const Scan &a, const ScanPlace &p, int64_t t0, float *te) {
-  for (int i = threadIdx.x; i < kTok * (W / 8); i += kScanThreads) {
-    const int u = i % (W / 8), t = i / (W / 8), c = p.c0 + 8 * u;
-    float e[8], z[8];
-    if (t0 + t < p.n && c < p.cend) {
-      gated<T>(a, p, t0 + t, c, e, z);
-      if (a.z)
+// dy and z of a thread's units as they lie in memory; then e = dy silu(z). Zeros behind the
+// sequence and the group.
+template <typename T> struct Gated {
+  RowVec<T, 8> dy[kLoads<W>], z[kLoads<W>];
+
+  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) e[k] *= z[k] * sigmoid(z[k]);
-    } else {
+    for (int i = 0; i < kLoads<W>; ++i) {
+      const Unit w = unit_of<W>(p, t0, i);
+      dy[i] = get_row<T>(a.dy, a.dys, p, t0, w);
+      if (a.z) z[i] = get_row<T>(a.z, a.zs, p, t0, w);
+    }
+  }
+  __device__ __forceinline__ void get(const Scan &a, const Unit &w, int i, float *e) const {
+    float g[8];
+    dy[i].get(e);
+    if (a.z) {
+      z[i].get(g);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) e[k] = 0.f;
+      for (int k = 0; k < 8; ++k) e[k] *= g[k] * sigmoid(g[k]);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) te[tile_at<float>(8 * u + k, t)] = e[k];
+    for (int k = 0; k < 8; ++k) e[k] = w.live ? e[k] : 0.f;
   }
-}
+};
 
-template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_parts(Scan a) {
+template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_parts(Scan a) {
   extern __shared__ __align__(16) float lds[];
-  float *ts = lds, *te = ts + W * kTok, *tb = te + W * kTok, *tc = tb + kStates * kTok;
+  float *tile = lds, *tb = tile + W * kTok, *tc = tb + kStates * kTok;
   float *tA = tc + kStates * kTok, *th = tA + kStates * W, *tq = th + kStates * W;
-  T *tx = reinterpret_cast<T *>(tq + kStates * W);
   const ScanPlace p = scan_place(a, W);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
   const int cl = 4 * kCh * wave + lane / 16;
   const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
   const int64_t t0 = (int64_t)p.seg * kTok;
-  load_steps<T, W>(a, p, t0, ts, tx);
-  load_gated<T>(a, p, t0, te);
+  if (t0 >= p.n) {   // no token: nothing is added
+    for (int i = threadIdx.x; i < min(W, p.cend - p.c0) * a.N; i += kScanThreads)
+      a.part[at_part + (int64_t)p.c0 * a.N + i] = a.part_r[at_part + (int64_t)p.c0 * a.N + i] = 0.f;
+    if (threadIdx.x < min(W, p.cend - p.c0))
+      a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + p.c0 + threadIdx.x] = 0.f;
+    return;
+  }
   float s[kCh][8], sx[kCh][8], e[kCh][8], ssum[kCh];
+  States<T> low_b, low_c;
+  {
+    // everything is requested at once; the tile holds the steps, then s x, then e
+    Steps<T, W> steps;
+    Gated<T> gated;
+    float in[kLoads<W>][8];
+    steps.load(a, p, t0);
+    gated.load(a, p, t0);
+    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N));
+    low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N));
+#pragma unroll
+    for (int i = 0; i < kLoads<W>; ++i) {
+      const Unit w = unit_of<W>(p, t0, i);
+      float own[8];
+      steps.template get<true>(a, w, i, own, in[i]);
+      put_unit(tile, w, own);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, s[i]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i), in[i]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, sx[i]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kLoads<W>; ++i) {
+      const Unit w = unit_of<W>(p, t0, i);
+      gated.get(a, w, i, in[i]);
+      put_unit(tile, w, in[i]);
+    }
+  }
   for (int n0 = 0; n0 < a.N; n0 += kStates) {
     const int count = min(kStates, a.N - n0);
-    load_states<T>(a.b, a.bs, p, t0, n0, count, tb);
-    load_states<T>(a.c, a.cs, p, t0, n0, count, tc);
+    if (n0) {
+      low_b.load(a.b, a.bs, p, t0, n0, count);
+      low_c.load(a.c, a.cs, p, t0, n0, count);
+    }
+    low_b.put(tb, p, t0, count);
+    low_c.put(tc, p, t0, count);
     load_channels<W>(a.A, p, a.N, n0, count, kLog2e, tA);
     __syncthreads();
     if (n0 == 0) {
 #pragma unroll
       for (int i = 0; i < kCh; ++i) {
-        lane_tokens(ts, cl + 4 * i, tl, s[i]);
-        lane_tokens(tx, cl + 4 * i, tl, sx[i]);
-        lane_tokens(te, cl + 4 * i, tl, e[i]);
+        tile_load(tile, cl + 4 * i, tl, e[i]);
         ssum[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          sx[i][j] *= s[i][j];
-          ssum[i] += s[i][j];
-        }
+        for (int j = 0; j < 8; ++j) ssum[i] += s[i][j];
         const float total = row_sum(ssum[i]);
         const int c = p.c0 + cl + 4 * i;
         if (tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
@@ -88,8 +122,8 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_par
     }
     for (int n = 0; n < count; ++n) {
       float Bv[8], Cv[8], S[kCh], Q[kCh], P[kCh], P2[kCh], h[kCh], q[kCh];
-      load8(tb + n * kTok + kLaneTok * tl, Bv);
-      load8(tc + n * kTok + kLaneTok * tl, Cv);
+      lane_load(tb + n * kTok, tl, Bv);
+      lane_load(tc + n * kTok, tl, Cv);
 #pragma unroll
       for (int i = 0; i < kCh; ++i) {
         const float A = tA[n * W + cl + 4 * i];
@@ -151,18 +185,36 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
   const int64_t t0 = (int64_t)p.seg * kTok;
   const bool some = t0 < p.n;
   float s[kCh][8], sx[kCh][8], e[kCh][8], ds[kCh][8], dsx[kCh][8], y[kCh][8], ssum[kCh];
+  States<T> low_b, low_c;
   if (some) {
-    load_steps<T, W>(a, p, t0, ts, tx);
-    load_gated<T>(a, p, t0, te);
+    Steps<T, W> steps;
+    Gated<T> gated;
+    steps.load(a, p, t0);
+    gated.load(a, p, t0);
+    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N));
+    low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N));
+#pragma unroll
+    for (int i = 0; i < kLoads<W>; ++i) {
+      const Unit w = unit_of<W>(p, t0, i);
+      float own[8], x[8];
+      steps.template get<false>(a, w, i, own, x);
+      put_unit(ts, w, own);
+      put_unit(tx, w, x);
+      gated.get(a, w, i, x);
+      put_unit(te, w, x);
+    }
   }
   for (int n0 = 0; n0 < a.N; n0 += kStates) {
     const int count = min(kStates, a.N - n0);
     if (!some) {
       for (int i = threadIdx.x; i < W * kStates; i += kScanThreads) th[i] = 0.f;
     } else {
-      load_states<T>(a.b, a.bs, p, t0, n0, count, tb);
-      load_states<T>(a.c, a.cs, p, t0, n0, count, tc);
-      for (int i = threadIdx.x + count * W; i < kStates * W; i += kScanThreads) tA[i] = th[i] = tq[i] = 0.f;
+      if (n0) {
+        low_b.load(a.b, a.bs, p, t0, n0, count);
+        low_c.load(a.c, a.cs, p, t0, n0, count);
+      }
+      low_b.put(tb, p, t0, count);
+      low_c.put(tc, p, t0, count);
       load_channels<W>(a.A, p, a.N, n0, count, 1.f, tA);
       load_channels<W>(a.part + at_part, p, a.N, n0, count, 1.f, th);
       load_channels<W>(a.part_r + at_part, p, a.N, n0, count, 1.f, tq);
@@ -171,9 +223,9 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
 #pragma unroll
         for (int i = 0; i < kCh; ++i) {
           float skip = 0.f;
-          lane_tokens(ts, cl + 4 * i, tl, s[i]);
-          lane_tokens(tx, cl + 4 * i, tl, sx[i]);
-          lane_tokens(te, cl + 4 * i, tl, e[i]);
+          tile_load(ts, cl + 4 * i, tl, s[i]);
+          tile_load(tx, cl + 4 * i, tl, sx[i]);
+          tile_load(te, cl + 4 * i, tl, e[i]);
           ssum[i] = 0.f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -194,8 +246,8 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
         for (int k = 0; k < each; ++k) {
           const int n = ((turn + wave) % kScanWaves) * each + k;
           float Bv[8], Cv[8], dB[8], dC[8];
-          load8(tb + n * kTok + kLaneTok * tl, Bv);
-          load8(tc + n * kTok + kLaneTok * tl, Cv);
+          lane_load(tb + n * kTok, tl, Bv);
+          lane_load(tc + n * kTok, tl, Cv);
 #pragma unroll
           for (int i = 0; i < kCh; ++i) {
             const int at_c = n * W + cl + 4 * i;
@@ -212,8 +264,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
 #pragma unroll
             for (int j = 7; j >= 0; --j) Q = at[j] * (ce[j] + Q);
             float P = exp2_hw(ssum[i] * A2), P2 = P;
-            row_scan<false>(S, P, h);
-            row_scan<true>(Q, P2, q);
+            row_scan_both(S, P, h, Q, P2, q);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const float before = h;
@@ -237,19 +288,25 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
             if (tl == 15) th[at_c] = dA;   // h before the chunk has been read
           }
           f32x4 low = join_rows(dB, dC);
-          f32x4 *to = reinterpret_cast<f32x4 *>(tlow + (lane / 32 * kStates + n) * kTok + kLaneTok * tl +
-                                                (lane / 16 % 2) * 4);
+          f32x4 *to = reinterpret_cast<f32x4 *>(tlow + (lane / 32 * kStates + n) * kTok + 4 * tl +
+                                                (lane / 16 % 2) * 64);
           if (turn) low += *to;
           *to = low;
         }
         __syncthreads();
       }
-      for (int i = threadIdx.x; i < kTok * kStates; i += kScanThreads) {
-        const int n = i % kStates, t = i / kStates;
-        if (n >= count || t0 + t >= p.n) continue;
-        const int64_t at = ((((int64_t)p.tile * a.B + p.b) * a.L + t0 + t) * a.G + p.g) * a.N + n0 + n;
-        a.part_b[at] = tlow[n * kTok + t];
-        a.part_c[at] = tlow[(kStates + n) * kTok + t];
+      {
+        const int n = threadIdx.x % kStates, t1 = threadIdx.x / kStates;
+        const int64_t base = ((((int64_t)p.tile * a.B + p.b) * a.L + t0) * a.G + p.g) * a.N + n0 + n;
+        const int64_t stride = (int64_t)a.G * a.N;
+        const int left = (int)min((int64_t)kTok, p.n - t0);
+#pragma unroll
+        for (int i = 0; i < kTok * kStates / kScanThreads; ++i) {
+          const int t = t1 + i * (kScanThreads / kStates);
+          if (n >= count || t >= left) continue;
+          a.part_b[base + t * stride] = tlow[n * kTok + token_at(t)];
+          a.part_c[base + t * stride] = tlow[(kStates + n) * kTok + token_at(t)];
+        }
       }
     }
     if (!some) __syncthreads();
@@ -259,52 +316,72 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
   if (some) {
 #pragma unroll
     for (int i = 0; i < kCh; ++i) {   // in place of what only this lane has read
-      const int at = tile_at<float>(cl + 4 * i, kLaneTok * tl);
-      store8_lds(ts + at, ds[i]);
-      store8_lds(tx + at, dsx[i]);
-      store8_lds(te + at, y[i]);
+      tile_store(ts, cl + 4 * i, tl, ds[i]);
+      tile_store(tx, cl + 4 * i, tl, dsx[i]);
+      tile_store(te, cl + 4 * i, tl, y[i]);
     }
     __syncthreads();
   }
-  for (int i = threadIdx.x; i < kTok * (W / 8); i += kScanThreads) {
-    const int u = i % (W / 8), t = i / (W / 8), c = p.c0 + 8 * u;
-    const int64_t tt = t0 + t;
-    const bool row = tt < a.L && c < p.cend, live = tt < p.n && c < p.cend;
-    float dx[8], ddt[8], dz[8];
+  Steps<T, W> steps;
+  Gated<T> gated;
+  if (some) {
+    steps.load(a, p, t0);
+    gated.load(a, p, t0);
+  }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) dx[k] = ddt[k] = dz[k] = 0.f;
-    if (live) {
-      RowVec<T, 8> r;
-      float x[8], raw[8], do_[8], z[8];
-      r.load(static_cast<const T *>(a.x) + p.b * a.xs.b + tt * a.xs.t + c);
-      r.get(x);
-      r.load(static_cast<const T *>(a.dt) + p.b * a.dts.b + tt * a.dts.t + c);
-      r.get(raw);
-      gated<T>(a, p, tt, c, do_, z);
+  for (int i = 0; i < kLoads<W>; ++i) {
+    const Unit w = unit_of<W>(p, t0, i);
+    float dx[8], ddt[8], dz[8];
+    if (w.live) {
+      float x[8], raw[8], e[8], z[8], step[8];
+      steps.x[i].get(x);
+      steps.dt[i].get(raw);
+      gated.dy[i].get(e);
+      if (a.z) gated.z[i].get(z);
+      if (a.bias)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) raw[k] += a.bias[w.c + k];
+      float skip[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) skip[k] = 0.f;
+      if (a.skip)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) skip[k] = a.skip[w.c + k];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int at = tile_at<float>(8 * u + k, t);
-        const float v = a.bias ? raw[k] + a.bias[c + k] : raw[k], skip = a.skip ? a.skip[c + k] : 0.f;
-        const float step = a.softplus ? softplus(v) : v;
-        float ek = do_[k];
-        if (a.z) {
-          const float k1 = sigmoid(z[k]);
-          ek *= z[k] * k1;
-          dz[k] = do_[k] * fmaf(skip, x[k], te[at]) * (k1 * fmaf(z[k], 1.f - k1, 1.f));
-        }
+        const int at = tile_at(8 * w.u + k, w.t);
         const float d = tx[at];
-        dx[k] = fmaf(step, d, skip * ek);
         ddt[k] = fmaf(x[k], d, ts[at]);
-        if (a.softplus) ddt[k] *= sigmoid(v);
+        dx[k] = d;
       }
-    }
-    if (a.dbias && some)
+      if (a.softplus) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) ts[tile_at<float>(8 * u + k, t)] = ddt[k];
-    if (!row) continue;
-    store_row<8>(static_cast<T *>(a.dx) + p.b * a.dxs.b + tt * a.dxs.t + c, dx);
-    store_row<8>(static_cast<T *>(a.ddt) + p.b * a.ddts.b + tt * a.ddts.t + c, ddt);
-    if (a.z) store_row<8>(static_cast<T *>(a.dz) + p.b * a.dzs.b + tt * a.dzs.t + c, dz);
+        for (int k = 0; k < 8; ++k) {
+          step[k] = softplus(raw[k]);
+          ddt[k] *= softplus_slope(raw[k], step[k]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) step[k] = raw[k];
+      }
+      if (a.z)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float g = sigmoid(z[k]), y = fmaf(skip[k], x[k], te[tile_at(8 * w.u + k, w.t)]);
+          dz[k] = e[k] * y * (g * fmaf(z[k], 1.f - g, 1.f));
+          e[k] *= z[k] * g;
+        }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) dx[k] = fmaf(step[k], dx[k], skip[k] * e[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) dx[k] = ddt[k] = dz[k] = 0.f;
+    }
+    if (a.dbias && some) put_unit(ts, w, ddt);
+    if (w.t >= a.L - t0 || w.c >= p.cend) continue;
+    put_row<T>(a.dx, a.dxs, p, t0, w, dx);
+    put_row<T>(a.ddt, a.ddts, p, t0, w, ddt);
+    if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, dz);
   }
   if (some && !a.dbias) return;
   __syncthreads();
@@ -313,7 +390,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
     float v[8], total = 0.f;
     const int c = p.c0 + cl + 4 * i;
     if (some) {
-      lane_tokens(ts, cl + 4 * i, tl, v);
+      tile_load(ts, cl + 4 * i, tl, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) total += v[j];
       total = row_sum(total);
@@ -386,8 +463,7 @@ template <typename K> hipError_t launch_tiles(K kernel, const Scan &a, size_t ld
 }  // namespace
 
 hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st) {
-  const size_t lds = sizeof(float) * (2 * W * kTok + 2 * kStates * kTok + 3 * kStates * W) +
-                     (dt == Dt::BF16 ? 2 : 4) * W * kTok;
+  const size_t lds = sizeof(float) * (W * kTok + 2 * kStates * kTok + 3 * kStates * W);
   return dt == Dt::BF16 ? launch_tiles(k_scan_parts<bf16>, a, lds, st)
                         : launch_tiles(k_scan_parts<float>, a, lds, st);
 }

@@ -18,17 +18,32 @@ constexpr int kScanWaves = 8;
 constexpr int kScanThreads = 64 * kScanWaves;
 constexpr int kStates = 16;         // states of one pass over a chunk
 
-// Place of (channel of the tile, token) in a [channels][kTok] tile: groups of four (fp32) or
-// eight (bf16) tokens change places by channel, so that a row's eight channels, written as
-// eight columns, meet different banks. A lane's eight tokens stay together.
-template <typename T> __device__ __forceinline__ int tile_at(int c, int t) {
-  if constexpr (sizeof(T) == 2) return c * kTok + ((((t >> 3) ^ (c >> 3)) & 15) << 3) + (t & 7);
-  else return c * kTok + ((((t >> 2) ^ (c >> 3 << 1)) & 31) << 2) + (t & 3);
+// Place of token t in a row of kTok: the first halves of the lanes' eight tokens, then the second
+// halves, so that the 16 lanes of a row read 16 bytes each from all the banks at once.
+__device__ __forceinline__ int token_at(int t) { return (t >> 3 << 2) + (t & 3) + ((t & 4) << 4); }
+// Place of (channel of the tile, token) in a [channels][kTok] tile: the lanes' places change by
+// the channel's eight, so that eight columns written side by side meet different banks.
+__device__ __forceinline__ int tile_at(int c, int t) { return c * kTok + token_at(t ^ ((c >> 3 & 15) << 3)); }
+// The eight tokens of a lane (`lane` of the row, as in the tile at 0), to and from registers.
+__device__ __forceinline__ void lane_load(const float *row, int lane, float *v) {
+  const f32x4 a = *reinterpret_cast<const f32x4 *>(row + 4 * lane);
+  const f32x4 b = *reinterpret_cast<const f32x4 *>(row + 4 * lane + 64);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = a[i];
+    v[4 + i] = b[i];
+  }
 }
-template <typename T> __device__ __forceinline__ void lane_tokens(const T *tile, int c, int tl, float *v) {
-  RowVec<T, 8> r;
-  r.load(tile + tile_at<T>(c, kLaneTok * tl));
-  r.get(v);
+__device__ __forceinline__ void lane_store(float *row, int lane, const float *v) {
+  *reinterpret_cast<f32x4 *>(row + 4 * lane) = f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<f32x4 *>(row + 4 * lane + 64) = f32x4{v[4], v[5], v[6], v[7]};
+}
+// The same of channel c of a tile.
+__device__ __forceinline__ void tile_load(const float *tile, int c, int tl, float *v) {
+  lane_load(tile + c * kTok, tl ^ (c >> 3 & 15), v);
+}
+__device__ __forceinline__ void tile_store(float *tile, int c, int tl, const float *v) {
+  lane_store(tile + c * kTok, tl ^ (c >> 3 & 15), v);
 }
 
 // The state h before each lane's tokens: on entry h holds, in every lane, the state before
@@ -74,6 +89,22 @@ __device__ __forceinline__ void row_scan(float &S, float &P, float &h) {
   else asm(FAVOR_SCAN1_ALL("row_shr") : "+v"(S), "+v"(P), "+v"(h));
 }
 
+// Both at once: S, P and h from the left, Q, P2 and q from the right.
+__device__ __forceinline__ void row_scan_both(float &S, float &P, float &h, float &Q, float &P2, float &q) {
+#define FAVOR_SCAN_BOTH(n)                                            \
+  "v_fmac_f32_dpp %0, %0, %1 row_shr:" n " row_mask:0xf bank_mask:0xf\n" \
+  "v_fmac_f32_dpp %3, %3, %4 row_shl:" n " row_mask:0xf bank_mask:0xf\n"
+#define FAVOR_SCAN_BOTH_P(n)                                          \
+  "v_mul_f32_dpp %1, %1, %1 row_shr:" n " row_mask:0xf bank_mask:0xf\n" \
+  "v_mul_f32_dpp %4, %4, %4 row_shl:" n " row_mask:0xf bank_mask:0xf\n"
+  asm("s_nop 1\n" FAVOR_SCAN_BOTH("1") FAVOR_SCAN_BOTH_P("1") FAVOR_SCAN_BOTH("2") FAVOR_SCAN_BOTH_P("2")
+          FAVOR_SCAN_BOTH("4") FAVOR_SCAN_BOTH_P("4") FAVOR_SCAN_BOTH("8")
+      "s_nop 1\n"
+      "v_mov_b32_dpp %2, %0 row_shr:1 row_mask:0xf bank_mask:0xf\n"
+      "v_mov_b32_dpp %5, %3 row_shl:1 row_mask:0xf bank_mask:0xf\n"
+      : "+v"(S), "+v"(P), "+v"(h), "+v"(Q), "+v"(P2), "+v"(q));
+}
+
 // The sum over the 16 lanes of a row, in its last lane.
 __device__ __forceinline__ float row_sum(float v) {
   v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x111, 0xf, 0xf, true));
@@ -104,85 +135,135 @@ __device__ __forceinline__ ScanPlace scan_place(const Scan &a, int width) {
   return p;
 }
 
-// Steps s = softplus(dt + bias) of eight channels of one token.
+// What a thread loads of a tile of kWidth channels: kLoads units of eight channels of one token.
+template <int kWidth> constexpr int kLoads = kTok * kWidth / 8 / kScanThreads;
+struct Unit {
+  int u, t, c;   // unit, token of the chunk, channel
+  int tl, cl;    // the same where they are inside the sequence and the group, else others that are
+  bool live;     // they are
+};
+template <int kWidth>
+__device__ __forceinline__ Unit unit_of(const ScanPlace &p, int64_t t0, int i) {
+  const int k = threadIdx.x + i * kScanThreads;
+  Unit w;
+  w.u = k % (kWidth / 8);
+  w.t = k / (kWidth / 8);
+  w.c = p.c0 + 8 * w.u;
+  const int left = (int)min((int64_t)kTok, p.n - t0);
+  w.live = w.t < left && w.c < p.cend;
+  w.tl = min(w.t, left - 1);
+  w.cl = w.c < p.cend ? w.c : p.c0;
+  return w;
+}
+// Loads ask for valid rows whether they are wanted or not (a chunk that is read has a token): a
+// condition around each would wait for one before the next is requested.
+// Rows of one chunk: a uniform base and 32-bit offsets (tokens are at most 2^25 bytes apart).
 template <typename T>
-__device__ __forceinline__ void steps_of(const Scan &a, const RowVec<T, 8> &raw, int c, float *s) {
-  raw.get(s);
+__device__ __forceinline__ T *chunk_rows(T *base, const Rows &r, const ScanPlace &p, int64_t t0) {
+  return base + p.b * r.b + t0 * r.t;
+}
+template <typename T>
+__device__ __forceinline__ RowVec<T, 8> get_row(const void *base, const Rows &r, const ScanPlace &p, int64_t t0,
+                                                const Unit &w) {
+  RowVec<T, 8> v;
+  v.load(chunk_rows(static_cast<const T *>(base), r, p, t0) +
+         ((uint32_t)w.tl * (uint32_t)r.t + (uint32_t)w.cl));
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void put_row(void *base, const Rows &r, const ScanPlace &p, int64_t t0, const Unit &w,
+                                        const float *v) {
+  store_row<8>(chunk_rows(static_cast<T *>(base), r, p, t0) + ((uint32_t)w.t * (uint32_t)r.t + (uint32_t)w.c), v);
+}
+__device__ __forceinline__ void put_unit(float *tile, const Unit &w, const float *v) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    if (a.bias) s[k] += a.bias[c + k];
-    if (a.softplus) s[k] = softplus(s[k]);
-  }
+  for (int k = 0; k < 8; ++k) tile[tile_at(8 * w.u + k, w.t)] = v[k];
 }
 
-// s and x of the tile's tokens t0 .. (zeros behind the sequence and the group).
-template <typename T, int kWidth, typename X>
-__device__ __forceinline__ void load_steps(const Scan &a, const ScanPlace &p, int64_t t0, float *ts, X *tx) {
-  constexpr int units = kWidth / 8;
+// Steps s = softplus(dt + bias) of eight channels.
+__device__ __forceinline__ void steps_of(const Scan &a, const Unit &w, float *s) {
+  if (a.bias)
 #pragma unroll
-  for (int i = threadIdx.x; i < kTok * units; i += kScanThreads) {
-    const int u = i % units, t = i / units, c = p.c0 + 8 * u;
-    float s[8], x[8];
-    if (t0 + t < p.n && c < p.cend) {
-      RowVec<T, 8> rx, rd;
-      rx.load(static_cast<const T *>(a.x) + p.b * a.xs.b + (t0 + t) * a.xs.t + c);
-      rd.load(static_cast<const T *>(a.dt) + p.b * a.dts.b + (t0 + t) * a.dts.t + c);
-      steps_of<T>(a, rd, c, s);
-      rx.get(x);
-    } else {
+    for (int k = 0; k < 8; ++k) s[k] += a.bias[w.cl + k];
+  if (a.softplus)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] = x[k] = 0.f;
+    for (int k = 0; k < 8; ++k) s[k] = softplus(s[k]);
+}
+
+// x and dt of a thread's units as they lie in memory, requested together; then s and s x (or
+// x) of them. Zeros behind the sequence and the group.
+template <typename T, int kWidth> struct Steps {
+  RowVec<T, 8> x[kLoads<kWidth>], dt[kLoads<kWidth>];
+
+  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0) {
+#pragma unroll
+    for (int i = 0; i < kLoads<kWidth>; ++i) {
+      const Unit w = unit_of<kWidth>(p, t0, i);
+      x[i] = get_row<T>(a.x, a.xs, p, t0, w);
+      dt[i] = get_row<T>(a.dt, a.dts, p, t0, w);
     }
+  }
+  template <bool kProduct>
+  __device__ __forceinline__ void get(const Scan &a, const Unit &w, int i, float *s, float *v) const {
+    x[i].get(v);
+    dt[i].get(s);
+    steps_of(a, w, s);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      ts[tile_at<float>(8 * u + k, t)] = s[k];
-      tx[tile_at<X>(8 * u + k, t)] = from_f32<X>(x[k]);
+      s[k] = w.live ? s[k] : 0.f;
+      v[k] = w.live ? v[k] : 0.f;
+      if (kProduct) v[k] *= s[k];
     }
   }
-}
+};
 
-// [states][kTok] tile of B or C (src of type T): states n0 .., zeros behind the sequence.
-template <typename T>
-__device__ __forceinline__ void load_states(const void *src, const Rows &r, const ScanPlace &p, int64_t t0,
-                                            int n0, int count, float *tile) {
-  const T *base = static_cast<const T *>(src) + p.b * r.b + p.g * r.h + n0;
-  for (int i = threadIdx.x; i < kTok * kStates; i += kScanThreads) {
-    const int n = i % kStates, t = i / kStates;
-    float v = 0.f;
-    if (n < count && t0 + t < p.n) v = to_f32(base[(t0 + t) * r.t + n]);
-    tile[n * kTok + t] = v;
-  }
-}
+// [states][kTok] tile of B or C: states n0 .., zeros behind the sequence. A thread keeps its
+// state and takes every 32nd token.
+template <typename T> struct States {
+  static constexpr int kStep = kScanThreads / kStates, kEach = kTok / kStep;
+  T v[kEach];
 
-__device__ __forceinline__ void load8(const float *p, float *v) {
-  const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+  __device__ __forceinline__ void load(const void *src, const Rows &r, const ScanPlace &p, int64_t t0, int n0,
+                                       int count) {
+    const T *base = chunk_rows(static_cast<const T *>(src), r, p, t0) + p.g * r.h + n0;
+    const int left = (int)min((int64_t)kTok, p.n - t0);
+    const uint32_t n = min((int)threadIdx.x % kStates, count - 1);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = a[i];
-    v[4 + i] = b[i];
+    for (int i = 0; i < kEach; ++i) {
+      const uint32_t t = min((int)threadIdx.x / kStates + i * kStep, left - 1);
+      v[i] = base[t * (uint32_t)r.t + n];
+    }
   }
-}
-__device__ __forceinline__ void store8_lds(float *p, const float *v) {
-  reinterpret_cast<f32x4 *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-  reinterpret_cast<f32x4 *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
-}
+  __device__ __forceinline__ void put(float *tile, const ScanPlace &p, int64_t t0, int count) const {
+    const int n = threadIdx.x % kStates, t1 = threadIdx.x / kStates;
+    const int left = (int)min((int64_t)kTok, p.n - t0);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      tile[n * kTok + token_at(t1 + i * kStep)] =
+          n < count && t1 + i * kStep < left ? to_f32(v[i]) : 0.f;
+  }
+};
 
-// The tile's channels, states n0 .. n0 + count - 1, of a [D][N] array (null: zeros), to and
-// from [count][kWidth] in LDS.
+// The tile's channels, states n0 .. n0 + count - 1 (at most kStates), of a [D][N] array (null:
+// zeros), to and from [kStates][kWidth] in LDS; states behind them are zeros.
 template <int kWidth>
 __device__ __forceinline__ void load_channels(const float *src, const ScanPlace &p, int N, int n0, int count,
                                               float scale, float *dst) {
-  for (int i = threadIdx.x; i < kWidth * count; i += kScanThreads) {
-    const int c = i / count, n = i - c * count;
-    dst[n * kWidth + c] = src && p.c0 + c < p.cend ? scale * src[(int64_t)(p.c0 + c) * N + n0 + n] : 0.f;
+#pragma unroll
+  for (int i = 0; i < kWidth * kStates / kScanThreads; ++i) {
+    const int k = threadIdx.x + i * kScanThreads, c = k / kStates, n = k % kStates;
+    float v = 0.f;
+    if (src) v = src[(int64_t)min(p.c0 + c, p.cend - 1) * N + n0 + min(n, count - 1)];
+    dst[n * kWidth + c] = n < count ? scale * v : 0.f;
   }
 }
 template <int kWidth>
 __device__ __forceinline__ void store_channels(float *dst, const ScanPlace &p, int N, int n0, int count,
                                                const float *src) {
-  for (int i = threadIdx.x; i < kWidth * count; i += kScanThreads) {
-    const int c = i / count, n = i - c * count;
-    if (p.c0 + c < p.cend) dst[(int64_t)(p.c0 + c) * N + n0 + n] = src[n * kWidth + c];
+#pragma unroll
+  for (int i = 0; i < kWidth * kStates / kScanThreads; ++i) {
+    const int k = threadIdx.x + i * kScanThreads, c = k / kStates, n = k % kStates;
+    if (n < count && p.c0 + c < p.cend) dst[(int64_t)(p.c0 + c) * N + n0 + n] = src[n * kWidth + c];
   }
 }
 

@@ -76,15 +76,16 @@ __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float rcp_hw(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ __forceinline__ float sigmoid(float x) { return rcp_hw(1.f + exp2_hw(-kLog2e * x)); }
 
-// max(x, 0) + log(1 + e), e = exp(-|x|). log(1 + e) = e log(u) / (u - 1) with u = 1 + e as
-// rounded (Kahan): the quotient's errors cancel, so it keeps its relative precision as e
-// falls. Where u rounds to 1 it is e itself.
+// max(x, 0) + log(1 + e), e = exp(-|x|). With u = 1 + e as rounded, log(1 + e) is log(u) + (what
+// the rounding left of e) / u, and u is 1 where that matters; so it keeps its relative
+// precision as e falls, down to e itself.
 __device__ __forceinline__ float softplus(float x) {
   const float e = exp2_hw(-kLog2e * fabsf(x));
-  const float u = 1.f + e, d = u - 1.f;
-  const float l = d > 0.f ? kLn2 * __builtin_amdgcn_logf(u) * (e * rcp_hw(d)) : e;
-  return fmaxf(x, 0.f) + (x != x ? x : l);
+  const float u = 1.f + e;
+  return fmaf(0.5f, x + fabsf(x), fmaf(kLn2, __builtin_amdgcn_logf(u), e - (u - 1.f)));
 }
+// softplus' slope at x, of which s is softplus(x): e^x / (1 + e^x) = e^(x - s).
+__device__ __forceinline__ float softplus_slope(float x, float s) { return exp2_hw(kLog2e * (x - s)); }
 
 // Sequences that hold the same place of a pool take their turns in order, all in the first
 // one's workgroup. Returns the sequence that follows b at its place (B: none), or -1 where b
