@@ -48,6 +48,7 @@ struct Scan {
   Rows xs, dts, bs, cs, zs, ys;
   int B, L, D, N, G, softplus;
   int chunks, nseg;                 // chunks of kScanTokens tokens in one segment; segments
+  int subs;                         // backward: tiles of one workgroup
   // nseg > 1: the states before each segment [B][nseg][D][N] (first: the segments' sums) and
   // the segments' sums of s [B][nseg][D]
   float *part, *steps;
@@ -60,16 +61,17 @@ struct Scan {
   float *part_r;                    // as part, for the gradient of the state, from the right
   float *part_a;                    // [B][nseg][D][N] sums of dA
   float *part_d, *part_s;           // [B][nseg][D] sums of dskip and of ddt
-  float *part_b, *part_c;           // [tiles of a group][B][L][G][N]
+  float *part_b, *part_c;           // [workgroups of a group's channels][B][L][G][N]
   Rows dys, dxs, ddts, dbs, dcs, dzs;
   // single tokens: h_out is the pool [n_slots][D][N]
   const int32_t *slots;
   int n_slots;
 };
 constexpr int kScanTokens = 128;     // of one chunk
-constexpr int kScanBackTile = 64;    // channels of one workgroup of the backward pass
-// The segments' sums, in part and steps; backward, where a segment is one chunk: in part_r too.
-hipError_t launch_scan_sums(const Scan &a, Dt dt, int tile, hipStream_t st);
+constexpr int kScanBackTile = 32;    // channels of one tile of the backward pass
+// The sums of the segments but the last, in part and steps; backward, where a segment is one
+// chunk: of all of them, and in part_r too.
+hipError_t launch_scan_sums(const Scan &a, Dt dt, hipStream_t st);
 hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st);
 // part (part_r): from sums to the states before (behind) each segment; backward: dh_in.
 hipError_t launch_scan_prefix(const Scan &a, bool backward, hipStream_t st);

@@ -170,20 +170,39 @@ favor_status validate(const favor_scan_desc *g, int op) {
   return FAVOR_OK;
 }
 
-// How a forward call is cut: channels of one workgroup, and segments of whole chunks.
+// How a forward call is cut: channels of one workgroup, and segments of whole chunks. A call
+// of several segments takes the sums of all but the last first, so their steps and decays are
+// computed twice. Whole calls in us, bf16, N = 16:
+//   One segment while its workgroups of 32 channels fill the 256 compute units, as long as
+//   there are 240 of them: B4 L4096 D2048 (256) 267, in two segments 281, in eight 289.
+//   Fewer: segments for 2048 workgroups. B1 L65536 D2048 in 8 / 16 / 32 segments 1266 / 1203 /
+//   1166; B1 L4096 in 8 / 32 96 / 89, in one 260; B6 L1999 D1000 N24 fp32 (192) in 8 180, in one
+//   210.
+//   Workgroups of 64 channels read B and C for twice as many, but have half the waves: from 512
+//   of them on, B8 L4096 D4096 736 instead of 770, with 256 of them (D2048) 452 instead of 433.
+//   In fp32 they spill.
 struct ScanCut {
   int tile, chunks, nseg;
 };
-constexpr int kScanBlocks = 2048;
+constexpr int kOneSegment = 240, kSegmentBlocks = 2048, kWideBlocks = 512;
 ScanCut cut_of(const favor_scan_desc *g) {
   ScanCut c;
-  c.tile = 32;
-  const int chunks = chunks_of(g);
-  const int64_t blocks = (int64_t)g->B * tiles_of(g, c.tile);
-  const int want = (int)std::min<int64_t>(std::max(chunks, 1), std::max<int64_t>(1, kScanBlocks / blocks));
-  c.chunks = std::max(1, (chunks + want - 1) / want);
-  c.nseg = std::max(1, (chunks + c.chunks - 1) / c.chunks);
+  const int chunks = std::max(chunks_of(g), 1);
+  const int64_t narrow = (int64_t)g->B * tiles_of(g, 32), wide = (int64_t)g->B * tiles_of(g, 64);
+  const int64_t want = narrow >= kOneSegment ? 1 : std::max<int64_t>(1, kSegmentBlocks / std::max<int64_t>(narrow, 1));
+  c.chunks = (int)((chunks + want - 1) / want);
+  c.nseg = (chunks + c.chunks - 1) / c.chunks;
+  c.tile = wide >= kWideBlocks && g->N <= 128 && dt_of(g->dtype) == Dt::BF16 ? 64 : 32;
   return c;
+}
+
+// Tiles that one workgroup of the backward pass takes one after the other.
+int subs_of(const favor_scan_desc *g) {
+  if (g->N > 16) return 1;   // dB and dC of more states do not stay in LDS
+  const int64_t rows = (int64_t)g->B * chunks_of(g);
+  for (int subs = 4; subs > 1; subs /= 2)
+    if (rows * tiles_of(g, subs * favor::kScanBackTile) >= 1024) return subs;
+  return 1;
 }
 
 // Parts of a workspace, each 256-byte aligned.
@@ -209,8 +228,8 @@ size_t carve_forward(const favor_scan_desc *g, const ScanCut &c, void *ws, favor
 size_t carve_backward(const favor_scan_desc *g, void *ws, favor::Scan *a) {
   Carver w{static_cast<char *>(ws)};
   const size_t BD = (size_t)g->B * chunks_of(g) * g->D;
-  const size_t low = (size_t)((g->D / g->groups + favor::kScanBackTile - 1) / favor::kScanBackTile) *
-                     g->B * g->L * g->groups * g->N;
+  const size_t low = (size_t)(tiles_of(g, subs_of(g) * favor::kScanBackTile) / g->groups) * g->B *
+                     g->L * g->groups * g->N;
   a->part = w.floats(BD * g->N);
   a->part_r = w.floats(BD * g->N);
   a->part_a = w.floats(BD * g->N);
@@ -473,7 +492,7 @@ favor_status favor_selective_scan(const favor_scan_desc *g, const void *x, const
     hipError_t e;
     {
       favor::LaunchTimer t(favor::kKerScanSums, stream);
-      e = favor::launch_scan_sums(a, type, g->N <= 128 ? 64 : 32, stream);
+      e = favor::launch_scan_sums(a, type, stream);
     }
     if (e != hipSuccess) return device_result(e, "favor_selective_scan segment sums");
     favor::LaunchTimer t(favor::kKerScanPrefix, stream);
@@ -532,6 +551,7 @@ favor_status favor_selective_scan_backward(
   a.h_in = state_in;
   a.chunks = 1;
   a.nseg = chunks_of(g);
+  a.subs = subs_of(g);
   a.dy = dy;
   a.dh_out = dstate_out;
   a.dh_in = dstate_in;

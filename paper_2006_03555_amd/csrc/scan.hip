@@ -66,7 +66,7 @@ __device__ __forceinline__ void forward_state(const float (&s)[kCh][8], const fl
 
 // kOut: the rows y and the state after the last token. Otherwise the sums of the segments.
 template <typename T, int kCh, bool kOut>
-__global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
+__global__ __launch_bounds__(kScanThreads, kOut && kCh == 2 ? 4 : 6) void k_scan(Scan a) {
   constexpr int W = kWide<kCh>;
   extern __shared__ __align__(16) float lds[];
   float *tile = lds, *tb = tile + W * kTok, *tc = tb + kStates * kTok;
@@ -80,8 +80,8 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
   if (kOut && a.nseg > 1) h0 = a.part + at_part;
   else if (kOut && a.h_in) h0 = a.h_in + p.b * DN;
   for (int n0 = 0; n0 < a.N; n0 += kStates) {
-    load_channels<W>(a.A, p, a.N, n0, min(kStates, a.N - n0), kLog2e, tA + n0 * W);
-    load_channels<W>(h0, p, a.N, n0, min(kStates, a.N - n0), 1.f, th + n0 * W);
+    load_channels<W>(a.A, p, a.N, n0, min(kStates, a.N - n0), kLog2e, tA + n0 * W, threadIdx.x);
+    load_channels<W>(h0, p, a.N, n0, min(kStates, a.N - n0), 1.f, th + n0 * W, threadIdx.x);
   }
   float seg_steps[kCh] = {};
   const int first = p.seg * a.chunks, last = min(first + a.chunks, (a.L + kTok - 1) / kTok);
@@ -89,6 +89,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
     const int64_t t0 = (int64_t)chunk * kTok;
     const bool some = t0 < p.n;
     if (!some && !kOut) break;
+    int tid = fresh_thread();
     if (some) {
       float s[kCh][8], sx[kCh][8], ssum[kCh], y[kCh][8];
       States<T> low_b, low_c;
@@ -96,22 +97,22 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
         // everything is requested at once; the tile holds the steps, then s x, then y
         Steps<T, W> steps;
         float in[kLoads<W>][8], own[kLoads<W>][8];
-        steps.load(a, p, t0);
-        low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N));
-        if (kOut) low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N));
+        steps.load(a, p, t0, tid);
+        low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
+        if (kOut) low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
 #pragma unroll
-        for (int i = 0; i < kLoads<W>; ++i) steps.template get<true>(a, unit_of<W>(p, t0, i), i, own[i], in[i]);
+        for (int i = 0; i < kLoads<W>; ++i) steps.template get<true>(a, unit_of<W>(p, t0, i, tid), i, own[i], in[i]);
         __syncthreads();   // the last chunk's rows have been read
 #pragma unroll
-        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i), own[i]);
+        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i, tid), own[i]);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, s[i]);
-        low_b.put(tb, p, t0, min(kStates, a.N));
-        if (kOut) low_c.put(tc, p, t0, min(kStates, a.N));
+        low_b.put(tb, p, t0, min(kStates, a.N), tid);
+        if (kOut) low_c.put(tc, p, t0, min(kStates, a.N), tid);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i), in[i]);
+        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i, tid), in[i]);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kCh; ++i) {
@@ -128,28 +129,19 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
       for (int n0 = 0; n0 < a.N; n0 += kStates) {
         const int count = min(kStates, a.N - n0);
         if (n0) {
-          low_b.load(a.b, a.bs, p, t0, n0, count);
-          if (kOut) low_c.load(a.c, a.cs, p, t0, n0, count);
+          tid = fresh_thread();
+          low_b.load(a.b, a.bs, p, t0, n0, count, tid);
+          if (kOut) low_c.load(a.c, a.cs, p, t0, n0, count, tid);
           __syncthreads();   // the last states' B and C have been read
-          low_b.put(tb, p, t0, count);
-          if (kOut) low_c.put(tc, p, t0, count);
+          low_b.put(tb, p, t0, count, tid);
+          if (kOut) low_c.put(tc, p, t0, count, tid);
           __syncthreads();
         }
-        // each state's values are read while the one before it is computed
-        StateIn<kCh, kOut> even, odd;
-        const auto read = [&](StateIn<kCh, kOut> &in, int n) {
-          n = min(n, count - 1);
+        for (int n = 0; n < count; ++n) {
           const int at = (n0 + n) * W + cl;
+          StateIn<kCh, kOut> in;
           in.load(tb + n * kTok, tc + n * kTok, tA + at, th + at, tl);
-        };
-        read(even, 0);
-        for (int n = 0; n < count; n += 2) {
-          float *carry = th + (n0 + n) * W + cl;
-          read(odd, n + 1);
-          forward_state<kCh, kOut>(s, sx, ssum, even, carry, tl, y);
-          if (n + 1 == count) break;
-          read(even, n + 2);
-          forward_state<kCh, kOut>(s, sx, ssum, odd, carry + W, tl, y);
+          forward_state<kCh, kOut>(s, sx, ssum, in, th + at, tl, y);
         }
       }
       if (kOut) {
@@ -158,10 +150,11 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
       }
     }
     RowVec<T, 8> rx[kLoads<W>], rz[kLoads<W>];
+    tid = fresh_thread();
     if (kOut && some) {
 #pragma unroll
       for (int i = 0; i < kLoads<W>; ++i) {
-        const Unit w = unit_of<W>(p, t0, i);
+        const Unit w = unit_of<W>(p, t0, i, tid);
         if (a.skip) rx[i] = get_row<T>(a.x, a.xs, p, t0, w);
         if (a.z) rz[i] = get_row<T>(a.z, a.zs, p, t0, w);
       }
@@ -170,7 +163,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i);
+      const Unit w = unit_of<W>(p, t0, i, tid);
       if (w.t >= a.L - t0 || w.c >= p.cend) continue;
       float y[8], v[8];
       if (w.live) {
@@ -199,7 +192,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan(Scan a) {
   else if (a.h_out && p.seg == a.nseg - 1) end = a.h_out + p.b * DN;
   if (end)
     for (int n0 = 0; n0 < a.N; n0 += kStates)
-      store_channels<W>(end, p, a.N, n0, min(kStates, a.N - n0), th + n0 * W);
+      store_channels<W>(end, p, a.N, n0, min(kStates, a.N - n0), th + n0 * W, threadIdx.x);
   if (!kOut) {
 #pragma unroll
     for (int i = 0; i < kCh; ++i) {
@@ -260,21 +253,19 @@ template <typename T, int kCh, bool kOut> hipError_t launch_as(const Scan &a, hi
     if (e != hipSuccess) return e;
   }
   const int tiles = a.G * ((a.D / a.G + W - 1) / W);
-  kernel<<<dim3((unsigned)(tiles * a.nseg), a.B), kScanThreads, lds, st>>>(a);
+  const int segments = kOut ? a.nseg : a.nseg - 1;   // nothing follows the last segment's sums
+  kernel<<<dim3((unsigned)(tiles * segments), a.B), kScanThreads, lds, st>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_scan(const Scan &a, Dt dt, int tile, hipStream_t st) {
-  if (tile == kWide<2>)
-    return dt == Dt::BF16 ? launch_as<bf16, 2, true>(a, st) : launch_as<float, 2, true>(a, st);
-  return dt == Dt::BF16 ? launch_as<bf16, 1, true>(a, st) : launch_as<float, 1, true>(a, st);
+  if (dt == Dt::F32) return launch_as<float, 1, true>(a, st);
+  return tile == kWide<2> ? launch_as<bf16, 2, true>(a, st) : launch_as<bf16, 1, true>(a, st);
 }
 
-hipError_t launch_scan_sums(const Scan &a, Dt dt, int tile, hipStream_t st) {
-  if (tile == kWide<2>)
-    return dt == Dt::BF16 ? launch_as<bf16, 2, false>(a, st) : launch_as<float, 2, false>(a, st);
+hipError_t launch_scan_sums(const Scan &a, Dt dt, hipStream_t st) {
   return dt == Dt::BF16 ? launch_as<bf16, 1, false>(a, st) : launch_as<float, 1, false>(a, st);
 }
 

@@ -17,19 +17,20 @@
 namespace favor {
 namespace {
 
-constexpr int W = kScanBackTile;
-constexpr int kCh = 2;
-static_assert(W == 4 * kScanWaves * kCh, "a workgroup's channels");
+// Channels per lane and workgroup of the first pass and of the third.
+constexpr int kCh = 2, W = 4 * kScanWaves * kCh;
+constexpr int kTile = kScanBackTile;
+static_assert(kTile == 4 * kScanWaves, "one channel per lane");
 
 // dy and z of a thread's units as they lie in memory; then e = dy silu(z). Zeros behind the
 // sequence and the group.
-template <typename T> struct Gated {
-  RowVec<T, 8> dy[kLoads<W>], z[kLoads<W>];
+template <typename T, int kWidth> struct Gated {
+  RowVec<T, 8> dy[kLoads<kWidth>], z[kLoads<kWidth>];
 
-  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0) {
+  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0, int tid) {
 #pragma unroll
-    for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i);
+    for (int i = 0; i < kLoads<kWidth>; ++i) {
+      const Unit w = unit_of<kWidth>(p, t0, i, tid);
       dy[i] = get_row<T>(a.dy, a.dys, p, t0, w);
       if (a.z) z[i] = get_row<T>(a.z, a.zs, p, t0, w);
     }
@@ -52,6 +53,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
   float *tile = lds, *tb = tile + W * kTok, *tc = tb + kStates * kTok;
   float *tA = tc + kStates * kTok, *th = tA + kStates * W, *tq = th + kStates * W;
   const ScanPlace p = scan_place(a, W);
+  int tid = threadIdx.x;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
   const int cl = 4 * kCh * wave + lane / 16;
   const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
@@ -68,15 +70,15 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
   {
     // everything is requested at once; the tile holds the steps, then s x, then e
     Steps<T, W> steps;
-    Gated<T> gated;
+    Gated<T, W> gated;
     float in[kLoads<W>][8];
-    steps.load(a, p, t0);
-    gated.load(a, p, t0);
-    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N));
-    low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N));
+    steps.load(a, p, t0, tid);
+    gated.load(a, p, t0, tid);
+    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
+    low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
 #pragma unroll
     for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i);
+      const Unit w = unit_of<W>(p, t0, i, tid);
       float own[8];
       steps.template get<true>(a, w, i, own, in[i]);
       put_unit(tile, w, own);
@@ -86,14 +88,14 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
     for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, s[i]);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i), in[i]);
+    for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i, tid), in[i]);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, sx[i]);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i);
+      const Unit w = unit_of<W>(p, t0, i, tid);
       gated.get(a, w, i, in[i]);
       put_unit(tile, w, in[i]);
     }
@@ -101,12 +103,12 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
   for (int n0 = 0; n0 < a.N; n0 += kStates) {
     const int count = min(kStates, a.N - n0);
     if (n0) {
-      low_b.load(a.b, a.bs, p, t0, n0, count);
-      low_c.load(a.c, a.cs, p, t0, n0, count);
+      low_b.load(a.b, a.bs, p, t0, n0, count, tid);
+      low_c.load(a.c, a.cs, p, t0, n0, count, tid);
     }
-    low_b.put(tb, p, t0, count);
-    low_c.put(tc, p, t0, count);
-    load_channels<W>(a.A, p, a.N, n0, count, kLog2e, tA);
+    low_b.put(tb, p, t0, count, tid);
+    low_c.put(tc, p, t0, count, tid);
+    load_channels<W>(a.A, p, a.N, n0, count, kLog2e, tA, tid);
     __syncthreads();
     if (n0 == 0) {
 #pragma unroll
@@ -147,8 +149,9 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
       }
     }
     __syncthreads();
-    store_channels<W>(a.part + at_part, p, a.N, n0, count, th);
-    store_channels<W>(a.part_r + at_part, p, a.N, n0, count, tq);
+    tid = fresh_thread();
+    store_channels<W>(a.part + at_part, p, a.N, n0, count, th, tid);
+    store_channels<W>(a.part_r + at_part, p, a.N, n0, count, tq, tid);
   }
 }
 
@@ -171,106 +174,119 @@ __device__ __forceinline__ f32x4 join_rows(const float (&v)[8], const float (&w)
   return o;
 }
 
-template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_backward(Scan a) {
+// A workgroup takes a.subs tiles of kTile channels one after the other, so that dB and dC are
+// sums over all of them before they leave it.
+template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_backward(Scan a) {
   extern __shared__ __align__(16) float lds[];
-  float *ts = lds, *tx = ts + W * kTok, *te = tx + W * kTok;
-  float *tb = te + W * kTok, *tc = tb + kStates * kTok;
+  float *t1 = lds, *t2 = t1 + kTile * kTok, *tb = t2 + kTile * kTok, *tc = tb + kStates * kTok;
   float *tlow = tc + kStates * kTok;   // dB, then dC
-  float *tA = tlow + 2 * kStates * kTok, *th = tA + kStates * W, *tq = th + kStates * W;
-  const ScanPlace p = scan_place(a, W);
+  float *tA = tlow + 2 * kStates * kTok, *th = tA + kStates * kTile, *tq = th + kStates * kTile;
+  ScanPlace p = scan_place(a, kTile * a.subs);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
-  const int cl = 4 * kCh * wave + lane / 16;
+  const int cl = 4 * wave + lane / 16;
   const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
   const int64_t at_sum = ((int64_t)p.b * a.nseg + p.seg) * a.D;
   const int64_t t0 = (int64_t)p.seg * kTok;
   const bool some = t0 < p.n;
-  float s[kCh][8], sx[kCh][8], e[kCh][8], ds[kCh][8], dsx[kCh][8], y[kCh][8], ssum[kCh];
-  States<T> low_b, low_c;
-  if (some) {
-    Steps<T, W> steps;
-    Gated<T> gated;
-    steps.load(a, p, t0);
-    gated.load(a, p, t0);
-    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N));
-    low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N));
-#pragma unroll
-    for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i);
-      float own[8], x[8];
-      steps.template get<false>(a, w, i, own, x);
-      put_unit(ts, w, own);
-      put_unit(tx, w, x);
-      gated.get(a, w, i, x);
-      put_unit(te, w, x);
-    }
-  }
-  for (int n0 = 0; n0 < a.N; n0 += kStates) {
-    const int count = min(kStates, a.N - n0);
+  for (int sub = 0; sub < a.subs && p.c0 < p.cend; ++sub, p.c0 += kTile) {
+    const int c = p.c0 + cl;   // this lane's channel
+    const bool channel = c < p.cend;
+    static_assert(kLoads<kTile> == 1, "one unit of a thread");
     if (!some) {
-      for (int i = threadIdx.x; i < W * kStates; i += kScanThreads) th[i] = 0.f;
-    } else {
-      if (n0) {
-        low_b.load(a.b, a.bs, p, t0, n0, count);
-        low_c.load(a.c, a.cs, p, t0, n0, count);
+      for (int i = threadIdx.x; i < min(kTile, p.cend - p.c0) * a.N; i += kScanThreads)
+        a.part_a[at_part + (int64_t)p.c0 * a.N + i] = 0.f;
+      if (tl == 15 && channel) {
+        if (a.dskip) a.part_d[at_sum + c] = 0.f;
+        if (a.dbias) a.part_s[at_sum + c] = 0.f;
       }
-      low_b.put(tb, p, t0, count);
-      low_c.put(tc, p, t0, count);
-      load_channels<W>(a.A, p, a.N, n0, count, 1.f, tA);
-      load_channels<W>(a.part + at_part, p, a.N, n0, count, 1.f, th);
-      load_channels<W>(a.part_r + at_part, p, a.N, n0, count, 1.f, tq);
-      __syncthreads();
-      if (n0 == 0) {
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) {
+      const Unit w = unit_of<kTile>(p, t0, 0, threadIdx.x);
+      const float none[8] = {};
+      if (w.t >= a.L - t0 || w.c >= p.cend) continue;
+      put_row<T>(a.dx, a.dxs, p, t0, w, none);
+      put_row<T>(a.ddt, a.ddts, p, t0, w, none);
+      if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, none);
+    } else {
+      float s[8], sx[8], e[8], ds[8], dsx[8], y[8], ssum = 0.f;
+      States<T> low_b, low_c;
+      int tid = fresh_thread();
+      {
+        const Unit w = unit_of<kTile>(p, t0, 0, tid);
+        Steps<T, kTile> steps;
+        Gated<T, kTile> gated;
+        float own[8], x[8];
+        steps.load(a, p, t0, tid);
+        gated.load(a, p, t0, tid);
+        if (sub == 0) {
+          low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
+          low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
+        }
+        steps.template get<false>(a, w, 0, own, x);
+        put_unit(t1, w, own);   // the last tile's readers are behind a barrier
+        put_unit(t2, w, x);
+        __syncthreads();
+        tile_load(t1, cl, tl, s);
+        tile_load(t2, cl, tl, sx);
+        __syncthreads();
+        gated.get(a, w, 0, x);
+        put_unit(t1, w, x);
+      }
+      for (int n0 = 0; n0 < a.N; n0 += kStates) {
+        const int count = min(kStates, a.N - n0);
+        if (n0) {
+          tid = fresh_thread();
+          low_b.load(a.b, a.bs, p, t0, n0, count, tid);
+          low_c.load(a.c, a.cs, p, t0, n0, count, tid);
+        }
+        if (sub == 0) {
+          low_b.put(tb, p, t0, count, tid);
+          low_c.put(tc, p, t0, count, tid);
+        }
+        load_channels<kTile>(a.A, p, a.N, n0, count, 1.f, tA, tid);
+        load_channels<kTile>(a.part + at_part, p, a.N, n0, count, 1.f, th, tid);
+        load_channels<kTile>(a.part_r + at_part, p, a.N, n0, count, 1.f, tq, tid);
+        __syncthreads();
+        if (n0 == 0) {
+          tile_load(t1, cl, tl, e);
           float skip = 0.f;
-          tile_load(ts, cl + 4 * i, tl, s[i]);
-          tile_load(tx, cl + 4 * i, tl, sx[i]);
-          tile_load(te, cl + 4 * i, tl, e[i]);
-          ssum[i] = 0.f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            skip = fmaf(e[i][j], sx[i][j], skip);
-            sx[i][j] *= s[i][j];
-            ssum[i] += s[i][j];
-            ds[i][j] = dsx[i][j] = y[i][j] = 0.f;
+            skip = fmaf(e[j], sx[j], skip);
+            sx[j] *= s[j];
+            ssum += s[j];
+            ds[j] = dsx[j] = y[j] = 0.f;
           }
           if (a.dskip) {
             const float total = row_sum(skip);
-            const int c = p.c0 + cl + 4 * i;
-            if (tl == 15 && c < p.cend) a.part_d[at_sum + c] = total;
+            if (tl == 15 && channel) a.part_d[at_sum + c] = total;
           }
         }
-      }
-      const int each = (count + kScanWaves - 1) / kScanWaves;   // states of a wave's turn
-      for (int turn = 0; turn < kScanWaves; ++turn) {
-        for (int k = 0; k < each; ++k) {
-          const int n = ((turn + wave) % kScanWaves) * each + k;
-          float Bv[8], Cv[8], dB[8], dC[8];
-          lane_load(tb + n * kTok, tl, Bv);
-          lane_load(tc + n * kTok, tl, Cv);
-#pragma unroll
-          for (int i = 0; i < kCh; ++i) {
-            const int at_c = n * W + cl + 4 * i;
+        const int each = (count + kScanWaves - 1) / kScanWaves;   // states of a wave's turn
+        for (int turn = 0; turn < kScanWaves; ++turn) {
+          for (int k = 0; k < each; ++k) {
+            const int n = ((turn + wave) % kScanWaves) * each + k, at_c = n * kTile + cl;
+            float Bv[8], Cv[8], at[8], bx[8], ce[8], dB[8], dC[8];
+            lane_load(tb + n * kTok, tl, Bv);
+            lane_load(tc + n * kTok, tl, Cv);
             const float A = tA[at_c], A2 = kLog2e * A;
-            float h = th[at_c], q = tq[at_c], at[8], bx[8], ce[8];
+            float h = th[at_c], q = tq[at_c];
             float S = tl == 0 ? h : 0.f, Q = tl == 15 ? q : 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              at[j] = exp2_hw(s[i][j] * A2);
-              bx[j] = sx[i][j] * Bv[j];
-              ce[j] = e[i][j] * Cv[j];
+              at[j] = exp2_hw(s[j] * A2);
+              bx[j] = sx[j] * Bv[j];
+              ce[j] = e[j] * Cv[j];
               S = fmaf(at[j], S, bx[j]);
             }
 #pragma unroll
             for (int j = 7; j >= 0; --j) Q = at[j] * (ce[j] + Q);
-            float P = exp2_hw(ssum[i] * A2), P2 = P;
+            float P = exp2_hw(ssum * A2), P2 = P;
             row_scan_both(S, P, h, Q, P2, q);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const float before = h;
               h = fmaf(at[j], h, bx[j]);
-              dC[j] = i ? fmaf(e[i][j], h, dC[j]) : e[i][j] * h;
-              y[i][j] = fmaf(Cv[j], h, y[i][j]);
+              dC[j] = e[j] * h;
+              y[j] = fmaf(Cv[j], h, y[j]);
               bx[j] = before;
             }
             float dA = 0.f;
@@ -278,126 +294,114 @@ template <typename T> __global__ __launch_bounds__(kScanThreads) void k_scan_bac
             for (int j = 7; j >= 0; --j) {
               const float g = ce[j] + q;
               q = at[j] * g;
-              dB[j] = i ? fmaf(g, sx[i][j], dB[j]) : g * sx[i][j];
-              dsx[i][j] = fmaf(g, Bv[j], dsx[i][j]);
+              dB[j] = g * sx[j];
+              dsx[j] = fmaf(g, Bv[j], dsx[j]);
               const float u = q * bx[j];
-              ds[i][j] = fmaf(A, u, ds[i][j]);
-              dA = fmaf(s[i][j], u, dA);
+              ds[j] = fmaf(A, u, ds[j]);
+              dA = fmaf(s[j], u, dA);
             }
             dA = row_sum(dA);
             if (tl == 15) th[at_c] = dA;   // h before the chunk has been read
+            f32x4 low = join_rows(dB, dC);
+            f32x4 *to = reinterpret_cast<f32x4 *>(tlow + (lane / 32 * kStates + n) * kTok + 4 * tl +
+                                                  (lane / 16 % 2) * 64);
+            if (turn || sub) low += *to;
+            *to = low;
           }
-          f32x4 low = join_rows(dB, dC);
-          f32x4 *to = reinterpret_cast<f32x4 *>(tlow + (lane / 32 * kStates + n) * kTok + 4 * tl +
-                                                (lane / 16 % 2) * 64);
-          if (turn) low += *to;
-          *to = low;
+          __syncthreads();
         }
+        tid = fresh_thread();
+        if (sub + 1 == a.subs || p.c0 + kTile >= p.cend) {
+          const int n = tid % kStates, first = tid / kStates;
+          const int64_t base = ((((int64_t)p.tile * a.B + p.b) * a.L + t0) * a.G + p.g) * a.N + n0 + n;
+          const int64_t stride = (int64_t)a.G * a.N;
+          const int left = (int)min((int64_t)kTok, p.n - t0);
+#pragma unroll
+          for (int i = 0; i < kTok * kStates / kScanThreads; ++i) {
+            const int t = first + i * (kScanThreads / kStates);
+            if (n >= count || t >= left) continue;
+            a.part_b[base + t * stride] = tlow[n * kTok + token_at(t)];
+            a.part_c[base + t * stride] = tlow[(kStates + n) * kTok + token_at(t)];
+          }
+        }
+        store_channels<kTile>(a.part_a + at_part, p, a.N, n0, count, th, tid);
         __syncthreads();
       }
-      {
-        const int n = threadIdx.x % kStates, t1 = threadIdx.x / kStates;
-        const int64_t base = ((((int64_t)p.tile * a.B + p.b) * a.L + t0) * a.G + p.g) * a.N + n0 + n;
-        const int64_t stride = (int64_t)a.G * a.N;
-        const int left = (int)min((int64_t)kTok, p.n - t0);
-#pragma unroll
-        for (int i = 0; i < kTok * kStates / kScanThreads; ++i) {
-          const int t = t1 + i * (kScanThreads / kStates);
-          if (n >= count || t >= left) continue;
-          a.part_b[base + t * stride] = tlow[n * kTok + token_at(t)];
-          a.part_c[base + t * stride] = tlow[(kStates + n) * kTok + token_at(t)];
-        }
-      }
-    }
-    if (!some) __syncthreads();
-    store_channels<W>(a.part_a + at_part, p, a.N, n0, count, th);
-    __syncthreads();
-  }
-  if (some) {
-#pragma unroll
-    for (int i = 0; i < kCh; ++i) {   // in place of what only this lane has read
-      tile_store(ts, cl + 4 * i, tl, ds[i]);
-      tile_store(tx, cl + 4 * i, tl, dsx[i]);
-      tile_store(te, cl + 4 * i, tl, y[i]);
-    }
-    __syncthreads();
-  }
-  Steps<T, W> steps;
-  Gated<T> gated;
-  if (some) {
-    steps.load(a, p, t0);
-    gated.load(a, p, t0);
-  }
-#pragma unroll
-  for (int i = 0; i < kLoads<W>; ++i) {
-    const Unit w = unit_of<W>(p, t0, i);
-    float dx[8], ddt[8], dz[8];
-    if (w.live) {
-      float x[8], raw[8], e[8], z[8], step[8];
-      steps.x[i].get(x);
-      steps.dt[i].get(raw);
-      gated.dy[i].get(e);
-      if (a.z) gated.z[i].get(z);
-      if (a.bias)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) raw[k] += a.bias[w.c + k];
-      float skip[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) skip[k] = 0.f;
-      if (a.skip)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) skip[k] = a.skip[w.c + k];
+      tid = fresh_thread();
+      const Unit w = unit_of<kTile>(p, t0, 0, tid);
+      Steps<T, kTile> steps;
+      Gated<T, kTile> gated;
+      float dx[8], ddt[8], dz[8];
+      steps.load(a, p, t0, tid);
+      gated.load(a, p, t0, tid);
+      tile_store(t1, cl, tl, ds);   // in place of what only this lane has read
+      tile_store(t2, cl, tl, dsx);
+      __syncthreads();
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int at = tile_at(8 * w.u + k, w.t);
-        const float d = tx[at];
-        ddt[k] = fmaf(x[k], d, ts[at]);
-        dx[k] = d;
+        ddt[k] = t1[at];
+        dx[k] = t2[at];
       }
-      if (a.softplus) {
+      __syncthreads();
+      if (a.z) tile_store(t1, cl, tl, y);
+      __syncthreads();
+      if (w.live) {
+        float x[8], raw[8], ev[8], z[8], step[8], skip[8];
+        steps.x[0].get(x);
+        steps.dt[0].get(raw);
+        gated.dy[0].get(ev);
+        if (a.z) gated.z[0].get(z);
+        if (a.bias)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          step[k] = softplus(raw[k]);
-          ddt[k] *= softplus_slope(raw[k], step[k]);
+          for (int k = 0; k < 8; ++k) raw[k] += a.bias[w.c + k];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) skip[k] = 0.f;
+        if (a.skip)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) skip[k] = a.skip[w.c + k];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) ddt[k] = fmaf(x[k], dx[k], ddt[k]);
+        if (a.softplus) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            step[k] = softplus(raw[k]);
+            ddt[k] *= softplus_slope(raw[k], step[k]);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) step[k] = raw[k];
         }
+        if (a.z)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float g = sigmoid(z[k]), v = fmaf(skip[k], x[k], t1[tile_at(8 * w.u + k, w.t)]);
+            dz[k] = ev[k] * v * (g * fmaf(z[k], 1.f - g, 1.f));
+            ev[k] *= z[k] * g;
+          }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dx[k] = fmaf(step[k], dx[k], skip[k] * ev[k]);
       } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) step[k] = raw[k];
+        for (int k = 0; k < 8; ++k) dx[k] = ddt[k] = dz[k] = 0.f;
       }
-      if (a.z)
+      if (w.t < a.L - t0 && w.c < p.cend) {
+        put_row<T>(a.dx, a.dxs, p, t0, w, dx);
+        put_row<T>(a.ddt, a.ddts, p, t0, w, ddt);
+        if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, dz);
+      }
+      if (a.dbias) {
+        float v[8], total = 0.f;
+        put_unit(t2, w, ddt);
+        __syncthreads();
+        tile_load(t2, cl, tl, v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float g = sigmoid(z[k]), y = fmaf(skip[k], x[k], te[tile_at(8 * w.u + k, w.t)]);
-          dz[k] = e[k] * y * (g * fmaf(z[k], 1.f - g, 1.f));
-          e[k] *= z[k] * g;
-        }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) dx[k] = fmaf(step[k], dx[k], skip[k] * e[k]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) dx[k] = ddt[k] = dz[k] = 0.f;
+        for (int j = 0; j < 8; ++j) total += v[j];
+        total = row_sum(total);
+        if (tl == 15 && channel) a.part_s[at_sum + c] = total;
+      }
+      __syncthreads();
     }
-    if (a.dbias && some) put_unit(ts, w, ddt);
-    if (w.t >= a.L - t0 || w.c >= p.cend) continue;
-    put_row<T>(a.dx, a.dxs, p, t0, w, dx);
-    put_row<T>(a.ddt, a.ddts, p, t0, w, ddt);
-    if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, dz);
-  }
-  if (some && !a.dbias) return;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kCh; ++i) {
-    float v[8], total = 0.f;
-    const int c = p.c0 + cl + 4 * i;
-    if (some) {
-      tile_load(ts, cl + 4 * i, tl, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) total += v[j];
-      total = row_sum(total);
-    }
-    if (tl != 15 || c >= p.cend) continue;
-    if (a.dbias) a.part_s[at_sum + c] = total;
-    if (a.dskip && !some) a.part_d[at_sum + c] = 0.f;
   }
 }
 
@@ -451,11 +455,12 @@ __global__ __launch_bounds__(kSumCols *kSumLanes) void k_scan_params(Scan a, int
   dst[col] = s;
 }
 
-template <typename K> hipError_t launch_tiles(K kernel, const Scan &a, size_t lds, hipStream_t st) {
+template <typename K>
+hipError_t launch_tiles(K kernel, const Scan &a, int width, size_t lds, hipStream_t st) {
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  const int tiles = a.G * ((a.D / a.G + W - 1) / W);
+  const int tiles = a.G * ((a.D / a.G + width - 1) / width);
   kernel<<<dim3((unsigned)(tiles * a.nseg), a.B), kScanThreads, lds, st>>>(a);
   return hipGetLastError();
 }
@@ -464,20 +469,20 @@ template <typename K> hipError_t launch_tiles(K kernel, const Scan &a, size_t ld
 
 hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st) {
   const size_t lds = sizeof(float) * (W * kTok + 2 * kStates * kTok + 3 * kStates * W);
-  return dt == Dt::BF16 ? launch_tiles(k_scan_parts<bf16>, a, lds, st)
-                        : launch_tiles(k_scan_parts<float>, a, lds, st);
+  return dt == Dt::BF16 ? launch_tiles(k_scan_parts<bf16>, a, W, lds, st)
+                        : launch_tiles(k_scan_parts<float>, a, W, lds, st);
 }
 
 hipError_t launch_scan_backward(const Scan &a, Dt dt, hipStream_t st) {
-  const size_t lds = sizeof(float) * (3 * W * kTok + 4 * kStates * kTok + 3 * kStates * W);
-  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, lds, st)
-                        : launch_tiles(k_scan_backward<float>, a, lds, st);
+  const size_t lds = sizeof(float) * (2 * kTile * kTok + 4 * kStates * kTok + 3 * kStates * kTile);
+  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, kTile * a.subs, lds, st)
+                        : launch_tiles(k_scan_backward<float>, a, kTile * a.subs, lds, st);
 }
 
 hipError_t launch_scan_backward_sums(const Scan &a, Dt dt, hipStream_t st) {
   const int64_t low = (int64_t)a.L * a.G * a.N;
   if (low > 0) {
-    const int tiles = (a.D / a.G + W - 1) / W;
+    const int tiles = (a.D / a.G + kTile * a.subs - 1) / (kTile * a.subs);
     const dim3 grid((unsigned)((low + kLowThreads - 1) / kLowThreads), a.B, 2);
     if (dt == Dt::BF16) k_scan_low<bf16><<<grid, kLowThreads, 0, st>>>(a, tiles);
     else k_scan_low<float><<<grid, kLowThreads, 0, st>>>(a, tiles);

@@ -135,6 +135,14 @@ __device__ __forceinline__ ScanPlace scan_place(const Scan &a, int width) {
   return p;
 }
 
+// The thread's number, as a value that each use forms its addresses from anew: kept over a whole
+// loop they would take the registers that the scan needs.
+__device__ __forceinline__ int fresh_thread() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 // What a thread loads of a tile of kWidth channels: kLoads units of eight channels of one token.
 template <int kWidth> constexpr int kLoads = kTok * kWidth / 8 / kScanThreads;
 struct Unit {
@@ -143,8 +151,8 @@ struct Unit {
   bool live;     // they are
 };
 template <int kWidth>
-__device__ __forceinline__ Unit unit_of(const ScanPlace &p, int64_t t0, int i) {
-  const int k = threadIdx.x + i * kScanThreads;
+__device__ __forceinline__ Unit unit_of(const ScanPlace &p, int64_t t0, int i, int tid) {
+  const int k = tid + i * kScanThreads;
   Unit w;
   w.u = k % (kWidth / 8);
   w.t = k / (kWidth / 8);
@@ -195,10 +203,10 @@ __device__ __forceinline__ void steps_of(const Scan &a, const Unit &w, float *s)
 template <typename T, int kWidth> struct Steps {
   RowVec<T, 8> x[kLoads<kWidth>], dt[kLoads<kWidth>];
 
-  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0) {
+  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0, int tid) {
 #pragma unroll
     for (int i = 0; i < kLoads<kWidth>; ++i) {
-      const Unit w = unit_of<kWidth>(p, t0, i);
+      const Unit w = unit_of<kWidth>(p, t0, i, tid);
       x[i] = get_row<T>(a.x, a.xs, p, t0, w);
       dt[i] = get_row<T>(a.dt, a.dts, p, t0, w);
     }
@@ -224,18 +232,18 @@ template <typename T> struct States {
   T v[kEach];
 
   __device__ __forceinline__ void load(const void *src, const Rows &r, const ScanPlace &p, int64_t t0, int n0,
-                                       int count) {
+                                       int count, int tid) {
     const T *base = chunk_rows(static_cast<const T *>(src), r, p, t0) + p.g * r.h + n0;
     const int left = (int)min((int64_t)kTok, p.n - t0);
-    const uint32_t n = min((int)threadIdx.x % kStates, count - 1);
+    const uint32_t n = min(tid % kStates, count - 1);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const uint32_t t = min((int)threadIdx.x / kStates + i * kStep, left - 1);
+      const uint32_t t = min(tid / kStates + i * kStep, left - 1);
       v[i] = base[t * (uint32_t)r.t + n];
     }
   }
-  __device__ __forceinline__ void put(float *tile, const ScanPlace &p, int64_t t0, int count) const {
-    const int n = threadIdx.x % kStates, t1 = threadIdx.x / kStates;
+  __device__ __forceinline__ void put(float *tile, const ScanPlace &p, int64_t t0, int count, int tid) const {
+    const int n = tid % kStates, t1 = tid / kStates;
     const int left = (int)min((int64_t)kTok, p.n - t0);
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
@@ -248,10 +256,10 @@ template <typename T> struct States {
 // zeros), to and from [kStates][kWidth] in LDS; states behind them are zeros.
 template <int kWidth>
 __device__ __forceinline__ void load_channels(const float *src, const ScanPlace &p, int N, int n0, int count,
-                                              float scale, float *dst) {
+                                              float scale, float *dst, int tid) {
 #pragma unroll
   for (int i = 0; i < kWidth * kStates / kScanThreads; ++i) {
-    const int k = threadIdx.x + i * kScanThreads, c = k / kStates, n = k % kStates;
+    const int k = tid + i * kScanThreads, c = k / kStates, n = k % kStates;
     float v = 0.f;
     if (src) v = src[(int64_t)min(p.c0 + c, p.cend - 1) * N + n0 + min(n, count - 1)];
     dst[n * kWidth + c] = n < count ? scale * v : 0.f;
@@ -259,10 +267,10 @@ __device__ __forceinline__ void load_channels(const float *src, const ScanPlace 
 }
 template <int kWidth>
 __device__ __forceinline__ void store_channels(float *dst, const ScanPlace &p, int N, int n0, int count,
-                                               const float *src) {
+                                               const float *src, int tid) {
 #pragma unroll
   for (int i = 0; i < kWidth * kStates / kScanThreads; ++i) {
-    const int k = threadIdx.x + i * kScanThreads, c = k / kStates, n = k % kStates;
+    const int k = tid + i * kScanThreads, c = k / kStates, n = k % kStates;
     if (n < count && p.c0 + c < p.cend) dst[(int64_t)(p.c0 + c) * N + n0 + n] = src[n * kWidth + c];
   }
 }
