@@ -19,6 +19,7 @@ namespace {
 constexpr int kMaxN = 64;
 constexpr int kCandidates = 256;   // of one tile, before it is taken in parts
 constexpr int kPieceWaves = 4;
+constexpr int kFew = 12;           // candidates that are put in one by one
 
 // Whole numbers in the order of the floats (-0 as 0); 0 is below every one of them.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -35,15 +36,32 @@ __device__ __forceinline__ uint64_t read_lane(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
+// The wave's number as a scalar: what follows from it is the same in all lanes.
+__device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+// The lanes of `who` before this one.
+__device__ __forceinline__ int before(uint64_t who) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+}
 // Orders a wave's LDS accesses against its own later ones.
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 
+// The largest of three, without the care for signalling NaNs.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+// Maxima whose product with log2 e is in range.
+constexpr float kScaled = 1e38f;
+__device__ __forceinline__ float scaled_to(float m) { return fminf(fmaxf(m, -kScaled), kScaled); }
+__device__ __forceinline__ float scaled(float m) { return scaled_to(m) * kLog2e; }
+
 // The n best keys of a wave: lane r has the r-th (0: none).
 struct WaveBest {
-  uint64_t *list, *sorted;   // LDS of this wave: kCandidates + kMaxN, kMaxN
+  uint64_t *list, *sorted;   // LDS of this wave: kCandidates + kMaxN + 8, kMaxN
   uint64_t top = 0, last = 0;
   int n;
 
@@ -51,15 +69,17 @@ struct WaveBest {
   __device__ __forceinline__ void join(int count) {
     const int lane = threadIdx.x % 64;
     const int have = __popcll(__ballot(top != 0));
-    if (top) list[count + lane] = top;
-    wave_fence();
     const int total = count + have;
+    if (top) list[count + lane] = top;
+    if (lane < 8) list[total + lane] = 0;   // whole groups of eight are read below
+    wave_fence();
     for (int i0 = 0; i0 < total; i0 += 64) {
       const int i = i0 + lane;
       const uint64_t mine = i < total ? list[i] : 0;
       int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < total; ++j) rank += list[j] > mine;
+      for (int j = 0; j < total; j += 8)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) rank += list[j + k] > mine;
       if (i < total && rank < n) sorted[rank] = mine;
     }
     wave_fence();
@@ -67,90 +87,136 @@ struct WaveBest {
     wave_fence();
     last = read_lane(top, n - 1);
   }
+  // One key, the same in all lanes: those behind it move on by a lane.
+  __device__ __forceinline__ void insert(uint64_t key) {
+    if (key <= last) return;
+    const int rank = __popcll(__ballot(top > key)), lane = threadIdx.x % 64;
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)top, 0x138, 0xf, 0xf, false);   // wave_shr:1
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(top >> 32), 0x138, 0xf, 0xf, false);
+    if (lane > rank) top = (uint64_t)hi << 32 | lo;
+    if (lane == rank) top = key;
+    if (lane >= n) top = 0;
+    last = read_lane(top, n - 1);
+  }
   // One key per lane (0: none).
   __device__ __forceinline__ void push(uint64_t key) {
     const bool better = key > last;
     const uint64_t who = __ballot(better);
     if (!who) return;
-    if (better) list[__popcll(who & ((1ull << (threadIdx.x % 64)) - 1))] = key;
+    if (better) list[before(who)] = key;
     join(__popcll(who));
   }
 };
 
-template <typename T> __device__ __forceinline__ void load_logits(const T *p, float *x) {
-  RowVec<T, 8> r;   // rows start anywhere: the hardware takes any alignment
-  __builtin_memcpy(&r, p, sizeof(r));
-  r.get(x);
-}
-
+// E logits per lane and tile; the next tile is requested before this one is looked at.
 template <typename T, int E>
 __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) {
-  __shared__ uint64_t lists[kPieceWaves][kCandidates + 2 * kMaxN];
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int64_t id = (int64_t)blockIdx.x * kPieceWaves + wave;
-  const int row = (int)(id / a.pieces), piece = (int)(id - (int64_t)row * a.pieces);
-  if (row >= a.B * a.K || (a.ended && a.ended[row])) return;
-  const T *x0 = static_cast<const T *>(a.logits) + row / a.K * a.ls.b + row % a.K * a.ls.h;
-  const int begin = piece * a.piece_len, end = min(begin + a.piece_len, a.V);
+  __shared__ uint64_t lists[kPieceWaves][kCandidates + 2 * kMaxN + 8];
+  constexpr int kTile = 64 * E;
+  const int wave = uniform_wave(), lane = threadIdx.x % 64;
+  const int of_row = (a.pieces + kPieceWaves - 1) / kPieceWaves;
+  const int row = blockIdx.x / of_row, piece = blockIdx.x % of_row * kPieceWaves + wave;
+  if (piece >= a.pieces || (a.ended && a.ended[row])) return;
+  const int64_t id = (int64_t)row * a.pieces + piece;
+  const int begin = piece * a.piece_len, left = min(a.piece_len, a.V - begin);
+  const T *x0 = static_cast<const T *>(a.logits) + row / a.K * a.ls.b + row % a.K * a.ls.h + begin + 8 * lane;
   WaveBest best;
   best.list = lists[wave];
-  best.sorted = lists[wave] + kCandidates + kMaxN;
+  best.sorted = lists[wave] + kCandidates + kMaxN + 8;
   best.n = a.n;
-  float m = -INFINITY, sum = 0.f;
-  for (int64_t t0 = begin; t0 < end; t0 += 64 * E) {
-    float x[E];
-    const bool whole = t0 + 64 * E <= end;
+  // sum of 2^(x log2 e - c), c = m log2 e as rounded: one fused multiply-add before each
+  // exponential. A NaN makes the sum one, +Inf makes it infinite.
+  float m = -INFINITY, c = -INFINITY, sum = 0.f;
+  const auto look = [&](const float (&x)[E], int t0) {   // a tile's values, -Inf behind the piece
+    float most = max3(x[0], x[1], x[2]);
 #pragma unroll
-    for (int v = 0; v < E / 8; ++v) {
-      const int64_t t = t0 + 512 * v + 8 * lane;
-      if (whole) load_logits(x0 + t, x + 8 * v);
-      else
+    for (int i = 3; i + 1 < E; i += 2) most = max3(most, x[i], x[i + 1]);
+    most = max3(most, x[E - 1], x[E - 1]);
+    m = max3(m, most, most);
+    const float now = scaled(m);
+    sum *= exp2_hw(c - now);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[8 * v + i] = t + i < end ? to_f32(x0[t + i]) : -INFINITY;
-    }
-    float most = x[0];
-#pragma unroll
-    for (int i = 1; i < E; ++i) most = fmaxf(most, x[i]);
-    // a piece of -Inf alone has the sum 0, one with a NaN or +Inf the sum NaN
-    const float higher = fmaxf(m, most), ref = higher == -INFINITY ? 0.f : higher;
-    sum *= exp2_hw((m - ref) * kLog2e);
-#pragma unroll
-    for (int i = 0; i < E; ++i) sum += exp2_hw((x[i] - ref) * kLog2e);
-    m = higher;
+    for (int i = 0; i < E; ++i) sum += exp2_hw(fmaf(x[i], kLog2e, -now));
+    c = now;
     float bound = best.last ? unordered((uint32_t)(best.last >> 32)) : -INFINITY;
-    if (t0 == begin) {
+    if (t0 == 0) {
       int groups = 1;
       while (groups < a.n) groups *= 2;
       bound = most;
       for (int d = groups; d < 64; d *= 2) bound = fmaxf(bound, __shfl_xor(bound, d));
       for (int d = 1; d < groups; d *= 2) bound = fminf(bound, __shfl_xor(bound, d));
     }
-    if (!__ballot(most >= bound)) continue;
+    if (!__ballot(most >= bound)) return;
     int count = 0;
+    const int t1 = begin + t0 + 8 * lane;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const int token = (int)(t0 + 512 * (i / 8) + 8 * lane + i % 8);
-      const bool in = x[i] >= bound && (whole || token < end);
+      const bool in = x[i] >= bound;   // (tokens behind the piece are -Inf, which is never offered)
       const uint64_t who = __ballot(in);
       if (!who) continue;
-      const int at = count + __popcll(who & ((1ull << lane) - 1));
-      if (in && at < kCandidates) best.list[at] = key_of(x[i], token);
+      const int at = count + before(who);
+      if (in && at < kCandidates) best.list[at] = key_of(x[i], t1 + 512 * (i / 8) + i % 8);
       count += __popcll(who);
     }
-    if (count <= kCandidates) {
-      if (count) best.join(count);
+    if (count <= kFew) {
+      wave_fence();
+      for (int i = 0; i < count; ++i) best.insert(best.list[i]);
+      wave_fence();
+    } else if (count <= kCandidates) {
+      best.join(count);
     } else {   // a row of many equal or rising logits
-#pragma unroll
       for (int i = 0; i < E; ++i) {
-        const int token = (int)(t0 + 512 * (i / 8) + 8 * lane + i % 8);
-        best.push(whole || token < end ? key_of(x[i], token) : 0);
+        const int t = t0 + 512 * (i / 8) + i % 8;
+        best.push(8 * lane + t < left ? key_of(to_f32(x0[t]), begin + 8 * lane + t) : 0);
       }
     }
+  };
+  // Whole tiles, the next one requested before this one is looked at (two sets of registers in
+  // turn, and requests without conditions: the last ones ask for a tile once more; a copy or a
+  // choice would wait for them). Rows start anywhere: any alignment will do.
+  using Raw = RowVec<T, 8>[E / 8];
+  const auto request = [&](Raw &to, int t0) {
+    const T *p = x0 + min(t0, left - kTile);
+#pragma unroll
+    for (int v = 0; v < E / 8; ++v) __builtin_memcpy(&to[v], p + 512 * v, sizeof(to[v]));
+  };
+  const auto take = [&](const Raw &from, int t0) {
+    float x[E];
+#pragma unroll
+    for (int v = 0; v < E / 8; ++v) from[v].get(x + 8 * v);
+    look(x, t0);
+  };
+  int t0 = 0;
+  if (left >= kTile) {
+    Raw even, odd;
+    request(even, 0);
+    for (;;) {
+      request(odd, t0 + kTile);
+      take(even, t0);
+      if ((t0 += kTile) + kTile > left) break;
+      request(even, t0 + kTile);
+      take(odd, t0);
+      if ((t0 += kTile) + kTile > left) break;
+    }
+  }
+  if (t0 < left) {
+    float x[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int t = t0 + 512 * (i / 8) + i % 8;
+      x[i] = 8 * lane + t < left ? to_f32(x0[t]) : -INFINITY;
+    }
+    look(x, t0);
   }
   float top = m;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  double total = (double)sum * exp2_hw((m - (top == -INFINITY ? 0.f : top)) * kLog2e);
+  sum *= exp2_hw(fmaf(-scaled_to(top), kLog2e, c));   // what c's rounding left is in it
+  if (fabsf(top) > kScaled && fabsf(top) < INFINITY) {   // log2 e times it is no number: once more
+    sum = 0.f;
+    for (int t = lane; t < left; t += 64) sum += exp2_hw((to_f32(x0[t - 8 * lane]) - top) * kLog2e);
+  }
+  double total = sum;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
   if (lane == 0) a.stats[id] = float2{top, (float)total};
@@ -161,10 +227,10 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
 // among all beams' (in a sorted list by halving).
 constexpr int kMergeWaves = 8;
 __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
-  __shared__ uint64_t lists[kMergeWaves][kCandidates + 2 * kMaxN];
+  __shared__ uint64_t lists[kMergeWaves][kCandidates + 2 * kMaxN + 8];
   extern __shared__ double score[];   // [K][n], best first
   int *token = reinterpret_cast<int *>(score + a.K * a.n), *count = token + a.K * a.n;
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, b = blockIdx.x, n = a.n;
+  const int wave = uniform_wave(), lane = threadIdx.x % 64, b = blockIdx.x, n = a.n;
   for (int k = wave; k < a.K; k += kMergeWaves) {
     const int64_t row = (int64_t)b * a.K + k;
     const double own = a.scores[row];
@@ -186,7 +252,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
     const double rest = log(sum);   // of the log-sum, beyond the maximum, which may be huge
     WaveBest best;
     best.list = lists[wave];
-    best.sorted = lists[wave] + kCandidates + kMaxN;
+    best.sorted = lists[wave] + kCandidates + kMaxN + 8;
     best.n = n;
     const int keys = a.pieces * n;
     for (int i = lane; i - lane < keys; i += 64)
@@ -295,9 +361,8 @@ __global__ __launch_bounds__(kCopyThreads) void k_beam_reorder(BeamReorder a) {
 }
 
 template <typename T> hipError_t launch_pieces_as(const BeamSelect &a, hipStream_t st) {
-  const int64_t waves = (int64_t)a.B * a.K * a.pieces;
-  const unsigned blocks = (unsigned)((waves + kPieceWaves - 1) / kPieceWaves);
-  if (a.piece_len >= 2048) k_beam_pieces<T, 32><<<blocks, 64 * kPieceWaves, 0, st>>>(a);
+  const unsigned blocks = (unsigned)(a.B * a.K * ((a.pieces + kPieceWaves - 1) / kPieceWaves));
+  if (a.piece_len >= 1024) k_beam_pieces<T, 16><<<blocks, 64 * kPieceWaves, 0, st>>>(a);
   else k_beam_pieces<T, 8><<<blocks, 64 * kPieceWaves, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -62,6 +62,15 @@ inline favor_status check_apart(const void *out, const char *name, const void *i
   return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s overlaps %s", name, other);
 }
 
+// The same of an output and an input of any sizes.
+inline favor_status check_disjoint(const void *out, const char *name, int64_t out_bytes,
+                                   const void *in, const char *other, int64_t in_bytes) {
+  if (!out || !in) return FAVOR_OK;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(out), b = reinterpret_cast<uintptr_t>(in);
+  if (a >= b ? a - b >= (uint64_t)in_bytes : b - a >= (uint64_t)out_bytes) return FAVOR_OK;
+  return fail(FAVOR_ERR_INVALID_ARGUMENT, "%s overlaps %s", name, other);
+}
+
 inline favor_status device_result(hipError_t e, const char *what) {
   if (e != hipSuccess) return fail(FAVOR_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
   return ok();

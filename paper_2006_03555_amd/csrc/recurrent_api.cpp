@@ -635,9 +635,16 @@ favor_status favor_beam_select(const favor_beam_desc *g, const void *logits, con
   FAVOR_TRY(check_ptr(out_scores, "out_scores", work, 4));
   FAVOR_TRY(check_ptr(parent, "parent", work, 4));
   FAVOR_TRY(check_ptr(token, "token", work, 4));
-  // the last launch reads scores and ended while others' rows are written
-  const int64_t outs = (int64_t)4 * g->B * g->n, ins = (int64_t)4 * g->B * g->K;
-  FAVOR_TRY(check_apart(out_scores, "out_scores", scores, "scores", std::max(outs, ins), false));
+  // entries are written while others' scores and ended are read
+  const int64_t outs = (int64_t)4 * g->B * g->n, ins = (int64_t)g->B * g->K;
+  const void *out[] = {out_scores, parent, token};
+  const char *names[] = {"out_scores", "parent", "token"};
+  for (int i = 0; i < 3; ++i) {
+    FAVOR_TRY(check_disjoint(out[i], names[i], outs, scores, "scores", 4 * ins));
+    FAVOR_TRY(check_disjoint(out[i], names[i], outs, ended, "ended", ins));
+    for (int j = 0; j < i; ++j)
+      FAVOR_TRY(check_disjoint(out[i], names[i], outs, out[j], names[j], outs));
+  }
   if (!work) return ok();
   size_t keys_at;
   FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g, &keys_at)));
