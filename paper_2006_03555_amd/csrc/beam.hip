@@ -254,9 +254,22 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
     best.list = lists[wave];
     best.sorted = lists[wave] + kCandidates + kMaxN + 8;
     best.n = n;
-    const int keys = a.pieces * n;
-    for (int i = lane; i - lane < keys; i += 64)
-      best.push(i < keys ? a.keys[row * keys + i] : 0);
+    // the k-th best of the pieces' r-th keys has r k >= n keys not below it: only those are joined
+    const int keys = a.pieces * n, r = (n + a.pieces - 1) / a.pieces;
+    WaveBest column = best;
+    column.n = (n + r - 1) / r;
+    column.push(lane < a.pieces ? a.keys[row * keys + lane * n + r - 1] : 0);
+    const uint64_t bound = column.last ? column.last : 1;
+    int held = 0;
+    for (int i = lane; i - lane < keys; i += 64) {
+      const uint64_t key = i < keys ? a.keys[row * keys + i] : 0;
+      const uint64_t who = __ballot(key >= bound);
+      if (key >= bound) best.list[held + before(who)] = key;
+      held += __popcll(who);
+      if (held <= kCandidates - 64 && i - lane + 64 < keys) continue;
+      if (held) best.join(held);
+      held = 0;
+    }
     const float x = unordered((uint32_t)(best.top >> 32));
     const double s = own + (((double)x - top) - rest);
     const bool offered = best.top && s - s == 0.0;
