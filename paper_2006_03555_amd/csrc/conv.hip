@@ -69,14 +69,15 @@ __global__ __launch_bounds__(kConvThreads) void k_conv(Conv a) {
       store_row<V>(so + (int64_t)i * a.D, v);
     }
   }
-  const int t1 = min(t0 + a.run, a.L);
-  for (int t = t0; t < t1; t += kAhead) {
-    RowVec<T, V> r[kAhead];
+  // Four rows at a time, the next four requested before: two sets of registers in turn, and
+  // requests without conditions (a row behind the last asks for the last one).
+  const int t1 = min(t0 + a.run, a.L), last = min(n, t1) - 1;
+  using Raw = RowVec<T, V>[kAhead];
+  const auto request = [&](Raw &r, int t) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (t + i < min(n, t1)) r[i].load(x + (t + i) * a.xs.t);
-      else r[i].zero();
-    }
+    for (int i = 0; i < kAhead; ++i) r[i].load(x + min(t + i, last) * a.xs.t);
+  };
+  const auto rows = [&](const Raw &r, int t) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (t + i >= t1) break;
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(kConvThreads) void k_conv(Conv a) {
         for (int j = 0; j < W - 1; ++j) u[k] = fmaf(w[k][j], win[j][k], u[k]);
         u[k] = fmaf(w[k][W - 1], v[k], u[k]);
         if (a.silu) u[k] *= sigmoid(u[k]);
-        if (t + i >= n) u[k] = 0.f;
+        if (t + i > last) u[k] = 0.f;
       }
       store_row<V>(y + (t + i) * a.ys.t, u);
 #pragma unroll
@@ -99,7 +100,20 @@ __global__ __launch_bounds__(kConvThreads) void k_conv(Conv a) {
         win[W - 2][k] = v[k];
       }
     }
+  };
+  int t = t0;
+  if (last >= t0) {
+    Raw even, odd;
+    request(even, t);
+    for (; t <= last; t += 2 * kAhead) {
+      request(odd, t + kAhead);
+      rows(even, t);
+      request(even, t + 2 * kAhead);
+      rows(odd, t + kAhead);
+    }
   }
+  const float none[V] = {};   // rows behind the sequence
+  for (; t < t1; ++t) store_row<V>(y + t * a.ys.t, none);
 }
 
 // A workgroup takes `units_wide` neighbouring units by 256 / units_wide runs, and sums the
@@ -108,7 +122,7 @@ constexpr int kBackWide = 16;
 template <typename T> constexpr int back_vec(int W) {
   return sizeof(T) == 2 && W <= 4 ? 8 : 4;   // more taps of more channels spill
 }
-constexpr int kBackRun = 32;
+constexpr int kBackRun = 32, kBackAhead = 2;   // rows in flight twice
 
 template <typename T, int W, int V>
 __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide, int tiles) {
@@ -155,25 +169,25 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide
       r.get(win[i + 1]);
     }
     // dx of token s needs g up to s + W - 1: the run's last tokens read W - 1 rows past it
-    const int end = min(t0 + kBackRun, a.L) + W - 1;
-    for (int t = t0; t < end; t += kAhead) {
-      RowVec<T, V> rx[kAhead], rd[kAhead];
+    const int end = min(t0 + kBackRun, a.L) + W - 1, last = min(n, end) - 1;
+    struct Raw {
+      RowVec<T, V> x[kBackAhead], d[kBackAhead];
+    };
+    const auto request = [&](Raw &r, int t) {   // as forward
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        if (t + i < min(n, end)) {
-          rx[i].load(x + (t + i) * a.xs.t);
-          rd[i].load(dy + (t + i) * a.dys.t);
-        } else {
-          rx[i].zero();
-          rd[i].zero();
-        }
+      for (int i = 0; i < kBackAhead; ++i) {
+        const int at = min(t + i, last);
+        r.x[i].load(x + at * a.xs.t);
+        r.d[i].load(dy + at * a.dys.t);
       }
+    };
+    const auto rows = [&](const Raw &r, int t) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
+      for (int i = 0; i < kBackAhead; ++i) {
         const int tt = t + i;
         if (tt >= end) break;
         float d[V], o[V];
-        rd[i].get(d);
+        r.d[i].get(d);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
 #pragma unroll
@@ -182,8 +196,8 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide
             g[j][k] = g[j + 1][k];
           }
         }
-        rx[i].get(win[W - 1]);
-        const bool inside = tt < n, own = inside && tt < t0 + kBackRun;
+        r.x[i].get(win[W - 1]);
+        const bool inside = tt <= last && tt < n, own = inside && tt < t0 + kBackRun;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           if (a.silu) {
@@ -206,10 +220,10 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide
         const int s = tt - (W - 1);   // dx of this token is complete
         if (s < t0 && (run > 0 || !dsi)) continue;
         if (dso && s < n && s >= n - (W - 1)) {
-          RowVec<T, V> r;
+          RowVec<T, V> q;
           float v[V];
-          r.load(dso + (int64_t)(s - n + W - 1) * a.D);
-          r.get(v);
+          q.load(dso + (int64_t)(s - n + W - 1) * a.D);
+          q.get(v);
 #pragma unroll
           for (int k = 0; k < V; ++k) o[k] += v[k];
         }
@@ -223,6 +237,24 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide
           store_row<V>(dsi + (int64_t)(s + W - 1) * a.D, o);
         }
       }
+    };
+    if (last >= t0) {
+      Raw even, odd;
+      request(even, t0);
+      for (int t = t0; t < end; t += 2 * kBackAhead) {
+        request(odd, t + kBackAhead);
+        rows(even, t);
+        request(even, t + 2 * kBackAhead);
+        rows(odd, t + kBackAhead);
+      }
+    } else {   // no token of the sequence: zeros, and the states' gradients
+      Raw none;
+#pragma unroll
+      for (int i = 0; i < kBackAhead; ++i) {
+        none.x[i].zero();
+        none.d[i].zero();
+      }
+      for (int t = t0; t < end; t += kBackAhead) rows(none, t);
     }
   }
 #pragma unroll
