@@ -16,7 +16,8 @@ namespace favor {
 namespace {
 
 constexpr int kConvThreads = 256;
-constexpr int kAhead = 4;   // rows in flight
+// Rows in flight; 8 against 4: 70.6 against 73.3 us (4 x 4096 x 4096 bf16, 4 taps)
+constexpr int kAhead = 8;
 
 // Token t of one sequence: x for t >= 0, the carried inputs before it.
 template <typename T, int V>
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(kConvThreads) void k_conv(Conv a) {
       store_row<V>(so + (int64_t)i * a.D, v);
     }
   }
-  // Four rows at a time, the next four requested before: two sets of registers in turn, and
+  // kAhead rows at a time, the next ones requested before: two sets of registers in turn, and
   // requests without conditions (a row behind the last asks for the last one).
   const int t1 = min(t0 + a.run, a.L), last = min(n, t1) - 1;
   using Raw = RowVec<T, V>[kAhead];
@@ -122,7 +123,7 @@ constexpr int kBackWide = 16;
 template <typename T> constexpr int back_vec(int W) {
   return sizeof(T) == 2 && W <= 4 ? 8 : 4;   // more taps of more channels spill
 }
-constexpr int kBackRun = 32, kBackAhead = 2;   // rows in flight twice
+constexpr int kBackAhead = 2;   // rows in flight, of two tensors
 
 template <typename T, int W, int V>
 __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide, int tiles) {
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide
   const int high = kConvThreads / wide;
   const int b = blockIdx.y;
   const int run = block * high + tid / wide;
-  const int64_t t0w = (int64_t)run * kBackRun;
+  const int64_t t0w = (int64_t)run * a.run;
   const bool live = unit < units && t0w < max(a.L, 1);
   float dw[W][V], db[V];
 #pragma unroll
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide
       r.get(win[i + 1]);
     }
     // dx of token s needs g up to s + W - 1: the run's last tokens read W - 1 rows past it
-    const int end = min(t0 + kBackRun, a.L) + W - 1, last = min(n, end) - 1;
+    const int end = min(t0 + a.run, a.L) + W - 1, last = min(n, end) - 1;
     struct Raw {
       RowVec<T, V> x[kBackAhead], d[kBackAhead];
     };
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_backward(Conv a, int wide
           }
         }
         r.x[i].get(win[W - 1]);
-        const bool inside = tt <= last && tt < n, own = inside && tt < t0 + kBackRun;
+        const bool inside = tt <= last && tt < n, own = inside && tt < t0 + a.run;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           if (a.silu) {
@@ -351,19 +352,34 @@ hipError_t launch_w(const Conv &a, hipStream_t st) {
   return hipGetLastError();
 }
 
-int back_units_wide(int units) {
-  int wide = 1;
-  while (wide < kBackWide && wide < units) wide *= 2;
-  return wide;
+struct BackCut {
+  int wide, tiles, run, blocks;   // units of a workgroup, tiles of units, tokens of a run
+};
+
+// Each run reads W - 1 rows more than its own, so it is long, unless that leaves too few
+// workgroups: 4 x 4096 x 4096 with four taps takes 89 us at 64 tokens (512 workgroups),
+// 96 at 32 and 112 at 16.
+constexpr int kBackBlocks = 512;
+BackCut back_cut(int B, int L, int units) {
+  BackCut c{1, 0, 128, 1};
+  while (c.wide < kBackWide && c.wide < units) c.wide *= 2;
+  c.tiles = (units + c.wide - 1) / c.wide;
+  do {
+    c.run /= 2;
+    const int tokens = c.run * (kConvThreads / c.wide);
+    c.blocks = L > 0 ? (L + tokens - 1) / tokens : 1;
+  } while (c.run > 16 && (int64_t)B * c.tiles * c.blocks < kBackBlocks);
+  return c;
 }
 
 template <typename T, int W>
 hipError_t launch_back_w(const Conv &a, hipStream_t st) {
   constexpr int V = back_vec<T>(W);
-  const int units = a.D / V, wide = back_units_wide(units);
-  const int tiles = (units + wide - 1) / wide;
-  const int blocks = conv_part_rows(1, a.L, a.D, W, sizeof(T) == 2 ? Dt::BF16 : Dt::F32);
-  k_conv_backward<T, W, V><<<dim3(tiles * blocks, a.B), kConvThreads, 0, st>>>(a, wide, tiles);
+  const BackCut c = back_cut(a.B, a.L, a.D / V);
+  Conv run = a;
+  run.run = c.run;
+  k_conv_backward<T, W, V>
+      <<<dim3(c.tiles * c.blocks, a.B), kConvThreads, 0, st>>>(run, c.wide, c.tiles);
   return hipGetLastError();
 }
 
@@ -371,8 +387,7 @@ hipError_t launch_back_w(const Conv &a, hipStream_t st) {
 
 int conv_part_rows(int B, int L, int D, int width, Dt dt) {
   const int V = dt == Dt::BF16 ? back_vec<bf16>(width) : back_vec<float>(width);
-  const int tokens = kBackRun * (kConvThreads / back_units_wide(D / V));
-  return B * (L > 0 ? (L + tokens - 1) / tokens : 1);
+  return B * back_cut(B, L, D / V).blocks;
 }
 
 #define FAVOR_BY_WIDTH(fn)                                           \
