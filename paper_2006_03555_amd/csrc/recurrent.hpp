@@ -98,7 +98,7 @@ hipError_t launch_beam_pieces(const BeamSelect &a, Dt dt, hipStream_t st);
 hipError_t launch_beam_merge(const BeamSelect &a, hipStream_t st);
 
 constexpr int kBeamPools = 64;       // pools of one launch
-constexpr int kBeamPieceUnits = 4096; // 16-byte units that one workgroup copies
+constexpr int kBeamPieceUnits = 2048; // 16-byte units that one workgroup copies
 struct BeamReorder {
   const int32_t *parent, *slots;   // [B][K]; slots nullable
   int32_t *new_slots;
