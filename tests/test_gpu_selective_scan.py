@@ -308,3 +308,22 @@ def test_long_and_wide(B, L, D, N):
             np.linalg.norm(to_host(g) - r) / np.linalg.norm(r))
         # a few dozen roundings of 2^-24 that do not conspire
         assert err < 40 * 2.0 ** -24, (name, err)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,L,D,N,G", [
+    (16, 300, 2080, 16, 2), (20, 300, 2080, 5, 2), (20, 259, 2048, 16, 1), (17, 40, 2048, 128, 1)])
+def test_many_workgroups(B, L, D, N, G, dtype):
+    """Batches that fill the card: wider workgroups forward (bf16), two and four tiles to a
+    workgroup backward. The gradients that come in are zero but for three sequences, so the
+    parameters' gradients are those of the three, with exact zeros of the others."""
+    some = [0, B // 2 + 1, B - 1]
+    i = inputs(B, L, D, N, G, dtype, 91)
+    for k in ("dy", "dstate"):
+        i[k][[b for b in range(B) if b not in some]] = 0
+    t = dev(i, dtype)
+    (y, s), grads = forward(t), backward(t)
+    of = lambda k, v: v if v is None or k in ("A", "skip", "bias") else v[some]
+    j = {k: of(k, v) for k, v in i.items()}
+    cut = [g if name in ("dA", "dD", "ddt_bias") else g[some] for g, name in zip(grads, GRADS)]
+    check(j, dtype, (y[some], s[some]), cut)
