@@ -360,11 +360,11 @@ __global__ __launch_bounds__(kCopyThreads) void k_beam_reorder(BeamReorder a) {
   if (from < 0 || from >= n_slots || to < 0 || to >= n_slots) return;
   const int64_t u0 = (int64_t)(blockIdx.x - a.first[lo]) * kBeamPieceUnits;
   const int count = (int)min((int64_t)kBeamPieceUnits, units - u0);
-  const float4 *src = a.pool[lo].data + (int64_t)from * units + u0;
-  float4 *dst = a.pool[lo].data + (int64_t)to * units + u0;
+  const f32x4 *src = static_cast<const f32x4 *>(a.pool[lo].data) + (int64_t)from * units + u0;
+  f32x4 *dst = static_cast<f32x4 *>(a.pool[lo].data) + (int64_t)to * units + u0;
   int i = threadIdx.x;
   for (; i + 3 * kCopyThreads < count; i += 4 * kCopyThreads) {
-    float4 v[4];
+    f32x4 v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = src[i + k * kCopyThreads];
 #pragma unroll

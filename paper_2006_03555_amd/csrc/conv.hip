@@ -385,9 +385,9 @@ hipError_t launch_back_w(const Conv &a, hipStream_t st) {
 
 }  // namespace
 
-int conv_part_rows(int B, int L, int D, int width, Dt dt) {
+int64_t conv_part_rows(int B, int L, int D, int width, Dt dt) {
   const int V = dt == Dt::BF16 ? back_vec<bf16>(width) : back_vec<float>(width);
-  return B * back_cut(B, L, D / V).blocks;
+  return (int64_t)B * back_cut(B, L, D / V).blocks;
 }
 
 #define FAVOR_BY_WIDTH(fn)                                           \

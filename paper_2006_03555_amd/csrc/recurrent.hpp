@@ -29,7 +29,7 @@ struct Conv {
   int n_slots;
 };
 hipError_t launch_conv(const Conv &a, Dt dt, hipStream_t st);
-int conv_part_rows(int B, int L, int D, int width, Dt dt);
+int64_t conv_part_rows(int B, int L, int D, int width, Dt dt);
 hipError_t launch_conv_backward(const Conv &a, Dt dt, hipStream_t st);
 // cols sums over rows of part [rows][cols]; conv: the columns [width + 1][D] go to dw and dbias.
 hipError_t launch_conv_sums(const Conv &a, int rows, hipStream_t st);
@@ -103,7 +103,7 @@ struct BeamReorder {
   const int32_t *parent, *slots;   // [B][K]; slots nullable
   int32_t *new_slots;
   int B, K, n_pools;
-  struct { float4 *data; int32_t units, n_slots; } pool[kBeamPools];   // units of 16 bytes per slot
+  struct { void *data; int32_t units, n_slots; } pool[kBeamPools];   // units of 16 bytes per slot
   int first[kBeamPools + 1];       // the first of a pool's pieces
 };
 hipError_t launch_beam_reorder(const BeamReorder &a, hipStream_t st);

@@ -35,12 +35,16 @@ favor_status check_dtype(const favor_dtype &d) {
     return fail(FAVOR_ERR_INVALID_ARGUMENT, "unknown dtype %d", dt);
   return FAVOR_OK;
 }
-favor_status check_sizes(int B, int L, int D) {
+// row: of the longest rows that a call has
+favor_status check_sizes(int B, int L, int D, int64_t row) {
   if (B < 0 || L < 0) return fail(FAVOR_ERR_INVALID_ARGUMENT, "negative size B=%d L=%d", B, L);
   if (D <= 0) return fail(FAVOR_ERR_INVALID_ARGUMENT, "D=%d must be positive", D);
   if (L > kMaxL) return fail(FAVOR_ERR_UNSUPPORTED, "L=%d exceeds 2^30", L);
   if (B > kMaxB) return fail(FAVOR_ERR_UNSUPPORTED, "B=%d exceeds 65535", B);
   if (D > kMaxD) return fail(FAVOR_ERR_UNSUPPORTED, "D=%d exceeds 65536", D);
+  if (B && L && row > kMaxStride / B / L)
+    return fail(FAVOR_ERR_UNSUPPORTED, "B=%d L=%d rows of %lld reach past 2^46 elements", B, L,
+                (long long)row);
   return FAVOR_OK;
 }
 
@@ -85,11 +89,15 @@ int conv_run(const favor_conv_desc *g) {
   return 8;
 }
 
+int64_t part_rows(const favor_conv_desc *g) {
+  return favor::conv_part_rows(g->B, g->L, g->D, g->width, dt_of(g->dtype));
+}
+
 favor_status validate(const favor_conv_desc *g, int op) {
   if (!g) return fail(FAVOR_ERR_INVALID_ARGUMENT, "descriptor is NULL");
   FAVOR_TRY(check_op(op));
   FAVOR_TRY(check_dtype(g->dtype));
-  FAVOR_TRY(check_sizes(g->B, g->L, g->D));
+  FAVOR_TRY(check_sizes(g->B, g->L, g->D, g->D));
   if (g->width <= 0) return fail(FAVOR_ERR_INVALID_ARGUMENT, "width=%d must be positive", g->width);
   if (g->width < 2 || g->width > 8)
     return fail(FAVOR_ERR_UNSUPPORTED, "width=%d not supported (2 to 8)", g->width);
@@ -101,15 +109,15 @@ favor_status validate(const favor_conv_desc *g, int op) {
     const int64_t size[3] = {g->B, 1, op == kOpStep ? 1 : g->L};
     FAVOR_TRY(check_rows(ts[i].name, *ts[i].s, size, g->D, 16 / bytes_of(g->dtype), 0, ts[i].out));
   }
-  if (((int64_t)g->L / 8 + 1) * (g->D / 4) / 256 > kMaxBlocks)
-    return fail(FAVOR_ERR_UNSUPPORTED, "L=%d D=%d is too large", g->L, g->D);
+  if (((int64_t)g->L / 8 + 1) * (g->D / 4) / 256 > kMaxBlocks ||
+      (op == kOpBackward && part_rows(g) > kMaxBlocks))
+    return fail(FAVOR_ERR_UNSUPPORTED, "B=%d L=%d D=%d is too large", g->B, g->L, g->D);
   return FAVOR_OK;
 }
 
 size_t workspace_of(const favor_conv_desc *g) {
   if (g->B == 0) return 0;
-  const size_t rows = favor::conv_part_rows(g->B, g->L, g->D, g->width, dt_of(g->dtype));
-  return round_up(rows * (g->width + 1) * g->D * sizeof(float), 256);
+  return round_up((size_t)part_rows(g) * (g->width + 1) * g->D * sizeof(float), 256);
 }
 
 favor::Conv conv_of(const favor_conv_desc *g, int L, const void *x, const float *weight,
@@ -143,7 +151,8 @@ favor_status validate(const favor_scan_desc *g, int op) {
   if (!g) return fail(FAVOR_ERR_INVALID_ARGUMENT, "descriptor is NULL");
   FAVOR_TRY(check_op(op));
   FAVOR_TRY(check_dtype(g->dtype));
-  FAVOR_TRY(check_sizes(g->B, g->L, g->D));
+  const int64_t low = (int64_t)g->groups * g->N;
+  FAVOR_TRY(check_sizes(g->B, g->L, g->D, std::max<int64_t>(g->D, low)));
   if (g->N <= 0 || g->groups <= 0)
     return fail(FAVOR_ERR_INVALID_ARGUMENT, "N=%d and groups=%d must be positive", g->N, g->groups);
   if (g->D % g->groups)
@@ -306,6 +315,14 @@ favor_status validate(const favor_beam_desc *g) {
   return FAVOR_OK;
 }
 
+// No byte of one is the other's; their sizes may pass 64 bits together.
+bool apart(const favor_beam_pool &a, const favor_beam_pool &b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.data), y = reinterpret_cast<uintptr_t>(b.data);
+  const favor_beam_pool &lower = x < y ? a : b;
+  if (x == y || !lower.bytes_per_slot) return x != y;
+  return (x < y ? y - x : x - y) / (uint64_t)lower.bytes_per_slot >= (uint64_t)lower.n_slots;
+}
+
 // Pieces of a row, one wave each: 16 waves for each of the 256 compute units, of 512 tokens at
 // least, and no more than one per lane of the wave that joins them.
 void cut_row(const favor_beam_desc *g, int *pieces, int *len) {
@@ -425,9 +442,8 @@ favor_status favor_conv_backward(const favor_conv_desc *g, const void *x, const 
   }
   if (e != hipSuccess) return device_result(e, "favor_conv_backward");
   favor::LaunchTimer t(favor::kKerColumnSums, stream);
-  return device_result(
-      favor::launch_conv_sums(a, favor::conv_part_rows(g->B, g->L, g->D, g->width, dt), stream),
-      "favor_conv_backward sums");
+  return device_result(favor::launch_conv_sums(a, (int)part_rows(g), stream),
+                       "favor_conv_backward sums");
 }
 
 favor_status favor_conv_step(const favor_conv_desc *g, const void *x, const float *weight,
@@ -701,8 +717,8 @@ favor_status favor_beam_reorder(int32_t B, int32_t K, const int32_t *parent, con
                   (long long)p.bytes_per_slot);
     FAVOR_TRY(check_ptr(p.data, "a pool", work && p.n_slots > 0 && p.bytes_per_slot > 0));
     for (int j = 0; j < i; ++j)
-      if (p.data && p.data == pools[j].data)
-        return fail(FAVOR_ERR_INVALID_ARGUMENT, "pools %d and %d are one", j, i);
+      if (p.data && pools[j].data && !apart(p, pools[j]))
+        return fail(FAVOR_ERR_INVALID_ARGUMENT, "pools %d and %d are one or overlap", j, i);
   }
   if (!work) return ok();
   for (int first = 0; first == 0 || first < n_pools; first += favor::kBeamPools) {
@@ -716,7 +732,7 @@ favor_status favor_beam_reorder(int32_t B, int32_t K, const int32_t *parent, con
     for (int i = 0; i < a.n_pools; ++i) {
       const favor_beam_pool &p = pools[first + i];
       const int64_t units = p.bytes_per_slot / 16;
-      a.pool[i] = {static_cast<float4 *>(p.data), (int32_t)units, p.n_slots};
+      a.pool[i] = {p.data, (int32_t)units, p.n_slots};
       a.first[i + 1] = a.first[i] + (int)((units + favor::kBeamPieceUnits - 1) / favor::kBeamPieceUnits);
     }
     hipError_t e;

@@ -3,6 +3,9 @@ oracle's own pins (library convolution, closed sums, differences, brute force), 
 the binding's refusals."""
 import ctypes
 import itertools
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -10,6 +13,8 @@ import pytest
 import paper_2006_03555_amd as fv
 from oracle import recurrent as rec
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM_INCLUDE = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
 P = ctypes.c_void_p
 A, NUL = P(1 << 20), P(0)   # an aligned address, never dereferenced
 
@@ -348,9 +353,43 @@ def test_beam_reorder_refusals():
             (dict(new=P((1 << 40) + 8)), 1, "overlaps"), (dict(pools=((NUL, 64, 6),)), 1, "pool"),
             (dict(pools=((at(3), 40, 6),)), 2, "multiples of 16"), (dict(pools=((at(3), -16, 6),)), 1, "negative"),
             (dict(pools=((P(8), 64, 6),)), 1, "aligned"), (dict(pools=((at(3), 64, -1),)), 1, "negative"),
-            (dict(pools=((at(3), 64, 6), (at(3), 64, 6))), 1, "are one")):
+            (dict(pools=((at(3), 64, 6), (at(3), 64, 6))), 1, "are one"),
+            (dict(pools=((at(3), 64, 6), (P(at(3).value + 64 * 6 - 16), 64, 6))), 1, "overlap"),
+            (dict(pools=((P(at(3).value + 16), 64, 6), (at(3), 1 << 34, 1 << 30))), 1, "overlap")):
         assert call(**kw) == status and word in fv.last_error(), (kw, fv.last_error())
     assert call(B=0, parent=NUL, new=NUL) == 0
+    # side by side: taken (with no entries, so that nothing is launched)
+    for other in (at(3).value + 64 * 6, at(3).value - 64 * 6):
+        assert call(B=0, pools=((at(3), 64, 6), (P(other), 64, 6))) == 0
+
+
+def test_neighbouring_outputs_do_not_overlap():
+    """Small tensors lie side by side: sizes of both sides count, not the larger one twice."""
+    g = fv.make_beam_desc(2, 3, 100, 64, fv.F32, end_token=5)
+    s = at(1).value   # scores: 24 bytes, out_scores: 512, ended: 6
+    for lo, status, word in ((s + 24, 3, "workspace"), (s + 20, 1, "out_scores overlaps scores"),
+                             (s - 512, 3, "workspace"), (s - 508, 1, "out_scores overlaps scores")):
+        assert _call_select(g, out=P(lo), n=1) == status and word in fv.last_error(), lo - s
+    e = at(2).value
+    for lo, status in ((e + 8, 3), (e + 4, 1), (e - 512, 3), (e - 508, 1)):
+        assert _call_select(g, token=P(lo), n=1) == status, lo - e
+
+
+def test_sizes_past_what_offsets_hold():
+    """Rows far apart, and more elements than 2^46, are refused before any size is formed."""
+    far = (1 << 25) // 4 + 4
+    for f in ("x", "dt", "z", "y"):
+        g = _scan(dtype=fv.F32, L=4, **{f: (4 * far, far, far)})
+        assert fv.validate_scan_desc(g, 0) == 2 and "2^25 bytes" in fv.last_error(), f
+        assert fv.validate_scan_desc(_scan(dtype=fv.F32, L=4, **{f: (4 * far, far, far - 4)}), 0) == 0
+    big = dict(B=65535, L=1 << 30)
+    for op in (0, 1):
+        assert fv.validate_conv_desc(_conv(D=8, **big), op) == 2 and "2^46" in fv.last_error()
+        assert fv.validate_scan_desc(_scan(D=8, N=1, **big), op) == 2 and "2^46" in fv.last_error()
+        assert fv.scan_workspace_size(_scan(D=8, N=1, **big), bool(op)) == 0
+    # 2^30 rows of parts are held in 64 bits
+    g = _conv(B=2048, L=1 << 30, D=8, width=2, dtype=fv.F32)
+    assert fv.validate_conv_desc(g, 1) == 0 and fv.conv_workspace_size(g) > 1 << 30
 
 
 def test_binding_refusals():
@@ -408,3 +447,32 @@ def test_binding_refusals():
         with pytest.raises(fv.FavorError) as e:
             call()
         assert text in str(e.value), (n, text, str(e.value))
+
+
+# ------------------------------------------------------------------ under sanitizers
+@pytest.fixture(scope="module")
+def fuzzer(tmp_path_factory):
+    gxx = shutil.which("g++")
+    if gxx is None or not os.path.isdir(os.path.join(ROCM_INCLUDE, "hip")):
+        pytest.skip("needs g++ and the HIP headers")
+    csrc = "paper_2006_03555_amd/csrc"
+    sources = ["tests/host/fuzz_recurrent.cpp", "tests/host/stubs.cpp",
+               f"{csrc}/recurrent_api.cpp", f"{csrc}/favor_api.cpp", f"{csrc}/timing.cpp"]
+    exe = str(tmp_path_factory.mktemp("host") / "fuzz_recurrent")
+    r = subprocess.run([gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined",
+                        "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer",
+                        "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INCLUDE, "-I", f"{ROOT}/include",
+                        *[os.path.join(ROOT, x) for x in sources], "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    return exe
+
+
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_calls_fuzzed_under_sanitizers(fuzzer, seed):
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=1",
+               UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
+    r = subprocess.run([fuzzer, str(seed), "40000"], capture_output=True, text=True, env=env,
+                       timeout=300)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
+    assert " 0 failures" in r.stdout
