@@ -75,7 +75,7 @@ hipError_t launch_scan_sums(const Scan &a, Dt dt, hipStream_t st);
 hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st);
 // part (part_r): from sums to the states before (behind) each segment; backward: dh_in.
 hipError_t launch_scan_prefix(const Scan &a, bool backward, hipStream_t st);
-hipError_t launch_scan(const Scan &a, Dt dt, int tile, hipStream_t st);
+hipError_t launch_scan(const Scan &a, Dt dt, hipStream_t st);
 hipError_t launch_scan_backward(const Scan &a, Dt dt, hipStream_t st);
 // dB and dC, dA, dskip and dbias from their parts.
 hipError_t launch_scan_backward_sums(const Scan &a, Dt dt, hipStream_t st);

@@ -179,29 +179,26 @@ favor_status validate(const favor_scan_desc *g, int op) {
   return FAVOR_OK;
 }
 
-// How a forward call is cut: channels of one workgroup, and segments of whole chunks. A call
-// of several segments takes the sums of all but the last first, so their steps and decays are
-// computed twice. Whole calls in us, bf16, N = 16:
+// How a forward call is cut into segments of whole chunks. A call of several segments takes the
+// sums of all but the last first, so their steps and decays are computed twice. Whole calls in
+// us, bf16, N = 16:
 //   One segment while its workgroups of 32 channels fill the 256 compute units, as long as
-//   there are 240 of them: B4 L4096 D2048 (256) 267, in two segments 281, in eight 289.
-//   Fewer: segments for 2048 workgroups. B1 L65536 D2048 in 8 / 16 / 32 segments 1266 / 1203 /
-//   1166; B1 L4096 in 8 / 32 96 / 89, in one 260; B6 L1999 D1000 N24 fp32 (192) in 8 180, in one
-//   210.
-//   Workgroups of 64 channels read B and C for twice as many, but have half the waves: from 512
-//   of them on, B8 L4096 D4096 736 instead of 770, with 256 of them (D2048) 452 instead of 433.
-//   In fp32 they spill.
+//   there are 240 of them: B4 L4096 D2048 (256) 220, in two segments 297, in eight 279; B8 368,
+//   498, 534.
+//   Fewer: segments for 2048 workgroups. B1 L65536 D2048 in 8 / 16 / 32 / 64 segments 1321 / 1199
+//   / 1133 / 1106; B1 L4096 in 8 / 32 102 / 90, in one 214; B3 L4096 (192) in 8 225, in one 216;
+//   B6 L1999 D1000 N24 fp32 (192) in 8 198, in one 194.
 struct ScanCut {
-  int tile, chunks, nseg;
+  int chunks, nseg;
 };
-constexpr int kOneSegment = 240, kSegmentBlocks = 2048, kWideBlocks = 512;
+constexpr int kOneSegment = 240, kSegmentBlocks = 2048;
 ScanCut cut_of(const favor_scan_desc *g) {
   ScanCut c;
   const int chunks = std::max(chunks_of(g), 1);
-  const int64_t narrow = (int64_t)g->B * tiles_of(g, 32), wide = (int64_t)g->B * tiles_of(g, 64);
-  const int64_t want = narrow >= kOneSegment ? 1 : std::max<int64_t>(1, kSegmentBlocks / std::max<int64_t>(narrow, 1));
+  const int64_t blocks = std::max<int64_t>(1, (int64_t)g->B * tiles_of(g, 32));
+  const int64_t want = blocks >= kOneSegment ? 1 : kSegmentBlocks / blocks;
   c.chunks = (int)((chunks + want - 1) / want);
   c.nseg = (chunks + c.chunks - 1) / c.chunks;
-  c.tile = wide >= kWideBlocks && g->N <= 128 && dt_of(g->dtype) == Dt::BF16 ? 64 : 32;
   return c;
 }
 
@@ -516,7 +513,7 @@ favor_status favor_selective_scan(const favor_scan_desc *g, const void *x, const
     if (e != hipSuccess) return device_result(e, "favor_selective_scan segment states");
   }
   favor::LaunchTimer t(favor::kKerScan, stream);
-  return device_result(favor::launch_scan(a, type, c.tile, stream), "favor_selective_scan");
+  return device_result(favor::launch_scan(a, type, stream), "favor_selective_scan");
 }
 
 favor_status favor_selective_scan_backward(

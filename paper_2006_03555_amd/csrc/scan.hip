@@ -5,76 +5,89 @@
 //
 // Bound by the vector unit: each (token, channel, state) takes a product and an exponential
 // (two issue slots), the input's product, the recurrence once inside the lane and once from
-// its true state, and the output's sum; B and C are read from LDS for two channels at a time.
-// Nothing of size tokens x channels x states leaves the registers.
+// its true state, and the output's sum: seven slots, and about three more for the row's scan and
+// the rows' way through LDS. Nothing of size tokens x channels x states leaves the registers.
+// B4 L4096 D2048 N16 in bf16 (one segment): 238 us, 2.3 T state steps/s; B1 L65536 D2048: sums of
+// 31 segments 500 us, then 725 us, 3.0 T/s.
 #include "scan_common.hpp"
 
 namespace favor {
 namespace {
 
-// Channels per lane: a workgroup's 8 waves take 32 * kCh channels.
-template <int kCh> constexpr int kWide = 4 * kScanWaves * kCh;
+constexpr int W = 4 * kScanWaves;   // channels of a workgroup
 
-// One (chunk, n) step of kCh channels: a = 2^(s A), S and P of the lane, the row's scan.
-// kOut: y += C h; h of the row's last lane goes back to `carry`.
-template <int kCh, bool kOut> struct StateIn {   // what a step reads from LDS
-  float B[8], C[8], A[kCh], h[kCh];
+// What a step of one state reads from LDS.
+template <bool kOut> struct StateIn {
+  float B[8], C[8], A, h;
 
   __device__ __forceinline__ void load(const float *b, const float *c, const float *A2, const float *carry, int tl) {
     lane_load(b, tl, B);
     if (kOut) lane_load(c, tl, C);
-#pragma unroll
-    for (int i = 0; i < kCh; ++i) {
-      A[i] = A2[4 * i];
-      h[i] = carry[4 * i];
-    }
+    A = *A2;
+    h = *carry;
   }
 };
-template <int kCh, bool kOut>
-__device__ __forceinline__ void forward_state(const float (&s)[kCh][8], const float (&sx)[kCh][8],
-                                              const float (&ssum)[kCh], const StateIn<kCh, kOut> &in,
-                                              float *carry, int tl, float (&y)[kCh][8]) {
-  float a[kCh][8], bx[kCh][8], S[kCh], P[kCh], h[kCh];
+// K states side by side: a = 2^(s A), S and P of the lane, the row's scan. kOut: y += C h; h of
+// the row's last lane goes back to carry.
+template <int K, bool kOut>
+__device__ __forceinline__ void forward_states(const float (&s)[8], const float (&sx)[8], float ssum,
+                                               const StateIn<kOut> (&in)[K], float *carry, int tl, float (&y)[8]) {
+  float a[K][8], bx[K][8], S[K], P[K], h[K];
 #pragma unroll
-  for (int i = 0; i < kCh; ++i) {
-    const float A = in.A[i];
-    h[i] = in.h[i];
+  for (int k = 0; k < K; ++k) {
+    h[k] = in[k].h;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      a[i][j] = exp2_hw(s[i][j] * A);
-      bx[i][j] = sx[i][j] * in.B[j];
+      a[k][j] = exp2_hw(s[j] * in[k].A);
+      bx[k][j] = sx[j] * in[k].B[j];
     }
-    S[i] = tl == 0 ? h[i] : 0.f;
+    S[k] = tl == 0 ? h[k] : 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) S[i] = fmaf(a[i][j], S[i], bx[i][j]);
-    P[i] = exp2_hw(ssum[i] * A);
+    for (int j = 0; j < 8; ++j) S[k] = fmaf(a[k][j], S[k], bx[k][j]);
+    P[k] = exp2_hw(ssum * in[k].A);
   }
-  if constexpr (kCh == 2) row_scan2<false>(S[0], P[0], h[0], S[1], P[1], h[1]);
+  if constexpr (K == 2) row_scan2<false>(S[0], P[0], h[0], S[1], P[1], h[1]);
   else row_scan<false>(S[0], P[0], h[0]);
 #pragma unroll
-  for (int i = 0; i < kCh; ++i) {
+  for (int k = 0; k < K; ++k) {
     if constexpr (kOut) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        h[i] = fmaf(a[i][j], h[i], bx[i][j]);
-        y[i][j] = fmaf(in.C[j], h[i], y[i][j]);
+        h[k] = fmaf(a[k][j], h[k], bx[k][j]);
+        y[j] = fmaf(in[k].C[j], h[k], y[j]);
       }
     }
-    if (tl == 15) carry[4 * i] = S[i];
+    if (tl == 15) carry[k * W] = S[k];
   }
 }
 
 // kOut: the rows y and the state after the last token. Otherwise the sums of the segments.
-template <typename T, int kCh, bool kOut>
-__global__ __launch_bounds__(kScanThreads, kOut && kCh == 2 ? 4 : 6) void k_scan(Scan a) {
-  constexpr int W = kWide<kCh>;
+// kAhead, for calls of one segment, whose few workgroups a compute unit does not overlap: a
+// chunk's rows are requested before the states of the one before are taken, two states go side
+// by side, and y has a tile of its own, so that the next rows need not wait for its readers. B4
+// L4096 D2048 N16 in bf16 takes 238 us with it and 298 without; segments' workgroups, of which
+// three share a unit, lose more by the registers (726 and 745 us at B1 L65536).
+template <typename T, bool kOut, bool kAhead> struct ScanLds {
+  static constexpr int kRaw = kPairTiles<T> * W * kTok;
+  static constexpr int kRows = kRaw + (kAhead ? W * kTok : 0);   // else y takes the place of x and dt
+  static constexpr int kLow = (kOut ? 2 : 1) * kStates * kTok;
+  static size_t bytes(int N) {
+    const int padded = (N + kStates - 1) / kStates * kStates;
+    return sizeof(float) * (kRows + kLow + 2 * (size_t)padded * W);
+  }
+};
+template <typename T, bool kOut, bool kAhead>
+__global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
+  constexpr int K = kAhead ? 2 : 1;
+  using Lds = ScanLds<T, kOut, kAhead>;
   extern __shared__ __align__(16) float lds[];
-  float *tile = lds, *tb = tile + W * kTok, *tc = tb + kStates * kTok;
+  float *tile = lds, *ty = kAhead ? tile + Lds::kRaw : tile;
+  float *tb = tile + Lds::kRows, *tc = tb + kStates * kTok;
   const int padded = (a.N + kStates - 1) / kStates * kStates;
-  float *tA = tc + (kOut ? kStates * kTok : 0), *th = tA + padded * W;
+  float *tA = tb + Lds::kLow, *th = tA + padded * W;
   const ScanPlace p = scan_place(a, W);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
-  const int cl = 4 * kCh * wave + lane / 16;   // this lane's first channel; the next is 4 on
+  const int cl = 4 * wave + lane / 16, c = min(p.c0 + cl, p.cend - 1);   // this lane's channel
   const int64_t DN = (int64_t)a.D * a.N, at_part = ((int64_t)p.b * a.nseg + p.seg) * DN;
   const float *h0 = nullptr;
   if (kOut && a.nseg > 1) h0 = a.part + at_part;
@@ -83,123 +96,108 @@ __global__ __launch_bounds__(kScanThreads, kOut && kCh == 2 ? 4 : 6) void k_scan
     load_channels<W>(a.A, p, a.N, n0, min(kStates, a.N - n0), kLog2e, tA + n0 * W, threadIdx.x);
     load_channels<W>(h0, p, a.N, n0, min(kStates, a.N - n0), 1.f, th + n0 * W, threadIdx.x);
   }
-  float seg_steps[kCh] = {};
+  const float bias = a.bias ? a.bias[c] : 0.f, skip = kOut && a.skip ? a.skip[c] : 0.f;
+  float seg_steps = 0.f;
   const int first = p.seg * a.chunks, last = min(first + a.chunks, (a.L + kTok - 1) / kTok);
-  for (int chunk = first; chunk < last; ++chunk) {
+  const int end = min(last, (p.n + kTok - 1) / kTok);   // of the chunks that have tokens
+  static_assert(kLoads<W> == 1, "one unit of a thread");
+  RowVec<T, 8> rx, rdt, rz;
+  States<T> low_b, low_c;
+  const auto request = [&](int chunk, int tid) {
     const int64_t t0 = (int64_t)chunk * kTok;
-    const bool some = t0 < p.n;
-    if (!some && !kOut) break;
+    const Unit w = unit_of<W>(p, t0, 0, tid);
+    rx = get_row<T>(a.x, a.xs, p, t0, w);
+    rdt = get_row<T>(a.dt, a.dts, p, t0, w);
+    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
+    if (kOut) low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
+  };
+  if (kAhead && first < end) request(first, fresh_thread());
+  for (int chunk = first; chunk < end; ++chunk) {
+    const int64_t t0 = (int64_t)chunk * kTok;
     int tid = fresh_thread();
-    if (some) {
-      float s[kCh][8], sx[kCh][8], ssum[kCh], y[kCh][8];
-      States<T> low_b, low_c;
-      {
-        // everything is requested at once; the tile holds the steps, then s x, then y
-        Steps<T, W> steps;
-        float in[kLoads<W>][8], own[kLoads<W>][8];
-        steps.load(a, p, t0, tid);
-        low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
-        if (kOut) low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
-#pragma unroll
-        for (int i = 0; i < kLoads<W>; ++i) steps.template get<true>(a, unit_of<W>(p, t0, i, tid), i, own[i], in[i]);
-        __syncthreads();   // the last chunk's rows have been read
-#pragma unroll
-        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i, tid), own[i]);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, s[i]);
-        low_b.put(tb, p, t0, min(kStates, a.N), tid);
-        if (kOut) low_c.put(tc, p, t0, min(kStates, a.N), tid);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i, tid), in[i]);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) {
-          tile_load(tile, cl + 4 * i, tl, sx[i]);
-          ssum[i] = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            ssum[i] += s[i][j];
-            y[i][j] = 0.f;
-          }
-          if (!kOut) seg_steps[i] += ssum[i];
-        }
-      }
-      for (int n0 = 0; n0 < a.N; n0 += kStates) {
-        const int count = min(kStates, a.N - n0);
-        if (n0) {
-          tid = fresh_thread();
-          low_b.load(a.b, a.bs, p, t0, n0, count, tid);
-          if (kOut) low_c.load(a.c, a.cs, p, t0, n0, count, tid);
-          __syncthreads();   // the last states' B and C have been read
-          low_b.put(tb, p, t0, count, tid);
-          if (kOut) low_c.put(tc, p, t0, count, tid);
-          __syncthreads();
-        }
-        for (int n = 0; n < count; ++n) {
-          const int at = (n0 + n) * W + cl;
-          StateIn<kCh, kOut> in;
-          in.load(tb + n * kTok, tc + n * kTok, tA + at, th + at, tl);
-          forward_state<kCh, kOut>(s, sx, ssum, in, th + at, tl, y);
-        }
-      }
-      if (kOut) {
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) tile_store(tile, cl + 4 * i, tl, y[i]);
-      }
+    if (!kAhead) {
+      request(chunk, tid);
+      if (chunk > first) __syncthreads();   // the last chunk's rows have been read
     }
-    RowVec<T, 8> rx[kLoads<W>], rz[kLoads<W>];
-    tid = fresh_thread();
-    if (kOut && some) {
-#pragma unroll
-      for (int i = 0; i < kLoads<W>; ++i) {
-        const Unit w = unit_of<W>(p, t0, i, tid);
-        if (a.skip) rx[i] = get_row<T>(a.x, a.xs, p, t0, w);
-        if (a.z) rz[i] = get_row<T>(a.z, a.zs, p, t0, w);
-      }
-    }
-    if (!kOut) continue;
+    put_pair<W>(tile, unit_of<W>(p, t0, 0, tid), rx, rdt);
+    low_b.put(tb, p, t0, min(kStates, a.N), tid);
+    if (kOut) low_c.put(tc, p, t0, min(kStates, a.N), tid);
     __syncthreads();
+    tid = fresh_thread();
+    if (kAhead) {
+      if (kOut)   // x stands in where there is no z
+        rz = get_row<T>(a.z ? a.z : a.x, a.z ? a.zs : a.xs, p, t0, unit_of<W>(p, t0, 0, tid));
+      request(min(chunk + 1, end - 1), tid);
+    }
+    float s[8], sx[8], ssum, y[8] = {};
+    get_pair<T, W>(tile, cl, tl, sx, s);
+    ssum = lane_steps(a, p, t0, tl, bias, s, sx);
 #pragma unroll
-    for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i, tid);
-      if (w.t >= a.L - t0 || w.c >= p.cend) continue;
-      float y[8], v[8];
-      if (w.live) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = tile[tile_at(8 * w.u + k, w.t)];
-        if (a.skip) {
-          rx[i].get(v);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = fmaf(a.skip[w.c + k], v[k], y[k]);
-        }
-        if (a.z) {
-          rz[i].get(v);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] *= v[k] * sigmoid(v[k]);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = 0.f;
+    for (int j = 0; j < 8; ++j) sx[j] *= s[j];
+    if (!kOut) seg_steps += ssum;
+    for (int n0 = 0; n0 < a.N; n0 += kStates) {
+      const int count = min(kStates, a.N - n0);
+      if (n0) {
+        tid = fresh_thread();
+        States<T> more_b, more_c;
+        more_b.load(a.b, a.bs, p, t0, n0, count, tid);
+        if (kOut) more_c.load(a.c, a.cs, p, t0, n0, count, tid);
+        __syncthreads();   // the last states' B and C have been read
+        more_b.put(tb, p, t0, count, tid);
+        if (kOut) more_c.put(tc, p, t0, count, tid);
+        __syncthreads();
       }
-      put_row<T>(a.y, a.ys, p, t0, w, y);
-    }
-  }
-  __syncthreads();
-  float *end = nullptr;
-  if (!kOut) end = a.part + at_part;
-  else if (a.h_out && p.seg == a.nseg - 1) end = a.h_out + p.b * DN;
-  if (end)
-    for (int n0 = 0; n0 < a.N; n0 += kStates)
-      store_channels<W>(end, p, a.N, n0, min(kStates, a.N - n0), th + n0 * W, threadIdx.x);
-  if (!kOut) {
+      for (int n = 0; n < count; n += K) {   // a state behind the last is zeros
+        const int at = (n0 + n) * W + cl;
+        StateIn<kOut> in[K];
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) {
-      const float total = row_sum(seg_steps[i]);
-      const int c = p.c0 + cl + 4 * i;
-      if (tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
+        for (int k = 0; k < K; ++k)
+          in[k].load(tb + (n + k) * kTok, tc + (n + k) * kTok, tA + at + k * W, th + at + k * W, tl);
+        forward_states<K, kOut>(s, sx, ssum, in, th + at, tl, y);
+      }
     }
+    if constexpr (!kOut) continue;
+    if (a.skip) {
+      float x[8], dt[8];
+      get_pair<T, W>(tile, cl, tl, x, dt);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = fmaf(skip, x[j], y[j]);
+    }
+    tile_store(ty, cl, tl, y);   // in place of what only this lane reads
+    tid = fresh_thread();
+    const Unit w = unit_of<W>(p, t0, 0, tid);
+    if (!kAhead && a.z) rz = get_row<T>(a.z, a.zs, p, t0, w);
+    __syncthreads();
+    if (w.t >= a.L - t0 || w.c >= p.cend) continue;
+    float v[8], o[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] = ty[tile_at(8 * w.u + k, w.t)];
+    if (a.z) {
+      rz.get(v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] *= v[k] * sigmoid(v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] = w.live ? o[k] : 0.f;
+    put_row<T>(a.y, a.ys, p, t0, w, o);
+  }
+  if (kOut)   // rows behind the sequence
+    for (int chunk = max(first, end); chunk < last; ++chunk) {
+      const int64_t t0 = (int64_t)chunk * kTok;
+      const Unit w = unit_of<W>(p, t0, 0, threadIdx.x);
+      const float none[8] = {};
+      if (w.t < a.L - t0 && w.c < p.cend) put_row<T>(a.y, a.ys, p, t0, w, none);
+    }
+  __syncthreads();
+  float *to = nullptr;
+  if (!kOut) to = a.part + at_part;
+  else if (a.h_out && p.seg == a.nseg - 1) to = a.h_out + p.b * DN;
+  if (to)
+    for (int n0 = 0; n0 < a.N; n0 += kStates)
+      store_channels<W>(to, p, a.N, n0, min(kStates, a.N - n0), th + n0 * W, threadIdx.x);
+  if (!kOut) {
+    const float total = row_sum(seg_steps);
+    if (tl == 15 && p.c0 + cl < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
   }
 }
 
@@ -242,11 +240,9 @@ template <bool kBackward> __global__ __launch_bounds__(kPrefixThreads) void k_sc
   else chain<false>(a, a.part, a.h_in ? a.h_in[b * DN + i] : 0.f, A2, at, at_s);
 }
 
-template <typename T, int kCh, bool kOut> hipError_t launch_as(const Scan &a, hipStream_t st) {
-  constexpr int W = kWide<kCh>;
-  const size_t lds = sizeof(float) * (W * kTok + (kOut ? 2 : 1) * kStates * kTok +
-                                     2 * (size_t)((a.N + kStates - 1) / kStates * kStates) * W);
-  const auto kernel = k_scan<T, kCh, kOut>;
+template <typename T, bool kOut, bool kAhead> hipError_t launch_as(const Scan &a, hipStream_t st) {
+  const size_t lds = ScanLds<T, kOut, kAhead>::bytes(a.N);
+  const auto kernel = k_scan<T, kOut, kAhead>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -257,16 +253,18 @@ template <typename T, int kCh, bool kOut> hipError_t launch_as(const Scan &a, hi
   kernel<<<dim3((unsigned)(tiles * segments), a.B), kScanThreads, lds, st>>>(a);
   return hipGetLastError();
 }
+template <typename T> hipError_t launch_rows(const Scan &a, hipStream_t st) {
+  return a.nseg == 1 ? launch_as<T, true, true>(a, st) : launch_as<T, true, false>(a, st);
+}
 
 }  // namespace
 
-hipError_t launch_scan(const Scan &a, Dt dt, int tile, hipStream_t st) {
-  if (dt == Dt::F32) return launch_as<float, 1, true>(a, st);
-  return tile == kWide<2> ? launch_as<bf16, 2, true>(a, st) : launch_as<bf16, 1, true>(a, st);
+hipError_t launch_scan(const Scan &a, Dt dt, hipStream_t st) {
+  return dt == Dt::BF16 ? launch_rows<bf16>(a, st) : launch_rows<float>(a, st);
 }
 
 hipError_t launch_scan_sums(const Scan &a, Dt dt, hipStream_t st) {
-  return dt == Dt::BF16 ? launch_as<bf16, 1, false>(a, st) : launch_as<float, 1, false>(a, st);
+  return dt == Dt::BF16 ? launch_as<bf16, false, false>(a, st) : launch_as<float, false, false>(a, st);
 }
 
 hipError_t launch_scan_prefix(const Scan &a, bool backward, hipStream_t st) {

@@ -225,6 +225,58 @@ template <typename T, int kWidth> struct Steps {
   }
 };
 
+// Two rows of a tile on their way from memory to lanes (x and dt, dy and z): in bf16 both in one
+// word, else a tile each.
+template <typename T> constexpr int kPairTiles = sizeof(T) == 2 ? 1 : 2;
+template <int kWidth>
+__device__ __forceinline__ void put_pair(float *tile, const Unit &w, const RowVec<bf16, 8> &v0, const RowVec<bf16, 8> &v1) {
+  const uint32_t a[4] = {v0.r.x, v0.r.y, v0.r.z, v0.r.w}, b[4] = {v1.r.x, v1.r.y, v1.r.z, v1.r.w};
+#pragma unroll
+  for (int k = 0; k < 8; ++k)   // the low or the high halves of two words
+    tile[tile_at(8 * w.u + k, w.t)] = __uint_as_float(
+        __builtin_amdgcn_perm(b[k / 2], a[k / 2], k % 2 ? 0x07060302u : 0x05040100u));
+}
+template <int kWidth>
+__device__ __forceinline__ void put_pair(float *tile, const Unit &w, const RowVec<float, 8> &v0, const RowVec<float, 8> &v1) {
+  float v[8];
+  v0.get(v);
+  put_unit(tile, w, v);
+  v1.get(v);
+  put_unit(tile + kWidth * kTok, w, v);
+}
+template <typename T, int kWidth>
+__device__ __forceinline__ void get_pair(const float *tile, int c, int tl, float (&v0)[8], float (&v1)[8]) {
+  tile_load(tile, c, tl, v0);
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t both = __float_as_uint(v0[j]);
+      v0[j] = __uint_as_float(both << 16);
+      v1[j] = __uint_as_float(both & 0xffff0000u);
+    }
+  } else {
+    tile_load(tile + kWidth * kTok, c, tl, v1);
+  }
+}
+// A lane's steps from its dt, and their sum; steps and x are zeros behind the sequence.
+__device__ __forceinline__ float lane_steps(const Scan &a, const ScanPlace &p, int64_t t0, int tl, float bias,
+                                            float (&s)[8], float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    s[j] += bias;
+    if (a.softplus) s[j] = softplus(s[j]);
+  }
+  const int left = (int)min((int64_t)kTok, p.n - t0) - 8 * tl;
+  if (left < 8)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j >= left) s[j] = x[j] = 0.f;
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum += s[j];
+  return sum;
+}
+
 // [states][kTok] tile of B or C: states n0 .., zeros behind the sequence. A thread keeps its
 // state and takes every 32nd token.
 template <typename T> struct States {

@@ -130,11 +130,10 @@ hipError_t launch_scan_prefix(const Scan &a, bool backward, hipStream_t) {
   else require(backward && a.L == 0, "segments");
   return hipSuccess;
 }
-hipError_t launch_scan(const Scan &a, Dt dt, int tile, hipStream_t) {
+hipError_t launch_scan(const Scan &a, Dt, hipStream_t) {
   scan_ok(a);
   if (a.L) segments_ok(a, a.nseg > 1);
-  require(tile == 32 || (tile == 64 && dt == Dt::BF16 && a.N <= 128), "tiles");
-  require(wide_tiles(a, tile) * a.nseg < INT_MAX, "grid");
+  require(wide_tiles(a, 32) * a.nseg < INT_MAX, "grid");
   return hipSuccess;
 }
 hipError_t launch_scan_backward(const Scan &a, Dt, hipStream_t) {
