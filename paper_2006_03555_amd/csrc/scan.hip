@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
     }
     float s[8], sx[8], ssum, y[8] = {};
     get_pair<T, W>(tile, cl, tl, sx, s);
-    ssum = lane_steps(a, p, t0, tl, bias, s, sx);
+    ssum = lane_steps(a, lane_left(p, t0, tl), bias, s, sx);
 #pragma unroll
     for (int j = 0; j < 8; ++j) sx[j] *= s[j];
     if (!kOut) seg_steps += ssum;

@@ -5,57 +5,72 @@
 //   dC_t = sum_d e_t h_t,  dB_t = sum_d g_t s_t x_t,  dA = sum_t s_t q_t h_{t-1},
 //   d(s x)_t = sum_n g_t B_t,  ds_t = sum_n A q_t h_{t-1} + x_t d(s x)_t,  dx_t = s_t d(s x)_t + skip e_t
 //
-// Every chunk of 128 tokens is a workgroup of its own: a first pass takes each chunk's sums of
-// h (from the left) and of q (from the right), a second chains them, and the third recomputes
-// h and q inside the chunk from the two states around it. Bound by the vector unit: about 23
-// issue slots per (token, channel, state) in the third pass. dB and dC are sums over channels: a
-// lane adds its two, the wave's four rows are joined by exchanging halves and rows (each exchange
-// leaves half as many values), and the waves add into LDS in turns, wave w at state i + w, so
-// that the order is fixed. What the workgroups of a group of channels leave is added up last.
+// Every chunk of 128 tokens is a workgroup of its own (or a few tiles of channels of it): a first
+// pass takes each chunk's sums of h (from the left) and of q (from the right), a second chains
+// them, and the third recomputes h and q inside the chunk from the two states around it. Bound by
+// the vector unit: about 25 issue slots per (token, channel, state) in the third pass, 9 in the
+// first. dB and dC are sums over channels: the wave's four rows of lanes are joined by exchanging
+// halves and rows (each exchange leaves half as many values), and the waves add into LDS in turns,
+// wave w at state i + w, so that the order is fixed. What the workgroups of a group of channels
+// leave is added up last. Rows reach the lanes through two tiles of LDS, two values to a word in
+// bf16, and their gradients leave the same way.
 #include "scan_common.hpp"
 
 namespace favor {
 namespace {
 
-// Channels per lane and workgroup of the first pass and of the third.
-constexpr int kCh = 2, W = 4 * kScanWaves * kCh;
-constexpr int kTile = kScanBackTile;
-static_assert(kTile == 4 * kScanWaves, "one channel per lane");
+constexpr int W = kScanBackTile;   // channels of a tile, one per lane
+static_assert(W == 4 * kScanWaves && kLoads<W> == 1, "one unit of a thread");
+template <typename T> constexpr bool kBoth = sizeof(T) == 2;   // two tiles hold all four rows
 
-// dy and z of a thread's units as they lie in memory; then e = dy silu(z). Zeros behind the
-// sequence and the group.
-template <typename T, int kWidth> struct Gated {
-  RowVec<T, 8> dy[kLoads<kWidth>], z[kLoads<kWidth>];
+// The rows x, dt, dy and z of a thread's unit (z: x stands in where there is none), by way of two
+// tiles to the lanes, where the four come again as often as they are asked for: in 16 bits they
+// stay in the tiles, else they are put there in turn.
+template <typename T> struct Rows4 {
+  RowVec<T, 8> x, dt, dy, z;
 
-  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0, int tid) {
-#pragma unroll
-    for (int i = 0; i < kLoads<kWidth>; ++i) {
-      const Unit w = unit_of<kWidth>(p, t0, i, tid);
-      dy[i] = get_row<T>(a.dy, a.dys, p, t0, w);
-      if (a.z) z[i] = get_row<T>(a.z, a.zs, p, t0, w);
-    }
+  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0, const Unit &w) {
+    x = get_row<T>(a.x, a.xs, p, t0, w);
+    dt = get_row<T>(a.dt, a.dts, p, t0, w);
+    dy = get_row<T>(a.dy, a.dys, p, t0, w);
+    z = get_row<T>(a.z ? a.z : a.x, a.z ? a.zs : a.xs, p, t0, w);
   }
-  __device__ __forceinline__ void get(const Scan &a, const Unit &w, int i, float *e) const {
-    float g[8];
-    dy[i].get(e);
-    if (a.z) {
-      z[i].get(g);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) e[k] *= g[k] * sigmoid(g[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) e[k] = w.live ? e[k] : 0.f;
+  __device__ __forceinline__ void put(float *tiles, const Unit &w) const {
+    put_pair<W>(tiles, w, x, dt);
+    if (kBoth<T>) put_pair<W>(tiles + W * kTok, w, dy, z);
+  }
+  __device__ __forceinline__ void put_rest(float *tiles, const Unit &w) const {   // for whole workgroups
+    if (kBoth<T>) return;
+    __syncthreads();
+    put_pair<W>(tiles, w, dy, z);
+    __syncthreads();
+  }
+  static __device__ __forceinline__ void get(const float *tiles, int c, int tl, float (&v0)[8], float (&v1)[8]) {
+    get_pair<T, W>(tiles, c, tl, v0, v1);
+  }
+  static __device__ __forceinline__ void get_rest(const float *tiles, int c, int tl, float (&v0)[8], float (&v1)[8]) {
+    get_pair<T, W>(tiles + (kBoth<T> ? W * kTok : 0), c, tl, v0, v1);
   }
 };
+// e = dy silu(z); zeros from token `left` on.
+__device__ __forceinline__ void lane_gated(const Scan &a, int left, float (&e)[8], const float (&z)[8]) {
+  if (a.z)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] *= z[j] * sigmoid(z[j]);
+  if (left < 8)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j >= left) e[j] = 0.f;
+}
 
 template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_parts(Scan a) {
   extern __shared__ __align__(16) float lds[];
-  float *tile = lds, *tb = tile + W * kTok, *tc = tb + kStates * kTok;
+  float *tiles = lds, *tb = tiles + 2 * W * kTok, *tc = tb + kStates * kTok;
   float *tA = tc + kStates * kTok, *th = tA + kStates * W, *tq = th + kStates * W;
   const ScanPlace p = scan_place(a, W);
   int tid = threadIdx.x;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
-  const int cl = 4 * kCh * wave + lane / 16;
+  const int cl = 4 * wave + lane / 16, c = p.c0 + cl;   // this lane's channel
   const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
   const int64_t t0 = (int64_t)p.seg * kTok;
   if (t0 >= p.n) {   // no token: nothing is added
@@ -65,87 +80,62 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
       a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + p.c0 + threadIdx.x] = 0.f;
     return;
   }
-  float s[kCh][8], sx[kCh][8], e[kCh][8], ssum[kCh];
+  const Unit w = unit_of<W>(p, t0, 0, tid);
+  Rows4<T> rows;
   States<T> low_b, low_c;
-  {
-    // everything is requested at once; the tile holds the steps, then s x, then e
-    Steps<T, W> steps;
-    Gated<T, W> gated;
-    float in[kLoads<W>][8];
-    steps.load(a, p, t0, tid);
-    gated.load(a, p, t0, tid);
-    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
-    low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
-#pragma unroll
-    for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i, tid);
-      float own[8];
-      steps.template get<true>(a, w, i, own, in[i]);
-      put_unit(tile, w, own);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, s[i]);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kLoads<W>; ++i) put_unit(tile, unit_of<W>(p, t0, i, tid), in[i]);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kCh; ++i) tile_load(tile, cl + 4 * i, tl, sx[i]);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kLoads<W>; ++i) {
-      const Unit w = unit_of<W>(p, t0, i, tid);
-      gated.get(a, w, i, in[i]);
-      put_unit(tile, w, in[i]);
-    }
-  }
+  rows.load(a, p, t0, w);
+  low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
+  low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
+  const float bias = a.bias ? a.bias[min(c, p.cend - 1)] : 0.f;
+  float s[8], sx[8], e[8], ssum = 0.f;
   for (int n0 = 0; n0 < a.N; n0 += kStates) {
     const int count = min(kStates, a.N - n0);
     if (n0) {
       low_b.load(a.b, a.bs, p, t0, n0, count, tid);
       low_c.load(a.c, a.cs, p, t0, n0, count, tid);
+    } else {
+      rows.put(tiles, w);
     }
     low_b.put(tb, p, t0, count, tid);
     low_c.put(tc, p, t0, count, tid);
     load_channels<W>(a.A, p, a.N, n0, count, kLog2e, tA, tid);
     __syncthreads();
     if (n0 == 0) {
+      float z[8];
+      rows.get(tiles, cl, tl, sx, s);
+      rows.put_rest(tiles, w);
+      rows.get_rest(tiles, cl, tl, e, z);
+      lane_gated(a, lane_left(p, t0, tl), e, z);
+      ssum = lane_steps(a, lane_left(p, t0, tl), bias, s, sx);
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) {
-        tile_load(tile, cl + 4 * i, tl, e[i]);
-        ssum[i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) ssum[i] += s[i][j];
-        const float total = row_sum(ssum[i]);
-        const int c = p.c0 + cl + 4 * i;
-        if (tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
-      }
+      for (int j = 0; j < 8; ++j) sx[j] *= s[j];
+      const float total = row_sum(ssum);
+      if (tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
     }
-    for (int n = 0; n < count; ++n) {
-      float Bv[8], Cv[8], S[kCh], Q[kCh], P[kCh], P2[kCh], h[kCh], q[kCh];
-      lane_load(tb + n * kTok, tl, Bv);
-      lane_load(tc + n * kTok, tl, Cv);
+    for (int n = 0; n < count; n += 2) {   // two states at once; one behind the last is zeros
+      float Bv[2][8], Cv[2][8], S[2], Q[2], P[2], P2[2], h[2] = {}, q[2] = {};
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) {
-        const float A = tA[n * W + cl + 4 * i];
+      for (int i = 0; i < 2; ++i) {
+        lane_load(tb + (n + i) * kTok, tl, Bv[i]);
+        lane_load(tc + (n + i) * kTok, tl, Cv[i]);
+        const float A = tA[(n + i) * W + cl];
         float at[8];
-        S[i] = Q[i] = h[i] = q[i] = 0.f;
+        S[i] = Q[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          at[j] = exp2_hw(s[i][j] * A);
-          S[i] = fmaf(at[j], S[i], sx[i][j] * Bv[j]);
+          at[j] = exp2_hw(s[j] * A);
+          S[i] = fmaf(at[j], S[i], sx[j] * Bv[i][j]);
         }
 #pragma unroll
-        for (int j = 7; j >= 0; --j) Q[i] = at[j] * fmaf(e[i][j], Cv[j], Q[i]);
-        P[i] = P2[i] = exp2_hw(ssum[i] * A);
+        for (int j = 7; j >= 0; --j) Q[i] = at[j] * fmaf(e[j], Cv[i][j], Q[i]);
+        P[i] = P2[i] = exp2_hw(ssum * A);
       }
       row_scan2<false>(S[0], P[0], h[0], S[1], P[1], h[1]);
       row_scan2<true>(Q[0], P2[0], q[0], Q[1], P2[1], q[1]);
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) {
-        if (tl == 15) th[n * W + cl + 4 * i] = S[i];
-        if (tl == 0) tq[n * W + cl + 4 * i] = Q[i];
+      for (int i = 0; i < 2; ++i) {
+        if (tl == 15) th[(n + i) * W + cl] = S[i];
+        if (tl == 0) tq[(n + i) * W + cl] = Q[i];
       }
     }
     __syncthreads();
@@ -153,6 +143,23 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
     store_channels<W>(a.part + at_part, p, a.N, n0, count, th, tid);
     store_channels<W>(a.part_r + at_part, p, a.N, n0, count, tq, tid);
   }
+}
+
+// Two values in a word, the first in its low half.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const bf16 v[2] = {from_f32<bf16>(lo), from_f32<bf16>(hi)};
+  return __builtin_bit_cast(uint32_t, v);
+}
+// The low or the high halves of eight words as a row.
+__device__ __forceinline__ void put_halves(void *base, const Rows &r, const ScanPlace &p, int64_t t0, const Unit &w,
+                                           const uint32_t (&d)[8], uint32_t halves) {
+  uint4 v;
+  v.x = __builtin_amdgcn_perm(d[1], d[0], halves);
+  v.y = __builtin_amdgcn_perm(d[3], d[2], halves);
+  v.z = __builtin_amdgcn_perm(d[5], d[4], halves);
+  v.w = __builtin_amdgcn_perm(d[7], d[6], halves);
+  bf16 *to = chunk_rows(static_cast<bf16 *>(base), r, p, t0) + ((uint32_t)w.t * (uint32_t)r.t + (uint32_t)w.c);
+  *reinterpret_cast<uint4 *>(to) = v;
 }
 
 // The sums of 16 values over the wave's four rows of lanes; row r keeps values 4 r' .. 4 r' + 3
@@ -174,61 +181,47 @@ __device__ __forceinline__ f32x4 join_rows(const float (&v)[8], const float (&w)
   return o;
 }
 
-// A workgroup takes a.subs tiles of kTile channels one after the other, so that dB and dC are
+// A workgroup takes a.subs tiles of W channels one after the other, so that dB and dC are
 // sums over all of them before they leave it.
 template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_backward(Scan a) {
   extern __shared__ __align__(16) float lds[];
-  float *t1 = lds, *t2 = t1 + kTile * kTok, *tb = t2 + kTile * kTok, *tc = tb + kStates * kTok;
+  float *tiles = lds, *tb = tiles + 2 * W * kTok, *tc = tb + kStates * kTok;
   float *tlow = tc + kStates * kTok;   // dB, then dC
-  float *tA = tlow + 2 * kStates * kTok, *th = tA + kStates * kTile, *tq = th + kStates * kTile;
-  ScanPlace p = scan_place(a, kTile * a.subs);
+  float *tA = tlow + 2 * kStates * kTok, *th = tA + kStates * W, *tq = th + kStates * W;
+  ScanPlace p = scan_place(a, W * a.subs);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
   const int cl = 4 * wave + lane / 16;
   const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
   const int64_t at_sum = ((int64_t)p.b * a.nseg + p.seg) * a.D;
   const int64_t t0 = (int64_t)p.seg * kTok;
   const bool some = t0 < p.n;
-  for (int sub = 0; sub < a.subs && p.c0 < p.cend; ++sub, p.c0 += kTile) {
+  for (int sub = 0; sub < a.subs && p.c0 < p.cend; ++sub, p.c0 += W) {
     const int c = p.c0 + cl;   // this lane's channel
     const bool channel = c < p.cend;
-    static_assert(kLoads<kTile> == 1, "one unit of a thread");
     if (!some) {
-      for (int i = threadIdx.x; i < min(kTile, p.cend - p.c0) * a.N; i += kScanThreads)
+      for (int i = threadIdx.x; i < min(W, p.cend - p.c0) * a.N; i += kScanThreads)
         a.part_a[at_part + (int64_t)p.c0 * a.N + i] = 0.f;
       if (tl == 15 && channel) {
         if (a.dskip) a.part_d[at_sum + c] = 0.f;
         if (a.dbias) a.part_s[at_sum + c] = 0.f;
       }
-      const Unit w = unit_of<kTile>(p, t0, 0, threadIdx.x);
+      const Unit w = unit_of<W>(p, t0, 0, threadIdx.x);
       const float none[8] = {};
       if (w.t >= a.L - t0 || w.c >= p.cend) continue;
       put_row<T>(a.dx, a.dxs, p, t0, w, none);
       put_row<T>(a.ddt, a.ddts, p, t0, w, none);
       if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, none);
     } else {
+      // a lane without a channel adds nothing to dB and dC
+      const int left = channel ? lane_left(p, t0, tl) : 0;
       float s[8], sx[8], e[8], ds[8], dsx[8], y[8], ssum = 0.f;
       States<T> low_b, low_c;
+      Rows4<T> rows;
       int tid = fresh_thread();
-      {
-        const Unit w = unit_of<kTile>(p, t0, 0, tid);
-        Steps<T, kTile> steps;
-        Gated<T, kTile> gated;
-        float own[8], x[8];
-        steps.load(a, p, t0, tid);
-        gated.load(a, p, t0, tid);
-        if (sub == 0) {
-          low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
-          low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
-        }
-        steps.template get<false>(a, w, 0, own, x);
-        put_unit(t1, w, own);   // the last tile's readers are behind a barrier
-        put_unit(t2, w, x);
-        __syncthreads();
-        tile_load(t1, cl, tl, s);
-        tile_load(t2, cl, tl, sx);
-        __syncthreads();
-        gated.get(a, w, 0, x);
-        put_unit(t1, w, x);
+      rows.load(a, p, t0, unit_of<W>(p, t0, 0, tid));
+      if (sub == 0) {
+        low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
+        low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
       }
       for (int n0 = 0; n0 < a.N; n0 += kStates) {
         const int count = min(kStates, a.N - n0);
@@ -236,23 +229,28 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
           tid = fresh_thread();
           low_b.load(a.b, a.bs, p, t0, n0, count, tid);
           low_c.load(a.c, a.cs, p, t0, n0, count, tid);
+        } else {
+          rows.put(tiles, unit_of<W>(p, t0, 0, tid));   // the last tile's readers are behind a barrier
         }
         if (sub == 0) {
           low_b.put(tb, p, t0, count, tid);
           low_c.put(tc, p, t0, count, tid);
         }
-        load_channels<kTile>(a.A, p, a.N, n0, count, 1.f, tA, tid);
-        load_channels<kTile>(a.part + at_part, p, a.N, n0, count, 1.f, th, tid);
-        load_channels<kTile>(a.part_r + at_part, p, a.N, n0, count, 1.f, tq, tid);
+        load_channels<W>(a.A, p, a.N, n0, count, 1.f, tA, tid);
+        load_channels<W>(a.part + at_part, p, a.N, n0, count, 1.f, th, tid);
+        load_channels<W>(a.part_r + at_part, p, a.N, n0, count, 1.f, tq, tid);
         __syncthreads();
         if (n0 == 0) {
-          tile_load(t1, cl, tl, e);
-          float skip = 0.f;
+          float z[8], skip = 0.f;
+          rows.get(tiles, cl, tl, sx, s);
+          rows.put_rest(tiles, unit_of<W>(p, t0, 0, tid));
+          rows.get_rest(tiles, cl, tl, e, z);
+          lane_gated(a, left, e, z);
+          ssum = lane_steps(a, left, a.bias ? a.bias[min(c, p.cend - 1)] : 0.f, s, sx);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             skip = fmaf(e[j], sx[j], skip);
             sx[j] *= s[j];
-            ssum += s[j];
             ds[j] = dsx[j] = y[j] = 0.f;
           }
           if (a.dskip) {
@@ -263,7 +261,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
         const int each = (count + kScanWaves - 1) / kScanWaves;   // states of a wave's turn
         for (int turn = 0; turn < kScanWaves; ++turn) {
           for (int k = 0; k < each; ++k) {
-            const int n = ((turn + wave) % kScanWaves) * each + k, at_c = n * kTile + cl;
+            const int n = ((turn + wave) % kScanWaves) * each + k, at_c = n * W + cl;
             float Bv[8], Cv[8], at[8], bx[8], ce[8], dB[8], dC[8];
             lane_load(tb + n * kTok, tl, Bv);
             lane_load(tc + n * kTok, tl, Cv);
@@ -311,7 +309,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
           __syncthreads();
         }
         tid = fresh_thread();
-        if (sub + 1 == a.subs || p.c0 + kTile >= p.cend) {
+        if (sub + 1 == a.subs || p.c0 + W >= p.cend) {
           const int n = tid % kStates, first = tid / kStates;
           const int64_t base = ((((int64_t)p.tile * a.B + p.b) * a.L + t0) * a.G + p.g) * a.N + n0 + n;
           const int64_t stride = (int64_t)a.G * a.N;
@@ -324,81 +322,77 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
             a.part_c[base + t * stride] = tlow[(kStates + n) * kTok + token_at(t)];
           }
         }
-        store_channels<kTile>(a.part_a + at_part, p, a.N, n0, count, th, tid);
+        store_channels<W>(a.part_a + at_part, p, a.N, n0, count, th, tid);
+        if (n0 + kStates < a.N) __syncthreads();
+      }
+      // the rows' gradients, where the lanes have the sums; in place of what only the lane reads
+      const float bias = a.bias ? a.bias[min(c, p.cend - 1)] : 0.f;
+      const float skip = a.skip ? a.skip[min(c, p.cend - 1)] : 0.f;
+      float x[8], raw[8], dy[8], z[8], dbias = 0.f;
+      if (!kBoth<T>) {
+        tid = fresh_thread();
+        rows.load(a, p, t0, unit_of<W>(p, t0, 0, tid));
+        rows.put(tiles, unit_of<W>(p, t0, 0, tid));
         __syncthreads();
       }
-      tid = fresh_thread();
-      const Unit w = unit_of<kTile>(p, t0, 0, tid);
-      Steps<T, kTile> steps;
-      Gated<T, kTile> gated;
-      float dx[8], ddt[8], dz[8];
-      steps.load(a, p, t0, tid);
-      gated.load(a, p, t0, tid);
-      tile_store(t1, cl, tl, ds);   // in place of what only this lane has read
-      tile_store(t2, cl, tl, dsx);
-      __syncthreads();
+      rows.get(tiles, cl, tl, x, raw);
+      rows.put_rest(tiles, unit_of<W>(p, t0, 0, tid));
+      rows.get_rest(tiles, cl, tl, dy, z);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int at = tile_at(8 * w.u + k, w.t);
-        ddt[k] = t1[at];
-        dx[k] = t2[at];
-      }
-      __syncthreads();
-      if (a.z) tile_store(t1, cl, tl, y);
-      __syncthreads();
-      if (w.live) {
-        float x[8], raw[8], ev[8], z[8], step[8], skip[8];
-        steps.x[0].get(x);
-        steps.dt[0].get(raw);
-        gated.dy[0].get(ev);
-        if (a.z) gated.z[0].get(z);
-        if (a.bias)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) raw[k] += a.bias[w.c + k];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) skip[k] = 0.f;
-        if (a.skip)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) skip[k] = a.skip[w.c + k];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) ddt[k] = fmaf(x[k], dx[k], ddt[k]);
-        if (a.softplus) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            step[k] = softplus(raw[k]);
-            ddt[k] *= softplus_slope(raw[k], step[k]);
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) step[k] = raw[k];
+      for (int j = 0; j < 8; ++j) {
+        ds[j] = fmaf(x[j], dsx[j], ds[j]);
+        if (a.softplus) ds[j] *= softplus_slope(raw[j] + bias, s[j]);
+        dbias += j < left ? ds[j] : 0.f;
+        dsx[j] = fmaf(s[j], dsx[j], skip * e[j]);
+        if (a.z) {
+          const float g = sigmoid(z[j]);
+          y[j] = dy[j] * fmaf(skip, x[j], y[j]) * (g * fmaf(z[j], 1.f - g, 1.f));
         }
-        if (a.z)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float g = sigmoid(z[k]), v = fmaf(skip[k], x[k], t1[tile_at(8 * w.u + k, w.t)]);
-            dz[k] = ev[k] * v * (g * fmaf(z[k], 1.f - g, 1.f));
-            ev[k] *= z[k] * g;
-          }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dx[k] = fmaf(step[k], dx[k], skip[k] * ev[k]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dx[k] = ddt[k] = dz[k] = 0.f;
-      }
-      if (w.t < a.L - t0 && w.c < p.cend) {
-        put_row<T>(a.dx, a.dxs, p, t0, w, dx);
-        put_row<T>(a.ddt, a.ddts, p, t0, w, ddt);
-        if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, dz);
       }
       if (a.dbias) {
-        float v[8], total = 0.f;
-        put_unit(t2, w, ddt);
-        __syncthreads();
-        tile_load(t2, cl, tl, v);
+        dbias = row_sum(dbias);
+        if (tl == 15 && channel) a.part_s[at_sum + c] = dbias;
+      }
+      tid = fresh_thread();
+      const Unit w = unit_of<W>(p, t0, 0, tid);
+      const bool mine = w.t < a.L - t0 && w.c < p.cend;
+      if constexpr (kBoth<T>) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) total += v[j];
-        total = row_sum(total);
-        if (tl == 15 && channel) a.part_s[at_sum + c] = total;
+        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(pack_bf16(dsx[j], ds[j]));
+        tile_store(tiles, cl, tl, x);
+        tile_store(tiles + W * kTok, cl, tl, y);
+        __syncthreads();
+        uint32_t d[8];
+        float o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int at = tile_at(8 * w.u + k, w.t);
+          d[k] = w.live ? __float_as_uint(tiles[at]) : 0;
+          o[k] = w.live ? tiles[W * kTok + at] : 0.f;
+        }
+        if (mine) {
+          put_halves(a.dx, a.dxs, p, t0, w, d, 0x05040100u);
+          put_halves(a.ddt, a.ddts, p, t0, w, d, 0x07060302u);
+          if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, o);
+        }
+      } else {
+        const auto rows_out = [&](void *dst, const Rows &r, const float *tile) {
+          float o[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) o[k] = w.live ? tile[tile_at(8 * w.u + k, w.t)] : 0.f;
+          if (mine) put_row<T>(dst, r, p, t0, w, o);
+        };
+        tile_store(tiles, cl, tl, dsx);
+        tile_store(tiles + W * kTok, cl, tl, ds);
+        __syncthreads();
+        rows_out(a.dx, a.dxs, tiles);
+        rows_out(a.ddt, a.ddts, tiles + W * kTok);
+        if (a.z) {
+          __syncthreads();
+          tile_store(tiles, cl, tl, y);
+          __syncthreads();
+          rows_out(a.dz, a.dzs, tiles);
+        }
       }
       __syncthreads();
     }
@@ -468,21 +462,21 @@ hipError_t launch_tiles(K kernel, const Scan &a, int width, size_t lds, hipStrea
 }  // namespace
 
 hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st) {
-  const size_t lds = sizeof(float) * (W * kTok + 2 * kStates * kTok + 3 * kStates * W);
+  const size_t lds = sizeof(float) * (2 * W * kTok + 2 * kStates * kTok + 3 * kStates * W);
   return dt == Dt::BF16 ? launch_tiles(k_scan_parts<bf16>, a, W, lds, st)
                         : launch_tiles(k_scan_parts<float>, a, W, lds, st);
 }
 
 hipError_t launch_scan_backward(const Scan &a, Dt dt, hipStream_t st) {
-  const size_t lds = sizeof(float) * (2 * kTile * kTok + 4 * kStates * kTok + 3 * kStates * kTile);
-  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, kTile * a.subs, lds, st)
-                        : launch_tiles(k_scan_backward<float>, a, kTile * a.subs, lds, st);
+  const size_t lds = sizeof(float) * (2 * W * kTok + 4 * kStates * kTok + 3 * kStates * W);
+  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, W * a.subs, lds, st)
+                        : launch_tiles(k_scan_backward<float>, a, W * a.subs, lds, st);
 }
 
 hipError_t launch_scan_backward_sums(const Scan &a, Dt dt, hipStream_t st) {
   const int64_t low = (int64_t)a.L * a.G * a.N;
   if (low > 0) {
-    const int tiles = (a.D / a.G + kTile * a.subs - 1) / (kTile * a.subs);
+    const int tiles = (a.D / a.G + W * a.subs - 1) / (W * a.subs);
     const dim3 grid((unsigned)((low + kLowThreads - 1) / kLowThreads), a.B, 2);
     if (dt == Dt::BF16) k_scan_low<bf16><<<grid, kLowThreads, 0, st>>>(a, tiles);
     else k_scan_low<float><<<grid, kLowThreads, 0, st>>>(a, tiles);

@@ -258,15 +258,17 @@ __device__ __forceinline__ void get_pair(const float *tile, int c, int tl, float
     tile_load(tile + kWidth * kTok, c, tl, v1);
   }
 }
-// A lane's steps from its dt, and their sum; steps and x are zeros behind the sequence.
-__device__ __forceinline__ float lane_steps(const Scan &a, const ScanPlace &p, int64_t t0, int tl, float bias,
-                                            float (&s)[8], float (&x)[8]) {
+// How many of a lane's eight tokens are inside the sequence (8 or more: all).
+__device__ __forceinline__ int lane_left(const ScanPlace &p, int64_t t0, int tl) {
+  return (int)min((int64_t)kTok, p.n - t0) - 8 * tl;
+}
+// A lane's steps from its dt, and their sum; steps and x are zeros from token `left` on.
+__device__ __forceinline__ float lane_steps(const Scan &a, int left, float bias, float (&s)[8], float (&x)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     s[j] += bias;
     if (a.softplus) s[j] = softplus(s[j]);
   }
-  const int left = (int)min((int64_t)kTok, p.n - t0) - 8 * tl;
   if (left < 8)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
