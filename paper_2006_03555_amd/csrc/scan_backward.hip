@@ -158,8 +158,7 @@ __device__ __forceinline__ void put_halves(void *base, const Rows &r, const Scan
   v.y = __builtin_amdgcn_perm(d[3], d[2], halves);
   v.z = __builtin_amdgcn_perm(d[5], d[4], halves);
   v.w = __builtin_amdgcn_perm(d[7], d[6], halves);
-  bf16 *to = chunk_rows(static_cast<bf16 *>(base), r, p, t0) + ((uint32_t)w.t * (uint32_t)r.t + (uint32_t)w.c);
-  *reinterpret_cast<uint4 *>(to) = v;
+  *reinterpret_cast<uint4 *>(row_out<bf16>(base, r, p, t0, w)) = v;
 }
 
 // The sums of 16 values over the wave's four rows of lanes; row r keeps values 4 r' .. 4 r' + 3
@@ -341,14 +340,19 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         ds[j] = fmaf(x[j], dsx[j], ds[j]);
-        if (a.softplus) ds[j] *= softplus_slope(raw[j] + bias, s[j]);
-        dbias += j < left ? ds[j] : 0.f;
         dsx[j] = fmaf(s[j], dsx[j], skip * e[j]);
-        if (a.z) {
+      }
+      if (a.softplus)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ds[j] *= softplus_slope(raw[j] + bias, s[j]);
+      if (a.z)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
           const float g = sigmoid(z[j]);
           y[j] = dy[j] * fmaf(skip, x[j], y[j]) * (g * fmaf(z[j], 1.f - g, 1.f));
         }
-      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dbias += j < left ? ds[j] : 0.f;
       if (a.dbias) {
         dbias = row_sum(dbias);
         if (tl == 15 && channel) a.part_s[at_sum + c] = dbias;

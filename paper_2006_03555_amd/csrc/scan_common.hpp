@@ -7,6 +7,8 @@
 // one fused multiply-add and one product each.
 #pragma once
 
+#include <type_traits>
+
 #include "recurrent.hpp"
 #include "vec_rows.hpp"
 
@@ -165,65 +167,39 @@ __device__ __forceinline__ Unit unit_of(const ScanPlace &p, int64_t t0, int i, i
 }
 // Loads ask for valid rows whether they are wanted or not (a chunk that is read has a token): a
 // condition around each would wait for one before the next is requested.
-// Rows of one chunk: a uniform base and 32-bit offsets (tokens are at most 2^25 bytes apart).
+// Rows of one chunk: a uniform base and 32-bit byte offsets (tokens are at most 2^25 bytes apart),
+// which the loads take as they are.
 template <typename T>
 __device__ __forceinline__ T *chunk_rows(T *base, const Rows &r, const ScanPlace &p, int64_t t0) {
   return base + p.b * r.b + t0 * r.t;
+}
+template <typename T> __device__ __forceinline__ T *at_byte(T *base, uint32_t offset) {
+  using Byte = std::conditional_t<std::is_const_v<T>, const char, char>;
+  return reinterpret_cast<T *>(reinterpret_cast<Byte *>(base) + offset);
+}
+template <typename T> __device__ __forceinline__ uint32_t row_bytes(const Rows &r, int t, int c) {
+  return (uint32_t)sizeof(T) * ((uint32_t)t * (uint32_t)r.t + (uint32_t)c);
 }
 template <typename T>
 __device__ __forceinline__ RowVec<T, 8> get_row(const void *base, const Rows &r, const ScanPlace &p, int64_t t0,
                                                 const Unit &w) {
   RowVec<T, 8> v;
-  v.load(chunk_rows(static_cast<const T *>(base), r, p, t0) +
-         ((uint32_t)w.tl * (uint32_t)r.t + (uint32_t)w.cl));
+  v.load(at_byte(chunk_rows(static_cast<const T *>(base), r, p, t0), row_bytes<T>(r, w.tl, w.cl)));
   return v;
+}
+template <typename T>
+__device__ __forceinline__ T *row_out(void *base, const Rows &r, const ScanPlace &p, int64_t t0, const Unit &w) {
+  return at_byte(chunk_rows(static_cast<T *>(base), r, p, t0), row_bytes<T>(r, w.t, w.c));
 }
 template <typename T>
 __device__ __forceinline__ void put_row(void *base, const Rows &r, const ScanPlace &p, int64_t t0, const Unit &w,
                                         const float *v) {
-  store_row<8>(chunk_rows(static_cast<T *>(base), r, p, t0) + ((uint32_t)w.t * (uint32_t)r.t + (uint32_t)w.c), v);
+  store_row<8>(row_out<T>(base, r, p, t0, w), v);
 }
 __device__ __forceinline__ void put_unit(float *tile, const Unit &w, const float *v) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) tile[tile_at(8 * w.u + k, w.t)] = v[k];
 }
-
-// Steps s = softplus(dt + bias) of eight channels.
-__device__ __forceinline__ void steps_of(const Scan &a, const Unit &w, float *s) {
-  if (a.bias)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[k] += a.bias[w.cl + k];
-  if (a.softplus)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[k] = softplus(s[k]);
-}
-
-// x and dt of a thread's units as they lie in memory, requested together; then s and s x (or
-// x) of them. Zeros behind the sequence and the group.
-template <typename T, int kWidth> struct Steps {
-  RowVec<T, 8> x[kLoads<kWidth>], dt[kLoads<kWidth>];
-
-  __device__ __forceinline__ void load(const Scan &a, const ScanPlace &p, int64_t t0, int tid) {
-#pragma unroll
-    for (int i = 0; i < kLoads<kWidth>; ++i) {
-      const Unit w = unit_of<kWidth>(p, t0, i, tid);
-      x[i] = get_row<T>(a.x, a.xs, p, t0, w);
-      dt[i] = get_row<T>(a.dt, a.dts, p, t0, w);
-    }
-  }
-  template <bool kProduct>
-  __device__ __forceinline__ void get(const Scan &a, const Unit &w, int i, float *s, float *v) const {
-    x[i].get(v);
-    dt[i].get(s);
-    steps_of(a, w, s);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      s[k] = w.live ? s[k] : 0.f;
-      v[k] = w.live ? v[k] : 0.f;
-      if (kProduct) v[k] *= s[k];
-    }
-  }
-};
 
 // Two rows of a tile on their way from memory to lanes (x and dt, dy and z): in bf16 both in one
 // word, else a tile each.
@@ -265,10 +241,10 @@ __device__ __forceinline__ int lane_left(const ScanPlace &p, int64_t t0, int tl)
 // A lane's steps from its dt, and their sum; steps and x are zeros from token `left` on.
 __device__ __forceinline__ float lane_steps(const Scan &a, int left, float bias, float (&s)[8], float (&x)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    s[j] += bias;
-    if (a.softplus) s[j] = softplus(s[j]);
-  }
+  for (int j = 0; j < 8; ++j) s[j] += bias;
+  if (a.softplus)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = softplus(s[j]);
   if (left < 8)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -289,20 +265,20 @@ template <typename T> struct States {
                                        int count, int tid) {
     const T *base = chunk_rows(static_cast<const T *>(src), r, p, t0) + p.g * r.h + n0;
     const int left = (int)min((int64_t)kTok, p.n - t0);
+    const uint32_t first = (uint32_t)(tid / kStates) * (uint32_t)r.t, last = (uint32_t)(left - 1) * (uint32_t)r.t;
     const uint32_t n = min(tid % kStates, count - 1);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint32_t t = min(tid / kStates + i * kStep, left - 1);
-      v[i] = base[t * (uint32_t)r.t + n];
-    }
+    for (int i = 0; i < kEach; ++i)
+      v[i] = *at_byte(base, (uint32_t)sizeof(T) * (min(first + i * kStep * (uint32_t)r.t, last) + n));
   }
   __device__ __forceinline__ void put(float *tile, const ScanPlace &p, int64_t t0, int count, int tid) const {
+    static_assert(kStep % 8 == 0, "places of tokens kStep apart");
     const int n = tid % kStates, t1 = tid / kStates;
-    const int left = (int)min((int64_t)kTok, p.n - t0);
+    const int left = n < count ? (int)min((int64_t)kTok, p.n - t0) : 0;
+    float *to = tile + n * kTok + token_at(t1);
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      tile[n * kTok + token_at(t1 + i * kStep)] =
-          n < count && t1 + i * kStep < left ? to_f32(v[i]) : 0.f;
+      to[token_at(i * kStep)] = t1 + i * kStep < left ? to_f32(v[i]) : 0.f;
   }
 };
 
