@@ -225,7 +225,7 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
 
 // A workgroup per entry: a wave joins the pieces of a beam, then each candidate finds its rank
 // among all beams' (in a sorted list by halving).
-constexpr int kMergeWaves = 8;
+constexpr int kMergeWaves = 8, kEarly = 8;
 __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
   __shared__ uint64_t lists[kMergeWaves][kCandidates + 2 * kMaxN + 8];
   extern __shared__ double score[];   // [K][n], best first
@@ -242,7 +242,16 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
       }
       continue;
     }
-    const float2 st = lane < a.pieces ? a.stats[row * a.pieces + lane] : float2{-INFINITY, 0.f};
+    // all that is small is requested at once: the pieces' statistics, their r-th keys, and as many
+    // of the keys as most calls have
+    const int keys = a.pieces * n, r = (n + a.pieces - 1) / a.pieces;
+    const uint64_t *of_row = a.keys + row * keys;
+    const float2 of_piece = a.stats[row * a.pieces + min(lane, a.pieces - 1)];
+    const uint64_t rth = of_row[min(lane, a.pieces - 1) * n + r - 1];
+    uint64_t early[kEarly];
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j) early[j] = of_row[min(64 * j + lane, keys - 1)];
+    const float2 st = lane < a.pieces ? of_piece : float2{-INFINITY, 0.f};
     float top = st.x;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
@@ -255,21 +264,24 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
     best.sorted = lists[wave] + kCandidates + kMaxN + 8;
     best.n = n;
     // the k-th best of the pieces' r-th keys has r k >= n keys not below it: only those are joined
-    const int keys = a.pieces * n, r = (n + a.pieces - 1) / a.pieces;
     WaveBest column = best;
     column.n = (n + r - 1) / r;
-    column.push(lane < a.pieces ? a.keys[row * keys + lane * n + r - 1] : 0);
+    column.push(lane < a.pieces ? rth : 0);
     const uint64_t bound = column.last ? column.last : 1;
     int held = 0;
-    for (int i = lane; i - lane < keys; i += 64) {
-      const uint64_t key = i < keys ? a.keys[row * keys + i] : 0;
-      const uint64_t who = __ballot(key >= bound);
-      if (key >= bound) best.list[held + before(who)] = key;
+    const auto take = [&](uint64_t key, int i0) {   // keys i0 .. i0 + 63 of the row
+      const bool good = i0 + lane < keys && key >= bound;
+      const uint64_t who = __ballot(good);
+      if (good) best.list[held + before(who)] = key;
       held += __popcll(who);
-      if (held <= kCandidates - 64 && i - lane + 64 < keys) continue;
+      if (held <= kCandidates - 64 && i0 + 64 < keys) return;
       if (held) best.join(held);
       held = 0;
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j)
+      if (64 * j < keys) take(early[j], 64 * j);
+    for (int i0 = 64 * kEarly; i0 < keys; i0 += 64) take(of_row[min(i0 + lane, keys - 1)], i0);
     const float x = unordered((uint32_t)(best.top >> 32));
     const double s = own + (((double)x - top) - rest);
     const bool offered = best.top && s - s == 0.0;
