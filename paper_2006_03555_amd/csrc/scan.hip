@@ -47,7 +47,7 @@ __device__ __forceinline__ void forward_states(const float (&s)[8], const float 
     P[k] = exp2_hw(ssum * in[k].A);
   }
   if constexpr (K == 2) row_scan2<false>(S[0], P[0], h[0], S[1], P[1], h[1]);
-  else row_scan<false>(S[0], P[0], h[0]);
+  else row_scan(S[0], P[0], h[0]);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     if constexpr (kOut) {

@@ -15,7 +15,6 @@
 namespace favor {
 
 constexpr int kTok = kScanTokens;   // tokens of a chunk: 16 lanes of 8
-constexpr int kLaneTok = 8;
 constexpr int kScanWaves = 8;
 constexpr int kScanThreads = 64 * kScanWaves;
 constexpr int kStates = 16;         // states of one pass over a chunk
@@ -76,19 +75,16 @@ __device__ __forceinline__ void row_scan2(float &S0, float &P0, float &h0, float
     asm(FAVOR_SCAN2_ALL("row_shr")
         : "+v"(S0), "+v"(P0), "+v"(h0), "+v"(S1), "+v"(P1), "+v"(h1));
 }
-#define FAVOR_SCAN1(shift)                                                     \
-  "v_fmac_f32_dpp %0, %0, %1 " shift " row_mask:0xf bank_mask:0xf\n"            \
-  "v_mul_f32_dpp %1, %1, %1 " shift " row_mask:0xf bank_mask:0xf\n"             \
+#define FAVOR_SCAN1(n)                                                   \
+  "v_fmac_f32_dpp %0, %0, %1 row_shr:" n " row_mask:0xf bank_mask:0xf\n" \
+  "v_mul_f32_dpp %1, %1, %1 row_shr:" n " row_mask:0xf bank_mask:0xf\n"  \
   "s_nop 1\n"
-#define FAVOR_SCAN1_ALL(dir)                                                   \
-  "s_nop 1\n" FAVOR_SCAN1(dir ":1") FAVOR_SCAN1(dir ":2") FAVOR_SCAN1(dir ":4") \
-  "v_fmac_f32_dpp %0, %0, %1 " dir ":8 row_mask:0xf bank_mask:0xf\n"           \
-  "s_nop 1\n"                                                                  \
-  "v_mov_b32_dpp %2, %0 " dir ":1 row_mask:0xf bank_mask:0xf\n"
-template <bool kRight>
-__device__ __forceinline__ void row_scan(float &S, float &P, float &h) {
-  if constexpr (kRight) asm(FAVOR_SCAN1_ALL("row_shl") : "+v"(S), "+v"(P), "+v"(h));
-  else asm(FAVOR_SCAN1_ALL("row_shr") : "+v"(S), "+v"(P), "+v"(h));
+__device__ __forceinline__ void row_scan(float &S, float &P, float &h) {   // from the left
+  asm("s_nop 1\n" FAVOR_SCAN1("1") FAVOR_SCAN1("2") FAVOR_SCAN1("4")
+      "v_fmac_f32_dpp %0, %0, %1 row_shr:8 row_mask:0xf bank_mask:0xf\n"
+      "s_nop 1\n"
+      "v_mov_b32_dpp %2, %0 row_shr:1 row_mask:0xf bank_mask:0xf\n"
+      : "+v"(S), "+v"(P), "+v"(h));
 }
 
 // Both at once: S, P and h from the left, Q, P2 and q from the right.

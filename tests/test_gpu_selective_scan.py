@@ -314,8 +314,8 @@ def test_long_and_wide(B, L, D, N):
 @pytest.mark.parametrize("B,L,D,N,G", [
     (16, 300, 2080, 16, 2), (20, 300, 2080, 5, 2), (20, 259, 2048, 16, 1), (17, 40, 2048, 128, 1)])
 def test_many_workgroups(B, L, D, N, G, dtype):
-    """Batches that fill the card: wider workgroups forward (bf16), two and four tiles to a
-    workgroup backward. The gradients that come in are zero but for three sequences, so the
+    """Batches that fill the card: one segment forward, two and four tiles to a workgroup
+    backward. The gradients that come in are zero but for three sequences, so the
     parameters' gradients are those of the three, with exact zeros of the others."""
     some = [0, B // 2 + 1, B - 1]
     i = inputs(B, L, D, N, G, dtype, 91)
@@ -327,3 +327,30 @@ def test_many_workgroups(B, L, D, N, G, dtype):
     j = {k: of(k, v) for k, v in i.items()}
     cut = [g if name in ("dA", "dD", "ddt_bias") else g[some] for g, name in zip(grads, GRADS)]
     check(j, dtype, (y[some], s[some]), cut)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L", [300, 5])
+def test_steps_of_nothing(L, dtype):
+    """A dt of the type's lowest value or -Inf is a step of zero: the state stays bit by bit,
+    x there has no gradient but through the skip, and dt none."""
+    import torch
+    i = inputs(2, L, 24, 16, 1, dtype, 17)
+    t = dev(i, dtype)
+    cut = L - 3
+    low = float(torch.finfo(t["dt"].dtype).min)
+    for value in (low, -np.inf):
+        u = dict(t, dt=t["dt"].clone())
+        u["dt"][:, cut:] = value
+        y, s = forward(u)
+        n = torch.full((2,), cut, dtype=torch.int32, device="cuda")
+        y1, s1 = forward(t, lengths=n)
+        assert torch.equal(s, s1) and torch.equal(y[:, :cut], y1[:, :cut])
+        assert torch.isfinite(y.float()).all()
+        g = dict(zip(GRADS, backward(u)))
+        for name, v in g.items():
+            assert torch.isfinite(v.float()).all(), name
+        assert not g["ddt"][:, cut:].any() and not g["dB"][:, cut:].any()
+        e = u["dy"].double() * torch.nn.functional.silu(u["z"].double())
+        want = (e * u["skip"].double())[:, cut:].cpu().numpy()
+        near(g["dx"][:, cut:], want, 16 * np.abs(want), dtype, "dx")
