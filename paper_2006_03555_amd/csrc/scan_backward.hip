@@ -180,6 +180,12 @@ __device__ __forceinline__ f32x4 join_rows(const float (&v)[8], const float (&w)
   return o;
 }
 
+// The lane's channel, formed anew: addresses of it are few and far between.
+__device__ __forceinline__ int fresh_channel(const ScanPlace &p) {
+  const int t = fresh_thread();
+  return p.c0 + 4 * (t / 64) + t % 64 / 16;
+}
+
 // A workgroup takes a.subs tiles of W channels one after the other, so that dB and dC are
 // sums over all of them before they leave it.
 template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_backward(Scan a) {
@@ -204,7 +210,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
         if (a.dskip) a.part_d[at_sum + c] = 0.f;
         if (a.dbias) a.part_s[at_sum + c] = 0.f;
       }
-      const Unit w = unit_of<W>(p, t0, 0, threadIdx.x);
+      const Unit w = unit_of<W>(p, t0, 0, fresh_thread());
       const float none[8] = {};
       if (w.t >= a.L - t0 || w.c >= p.cend) continue;
       put_row<T>(a.dx, a.dxs, p, t0, w, none);
@@ -217,21 +223,21 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
       States<T> low_b, low_c;
       Rows4<T> rows;
       int tid = fresh_thread();
-      rows.load(a, p, t0, unit_of<W>(p, t0, 0, tid));
       if (sub == 0) {
         low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
         low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
+        low_b.put(tb, p, t0, min(kStates, a.N), tid);
+        low_c.put(tc, p, t0, min(kStates, a.N), tid);
+        tid = fresh_thread();
       }
+      rows.load(a, p, t0, unit_of<W>(p, t0, 0, tid));
+      rows.put(tiles, unit_of<W>(p, t0, 0, tid));   // the last tile's readers are behind a barrier
       for (int n0 = 0; n0 < a.N; n0 += kStates) {
         const int count = min(kStates, a.N - n0);
         if (n0) {
           tid = fresh_thread();
           low_b.load(a.b, a.bs, p, t0, n0, count, tid);
           low_c.load(a.c, a.cs, p, t0, n0, count, tid);
-        } else {
-          rows.put(tiles, unit_of<W>(p, t0, 0, tid));   // the last tile's readers are behind a barrier
-        }
-        if (sub == 0) {
           low_b.put(tb, p, t0, count, tid);
           low_c.put(tc, p, t0, count, tid);
         }
@@ -245,7 +251,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
           rows.put_rest(tiles, unit_of<W>(p, t0, 0, tid));
           rows.get_rest(tiles, cl, tl, e, z);
           lane_gated(a, left, e, z);
-          ssum = lane_steps(a, left, a.bias ? a.bias[min(c, p.cend - 1)] : 0.f, s, sx);
+          ssum = lane_steps(a, left, a.bias ? a.bias[min(fresh_channel(p), p.cend - 1)] : 0.f, s, sx);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             skip = fmaf(e[j], sx[j], skip);
@@ -254,7 +260,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
           }
           if (a.dskip) {
             const float total = row_sum(skip);
-            if (tl == 15 && channel) a.part_d[at_sum + c] = total;
+            if (tl == 15 && channel) a.part_d[at_sum + fresh_channel(p)] = total;
           }
         }
         const int each = (count + kScanWaves - 1) / kScanWaves;   // states of a wave's turn
@@ -325,8 +331,8 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
         if (n0 + kStates < a.N) __syncthreads();
       }
       // the rows' gradients, where the lanes have the sums; in place of what only the lane reads
-      const float bias = a.bias ? a.bias[min(c, p.cend - 1)] : 0.f;
-      const float skip = a.skip ? a.skip[min(c, p.cend - 1)] : 0.f;
+      const float bias = a.bias ? a.bias[min(fresh_channel(p), p.cend - 1)] : 0.f;
+      const float skip = a.skip ? a.skip[min(fresh_channel(p), p.cend - 1)] : 0.f;
       float x[8], raw[8], dy[8], z[8], dbias = 0.f;
       if (!kBoth<T>) {
         tid = fresh_thread();
@@ -355,7 +361,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
       for (int j = 0; j < 8; ++j) dbias += j < left ? ds[j] : 0.f;
       if (a.dbias) {
         dbias = row_sum(dbias);
-        if (tl == 15 && channel) a.part_s[at_sum + c] = dbias;
+        if (tl == 15 && channel) a.part_s[at_sum + fresh_channel(p)] = dbias;
       }
       tid = fresh_thread();
       const Unit w = unit_of<W>(p, t0, 0, tid);
