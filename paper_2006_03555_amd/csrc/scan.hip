@@ -222,7 +222,8 @@ __device__ __forceinline__ void chain(const Scan &a, float *part, float h, float
       if (i + j >= a.nseg) break;
       const int k = kRight ? a.nseg - 1 - i - j : i + j;
       part[at + k * DN] = h;
-      h = fmaf(exp2_hw(s[j] * A2), h, S[j]);
+      const float e = exp2_hw(0.5f * s[j] * A2);   // a growing segment may pass e^88, and h be 0
+      h = h == 0.f ? S[j] : fmaf(e, e * h, S[j]);
     }
   }
   if (kRight) {

@@ -354,3 +354,23 @@ def test_steps_of_nothing(L, dtype):
         e = u["dy"].double() * torch.nn.functional.silu(u["z"].double())
         want = (e * u["skip"].double())[:, cut:].cpu().numpy()
         near(g["dx"][:, cut:], want, 16 * np.abs(want), dtype, "dx")
+
+
+def test_growth_past_the_range_of_a_segment():
+    """A positive A whose growth over 128 tokens is in fp32's range, but not over a segment of
+    several chunks: a state of zero stays zero until inputs come, and decays elsewhere."""
+    B, L, D, N = 1, 16640, 1024, 2
+    i = inputs(B, L, D, N, 1, "f32", 5, z=False, bias=False, state=False, soft=False)
+    i["dt"][:] = 0.5
+    i["A"][:, 0], i["A"][:, 1] = 1.0, -1.0   # e^64 in 128 tokens, e^128 in 256
+    i["x"][:, :L - 100] = 0
+    t = dev(i, "f32")
+    y, s = _fv().selective_scan(t["x"], t["dt"], t["A"], t["Bm"], t["C"], t["skip"],
+                                softplus=False, return_state=True)
+    tail = {k: v if v is None or k in ("A", "skip") else v[:, L - 100:] for k, v in i.items()}
+    o = dict(skip=i["skip"], z=None, bias=None, soft=False, lengths=None, state=None)
+    ref, sref = rec.scan(*_args(tail), **o)
+    units = rec.scan_bounds(*_args(tail), tail["dy"], **o)
+    near(y[:, L - 100:], ref, units[0], "f32", "y")
+    near(s, sref, units[1], "f32", "state")
+    assert not y[:, :L - 100].any()
