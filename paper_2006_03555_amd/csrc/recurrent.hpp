@@ -48,6 +48,7 @@ struct Scan {
   Rows xs, dts, bs, cs, zs, ys;
   int B, L, D, N, G, softplus;
   int chunks, nseg;                 // chunks of kScanTokens tokens in one segment; segments
+  int sum_states;                   // states of a workgroup of the segments' sums (of kScanStates)
   int subs;                         // backward: tiles of one workgroup
   // nseg > 1: the states before each segment [B][nseg][D][N] (first: the segments' sums) and
   // the segments' sums of s [B][nseg][D]
@@ -68,6 +69,7 @@ struct Scan {
   int n_slots;
 };
 constexpr int kScanTokens = 128;     // of one chunk
+constexpr int kScanStates = 16;      // of one pass over a chunk
 constexpr int kScanBackTile = 32;    // channels of one tile of the backward pass
 // The sums of the segments but the last, in part and steps; backward, where a segment is one
 // chunk: of all of them, and in part_r too.

@@ -202,6 +202,16 @@ ScanCut cut_of(const favor_scan_desc *g) {
   return c;
 }
 
+// States that one workgroup of the chunks' sums takes in the backward pass: a pass' 16 while that
+// leaves few workgroups, else all of them, which read the rows once. Whole calls in us, by 16 / all:
+// B2 L777 D512 N64 fp32 (224 workgroups of all) 121 / 130, B1 L300 D512 N48 (48) 78 / 91; B6 L1999
+// D1000 N24 fp32 (3072) 489 / 474. Forward, where only half as much comes with the rows, 16 are
+// never slower: B1 L4096 D2048 N64 262 / 286, B6 L1999 D1000 N24 fp32 190 / 194.
+constexpr int kSumBlocks = 1024;
+int sum_states_of(const favor_scan_desc *g) {
+  return (int64_t)g->B * tiles_of(g, favor::kScanBackTile) * chunks_of(g) < kSumBlocks ? favor::kScanStates : g->N;
+}
+
 // Tiles that one workgroup of the backward pass takes one after the other: their sums of dB and dC
 // stay in LDS, and the workspace is as many times smaller. Whole calls in us with 1 / 2 / 4 tiles,
 // bf16: B4 L4096 D2048 N16 831 / 830 / 783, B2 L4096 D4096 N8 646 / 608 / 584; with too few
@@ -503,6 +513,7 @@ favor_status favor_selective_scan(const favor_scan_desc *g, const void *x, const
   a.h_out = state_out;
   a.chunks = c.chunks;
   a.nseg = c.nseg;
+  a.sum_states = favor::kScanStates;
   const Dt type = dt_of(g->dtype);
   if (c.nseg > 1) {
     hipError_t e;
@@ -567,6 +578,7 @@ favor_status favor_selective_scan_backward(
   a.h_in = state_in;
   a.chunks = 1;
   a.nseg = chunks_of(g);
+  a.sum_states = sum_states_of(g);
   a.subs = subs_of(g);
   a.dy = dy;
   a.dh_out = dstate_out;

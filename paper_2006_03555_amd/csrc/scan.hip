@@ -71,8 +71,8 @@ template <typename T, bool kOut, bool kAhead> struct ScanLds {
   static constexpr int kRaw = kPairTiles<T> * W * kTok;
   static constexpr int kRows = kRaw + (kAhead ? W * kTok : 0);   // else y takes the place of x and dt
   static constexpr int kLow = (kOut ? 2 : 1) * kStates * kTok;
-  static size_t bytes(int N) {
-    const int padded = (N + kStates - 1) / kStates * kStates;
+  static size_t bytes(const Scan &a) {
+    const int padded = ((kOut ? a.N : a.sum_states) + kStates - 1) / kStates * kStates;
     return sizeof(float) * (kRows + kLow + 2 * (size_t)padded * W);
   }
 };
@@ -83,7 +83,9 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
   extern __shared__ __align__(16) float lds[];
   float *tile = lds, *ty = kAhead ? tile + Lds::kRaw : tile;
   float *tb = tile + Lds::kRows, *tc = tb + kStates * kTok;
-  const int padded = (a.N + kStates - 1) / kStates * kStates;
+  // the states of this workgroup; those of a chunk's pass are n0 to n0 + count - 1
+  const int first_n = kOut ? 0 : blockIdx.z * a.sum_states, end_n = kOut ? a.N : min(first_n + a.sum_states, a.N);
+  const int padded = (end_n - first_n + kStates - 1) / kStates * kStates;
   float *tA = tb + Lds::kLow, *th = tA + padded * W;
   const ScanPlace p = scan_place(a, W);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tl = lane % 16;
@@ -92,9 +94,10 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
   const float *h0 = nullptr;
   if (kOut && a.nseg > 1) h0 = a.part + at_part;
   else if (kOut && a.h_in) h0 = a.h_in + p.b * DN;
-  for (int n0 = 0; n0 < a.N; n0 += kStates) {
-    load_channels<W>(a.A, p, a.N, n0, min(kStates, a.N - n0), kLog2e, tA + n0 * W, threadIdx.x);
-    load_channels<W>(h0, p, a.N, n0, min(kStates, a.N - n0), 1.f, th + n0 * W, threadIdx.x);
+  for (int n0 = first_n; n0 < end_n; n0 += kStates) {
+    const int count = min(kStates, end_n - n0), at = (n0 - first_n) * W;
+    load_channels<W>(a.A, p, a.N, n0, count, kLog2e, tA + at, threadIdx.x);
+    load_channels<W>(h0, p, a.N, n0, count, 1.f, th + at, threadIdx.x);
   }
   const float bias = a.bias ? a.bias[c] : 0.f, skip = kOut && a.skip ? a.skip[c] : 0.f;
   float seg_steps = 0.f;
@@ -108,8 +111,8 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
     const Unit w = unit_of<W>(p, t0, 0, tid);
     rx = get_row<T>(a.x, a.xs, p, t0, w);
     rdt = get_row<T>(a.dt, a.dts, p, t0, w);
-    low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
-    if (kOut) low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
+    low_b.load(a.b, a.bs, p, t0, first_n, min(kStates, end_n - first_n), tid);
+    if (kOut) low_c.load(a.c, a.cs, p, t0, first_n, min(kStates, end_n - first_n), tid);
   };
   if (kAhead && first < end) request(first, fresh_thread());
   for (int chunk = first; chunk < end; ++chunk) {
@@ -120,8 +123,8 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
       if (chunk > first) __syncthreads();   // the last chunk's rows have been read
     }
     put_pair<W>(tile, unit_of<W>(p, t0, 0, tid), rx, rdt);
-    low_b.put(tb, p, t0, min(kStates, a.N), tid);
-    if (kOut) low_c.put(tc, p, t0, min(kStates, a.N), tid);
+    low_b.put(tb, p, t0, min(kStates, end_n - first_n), tid);
+    if (kOut) low_c.put(tc, p, t0, min(kStates, end_n - first_n), tid);
     __syncthreads();
     tid = fresh_thread();
     if (kAhead) {
@@ -135,9 +138,9 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) sx[j] *= s[j];
     if (!kOut) seg_steps += ssum;
-    for (int n0 = 0; n0 < a.N; n0 += kStates) {
-      const int count = min(kStates, a.N - n0);
-      if (n0) {
+    for (int n0 = first_n; n0 < end_n; n0 += kStates) {
+      const int count = min(kStates, end_n - n0);
+      if (n0 > first_n) {
         tid = fresh_thread();
         States<T> more_b, more_c;
         more_b.load(a.b, a.bs, p, t0, n0, count, tid);
@@ -148,7 +151,7 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
         __syncthreads();
       }
       for (int n = 0; n < count; n += K) {   // a state behind the last is zeros
-        const int at = (n0 + n) * W + cl;
+        const int at = (n0 - first_n + n) * W + cl;
         StateIn<kOut> in[K];
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -193,9 +196,9 @@ __global__ __launch_bounds__(kScanThreads, kAhead ? 4 : 6) void k_scan(Scan a) {
   if (!kOut) to = a.part + at_part;
   else if (a.h_out && p.seg == a.nseg - 1) to = a.h_out + p.b * DN;
   if (to)
-    for (int n0 = 0; n0 < a.N; n0 += kStates)
-      store_channels<W>(to, p, a.N, n0, min(kStates, a.N - n0), th + n0 * W, threadIdx.x);
-  if (!kOut) {
+    for (int n0 = first_n; n0 < end_n; n0 += kStates)
+      store_channels<W>(to, p, a.N, n0, min(kStates, end_n - n0), th + (n0 - first_n) * W, threadIdx.x);
+  if (!kOut && first_n == 0) {
     const float total = row_sum(seg_steps);
     if (tl == 15 && p.c0 + cl < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
   }
@@ -242,7 +245,7 @@ template <bool kBackward> __global__ __launch_bounds__(kPrefixThreads) void k_sc
 }
 
 template <typename T, bool kOut, bool kAhead> hipError_t launch_as(const Scan &a, hipStream_t st) {
-  const size_t lds = ScanLds<T, kOut, kAhead>::bytes(a.N);
+  const size_t lds = ScanLds<T, kOut, kAhead>::bytes(a);
   const auto kernel = k_scan<T, kOut, kAhead>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
@@ -251,7 +254,8 @@ template <typename T, bool kOut, bool kAhead> hipError_t launch_as(const Scan &a
   }
   const int tiles = a.G * ((a.D / a.G + W - 1) / W);
   const int segments = kOut ? a.nseg : a.nseg - 1;   // nothing follows the last segment's sums
-  kernel<<<dim3((unsigned)(tiles * segments), a.B), kScanThreads, lds, st>>>(a);
+  const int parts = kOut ? 1 : (a.N + a.sum_states - 1) / a.sum_states;
+  kernel<<<dim3((unsigned)(tiles * segments), a.B, parts), kScanThreads, lds, st>>>(a);
   return hipGetLastError();
 }
 template <typename T> hipError_t launch_rows(const Scan &a, hipStream_t st) {

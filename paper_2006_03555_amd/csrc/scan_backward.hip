@@ -74,7 +74,9 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
   const int cl = 4 * wave + lane / 16, c = p.c0 + cl;   // this lane's channel
   const int64_t at_part = ((int64_t)p.b * a.nseg + p.seg) * a.D * a.N;
   const int64_t t0 = (int64_t)p.seg * kTok;
+  const int first_n = blockIdx.z * a.sum_states, end_n = min(first_n + a.sum_states, a.N);
   if (t0 >= p.n) {   // no token: nothing is added
+    if (blockIdx.z) return;
     for (int i = threadIdx.x; i < min(W, p.cend - p.c0) * a.N; i += kScanThreads)
       a.part[at_part + (int64_t)p.c0 * a.N + i] = a.part_r[at_part + (int64_t)p.c0 * a.N + i] = 0.f;
     if (threadIdx.x < min(W, p.cend - p.c0))
@@ -85,13 +87,13 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
   Rows4<T> rows;
   States<T> low_b, low_c;
   rows.load(a, p, t0, w);
-  low_b.load(a.b, a.bs, p, t0, 0, min(kStates, a.N), tid);
-  low_c.load(a.c, a.cs, p, t0, 0, min(kStates, a.N), tid);
+  low_b.load(a.b, a.bs, p, t0, first_n, min(kStates, end_n - first_n), tid);
+  low_c.load(a.c, a.cs, p, t0, first_n, min(kStates, end_n - first_n), tid);
   const float bias = a.bias ? a.bias[min(c, p.cend - 1)] : 0.f;
   float s[8], sx[8], e[8], ssum = 0.f;
-  for (int n0 = 0; n0 < a.N; n0 += kStates) {
-    const int count = min(kStates, a.N - n0);
-    if (n0) {
+  for (int n0 = first_n; n0 < end_n; n0 += kStates) {
+    const int count = min(kStates, end_n - n0);
+    if (n0 > first_n) {
       low_b.load(a.b, a.bs, p, t0, n0, count, tid);
       low_c.load(a.c, a.cs, p, t0, n0, count, tid);
     } else {
@@ -101,7 +103,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
     low_c.put(tc, p, t0, count, tid);
     load_channels<W>(a.A, p, a.N, n0, count, kLog2e, tA, tid);
     __syncthreads();
-    if (n0 == 0) {
+    if (n0 == first_n) {
       float z[8];
       rows.get(tiles, cl, tl, sx, s);
       rows.put_rest(tiles, w);
@@ -111,7 +113,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
 #pragma unroll
       for (int j = 0; j < 8; ++j) sx[j] *= s[j];
       const float total = row_sum(ssum);
-      if (tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
+      if (first_n == 0 && tl == 15 && c < p.cend) a.steps[((int64_t)p.b * a.nseg + p.seg) * a.D + c] = total;
     }
     for (int n = 0; n < count; n += 2) {   // two states at once; one behind the last is zeros
       float Bv[2][8], Cv[2][8], S[2], Q[2], P[2], P2[2], h[2] = {}, q[2] = {};
@@ -461,12 +463,12 @@ __global__ __launch_bounds__(kSumCols *kSumLanes) void k_scan_params(Scan a, int
 }
 
 template <typename K>
-hipError_t launch_tiles(K kernel, const Scan &a, int width, size_t lds, hipStream_t st) {
+hipError_t launch_tiles(K kernel, const Scan &a, int width, int parts, size_t lds, hipStream_t st) {
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
   const int tiles = a.G * ((a.D / a.G + width - 1) / width);
-  kernel<<<dim3((unsigned)(tiles * a.nseg), a.B), kScanThreads, lds, st>>>(a);
+  kernel<<<dim3((unsigned)(tiles * a.nseg), a.B, parts), kScanThreads, lds, st>>>(a);
   return hipGetLastError();
 }
 
@@ -474,14 +476,15 @@ hipError_t launch_tiles(K kernel, const Scan &a, int width, size_t lds, hipStrea
 
 hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st) {
   const size_t lds = sizeof(float) * (2 * W * kTok + 2 * kStates * kTok + 3 * kStates * W);
-  return dt == Dt::BF16 ? launch_tiles(k_scan_parts<bf16>, a, W, lds, st)
-                        : launch_tiles(k_scan_parts<float>, a, W, lds, st);
+  const int parts = (a.N + a.sum_states - 1) / a.sum_states;
+  return dt == Dt::BF16 ? launch_tiles(k_scan_parts<bf16>, a, W, parts, lds, st)
+                        : launch_tiles(k_scan_parts<float>, a, W, parts, lds, st);
 }
 
 hipError_t launch_scan_backward(const Scan &a, Dt dt, hipStream_t st) {
   const size_t lds = sizeof(float) * (2 * W * kTok + 4 * kStates * kTok + 3 * kStates * W);
-  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, W * a.subs, lds, st)
-                        : launch_tiles(k_scan_backward<float>, a, W * a.subs, lds, st);
+  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, W * a.subs, 1, lds, st)
+                        : launch_tiles(k_scan_backward<float>, a, W * a.subs, 1, lds, st);
 }
 
 hipError_t launch_scan_backward_sums(const Scan &a, Dt dt, hipStream_t st) {

@@ -17,7 +17,7 @@ namespace favor {
 constexpr int kTok = kScanTokens;   // tokens of a chunk: 16 lanes of 8
 constexpr int kScanWaves = 8;
 constexpr int kScanThreads = 64 * kScanWaves;
-constexpr int kStates = 16;         // states of one pass over a chunk
+constexpr int kStates = kScanStates;
 
 // Place of token t in a row of kTok: the first halves of the lanes' eight tokens, then the second
 // halves, so that the 16 lanes of a row read 16 bytes each from all the banks at once.

@@ -374,3 +374,19 @@ def test_growth_past_the_range_of_a_segment():
     near(y[:, L - 100:], ref, units[0], "f32", "y")
     near(s, sref, units[1], "f32", "state")
     assert not y[:, :L - 100].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [17, 40])
+def test_padded_batch_of_many_states(N, dtype):
+    """More than 16 states: the sums' workgroups take 16 each, also where a chunk has no token."""
+    import torch
+    B, L, D, lengths = 5, 270, 48, [0, 1, 128, 129, 270]
+    i = inputs(B, L, D, N, 2, dtype, 23)
+    t = dev(i, dtype)
+    for k in ("x", "dt", "z", "dy", "Bm", "C"):
+        for b, n in enumerate(lengths):
+            t[k][b, n:] = float("nan")
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    (y, s), grads = forward(t, lengths=n), backward(t, lengths=n)
+    check(i, dtype, (y, s), grads, lengths=np.array(lengths))
