@@ -319,3 +319,67 @@ def test_calls_repeat_bit_by_bit():
         _step(i, o, None)
         torch.cuda.synchronize()
         _equal(o, first, rep)
+
+
+def test_rows_far_apart():
+    """Tokens as far apart as the scan takes them (offsets past 32 bits): as contiguous rows."""
+    import torch
+    fv = _fv()
+    i, o = _buffers(1, 300, 16, 8, 4, 1, 8)
+    _fill(i, 4)
+    i["lens"].fill_(300)
+    far = torch.empty(1 + 299 * (1 << 24) + 64, dtype=torch.bfloat16, device="cuda")   # 10 GB
+    rows = lambda at, n=16: far[at:].as_strided((1, 300, n), (0, 1 << 24, 1))
+    names = dict(x=0, dt=16, z=32, dy=48)
+    g = {k: rows(at) for k, at in names.items()}
+    scan = lambda t: (*fv.selective_scan(t["x"], t["dt"], i["A"], i["Bm"], i["C"], i["skip"], t["z"],
+                                         i["dtb"], state_in=i["hs"], return_state=True),
+                      *fv.selective_scan_backward(t["x"], t["dt"], i["A"], i["Bm"], i["C"], t["dy"],
+                                                  i["skip"], t["z"], i["dtb"], state_in=i["hs"]))
+    conv = lambda t: (fv.causal_conv(t["x"], i["w"], i["bias"], True),
+                      *fv.causal_conv_backward(t["x"], i["w"], t["dy"], i["bias"], True))
+    want = [v.clone() for v in (*scan(i), *conv(i))]
+    for k, v in g.items():
+        v.copy_(i[k])
+    assert g["dy"].stride(1) * 2 == 1 << 25
+    for got, ref in zip((*scan(g), *conv(g)), want):
+        assert torch.equal(got, ref)
+    # and outputs: y and dx in rows of their own
+    y, dx = rows(0), rows(16)
+    fv.selective_scan(i["x"], i["dt"], i["A"], i["Bm"], i["C"], i["skip"], i["z"], i["dtb"],
+                      state_in=i["hs"], out=y)
+    fv.causal_conv_backward(i["x"], i["w"], i["dy"], i["bias"], True, dx=dx)
+    assert torch.equal(y, want[0]) and torch.equal(dx, want[11])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_broadcast_inputs(dtype):
+    """Inputs that are one row or one sequence for all, as views: as their copies."""
+    import torch
+    fv = _fv()
+    B, L = 3, 140
+    i, _ = _buffers(B, L, 48, 8, 3, 1, 8, dtype=dtype)
+    _fill(i, 6)
+    wide = dict(i, x=i["x"][:1].expand(B, L, 48), dt=i["dt"][:, :1].expand(B, L, 48),
+                z=i["z"][:1, :1].expand(B, L, 48), dy=i["dy"][:1, :1].expand(B, L, 48),
+                Bm=i["Bm"][:, :, :1].expand(B, L, 2, 8), C=i["C"][:1].expand(B, L, 2, 8))
+    whole = {k: v.contiguous() for k, v in wide.items()}
+
+    def run(t):
+        a = [t[k] for k in ("x", "dt", "A", "Bm", "C")]
+        return (fv.causal_conv(t["x"], t["w"], t["bias"], True),
+                *fv.causal_conv_backward(t["x"], t["w"], t["dy"], t["bias"], True),
+                fv.selective_scan(*a, t["skip"], t["z"], t["dtb"]),
+                *fv.selective_scan_backward(*a, t["dy"], t["skip"], t["z"], t["dtb"]))
+
+    for got, ref in zip(run(wide), run(whole)):
+        assert torch.equal(got, ref)
+
+
+def test_reorder_without_pools():
+    """Only the places are worked out."""
+    import torch
+    slots = torch.tensor([[5, 2, 9], [1, 0, 7]], dtype=torch.int32, device="cuda")
+    parent = torch.tensor([[1, 1, 0], [2, 2, 2]], dtype=torch.int32, device="cuda")
+    ref, _ = rec.beam_reorder(parent.tolist(), slots.tolist(), [])
+    assert np.array_equal(_fv().beam_reorder(parent, slots, []).cpu().numpy(), ref)
