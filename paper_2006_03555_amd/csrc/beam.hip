@@ -11,7 +11,7 @@
 // entry. A lane's tokens and the order of its sums depend on the row's length alone, so equal
 // rows have equal scores wherever they lie in memory. Scores are compared in 64 bits.
 // 32 entries of 8 beams of 131072 logits in bf16, a quarter of them ended: 21 us (2.5 TB/s) and 8
-// for the merge; 4 beams of 50001 in fp32: 5.8 and 5.5, all latency.
+// for the merge; 4 beams of 50001 in fp32: 5.2 and 5.6, all latency.
 #include "recurrent.hpp"
 #include "vec_rows.hpp"
 
@@ -55,6 +55,47 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
+}
+// v of the lane and of its partner at distance kDistance, in either order, where blocks of
+// kDistance lanes hold one value each (a mirror then is as good as an exchange).
+template <int kDistance> __device__ __forceinline__ void partners(uint32_t v, uint32_t &a, uint32_t &b) {
+  if constexpr (kDistance >= 16) {
+    const auto r = kDistance == 16 ? __builtin_amdgcn_permlane16_swap(v, v, false, false)
+                                   : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    a = r[0];
+    b = r[1];
+  } else {
+    constexpr int kControl = kDistance == 1 ? 0xb1 : kDistance == 2 ? 0x4e : kDistance == 4 ? 0x141 : 0x140;
+    a = v;
+    b = __builtin_amdgcn_update_dpp(0, v, kControl, 0xf, 0xf, true);
+  }
+}
+template <int kDistance, typename F> __device__ __forceinline__ float with_partner(float v, F &&f) {
+  uint32_t a, b;
+  partners<kDistance>(__float_as_uint(v), a, b);
+  return f(__uint_as_float(a), __uint_as_float(b));
+}
+template <int kDistance> __device__ __forceinline__ double add_partner(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  uint32_t a0, b0, a1, b1;
+  partners<kDistance>((uint32_t)u, a0, b0);
+  partners<kDistance>((uint32_t)(u >> 32), a1, b1);
+  return __builtin_bit_cast(double, (uint64_t)a1 << 32 | a0) + __builtin_bit_cast(double, (uint64_t)b1 << 32 | b0);
+}
+// Over the wave, step by step: f(distance, own, partner's).
+template <typename F> __device__ __forceinline__ float over_wave(float v, F &&f) {
+  v = with_partner<1>(v, [&](float a, float b) { return f(1, a, b); });
+  v = with_partner<2>(v, [&](float a, float b) { return f(2, a, b); });
+  v = with_partner<4>(v, [&](float a, float b) { return f(4, a, b); });
+  v = with_partner<8>(v, [&](float a, float b) { return f(8, a, b); });
+  v = with_partner<16>(v, [&](float a, float b) { return f(16, a, b); });
+  return with_partner<32>(v, [&](float a, float b) { return f(32, a, b); });
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return over_wave(v, [](int, float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  return add_partner<32>(add_partner<16>(add_partner<8>(add_partner<4>(add_partner<2>(add_partner<1>(v))))));
 }
 // Maxima whose product with log2 e is in range.
 constexpr float kScaled = 1e38f;
@@ -142,11 +183,9 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
     c = now;
     float bound = best.last ? unordered((uint32_t)(best.last >> 32)) : -INFINITY;
     if (t0 == 0) {
-      int groups = 1;
-      while (groups < a.n) groups *= 2;
-      bound = most;
-      for (int d = groups; d < 64; d *= 2) bound = fmaxf(bound, __shfl_xor(bound, d));
-      for (int d = 1; d < groups; d *= 2) bound = fminf(bound, __shfl_xor(bound, d));
+      int group = 64;   // lanes of one of n groups or more
+      while (64 / group < a.n) group /= 2;
+      bound = over_wave(most, [&](int d, float u, float v) { return d < group ? fmaxf(u, v) : fminf(u, v); });
     }
     if (!__ballot(most >= bound)) return;
     int count = 0;
@@ -210,17 +249,13 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
     }
     look(x, t0);
   }
-  float top = m;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  const float top = wave_max(m);
   sum *= exp2_hw(fmaf(-scaled_to(top), kLog2e, c));   // what c's rounding left is in it
   if (fabsf(top) > kScaled && fabsf(top) < INFINITY) {   // log2 e times it is no number: once more
     sum = 0.f;
     for (int t = lane; t < left; t += 64) sum += exp2_hw((to_f32(x0[t - 8 * lane]) - top) * kLog2e);
   }
-  double total = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+  const double total = wave_sum(sum);
   if (lane == 0) a.stats[id] = float2{top, (float)total};
   if (lane < a.n) a.keys[id * a.n + lane] = best.top;
 }
@@ -254,12 +289,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
 #pragma unroll
     for (int j = 0; j < kEarly; ++j) early[j] = of_row[min(64 * j + lane, keys - 1)];
     const float2 st = lane < a.pieces ? of_piece : float2{-INFINITY, 0.f};
-    float top = st.x;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    double sum = (double)st.y * exp2_hw((st.x - (top == -INFINITY ? 0.f : top)) * kLog2e);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    const float top = wave_max(st.x);
+    const double sum = wave_sum((double)st.y * exp2_hw((st.x - (top == -INFINITY ? 0.f : top)) * kLog2e));
     const double rest = log(sum);   // of the log-sum, beyond the maximum, which may be huge
     WaveBest best;
     best.list = lists[wave];
