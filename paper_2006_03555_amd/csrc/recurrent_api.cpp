@@ -188,15 +188,20 @@ favor_status validate(const favor_scan_desc *g, int op) {
 //   Fewer: segments for 2048 workgroups. B1 L65536 D2048 in 8 / 16 / 32 / 64 segments 1321 / 1199
 //   / 1133 / 1106; B1 L4096 in 8 / 32 102 / 90, in one 214; B3 L4096 (192) in 8 225, in one 216;
 //   B6 L1999 D1000 N24 fp32 (192) in 8 198, in one 194.
+//   One segment too where three passes over a chunk (16 states each) or fewer are all of it: two
+//   more launches cost as much. B1 L256 D512 16.4 in one, 21.4 in two; B2 L384 D2048 23.6, in three
+//   29.1; B1 L384 D512 22.7, in three 21.7; B1 L512 D512 28.9, in four 21.9; N64 fp32 L256 D2048
+//   50.9, in two 40.5.
 struct ScanCut {
   int chunks, nseg;
 };
-constexpr int kOneSegment = 240, kSegmentBlocks = 2048;
+constexpr int kOneSegment = 240, kSegmentBlocks = 2048, kFewPasses = 3;
 ScanCut cut_of(const favor_scan_desc *g) {
   ScanCut c;
   const int chunks = std::max(chunks_of(g), 1);
   const int64_t blocks = std::max<int64_t>(1, (int64_t)g->B * tiles_of(g, 32));
-  const int64_t want = blocks >= kOneSegment ? 1 : kSegmentBlocks / blocks;
+  const int passes = chunks * ((g->N + favor::kScanStates - 1) / favor::kScanStates);
+  const int64_t want = blocks >= kOneSegment || passes <= kFewPasses ? 1 : kSegmentBlocks / blocks;
   c.chunks = (int)((chunks + want - 1) / want);
   c.nseg = (chunks + c.chunks - 1) / c.chunks;
   return c;
