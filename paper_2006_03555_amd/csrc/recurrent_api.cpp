@@ -185,9 +185,10 @@ favor_status validate(const favor_scan_desc *g, int op) {
 //   One segment while its workgroups of 32 channels fill the 256 compute units, as long as
 //   there are 240 of them: B4 L4096 D2048 (256) 220, in two segments 297, in eight 279; B8 368,
 //   498, 534.
-//   Fewer: segments for 2048 workgroups. B1 L65536 D2048 in 8 / 16 / 32 / 64 segments 1321 / 1199
-//   / 1133 / 1106; B1 L4096 in 8 / 32 102 / 90, in one 214; B3 L4096 (192) in 8 225, in one 216;
-//   B6 L1999 D1000 N24 fp32 (192) in 8 198, in one 194.
+//   Fewer: segments for 4096 workgroups. For 1024 / 2048 / 4096 / 8192 of them B1 L65536 D2048 1181
+//   / 1120 / 1096 / 1093, B2 L4096 157 / 149 / 145 / 144, B1 L8192 D2048 N64 fp32 540 / 540 / 546 /
+//   546. B1 L4096 82 in 32 segments and 214 in one, B3 L4096 (192) 213 in 16 and 216 in one, B6
+//   L1999 D1000 N24 fp32 (192) 186 in 16 and 194 in one.
 //   One segment too where three passes over a chunk (16 states each) or fewer are all of it: two
 //   more launches cost as much. B1 L256 D512 16.4 in one, 21.4 in two; B2 L384 D2048 23.6, in three
 //   29.1; B1 L384 D512 22.7, in three 21.7; B1 L512 D512 28.9, in four 21.9; N64 fp32 L256 D2048
@@ -195,7 +196,7 @@ favor_status validate(const favor_scan_desc *g, int op) {
 struct ScanCut {
   int chunks, nseg;
 };
-constexpr int kOneSegment = 240, kSegmentBlocks = 2048, kFewPasses = 3;
+constexpr int kOneSegment = 240, kSegmentBlocks = 4096, kFewPasses = 3;
 ScanCut cut_of(const favor_scan_desc *g) {
   ScanCut c;
   const int chunks = std::max(chunks_of(g), 1);
