@@ -190,8 +190,8 @@ __device__ __forceinline__ int fresh_channel(const ScanPlace &p) {
 }
 
 // A workgroup takes a.subs tiles of W channels one after the other, so that dB and dC are
-// sums over all of them before they leave it.
-template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_backward(Scan a) {
+// sums over all of them before they leave it. kGate: there is a z, whose gradient needs y again.
+template <typename T, bool kGate> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_backward(Scan a) {
   extern __shared__ __align__(16) float lds[];
   float *tiles = lds, *tb = tiles + 2 * W * kTok, *tc = tb + kStates * kTok;
   float *tlow = tc + kStates * kTok;   // dB, then dC
@@ -218,7 +218,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
       if (w.t >= a.L - t0 || w.c >= p.cend) continue;
       put_row<T>(a.dx, a.dxs, p, t0, w, none);
       put_row<T>(a.ddt, a.ddts, p, t0, w, none);
-      if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, none);
+      if (kGate) put_row<T>(a.dz, a.dzs, p, t0, w, none);
     } else {
       // a lane without a channel adds nothing to dB and dC
       const int left = channel ? lane_left(p, t0, tl) : 0;
@@ -292,7 +292,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
               const float before = h;
               h = fmaf(at[j], h, bx[j]);
               dC[j] = e[j] * h;
-              y[j] = fmaf(Cv[j], h, y[j]);
+              if (kGate) y[j] = fmaf(Cv[j], h, y[j]);
               bx[j] = before;
             }
             float dA = 0.f;
@@ -354,7 +354,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
       if (a.softplus)
 #pragma unroll
         for (int j = 0; j < 8; ++j) ds[j] *= softplus_slope(raw[j] + bias, s[j]);
-      if (a.z)
+      if (kGate)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float g = sigmoid(z[j]);
@@ -373,7 +373,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(pack_bf16(dsx[j], ds[j]));
         tile_store(tiles, cl, tl, x);
-        tile_store(tiles + W * kTok, cl, tl, y);
+        if (kGate) tile_store(tiles + W * kTok, cl, tl, y);
         __syncthreads();
         uint32_t d[8];
         float o[8];
@@ -381,12 +381,12 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
         for (int k = 0; k < 8; ++k) {
           const int at = tile_at(8 * w.u + k, w.t);
           d[k] = w.live ? __float_as_uint(tiles[at]) : 0;
-          o[k] = w.live ? tiles[W * kTok + at] : 0.f;
+          o[k] = kGate && w.live ? tiles[W * kTok + at] : 0.f;
         }
         if (mine) {
           put_halves(a.dx, a.dxs, p, t0, w, d, 0x05040100u);
           put_halves(a.ddt, a.ddts, p, t0, w, d, 0x07060302u);
-          if (a.z) put_row<T>(a.dz, a.dzs, p, t0, w, o);
+          if (kGate) put_row<T>(a.dz, a.dzs, p, t0, w, o);
         }
       } else {
         const auto rows_out = [&](void *dst, const Rows &r, const float *tile) {
@@ -400,7 +400,7 @@ template <typename T> __global__ __launch_bounds__(kScanThreads, 4) void k_scan_
         __syncthreads();
         rows_out(a.dx, a.dxs, tiles);
         rows_out(a.ddt, a.ddts, tiles + W * kTok);
-        if (a.z) {
+        if (kGate) {
           __syncthreads();
           tile_store(tiles, cl, tl, y);
           __syncthreads();
@@ -483,8 +483,9 @@ hipError_t launch_scan_backward_parts(const Scan &a, Dt dt, hipStream_t st) {
 
 hipError_t launch_scan_backward(const Scan &a, Dt dt, hipStream_t st) {
   const size_t lds = sizeof(float) * (2 * W * kTok + 4 * kStates * kTok + 3 * kStates * W);
-  return dt == Dt::BF16 ? launch_tiles(k_scan_backward<bf16>, a, W * a.subs, 1, lds, st)
-                        : launch_tiles(k_scan_backward<float>, a, W * a.subs, 1, lds, st);
+  const auto launch = [&](auto kernel) { return launch_tiles(kernel, a, W * a.subs, 1, lds, st); };
+  if (dt == Dt::BF16) return a.z ? launch(k_scan_backward<bf16, true>) : launch(k_scan_backward<bf16, false>);
+  return a.z ? launch(k_scan_backward<float, true>) : launch(k_scan_backward<float, false>);
 }
 
 hipError_t launch_scan_backward_sums(const Scan &a, Dt dt, hipStream_t st) {
