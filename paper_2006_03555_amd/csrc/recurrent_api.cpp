@@ -211,7 +211,7 @@ ScanCut cut_of(const favor_scan_desc *g) {
 // States that one workgroup of the chunks' sums takes in the backward pass: a pass' 16 while that
 // leaves few workgroups, else all of them, which read the rows once. Whole calls in us, by 16 / all:
 // B2 L777 D512 N64 fp32 (224 workgroups of all) 121 / 130, B1 L300 D512 N48 (48) 78 / 91; B6 L1999
-// D1000 N24 fp32 (3072) 489 / 474. Forward, where only half as much comes with the rows, 16 are
+// D1000 N24 fp32 (3000 or so) 489 / 474. Forward, where only half as much comes with the rows, 16 are
 // never slower: B1 L4096 D2048 N64 262 / 286, B6 L1999 D1000 N24 fp32 190 / 194.
 constexpr int kSumBlocks = 1024;
 int sum_states_of(const favor_scan_desc *g) {
