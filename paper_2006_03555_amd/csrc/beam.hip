@@ -97,10 +97,17 @@ __device__ __forceinline__ float wave_max(float v) {
 __device__ __forceinline__ double wave_sum(double v) {
   return add_partner<32>(add_partner<16>(add_partner<8>(add_partner<4>(add_partner<2>(add_partner<1>(v))))));
 }
-// Maxima whose product with log2 e is in range.
-constexpr float kScaled = 1e38f;
+// Maxima whose product with log2 e is rounded by at most 64: 2 to what that leaves is in range.
+// Past them (a mask of -1e10 or of the type's lowest value) the maximum is taken off before the
+// product; neighbouring floats are 64 or more apart there, so all but the maximum itself adds
+// nothing.
+constexpr float kScaled = 0x1p30f;
 __device__ __forceinline__ float scaled_to(float m) { return fminf(fmaxf(m, -kScaled), kScaled); }
 __device__ __forceinline__ float scaled(float m) { return scaled_to(m) * kLog2e; }
+__device__ __forceinline__ bool past_scaled(float m) {   // and finite
+  constexpr uint32_t from = 2 * 0x4e800000u + 1, to = 2 * 0x7f800000u;   // by twice the bits of 2^30, of Inf
+  return 2 * __float_as_uint(m) - from < to - from;
+}
 
 // The n best keys of a wave: lane r has the r-th (0: none).
 struct WaveBest {
@@ -175,12 +182,21 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
 #pragma unroll
     for (int i = 3; i + 1 < E; i += 2) most = max3(most, x[i], x[i + 1]);
     most = max3(most, x[E - 1], x[E - 1]);
+    const float was = m;
     m = max3(m, most, most);
     const float now = scaled(m);
-    sum *= exp2_hw(c - now);
+    if (!__ballot(past_scaled(m))) {
+      sum *= exp2_hw(c - now);
 #pragma unroll
-    for (int i = 0; i < E; ++i) sum += exp2_hw(fmaf(x[i], kLog2e, -now));
-    c = now;
+      for (int i = 0; i < E; ++i) sum += exp2_hw(fmaf(x[i], kLog2e, -now));
+      c = now;
+    } else {
+      const bool past = past_scaled(m);
+      sum *= exp2_hw(past ? (was - m) * kLog2e : c - now);
+#pragma unroll
+      for (int i = 0; i < E; ++i) sum += exp2_hw(past ? (x[i] - m) * kLog2e : fmaf(x[i], kLog2e, -now));
+      c = past ? -INFINITY : now;   // nothing beside a maximum that is not past it
+    }
     float bound = best.last ? unordered((uint32_t)(best.last >> 32)) : -INFINITY;
     if (t0 == 0) {
       int group = 64;   // lanes of one of n groups or more
@@ -250,11 +266,8 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
     look(x, t0);
   }
   const float top = wave_max(m);
-  sum *= exp2_hw(fmaf(-scaled_to(top), kLog2e, c));   // what c's rounding left is in it
-  if (fabsf(top) > kScaled && fabsf(top) < INFINITY) {   // log2 e times it is no number: once more
-    sum = 0.f;
-    for (int t = lane; t < left; t += 64) sum += exp2_hw((to_f32(x0[t - 8 * lane]) - top) * kLog2e);
-  }
+  // what c's rounding left is in it
+  sum *= exp2_hw(past_scaled(m) ? (m - top) * kLog2e : fmaf(-fmaxf(top, -kScaled), kLog2e, c));
   const double total = wave_sum(sum);
   if (lane == 0) a.stats[id] = float2{top, (float)total};
   if (lane < a.n) a.keys[id * a.n + lane] = best.top;

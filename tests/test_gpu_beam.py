@@ -110,6 +110,26 @@ def test_masks_and_what_is_no_number(dtype):
     same(select(x, s, 10, dtype), rec.beam_select(x, s, 10), V, 20)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [2.0 ** 24, 1e9, 1.07e9, 1.08e9, 1e10, 1e12, 1e20, 1e30, 9e37, 2e38])
+def test_masks_of_any_size(value, dtype):
+    """Masks and logits whose product with log2 e has few or no digits left for an exponential:
+    they count as nothing beside others, and as they are where there are no others."""
+    V = 6000
+    x, s = data(6, 2, V, dtype, 9)
+    r = np.random.default_rng(10)
+    x[0, :, 3:] = -value                       # whole pieces and all lanes but one masked
+    x[1, :, 1:V - 1] = -value
+    x[2][r.random((2, V)) < 0.9] = -value
+    x[3] = -value                              # nothing else
+    x[4, 0] += value                           # logits as large themselves
+    x[5, 0] = value
+    x[5, 0, ::7] = -value
+    x = _round(x, dtype)
+    for n in (1, 4, 30):
+        same(select(x, s, n, dtype), rec.beam_select(x, s, n), V, 20)
+
+
 def test_ended_beams():
     x, s = data(4, 5, 900, "f32", 8)
     ended = np.zeros((4, 5), bool)
