@@ -496,7 +496,8 @@ FAVOR_API favor_status favor_conv(const favor_conv_desc *g, const void *x, const
 
 /*
  * Gradients from dy and dstate_out (nullable: zeros) of x, weight [D][width], bias (dbias
- * nullable) and state_in (dstate_in nullable; overlaps neither state nor dstate_out).
+ * nullable) and state_in (dstate_in nullable; overlaps neither state nor dstate_out). With no
+ * sequence (B = 0) or no token the parameters' gradients are zeros.
  * Nothing from the forward call is needed. Deterministic. Workspace:
  * favor_conv_workspace_size(g) bytes, 256-byte aligned; its contents do not matter.
  */
@@ -566,7 +567,8 @@ FAVOR_API favor_status favor_selective_scan(const favor_scan_desc *g, const void
  *   ds = sum_n A q_t h_{t-1} + x sum_n (C e + q_{t+1}) B,  ddt = ds softplus'(dt + dt_bias)
  *   dx = s sum_n (C e + q_{t+1}) B + skip e,  dz = dy (C h + skip x) silu'(z),  dskip = sum e x
  * and ddt_bias = sum ddt. dskip, dz and ddt_bias are required where skip, z and dt_bias are
- * given, and not written otherwise. dstate_in (nullable) may be dstate_out, and overlaps
+ * given, and not written otherwise. With no sequence (B = 0) or no token the parameters' gradients
+ * are zeros. dstate_in (nullable) may be dstate_out, and overlaps
  * neither it nor state_in otherwise. Nothing from the forward call is needed. Deterministic.
  */
 FAVOR_API favor_status favor_selective_scan_backward(

@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kSumCols *kSumLanes) void k_conv_sums(Conv a, int r
   const int64_t col = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
   const int lane = threadIdx.x / kSumCols;
   float s = 0.f;
-  if (col < cols)
+  if (col < cols && a.part)
 #pragma unroll 8
     for (int r = lane; r < rows; r += kSumLanes) s += a.part[r * cols + col];
   part[lane][threadIdx.x % kSumCols] = s;

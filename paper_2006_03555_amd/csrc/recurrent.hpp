@@ -31,7 +31,7 @@ struct Conv {
 hipError_t launch_conv(const Conv &a, Dt dt, hipStream_t st);
 int64_t conv_part_rows(int B, int L, int D, int width, Dt dt);
 hipError_t launch_conv_backward(const Conv &a, Dt dt, hipStream_t st);
-// cols sums over rows of part [rows][cols]; conv: the columns [width + 1][D] go to dw and dbias.
+// Sums over the rows of part [rows][width + 1][D] (null: zeros), to dw and dbias.
 hipError_t launch_conv_sums(const Conv &a, int rows, hipStream_t st);
 hipError_t launch_conv_step(const Conv &a, Dt dt, hipStream_t st);
 

@@ -426,7 +426,7 @@ favor_status favor_conv_backward(const favor_conv_desc *g, const void *x, const 
   const char *names[] = {"x", "dy", "dx"};
   FAVOR_TRY(check_all(ptrs, names, 3, 2, work));
   FAVOR_TRY(check_ptr(weight, "weight", any, 4));
-  FAVOR_TRY(check_ptr(dweight, "dweight", any, 4));
+  FAVOR_TRY(check_ptr(dweight, "dweight", any || dweight, 4));
   FAVOR_TRY(check_optional(bias, "bias", 4));
   FAVOR_TRY(check_optional(dbias, "dbias", 4));
   FAVOR_TRY(check_optional(lengths, "lengths", 4));
@@ -437,7 +437,7 @@ favor_status favor_conv_backward(const favor_conv_desc *g, const void *x, const 
   FAVOR_TRY(check_apart(dstate_in, "dstate_in", dstate_out, "dstate_out", state_bytes(g), false));
   const int64_t params = (int64_t)sizeof(float) * g->D * g->width;
   FAVOR_TRY(check_apart(dweight, "dweight", weight, "weight", params, false));
-  if (!any) return ok();
+  if (!any && !dweight) return ok();
   FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g)));
   favor::Conv a = conv_of(g, g->L, x, weight, bias, lengths);
   a.state_in = state_in;
@@ -449,16 +449,16 @@ favor_status favor_conv_backward(const favor_conv_desc *g, const void *x, const 
   a.dstate_in = dstate_in;
   a.dw = dweight;
   a.dbias = dbias;
-  a.part = static_cast<float *>(ws);
+  a.part = any ? static_cast<float *>(ws) : nullptr;   // of no sequence: zeros
   const Dt dt = dt_of(g->dtype);
-  hipError_t e;
-  {
+  hipError_t e = hipSuccess;
+  if (any) {
     favor::LaunchTimer t(favor::kKerConvBwd, stream);
     e = favor::launch_conv_backward(a, dt, stream);
   }
   if (e != hipSuccess) return device_result(e, "favor_conv_backward");
   favor::LaunchTimer t(favor::kKerColumnSums, stream);
-  return device_result(favor::launch_conv_sums(a, (int)part_rows(g), stream),
+  return device_result(favor::launch_conv_sums(a, any ? (int)part_rows(g) : 1, stream),
                        "favor_conv_backward sums");
 }
 
@@ -567,9 +567,9 @@ favor_status favor_selective_scan_backward(
     }
   }
   FAVOR_TRY(check_params(A, skip, dt_bias, g->N, any));
-  FAVOR_TRY(check_ptr(dA, "dA", any, 4));
-  FAVOR_TRY(check_ptr(dskip, "dskip", any && skip, 4));
-  FAVOR_TRY(check_ptr(ddt_bias, "ddt_bias", any && dt_bias, 4));
+  FAVOR_TRY(check_ptr(dA, "dA", any || dA, 4));
+  FAVOR_TRY(check_ptr(dskip, "dskip", skip && (any || dskip), 4));
+  FAVOR_TRY(check_ptr(ddt_bias, "ddt_bias", dt_bias && (any || ddt_bias), 4));
   FAVOR_TRY(check_optional(lengths, "lengths", 4));
   FAVOR_TRY(check_optional(state_in, "state_in"));
   FAVOR_TRY(check_optional(dstate_out, "dstate_out"));
@@ -577,13 +577,14 @@ favor_status favor_selective_scan_backward(
   FAVOR_TRY(check_apart(dstate_in, "dstate_in", dstate_out, "dstate_out", state_bytes(g), true));
   FAVOR_TRY(check_apart(dstate_in, "dstate_in", state_in, "state_in", state_bytes(g), false));
   FAVOR_TRY(check_apart(dA, "dA", A, "A", (int64_t)sizeof(float) * g->D * g->N, false));
-  if (!any) return ok();
+  if (!any && !dA) return ok();
   FAVOR_TRY(check_workspace(ws, ws_bytes, workspace_of(g, kOpBackward)));
   favor::Scan a = scan_of(g, g->L, x, dt, A, Bm, C, skip, z, dt_bias, lengths);
   if (work) carve_backward(g, ws, &a);
   a.h_in = state_in;
   a.chunks = 1;
-  a.nseg = chunks_of(g);
+  a.nseg = any ? chunks_of(g) : 0;
+  if (!any) a.B = 1, a.L = 0;   // no sequence: as one without tokens, the parameters' gradients are zeros
   a.sum_states = sum_states_of(g);
   a.subs = subs_of(g);
   a.dy = dy;
@@ -610,7 +611,7 @@ favor_status favor_selective_scan_backward(
     e = favor::launch_scan_backward_parts(a, type, stream);
   }
   if (e != hipSuccess) return device_result(e, "favor_selective_scan_backward chunk sums");
-  if (work || dstate_in) {
+  if (any && (work || dstate_in)) {
     favor::LaunchTimer t(favor::kKerScanPrefix, stream);
     e = favor::launch_scan_prefix(a, true, stream);
   }

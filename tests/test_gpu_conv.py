@@ -222,6 +222,21 @@ def test_empty_calls():
     assert fv.causal_conv(torch.zeros((0, 5, 8), device="cuda"), w).shape == (0, 5, 8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_no_sequence(dtype):
+    """The filters' gradients of an empty batch are sums of nothing, whatever their memory held."""
+    import torch
+    fv = _fv()
+    x = torch.zeros((0, 5, 72), device="cuda", dtype=torch_dtype(dtype))
+    w, b = torch.ones((72, 4), device="cuda"), torch.ones(72, device="cuda")
+    dw, db = torch.full_like(w, 7.0), torch.full_like(b, 7.0)
+    dx, *got, ds = fv.causal_conv_backward(x, w, x, b, True, return_state_grad=True, dweight=dw, dbias=db)
+    assert got[0] is dw and got[1] is db and not dw.any() and not db.any()
+    assert dx.shape == x.shape and ds.shape == (0, 3, 72)
+    fv.causal_conv_backward(x, w, x, dweight=dw.fill_(7))
+    assert not dw.any()
+
+
 def test_gradients_against_differences():
     """The kernels' own loss moves as their gradients say (fp32; central differences)."""
     import torch

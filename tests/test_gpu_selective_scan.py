@@ -250,6 +250,21 @@ def test_empty_calls():
     _ = fv
 
 
+def test_gradients_of_no_sequence():
+    """The parameters' gradients of an empty batch are sums of nothing, whatever their memory held."""
+    import torch
+    fv = _fv()
+    i = inputs(1, 150, 8, 3, 1, "f32", 2)
+    t = {k: v if k in ("A", "skip", "bias") else v[:0] for k, v in dev(i, "f32").items()}
+    into = {k: torch.full_like(t[n], 7.0) for k, n in (("dA", "A"), ("dD", "skip"), ("ddt_bias", "bias"))}
+    g = dict(zip(GRADS, backward(t, **into)))
+    for k, v in into.items():
+        assert g[k] is v and not v.any(), k
+    assert g["dx"].shape == (0, 150, 8) and g["dstate"].shape == (0, 8, 3)
+    fv.selective_scan_backward(t["x"], t["dt"], t["A"], t["Bm"], t["C"], t["dy"], dA=into["dA"].fill_(7))
+    assert not into["dA"].any()
+
+
 def test_not_a_number_stays_in_its_channel():
     import torch
     i = inputs(2, 300, 24, 16, 1, "f32", 61)
