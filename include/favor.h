@@ -477,7 +477,7 @@ FAVOR_API favor_status favor_dropout(const void *x, const void *residual, void *
  * the oldest first.
  *
  * Supported: width 2 to 8; D a multiple of 8 up to 65536; dtype (x, y, states and their
- * gradients) F32 or BF16, sums in fp32; 0 <= L <= 2^30, B <= 65535, B L D <= 2^46. lengths
+ * gradients) F32 or BF16, sums in fp32; 0 <= L <= 2^30, B <= 65535, L D <= 2^38, B L D <= 2^46. lengths
  * [B] int32 (nullable, device): as for favor_attn_decay: rows behind a sequence are not read
  * and their rows of y and dx are written as zeros.
  */
@@ -532,8 +532,8 @@ FAVOR_API favor_status favor_conv_step(const favor_conv_desc *g, const void *x,
  * at most 2^25 bytes apart. A [D][N], skip and dt_bias [D] fp32. States [B][D][N] fp32, contiguous.
  *
  * Supported: N from 1 to 256; D up to 65536 with D / groups a multiple of 8; dtype (x, dt, B,
- * C, z, y and their gradients) F32 or BF16; 0 <= L <= 2^30, B <= 65535, B L D and B L groups N
- * <= 2^46. Steps, states and sums are fp32 for both. A is meant to be negative; for a positive one exp(A times the steps of
+ * C, z, y and their gradients) F32 or BF16; 0 <= L <= 2^30, B <= 65535, L D <= 2^38, B L D and
+ * B L groups N <= 2^46. Steps, states and sums are fp32 for both. A is meant to be negative; for a positive one exp(A times the steps of
  * any 128 tokens) has to be in fp32's range, and A must be finite. lengths as for favor_conv
  * (B's and C's padding is not read either, its gradients are zeros). A NaN or infinity reaches
  * the results of its own channel (in B or C: of its group) from its token on, and gradients as the

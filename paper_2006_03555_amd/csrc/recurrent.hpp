@@ -48,6 +48,7 @@ struct Scan {
   Rows xs, dts, bs, cs, zs, ys;
   int B, L, D, N, G, softplus;
   int chunks, nseg;                 // chunks of kScanTokens tokens in one segment; segments
+  int seg0;                         // the first segment of this launch
   int sum_states;                   // states of a workgroup of the segments' sums (of kScanStates)
   int subs;                         // backward: tiles of one workgroup
   // nseg > 1: the states before each segment [B][nseg][D][N] (first: the segments' sums) and
@@ -71,6 +72,9 @@ struct Scan {
 constexpr int kScanTokens = 128;     // of one chunk
 constexpr int kScanStates = 16;      // of one pass over a chunk
 constexpr int kScanBackTile = 32;    // channels of one tile of the backward pass
+// Workgroups of one launch over chunks (of rows of B and C): a launch takes less than 2^32 threads,
+// so what is longer takes several launches (turns).
+constexpr int kScanBlocks = 1 << 20, kLowBlocks = 1 << 16;
 // The sums of the segments but the last, in part and steps; backward, where a segment is one
 // chunk: of all of them, and in part_r too.
 hipError_t launch_scan_sums(const Scan &a, Dt dt, hipStream_t st);
@@ -102,6 +106,7 @@ hipError_t launch_beam_merge(const BeamSelect &a, hipStream_t st);
 constexpr int kBeamPools = 64;       // pools of one launch
 // 16-byte units that one workgroup copies; 8 x 8 beams, 24 layers 43 us with 2048, 45 with 4096
 constexpr int kBeamPieceUnits = 2048;
+constexpr int kBeamPieces = 1 << 23;   // of one launch (its threads are less than 2^32)
 struct BeamReorder {
   const int32_t *parent, *slots;   // [B][K]; slots nullable
   int32_t *new_slots;

@@ -18,6 +18,7 @@ using namespace favor::host;
 enum Op { kOpForward = 0, kOpBackward = 1, kOpStep = 2 };
 constexpr int kMaxD = 65536, kMaxB = 65535;
 constexpr int64_t kMaxBlocks = 0x7fffffff;
+constexpr int64_t kMaxRows = (int64_t)1 << 38;   // elements of one sequence
 // the scan reaches a chunk's 128 rows by 32-bit offsets
 constexpr int64_t kMaxTokenBytes = 1 << 25;
 
@@ -109,8 +110,10 @@ favor_status validate(const favor_conv_desc *g, int op) {
     const int64_t size[3] = {g->B, 1, op == kOpStep ? 1 : g->L};
     FAVOR_TRY(check_rows(ts[i].name, *ts[i].s, size, g->D, 16 / bytes_of(g->dtype), 0, ts[i].out));
   }
-  if (((int64_t)g->L / 8 + 1) * (g->D / 4) / 256 > kMaxBlocks ||
-      (op == kOpBackward && part_rows(g) > kMaxBlocks))
+  // what one launch takes: a thread has 8 tokens of 4 channels at least, 32 of them in a long call
+  if ((int64_t)g->L * g->D > kMaxRows)
+    return fail(FAVOR_ERR_UNSUPPORTED, "L=%d D=%d: a sequence of more than 2^38 elements", g->L, g->D);
+  if (op == kOpBackward && part_rows(g) > kMaxBlocks)
     return fail(FAVOR_ERR_UNSUPPORTED, "B=%d L=%d D=%d is too large", g->B, g->L, g->D);
   return FAVOR_OK;
 }
@@ -173,9 +176,11 @@ favor_status validate(const favor_scan_desc *g, int op) {
                          ts[i].low ? 1 : 16 / bytes_of(g->dtype), kMaxTokenBytes / bytes_of(g->dtype),
                          ts[i].out));
   }
-  if ((int64_t)tiles_of(g, favor::kScanBackTile) * chunks_of(g) > kMaxBlocks ||
-      (int64_t)g->L * g->groups * g->N / 256 > kMaxBlocks)
-    return fail(FAVOR_ERR_UNSUPPORTED, "L=%d D=%d N=%d is too large", g->L, g->D, g->N);
+  // counts that the kernels hold in 32 bits
+  if ((int64_t)g->L * g->D > kMaxRows)
+    return fail(FAVOR_ERR_UNSUPPORTED, "L=%d D=%d: a sequence of more than 2^38 elements", g->L, g->D);
+  if ((int64_t)g->B * chunks_of(g) > kMaxBlocks)
+    return fail(FAVOR_ERR_UNSUPPORTED, "B=%d L=%d is too large", g->B, g->L);
   return FAVOR_OK;
 }
 
@@ -740,20 +745,24 @@ favor_status favor_beam_reorder(int32_t B, int32_t K, const int32_t *parent, con
         return fail(FAVOR_ERR_INVALID_ARGUMENT, "pools %d and %d are one or overlap", j, i);
   }
   if (!work) return ok();
-  for (int first = 0; first == 0 || first < n_pools; first += favor::kBeamPools) {
+  for (int first = 0; first == 0 || first < n_pools;) {
     favor::BeamReorder a{};
     a.parent = parent;
     a.slots = slots;
     a.new_slots = new_slots;
     a.B = B;
     a.K = K;
-    a.n_pools = std::min(favor::kBeamPools, n_pools - first);
-    for (int i = 0; i < a.n_pools; ++i) {
-      const favor_beam_pool &p = pools[first + i];
+    while (a.n_pools < favor::kBeamPools && first + a.n_pools < n_pools) {
+      const favor_beam_pool &p = pools[first + a.n_pools];
       const int64_t units = p.bytes_per_slot / 16;
+      const int pieces = (int)((units + favor::kBeamPieceUnits - 1) / favor::kBeamPieceUnits);
+      const int i = a.n_pools;
+      if (i && a.first[i] + pieces > favor::kBeamPieces) break;   // the next launch's
       a.pool[i] = {p.data, (int32_t)units, p.n_slots};
-      a.first[i + 1] = a.first[i] + (int)((units + favor::kBeamPieceUnits - 1) / favor::kBeamPieceUnits);
+      a.first[i + 1] = a.first[i] + pieces;
+      a.n_pools = i + 1;
     }
+    first += std::max(1, a.n_pools);
     hipError_t e;
     {
       favor::LaunchTimer t(favor::kKerBeamReorder, stream);

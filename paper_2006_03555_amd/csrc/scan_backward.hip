@@ -15,6 +15,8 @@
 // leave is added up last. Rows reach the lanes through two tiles of LDS, two values to a word in
 // bf16, and their gradients leave the same way. B4 L4096 D2048 N16 in bf16: 196 to 216 us, 18 and
 // 515 to 530; the vector unit is busy for 91% and 90% of the first and the third.
+#include <algorithm>
+
 #include "scan_common.hpp"
 
 namespace favor {
@@ -416,17 +418,17 @@ template <typename T, bool kGate> __global__ __launch_bounds__(kScanThreads, 4) 
 constexpr int kLowThreads = 256;
 template <typename T> __global__ __launch_bounds__(kLowThreads) void k_scan_low(Scan a, int tiles) {
   const int64_t GN = (int64_t)a.G * a.N, per = (int64_t)a.L * GN;
-  const int64_t i = (int64_t)blockIdx.x * kLowThreads + threadIdx.x;
-  if (i >= per) return;
   const int b = blockIdx.y;
-  const int t = (int)(i / GN), gn = (int)(i - t * GN), g = gn / a.N, n = gn - g * a.N;
   const float *part = blockIdx.z ? a.part_c : a.part_b;
-  float sum = 0.f;
-  if (t < clamped_length(a.lengths, b, a.L))
-#pragma unroll 8
-    for (int k = 0; k < tiles; ++k) sum += part[((int64_t)k * a.B + b) * per + i];
   const Rows &r = blockIdx.z ? a.dcs : a.dbs;
-  static_cast<T *>(blockIdx.z ? a.dc : a.db)[b * r.b + g * r.h + t * r.t + n] = from_f32<T>(sum);
+  for (int64_t i = (int64_t)blockIdx.x * kLowThreads + threadIdx.x; i < per; i += (int64_t)gridDim.x * kLowThreads) {
+    const int t = (int)(i / GN), gn = (int)(i - t * GN), g = gn / a.N, n = gn - g * a.N;
+    float sum = 0.f;
+    if (t < clamped_length(a.lengths, b, a.L))
+#pragma unroll 8
+      for (int k = 0; k < tiles; ++k) sum += part[((int64_t)k * a.B + b) * per + i];
+    static_cast<T *>(blockIdx.z ? a.dc : a.db)[b * r.b + g * r.h + t * r.t + n] = from_f32<T>(sum);
+  }
 }
 
 // dA, dskip and dbias: over sequences and chunks. 64 columns by 16 row lanes, joined in order.
@@ -467,9 +469,15 @@ hipError_t launch_tiles(K kernel, const Scan &a, int width, int parts, size_t ld
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  const int tiles = a.G * ((a.D / a.G + width - 1) / width);
-  kernel<<<dim3((unsigned)(tiles * a.nseg), a.B, parts), kScanThreads, lds, st>>>(a);
-  return hipGetLastError();
+  const int tiles = a.G * ((a.D / a.G + width - 1) / width), each = kScanBlocks / tiles;
+  Scan part = a;
+  for (part.seg0 = 0; part.seg0 < a.nseg; part.seg0 += each) {
+    const int segments = std::min(each, a.nseg - part.seg0);
+    kernel<<<dim3((unsigned)(tiles * segments), a.B, parts), kScanThreads, lds, st>>>(part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -492,7 +500,7 @@ hipError_t launch_scan_backward_sums(const Scan &a, Dt dt, hipStream_t st) {
   const int64_t low = (int64_t)a.L * a.G * a.N;
   if (low > 0) {
     const int tiles = (a.D / a.G + W * a.subs - 1) / (W * a.subs);
-    const dim3 grid((unsigned)((low + kLowThreads - 1) / kLowThreads), a.B, 2);
+    const dim3 grid((unsigned)std::min<int64_t>(kLowBlocks, (low + kLowThreads - 1) / kLowThreads), a.B, 2);
     if (dt == Dt::BF16) k_scan_low<bf16><<<grid, kLowThreads, 0, st>>>(a, tiles);
     else k_scan_low<float><<<grid, kLowThreads, 0, st>>>(a, tiles);
     const hipError_t e = hipGetLastError();

@@ -125,6 +125,7 @@ __device__ __forceinline__ ScanPlace scan_place(const Scan &a, int width) {
   p.b = blockIdx.y;
   p.seg = blockIdx.x / tiles;
   const int i = blockIdx.x - p.seg * tiles;
+  p.seg += a.seg0;
   p.g = i / of_group;
   p.tile = i - p.g * of_group;
   p.c0 = p.g * dg + p.tile * width;

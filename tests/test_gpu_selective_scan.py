@@ -405,3 +405,27 @@ def test_padded_batch_of_many_states(N, dtype):
     n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
     (y, s), grads = forward(t, lengths=n), backward(t, lengths=n)
     check(i, dtype, (y, s), grads, lengths=np.array(lengths))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_workgroups_than_a_launch_takes(dtype):
+    """More than 2^20 workgroups over chunks and 2^24 values of B and C in one backward pass: a
+    long sequence that forgets everything every 1024 tokens has the gradients of the stretches as
+    a batch, bit by bit."""
+    import torch
+    fv = _fv()
+    P, T, G, N = 1024, 2051, 64, 1       # 64 groups of 8 channels, 8 chunks a stretch
+    L, D = T * P, 8 * G
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    draw = lambda *s: torch.randn(s, generator=gen, device="cuda", dtype=torch_dtype(dtype))
+    x, dt, dy = draw(1, L, D), draw(1, L, D), draw(1, L, D)
+    B, C = draw(1, L, G, N), draw(1, L, G, N)
+    dt[:, ::P] = 300   # exp(-300) is 0 in fp32: nothing goes past a stretch's first token
+    A = -1 - torch.rand((D, N), generator=gen, device="cuda")
+    whole = fv.selective_scan_backward(x, dt, A, B, C, dy)
+    rows = lambda v: v.view((T, P) + v.shape[2:])
+    batch = fv.selective_scan_backward(rows(x), rows(dt), A, rows(B), rows(C), rows(dy))
+    for w, b, name in zip(whole, batch, GRADS):
+        if w is not None:
+            assert torch.isfinite(w).all() and w.any(), name
+            assert torch.equal(w.view(b.shape), b), name

@@ -392,6 +392,19 @@ def test_sizes_past_what_offsets_hold():
     assert fv.validate_conv_desc(g, 1) == 0 and fv.conv_workspace_size(g) > 1 << 30
 
 
+def test_sizes_past_one_launch():
+    """A launch takes less than 2^32 threads: what a card holds is taken, longer rows are refused
+    before anything is launched."""
+    for g in (_scan(B=1, L=1 << 26, D=8, N=64, groups=1), _scan(B=1, L=1 << 20, D=128, N=256, groups=16),
+              _scan(B=1, L=1 << 30, D=8, N=1, groups=1), _scan(B=1, L=1 << 30, D=256, N=1, groups=32)):
+        assert fv.validate_scan_desc(g, 1) == 0 and fv.scan_workspace_size(g, True) > 0
+    for L, status in (((1 << 22), 0), ((1 << 22) + 1, 2)):
+        for op in (0, 1):
+            assert fv.validate_scan_desc(_scan(B=1, L=L, D=65536, N=1, groups=1), op) == status
+            assert fv.validate_conv_desc(_conv(B=1, L=L, D=65536), op) == status
+            assert status == 0 or "2^38" in fv.last_error()
+
+
 def test_binding_refusals():
     import torch
     z = torch.zeros
@@ -476,3 +489,19 @@ def test_calls_fuzzed_under_sanitizers(fuzzer, seed):
                        timeout=300)
     assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
     assert " 0 failures" in r.stdout
+
+
+def test_launches_of_many_and_huge_pools(tmp_path):
+    gxx = shutil.which("g++")
+    if gxx is None or not os.path.isdir(os.path.join(ROCM_INCLUDE, "hip")):
+        pytest.skip("needs g++ and the HIP headers")
+    csrc = "paper_2006_03555_amd/csrc"
+    sources = ["tests/host/reorder_launches.cpp", "tests/host/stubs.cpp",
+               f"{csrc}/recurrent_api.cpp", f"{csrc}/favor_api.cpp", f"{csrc}/timing.cpp"]
+    exe = str(tmp_path / "reorder_launches")
+    r = subprocess.run([gxx, "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INCLUDE, "-I",
+                        f"{ROOT}/include", *[os.path.join(ROOT, x) for x in sources], "-o", exe,
+                        "-Wl,--unresolved-symbols=ignore-all"], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, r.stdout + r.stderr
