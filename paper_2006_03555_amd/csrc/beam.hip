@@ -12,6 +12,8 @@
 // rows have equal scores wherever they lie in memory. Scores are compared in 64 bits.
 // 32 entries of 8 beams of 131072 logits in bf16, a quarter of them ended: 21 us (2.5 TB/s) and 8
 // for the merge; 4 beams of 50001 in fp32: 5.2 and 5.6, all latency.
+#include <cfloat>
+
 #include "recurrent.hpp"
 #include "vec_rows.hpp"
 
@@ -197,18 +199,21 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
       for (int i = 0; i < E; ++i) sum += exp2_hw(past ? (x[i] - m) * kLog2e : fmaf(x[i], kLog2e, -now));
       c = past ? -INFINITY : now;   // nothing beside a maximum that is not past it
     }
-    float bound = best.last ? unordered((uint32_t)(best.last >> 32)) : -INFINITY;
+    // what a candidate reaches: more than the worst kept logit (an equal one of a later token comes
+    // behind it), and a finite one (a mask of -Inf is never offered)
+    float bound = best.last ? unordered((uint32_t)(best.last >> 32) + 1) : -FLT_MAX;
     if (t0 == 0) {
       int group = 64;   // lanes of one of n groups or more
       while (64 / group < a.n) group /= 2;
       bound = over_wave(most, [&](int d, float u, float v) { return d < group ? fmaxf(u, v) : fminf(u, v); });
+      bound = fmaxf(bound, -FLT_MAX);
     }
     if (!__ballot(most >= bound)) return;
     int count = 0;
     const int t1 = begin + t0 + 8 * lane;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const bool in = x[i] >= bound;   // (tokens behind the piece are -Inf, which is never offered)
+      const bool in = x[i] >= bound;   // (tokens behind the piece are -Inf)
       const uint64_t who = __ballot(in);
       if (!who) continue;
       const int at = count + before(who);
@@ -224,7 +229,8 @@ __global__ __launch_bounds__(64 * kPieceWaves) void k_beam_pieces(BeamSelect a) 
     } else {   // a row of many equal or rising logits
       for (int i = 0; i < E; ++i) {
         const int t = t0 + 512 * (i / 8) + i % 8;
-        best.push(8 * lane + t < left ? key_of(to_f32(x0[t]), begin + 8 * lane + t) : 0);
+        const float v = 8 * lane + t < left ? to_f32(x0[t]) : -INFINITY;
+        best.push(v >= bound ? key_of(v, begin + 8 * lane + t) : 0);
       }
     }
   };

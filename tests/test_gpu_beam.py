@@ -130,6 +130,24 @@ def test_masks_of_any_size(value, dtype):
         same(select(x, s, n, dtype), rec.beam_select(x, s, n), V, 20)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [-np.inf, -3.38e38, -1e4, 0.0])
+def test_masked_vocabulary(value, dtype):
+    """Few tokens of many are left, more and fewer than are chosen; the masked ones are equal."""
+    V = 30011
+    x, s = data(4, 3, V, dtype, 12)
+    r = np.random.default_rng(13)
+    for b, few in enumerate((1, 6, 40, 300)):
+        for k in range(3):
+            keep = r.choice(V, few, replace=False)
+            row = np.full(V, value, np.float32)
+            row[keep] = x[b, k, keep]
+            x[b, k] = row
+    x = _round(x, dtype)
+    for n in (1, 8, 64):
+        same(select(x, s, n, dtype), rec.beam_select(x, s, n), V, 20)
+
+
 def test_ended_beams():
     x, s = data(4, 5, 900, "f32", 8)
     ended = np.zeros((4, 5), bool)
