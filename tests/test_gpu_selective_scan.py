@@ -429,3 +429,108 @@ def test_more_workgroups_than_a_launch_takes(dtype):
         if w is not None:
             assert torch.isfinite(w).all() and w.any(), name
             assert torch.equal(w.view(b.shape), b), name
+
+
+# ------------------------------------------------------------------ forward calls in segments
+def _segments(B, L, D, N, G):
+    """(segments, chunks of one) of a forward call, by the size of its workspace: the states before
+    each segment and their sums of steps."""
+    fv = _fv()
+    n = fv.scan_workspace_size(fv.make_scan_desc(B, L, D, N, fv.F32, G))
+    per, chunks = 4 * B * D * (N + 1), -(-L // 128)
+    nseg = round(n / per) if n else 1
+    assert abs(n - nseg * per) <= 512 or nseg == 1
+    return nseg, -(-chunks // nseg)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,lengths", [(5, None), (20, None), (16, [6500, 2500])])
+def test_carry_between_chunks_of_a_segment(N, lengths, dtype):
+    """Segments of three chunks: the state goes on inside a segment, in the sums and in the rows,
+    with ends in the middle of a segment and of a chunk."""
+    import torch
+    B, L, G = 1 if lengths is None else 2, 6875, 210 if lengths is None else 105
+    D = 8 * G
+    assert _segments(B, L, D, N, G) == (18, 3)
+    i = inputs(B, L, D, N, G, dtype, 7 * N)
+    i["A"] *= np.float32(0.02)   # what is 128 tokens old still counts
+    i["bias"] -= 3
+    t = dev(i, dtype)
+    kw = {} if lengths is None else dict(lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    y, s = forward(t, **kw)
+    groups = [0, G // 2, G - 1]
+    c = np.concatenate([np.arange(8 * g, 8 * g + 8) for g in groups])
+    j = {k: None if v is None else v[:, :, groups] if k in ("Bm", "C") else v[c] if k in ("A", "skip", "bias")
+         else v[:, c] if k in ("state", "dstate") else v[..., c] for k, v in i.items()}
+    o = _opts(j, True, lengths)
+    ref, sref = rec.scan(*_args(j), **o)
+    units = rec.scan_bounds(*_args(j), j["dy"], dstate=j["dstate"], **o)
+    near(y[..., c], ref, units[0], dtype, "y")
+    near(s[:, c], sref, units[1], "f32", "state")
+    # a carry that is lost anywhere is outside these bounds
+    cut = 384 * 3 + 128
+    lost = {k: v[:, cut:cut + 100] if k in ("x", "dt", "Bm", "C", "z", "dy") else v for k, v in j.items()}
+    wrong, _ = rec.scan(*_args(lost), **dict(_opts(lost, True, None), state=None))
+    bad = np.abs(wrong - ref[:, cut:cut + 100]) > 1.05 * 2.0 ** -24 * units[0][:, cut:cut + 100] + (
+        2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref[:, cut:cut + 100])
+    assert bad[0].any(0).all()   # in every channel
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("skip,z,bias,state,soft", [
+    (0, 0, 0, 0, 1), (1, 0, 0, 1, 0), (0, 1, 1, 1, 0), (0, 0, 1, 1, 1), (1, 1, 0, 0, 1)])
+def test_segments_without_parts(skip, z, bias, state, soft, dtype):
+    assert _segments(2, 700, 24, 7, 1) == (6, 1)
+    i = inputs(2, 700, 24, 7, 1, dtype, 19, skip, z, bias, state, soft)
+    t = dev(i, dtype)
+    check(i, dtype, forward(t, softplus=bool(soft)), backward(t, softplus=bool(soft)), bool(soft))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_padded_batch_in_segments(dtype):
+    """As test_padded_batch, with segments before, around and behind each end."""
+    import torch
+    B, L = 6, 700
+    lengths = [700, 0, 1, 256, 257, 640]
+    assert _segments(B, L, 16, 9, 2) == (6, 1)
+    i = inputs(B, L, 16, 9, 2, dtype, 6)
+    t = dev(i, dtype)
+    for b, n in enumerate(lengths):
+        for k in ("x", "dt", "Bm", "C", "z", "dy"):
+            t[k][b, n:] = float("nan") if b % 2 else float("inf")
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    got, grads = forward(t, lengths=lens), backward(t, lengths=lens)
+    check(i, dtype, got, grads, True, lengths)
+    for b, n in enumerate(lengths):
+        for v in (got[0], grads[0], grads[1], grads[3], grads[4], grads[6]):
+            assert not v[b, n:].any()
+    assert torch.equal(got[1][1], t["state"][1]) and torch.equal(grads[8][1], t["dstate"][1])
+
+
+@pytest.mark.parametrize("state", [0, 1])
+@pytest.mark.parametrize("name", ["x", "dt"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_not_a_number_stays_in_its_channel_in_segments(value, name, state):
+    """One in a middle segment reaches its own channel alone, from its token on, and the gradients
+    of no other channel's rows."""
+    import torch
+    B, L, D, at = 2, 700, 24, 330
+    assert _segments(B, L, D, 16, 1) == (6, 1)
+    i = inputs(B, L, D, 16, 1, "f32", 62, state=state)
+    t = dev(i, "f32")
+    want, grads = forward(t), backward(t)
+    u = dict(t, **{name: t[name].clone()})
+    u[name][0, at, 5] = value
+    y, s = forward(u)
+    hit = torch.zeros((B, L, D), dtype=torch.bool, device="cuda")
+    hit[0, at:, 5] = True
+    assert torch.equal(y[~hit], want[0][~hit])
+    assert not torch.isfinite(y[0, at, 5])
+    if value != value:
+        assert y[hit].isnan().all() and s[0, 5].isnan().all()
+    clean = torch.ones((B, D), dtype=torch.bool, device="cuda")
+    clean[0, 5] = False
+    assert torch.equal(s[clean], want[1][clean])
+    after = backward(u)
+    for k in (0, 1, 6):   # dx, ddt, dz
+        assert torch.equal(after[k].transpose(1, 2)[clean], grads[k].transpose(1, 2)[clean])
