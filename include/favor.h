@@ -603,9 +603,9 @@ FAVOR_API favor_status favor_validate_scan_desc(const favor_scan_desc *g, int op
  * aligned: any V and slices of a padded vocabulary. scores [B][K] fp32. ended [B][K] bytes
  * (nullable): a beam that has ended (not 0) offers only itself, with end_token and its own
  * score, and its logits are not read. end_token < 0: there is none (then ended must be NULL).
- * Only finite scores are offered: a beam of score -Inf, a token of logit -Inf and a beam with a
- * NaN or +Inf among its logits (whose sum is no number) offer nothing. Where fewer than n are
- * offered the rest has score -Inf, parent 0 and token end_token (0 without one).
+ * Only scores that are finite in fp32 are offered: a beam of score -Inf, a token of logit -Inf and
+ * a beam with a NaN or +Inf among its logits (whose sum is no number) offer nothing. Where fewer
+ * than n are offered the rest has score -Inf, parent 0 and token end_token (0 without one).
  *
  * Supported: K and n up to 64, V from 1 to 2^30, B K <= 65535. Workspace:
  * favor_beam_workspace_size(g) bytes, 256-byte aligned; its contents do not matter.

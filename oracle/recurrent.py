@@ -258,7 +258,8 @@ def beam_select(logits, scores, n, ended=None, end_token=-1):
             with np.errstate(all="ignore"):
                 p = row - top - np.log(np.exp(row - top).sum()) + scores[b, k]
             found += [(p[v], k, row[v], v) for v in np.argsort(-row, kind="stable")[:n]]
-        found = [f for f in found if np.isfinite(f[0])]
+        with np.errstate(over="ignore"):   # finite as they are returned, in fp32
+            found = [f for f in found if np.isfinite(np.float32(f[0]))]
         found.sort(key=lambda f: (-f[0], f[1], -f[2], f[3]))
         for i, f in enumerate(found[:n]):
             out[b, i], parent[b, i], token[b, i] = f[0], f[1], f[3]

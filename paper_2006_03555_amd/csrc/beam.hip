@@ -336,7 +336,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_beam_merge(BeamSelect a) {
     for (int i0 = 64 * kEarly; i0 < keys; i0 += 64) take(of_row[min(i0 + lane, keys - 1)], i0);
     const float x = unordered((uint32_t)(best.top >> 32));
     const double s = own + (((double)x - top) - rest);
-    const bool offered = best.top && s - s == 0.0;
+    const bool offered = best.top && fabsf((float)s) < INFINITY;   // as it is returned
     if (offered) {
       score[k * n + lane] = s;
       token[k * n + lane] = (int)~(uint32_t)best.top;

@@ -148,6 +148,19 @@ def test_masked_vocabulary(value, dtype):
         same(select(x, s, n, dtype), rec.beam_select(x, s, n), V, 20)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_past_fp32(dtype):
+    """A second masked token in a row leaves fp32's range: its score would be -Inf, so it is not
+    offered, and what is left over has parent 0 and the end's token."""
+    low = -3.3e38
+    x = _round(np.array([[[1, low, low], [low, 2, low]]], np.float32), dtype)
+    s = np.array([[-3.2e38, -1]], np.float32)
+    got = select(x, s, 6, dtype, end_token=2)
+    same(got, rec.beam_select(x, s, 6, None, 2), 3, 20)
+    assert got[1].tolist() == [[1, 0, 1, 1, 0, 0]] and got[2].tolist() == [[1, 0, 0, 2, 2, 2]]
+    assert got[0].isinf().tolist() == [[False] * 4 + [True] * 2]
+
+
 def test_ended_beams():
     x, s = data(4, 5, 900, "f32", 8)
     ended = np.zeros((4, 5), bool)
