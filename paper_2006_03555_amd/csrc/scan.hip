@@ -62,11 +62,14 @@ __device__ __forceinline__ void forward_states(const float (&s)[8], const float 
 }
 
 // kOut: the rows y and the state after the last token. Otherwise the sums of the segments.
-// kAhead, for calls of one segment, whose few workgroups a compute unit does not overlap: a
-// chunk's rows are requested before the states of the one before are taken, two states go side
-// by side, and y has a tile of its own, so that the next rows need not wait for its readers. B4
-// L4096 D2048 N16 in bf16 takes 238 us with it and 298 without; segments' workgroups, of which
-// three share a unit, lose more by the registers (726 and 745 us at B1 L65536).
+// kAhead, for calls of one segment in bf16, whose few workgroups a compute unit does not overlap:
+// a chunk's rows are requested before the states of the one before are taken, two states go side
+// by side, and y has a tile of its own, so that the next rows need not wait for its readers. Whole
+// calls with it and without: B4 L4096 D2048 N16 230 and 239 us, B4 L2048 D2048 N64 370 and 391 (with
+// four workgroups to a unit the registers cost more than it gains: B16 L1024 D4096 N16 357 and 340).
+// In fp32, whose rows take twice the registers, it would spill and lose everywhere (B4 L4096 D2048
+// N16 292 and 267, B1 L128 D512 N16 10.8 and 10.3), and so would segments' workgroups, of which
+// three share a unit (745 and 726 at B1 L65536 D2048).
 template <typename T, bool kOut, bool kAhead> struct ScanLds {
   static constexpr int kRaw = kPairTiles<T> * W * kTok;
   static constexpr int kRows = kRaw + (kAhead ? W * kTok : 0);   // else y takes the place of x and dt
@@ -259,7 +262,9 @@ template <typename T, bool kOut, bool kAhead> hipError_t launch_as(const Scan &a
   return hipGetLastError();
 }
 template <typename T> hipError_t launch_rows(const Scan &a, hipStream_t st) {
-  return a.nseg == 1 ? launch_as<T, true, true>(a, st) : launch_as<T, true, false>(a, st);
+  if constexpr (sizeof(T) == 2)
+    if (a.nseg == 1) return launch_as<T, true, true>(a, st);
+  return launch_as<T, true, false>(a, st);
 }
 
 }  // namespace
