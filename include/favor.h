@@ -477,8 +477,8 @@ FAVOR_API favor_status favor_dropout(const void *x, const void *residual, void *
  * the oldest first.
  *
  * Supported: width 2 to 8; D a multiple of 8 up to 65536; dtype (x, y, states and their
- * gradients) F32 or BF16, sums in fp32; 0 <= L <= 2^30, B <= 65535, L D <= 2^38, B L D <= 2^46. lengths
- * [B] int32 (nullable, device): as for favor_attn_decay: rows behind a sequence are not read
+ * gradients) F32 or BF16, sums in fp32; 0 <= L <= 2^30, B <= 65535, L D <= 2^38, B L D <= 2^46.
+ * lengths [B] int32 (nullable, device): as for favor_attn_decay: rows behind a sequence are not read
  * and their rows of y and dx are written as zeros.
  */
 typedef struct {
@@ -510,9 +510,9 @@ FAVOR_API favor_status favor_conv_backward(const favor_conv_desc *g, const void 
 FAVOR_API size_t favor_conv_workspace_size(const favor_conv_desc *g);
 
 /*
- * One token of B sequences: x, y [B][D] (batch strides; L has no effect) and the states
- * [n_slots][width - 1][D], updated in place. slots as for favor_attn_decay_step: a place
- * outside 0 .. n_slots - 1 is padding and gives y = 0, sequences that name the same place
+ * One token of B sequences: x, y [B][D] (batch strides; L has no effect within its range) and
+ * the states [n_slots][width - 1][D], updated in place. slots as for favor_attn_decay_step: a
+ * place outside 0 .. n_slots - 1 is padding and gives y = 0, sequences that name the same place
  * take their turns in order.
  */
 FAVOR_API favor_status favor_conv_step(const favor_conv_desc *g, const void *x,
@@ -533,8 +533,9 @@ FAVOR_API favor_status favor_conv_step(const favor_conv_desc *g, const void *x,
  *
  * Supported: N from 1 to 256; D up to 65536 with D / groups a multiple of 8; dtype (x, dt, B,
  * C, z, y and their gradients) F32 or BF16; 0 <= L <= 2^30, B <= 65535, L D <= 2^38, B L D and
- * B L groups N <= 2^46. Steps, states and sums are fp32 for both. A is meant to be negative; for a positive one exp(A times the steps of
- * any 128 tokens) has to be in fp32's range, and A must be finite. lengths as for favor_conv
+ * B L groups N <= 2^46. Steps, states and sums are fp32 for both, and what is below 2^-126 as an
+ * exponential is 0. A is meant to be negative; for a positive one exp(A times the steps of any 128
+ * tokens) has to be in fp32's range, and A must be finite. lengths as for favor_conv
  * (B's and C's padding is not read either, its gradients are zeros). A NaN or infinity reaches
  * the results of its own channel (in B or C: of its group) from its token on, and gradients as the
  * formulas carry it; in the backward pass it may reach all of its chunk of 128 tokens.
@@ -547,8 +548,13 @@ typedef struct {
   favor_strides grad_y, grad_x, grad_dt, grad_b, grad_c, grad_z;   /* backward pass only */
 } favor_scan_desc;
 
-/* Bytes of device workspace for favor_selective_scan (backward = 0) or its backward pass (1),
- * 256-byte aligned; 0 if none is needed or g is invalid. Its contents do not matter. */
+/*
+ * Bytes of device workspace for favor_selective_scan (backward = 0) or its backward pass (1),
+ * 256-byte aligned; 0 if none is needed or g is invalid. Its contents do not matter. Backward, in
+ * floats: 3 B chunks D N for states and dA (chunks of 128 tokens), and 2 B L groups N for dB and dC
+ * for each workgroup of a group's channels: up to 128 channels of a large call with N <= 16, 32 of
+ * others. So that part grows fourfold from N = 16 to 17, and B4 L4096 D4096 N64 takes 1.5 GB.
+ */
 FAVOR_API size_t favor_scan_workspace_size(const favor_scan_desc *g, int backward);
 
 /* state_in (nullable), state_out (nullable; may be state_in, and overlaps it not otherwise):
@@ -578,8 +584,9 @@ FAVOR_API favor_status favor_selective_scan_backward(
     void *dx, void *ddt, float *dA, void *dB, void *dC, float *dskip, void *dz,
     float *ddt_bias, float *dstate_in, void *ws, size_t ws_bytes, hipStream_t stream);
 
-/* One token of B sequences: x, dt, z, y [B][D], Bm, C [B][groups][N] (token strides and L have
- * no effect), the states [n_slots][D][N] updated in place; slots as for favor_conv_step. */
+/* One token of B sequences: x, dt, z, y [B][D], Bm, C [B][groups][N] (token strides and L, within
+ * its range, have no effect), the states [n_slots][D][N] updated in place; slots as for
+ * favor_conv_step. */
 FAVOR_API favor_status favor_selective_scan_step(const favor_scan_desc *g, const void *x,
                                                  const void *dt, const float *A, const void *Bm,
                                                  const void *C, const float *skip, const void *z,
@@ -597,7 +604,9 @@ FAVOR_API favor_status favor_validate_scan_desc(const favor_scan_desc *g, int op
  *   score(k, v) = scores[k] + x[k][v] - log sum_u exp x[k][u]
  * in falling order: out_scores [B][n] fp32, parent [B][n] (the beam k) and token [B][n] int32.
  * Ties go to the lower beam, then in one beam to the higher logit and the lower token. Sums of
- * exponentials are fp32 per lane and joined in 64 bits; scores are compared in 64 bits.
+ * exponentials are fp32 per lane and joined in 64 bits; scores are compared in 64 bits. In one
+ * call equal rows have equal scores; how a row is cut depends on V and on B K, so with another
+ * number of rows its score may be rounded otherwise. Logits of any size are taken.
  *
  * logits [B][K][V] of dtype, V contiguous, strides in elements (both 0 = contiguous), not
  * aligned: any V and slices of a padded vocabulary. scores [B][K] fp32. ended [B][K] bytes

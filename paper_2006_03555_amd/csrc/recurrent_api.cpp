@@ -188,16 +188,16 @@ favor_status validate(const favor_scan_desc *g, int op) {
 // sums of all but the last first, so their steps and decays are computed twice. Whole calls in
 // us, bf16, N = 16:
 //   One segment while its workgroups of 32 channels fill the 256 compute units, as long as
-//   there are 240 of them: B4 L4096 D2048 (256) 220, in two segments 297, in eight 279; B8 368,
-//   498, 534.
+//   there are 240 of them: B4 L4096 D2048 (256) 230, in two segments 285, in eight 274 (fp32 267,
+//   314, 300); B8 374, 493, 534.
 //   Fewer: segments for 4096 workgroups. For 1024 / 2048 / 4096 / 8192 of them B1 L65536 D2048 1181
-//   / 1120 / 1096 / 1093, B2 L4096 157 / 149 / 145 / 144, B1 L8192 D2048 N64 fp32 540 / 540 / 546 /
-//   546. B1 L4096 82 in 32 segments and 214 in one, B3 L4096 (192) 213 in 16 and 216 in one, B6
-//   L1999 D1000 N24 fp32 (192) 186 in 16 and 194 in one.
+//   / 1127 / 1110 / 1107, B2 L4096 156 / 150 / 145 / 145, B1 L8192 D2048 N64 fp32 540 / 540 / 546 /
+//   546. B1 L4096 83 in 32 segments and 219 in one, B3 L4096 (192) 216 in 16 and 221 in one (fp32
+//   229 and 263), but B6 L1999 D1000 N24 fp32 (192) 192 in 16 and 184 in one.
 //   One segment too where three passes over a chunk (16 states each) or fewer are all of it: two
-//   more launches cost as much. B1 L256 D512 16.4 in one, 21.4 in two; B2 L384 D2048 23.6, in three
-//   29.1; B1 L384 D512 22.7, in three 21.7; B1 L512 D512 28.9, in four 21.9; N64 fp32 L256 D2048
-//   50.9, in two 40.5.
+//   more launches cost as much. B1 L256 D512 16.4 in one, 22.0 in two; B2 L384 D2048 23.4, in three
+//   28.0; B1 L384 D512 22.8, in three 22.3; B1 L512 D512 29.5, in four 22.4; N64 fp32 L256 D2048
+//   50.1, in two 40.7.
 struct ScanCut {
   int chunks, nseg;
 };

@@ -5,10 +5,11 @@
 //
 // Bound by the vector unit: each (token, channel, state) takes a product and an exponential
 // (two issue slots), the input's product, the recurrence once inside the lane and once from
-// its true state, and the output's sum: seven slots, and about three more for the row's scan and
-// the rows' way through LDS. Nothing of size tokens x channels x states leaves the registers.
-// B4 L4096 D2048 N16 in bf16 (one segment): 238 us, 2.3 T state steps/s; B1 L65536 D2048: sums of
-// 31 segments 500 us, then 725 us, 3.0 T/s.
+// its true state, and the output's sum: seven slots, and 10.6 as counted with the row's scan and
+// the rows' way through LDS (the segments' sums, without an output: 8.7). Nothing of size tokens
+// x channels x states leaves the registers. B4 L4096 D2048 N16 in bf16 (one segment): 225 to 264
+// us, 2.0 to 2.4 T state steps/s; B1 L65536 D2048: sums of 63 of its 64 segments 505 us, prefix 13,
+// then 749 us, 2.9 T/s.
 #include "scan_common.hpp"
 
 namespace favor {

@@ -77,15 +77,16 @@ __device__ __forceinline__ float rcp_hw(float x) { return __builtin_amdgcn_rcpf(
 __device__ __forceinline__ float sigmoid(float x) { return rcp_hw(1.f + exp2_hw(-kLog2e * x)); }
 
 // max(x, 0) + log(1 + e), e = exp(-|x|). With u = 1 + e as rounded, log(1 + e) is log(u) + (what
-// the rounding left of e) / u, and u is 1 where that matters; so it keeps its relative
-// precision as e falls, down to e itself. 0 at -Inf; a NaN comes through e.
+// the rounding left of e) / u, and u is 1 where that matters; so as e falls it is as precise as e
+// itself, whose exponent's rounding is |x| 2^-24 of it (80 units at x = -80). 0 at -Inf; a NaN comes
+// through e.
 __device__ __forceinline__ float softplus(float x) {
   const float e = exp2_hw(-kLog2e * fabsf(x));
   const float u = 1.f + e;
   const float over = __builtin_amdgcn_fmed3f(x, 0.f, INFINITY);   // max(x, 0)
   return over + fmaf(kLn2, __builtin_amdgcn_logf(u), e - (u - 1.f));
 }
-// softplus' slope at x, of which s is softplus(x): e^x / (1 + e^x) = e^(x - s).
+// softplus' slope at x, of which s is softplus(x): e^x / (1 + e^x) = e^(x - s), within |x - s| 2^-24.
 __device__ __forceinline__ float softplus_slope(float x, float s) { return exp2_hw(kLog2e * (x - s)); }
 
 // Sequences that hold the same place of a pool take their turns in order, all in the first
