@@ -111,7 +111,7 @@ favor_status validate(const favor_conv_desc *g, int op) {
     FAVOR_TRY(check_rows(ts[i].name, *ts[i].s, size, g->D, 16 / bytes_of(g->dtype), 0, ts[i].out));
   }
   // what one launch takes: a thread has 8 tokens of 4 channels at least, 32 of them in a long call
-  if ((int64_t)g->L * g->D > kMaxRows)
+  if (op != kOpStep && (int64_t)g->L * g->D > kMaxRows)
     return fail(FAVOR_ERR_UNSUPPORTED, "L=%d D=%d: a sequence of more than 2^38 elements", g->L, g->D);
   if (op == kOpBackward && part_rows(g) > kMaxBlocks)
     return fail(FAVOR_ERR_UNSUPPORTED, "B=%d L=%d D=%d is too large", g->B, g->L, g->D);
@@ -177,9 +177,9 @@ favor_status validate(const favor_scan_desc *g, int op) {
                          ts[i].out));
   }
   // counts that the kernels hold in 32 bits
-  if ((int64_t)g->L * g->D > kMaxRows)
+  if (op != kOpStep && (int64_t)g->L * g->D > kMaxRows)
     return fail(FAVOR_ERR_UNSUPPORTED, "L=%d D=%d: a sequence of more than 2^38 elements", g->L, g->D);
-  if ((int64_t)g->B * chunks_of(g) > kMaxBlocks)
+  if (op != kOpStep && (int64_t)g->B * chunks_of(g) > kMaxBlocks)
     return fail(FAVOR_ERR_UNSUPPORTED, "B=%d L=%d is too large", g->B, g->L);
   return FAVOR_OK;
 }

@@ -403,6 +403,9 @@ def test_sizes_past_one_launch():
             assert fv.validate_scan_desc(_scan(B=1, L=L, D=65536, N=1, groups=1), op) == status
             assert fv.validate_conv_desc(_conv(B=1, L=L, D=65536), op) == status
             assert status == 0 or "2^38" in fv.last_error()
+        for g, check in ((_scan(B=1, L=L, D=65536, N=1, groups=1), fv.validate_scan_desc),
+                         (_conv(B=1, L=L, D=65536), fv.validate_conv_desc)):
+            assert check(g, 2) == 0   # a single token's L has no effect
 
 
 def test_binding_refusals():
